@@ -380,6 +380,132 @@ pkv_status_t pkv_plan_query(const pkv_plan_t* plan, pkv_plan_info_t* info);
  * PKV_ERR_INVALID_ARGUMENT (NULL plan or bytes, req outside [0, num_requests)). */
 pkv_status_t pkv_plan_payload_bytes(const pkv_plan_t* plan, int32_t req, uint64_t* bytes);
 
+/* ----------------------------------------------------------------------------
+ * Serving from a paged cache: rows written as tokens come, quantised on the
+ * way where the cache holds codes, read back, and attention over them.
+ *
+ * A cache of tag FP16 is the 16-bit cache that pkv_restore writes
+ * (pkv_model_t's kv_layout and out_dtype).  A cache of another tag stays
+ * quantised: each row (one token, one head, K or V) has its own binary16 scale
+ * and zero, by the rule of the checkpoint write (zero = the largest binary16 <=
+ * min, scale = the smallest binary16 >= (max - zero)/(2^bits - 1), code =
+ * round-half-even((x - zero)/scale); x finite, |x| <= 65504), and stands for
+ * code * scale + zero.  One token costs num_kv_heads * (head_dim *
+ * (key bits + value bits) / 8 + 8) bytes per layer: 136 per head of 128
+ * channels in 4 bits, against 512 in 16.
+ *   codes  (device): [L][pool_pages][H][K tile | V tile], a tile [P][D] of
+ *     the tag's key or value bits, 4-bit channels 2j in the low nibble of byte j;
+ *   scales (device, binary16): [L][pool_pages][H][2 (K, V)][P][2 (scale, zero)].
+ *
+ * The calls take what an engine keeps on the device (lengths, page tables), so
+ * they enqueue without a copy or a wait, allocate nothing and may be captured
+ * in a HIP graph that is replayed while those arrays change.  So the host
+ * cannot check their contents, and the kernels do: a logical page past
+ * pages_per_seq or mapped outside [0, pool_pages) (-1 = unmapped) is not
+ * there (a row of it is not written, reads as zero and takes no part in
+ * attention), and lengths and starts are clamped to their bounds below.
+ * ---------------------------------------------------------------------------- */
+
+/* The cache of one layer of a call.  FP16: k_cache, v_cache and cache_bytes as
+ * in pkv_restore, codes and scales unused; other tags: codes (16-byte
+ * aligned) and scales (16-byte aligned) of at least pkv_cache_size's bytes,
+ * k_cache and v_cache unused. */
+typedef struct {
+  int32_t tag;           /* pkv_tag_t */
+  int32_t layer;         /* 0 <= layer < num_layers */
+  void* k_cache;
+  void* v_cache;
+  uint64_t cache_bytes;
+  void* codes;
+  uint64_t code_bytes;
+  void* scales;
+  uint64_t scale_bytes;
+} pkv_paged_cache_t;
+
+/* The rows of a call: num_tokens tokens dealt to num_seqs sequences.  Rows
+ * [token_start[s], token_start[s + 1]) of the call's row buffers belong to
+ * sequence s.  Row i sits at logical position positions[i] of its sequence, or,
+ * with positions == NULL, the rows are the last of the kv_lens[s] tokens; a
+ * negative position has no row.  Rows of no sequence are neither read nor
+ * written.  Arrays are device memory, 4-byte aligned; num_seqs, num_tokens >= 0,
+ * num_tokens * num_q_heads < 2^31, pages_per_seq >= 1,
+ * pages_per_seq * page_size <= 2^30. */
+typedef struct {
+  int32_t num_seqs;
+  int32_t num_tokens;
+  int32_t max_tokens;         /* bound of a sequence's rows: 1 for a decode step; 0 = num_tokens */
+  int32_t pages_per_seq;      /* row length of page_table */
+  int64_t max_kv_len;         /* bound of kv_lens, for the launch; 0 = pages_per_seq * page_size */
+  const int32_t* token_start; /* [num_seqs + 1], ascending from 0 */
+  const int32_t* kv_lens;     /* [num_seqs] tokens in the cache, the call's own included */
+  const int32_t* positions;   /* [num_tokens] or NULL */
+  const int32_t* page_table;  /* [num_seqs][pages_per_seq] physical pages, -1 = unmapped */
+} pkv_batch_t;
+
+/* Bytes of codes and scales of a quantised cache of all layers (0 and 0 for
+ * FP16).  Host only.  Errors: PKV_ERR_INVALID_ARGUMENT, PKV_ERR_BAD_TAG. */
+pkv_status_t pkv_cache_size(const pkv_model_t* model, int32_t tag, uint64_t* code_bytes, uint64_t* scale_bytes);
+
+/* Write the batch's rows k, v into the cache at their positions, quantised by
+ * its tag (FP16: copied).  Row i of head h starts at k + i * token_stride +
+ * h * head_stride elements of out_dtype (v likewise); both 16-byte aligned,
+ * strides multiples of 8 and head_stride >= head_dim (views of a fused
+ * projection will do).  Two rows of a call at one place leave either.  Every
+ * other byte of the cache stays.  One kernel on `hip_stream`.  Errors:
+ * PKV_ERR_INVALID_ARGUMENT, PKV_ERR_BAD_TAG, PKV_ERR_DEVICE. */
+pkv_status_t pkv_cache_append(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                              const void* k, const void* v, int64_t token_stride, int64_t head_stride,
+                              void* hip_stream);
+
+/* Read the batch's rows back from the cache into k, v (layout as above;
+ * rows must not overlap): code * scale + zero in single precision, rounded once to
+ * out_dtype (FP16 tag: copied); a row that is not there is zero.  One kernel
+ * on `hip_stream`.  Errors as pkv_cache_append. */
+pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch, void* k,
+                            void* v, int64_t token_stride, int64_t head_stride, void* hip_stream);
+
+/* Attention of the batch's rows over the cache.  Row i of a sequence at position
+ * p sees the cached tokens t with t < kv_lens, t <= p and, if window > 0,
+ * p - t < window or t < sinks (the last `window` tokens and the first `sinks`).
+ * With s_t = scale * q . k_t over what it sees,
+ *   out = sum_t exp(s_t) v_t / sum_t exp(s_t),   lse = log sum_t exp(s_t);
+ * a row that sees nothing has out = 0 and lse = -inf.  Query head h reads KV
+ * head h / (num_q_heads / num_kv_heads).  head_dim 64, 128 or 256.
+ *   q, out : [num_tokens][num_q_heads][head_dim] of out_dtype at the strides
+ *     (elements; alignment as in pkv_cache_append); out must not overlap an input;
+ *   lse    : float [num_tokens][num_q_heads], or NULL;
+ *   workspace : device memory of pkv_attention_workspace's bytes (0: may be
+ *     NULL), 16-byte aligned, contents of no matter before and after; calls
+ *     that may overlap need one each.
+ * Sums, maxima and lse are single precision.  Quantised caches: q.code sums are
+ * exact products (codes and queries are exact in the matrix instructions'
+ * binary16 operands, queries scaled by a power of two), probabilities are rounded
+ * to binary16; 16-bit caches: probabilities are rounded to out_dtype.  What a
+ * cache holds at places that no row of the call sees (NaN, infinities) does
+ * not matter; a place that some row of a sequence sees should hold finite values.
+ * At most two kernels on `hip_stream`.  Errors as pkv_cache_append. */
+typedef struct {
+  int32_t num_q_heads; /* a multiple of num_kv_heads */
+  int32_t window;      /* 0 = no window */
+  int32_t sinks;       /* >= 0; without a window it changes nothing */
+  float scale;         /* finite, > 0; usually 1 / sqrt(head_dim) */
+  const void* q;
+  int64_t q_token_stride, q_head_stride;
+  void* out;
+  int64_t out_token_stride, out_head_stride;
+  float* lse;
+  void* workspace;
+  uint64_t workspace_bytes;
+} pkv_attention_t;
+
+/* Workspace bytes of pkv_attention for these sizes (pointers are not looked
+ * at).  Host only.  Errors: PKV_ERR_INVALID_ARGUMENT, PKV_ERR_BAD_TAG. */
+pkv_status_t pkv_attention_workspace(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                                     const pkv_attention_t* attention, uint64_t* bytes);
+
+pkv_status_t pkv_attention(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                           const pkv_attention_t* attention, void* hip_stream);
+
 /* Static description of a status code. */
 const char* pkv_status_string(pkv_status_t status);
 

@@ -26,7 +26,8 @@ PKV_ERR_DEVICE = -7
 # Every symbol include/pkv.h declares.
 EXPORTED = ("pkv_payload_size", "pkv_restore_plan", "pkv_restore", "pkv_restore_from_host", "pkv_free",
             "pkv_plan_query", "pkv_status_string", "pkv_checkpoint_plan", "pkv_quantize_gather", "pkv_plan_repair",
-            "pkv_plan_payload_bytes", "pkv_restore_from_host_noalloc")
+            "pkv_plan_payload_bytes", "pkv_restore_from_host_noalloc", "pkv_cache_size", "pkv_cache_append",
+            "pkv_cache_read", "pkv_attention_workspace", "pkv_attention")
 
 
 class PkvModel(ctypes.Structure):
@@ -56,6 +57,26 @@ class PkvPlanInfo(ctypes.Structure):
                 ("cache_bytes", ctypes.c_uint64), ("bytes_read", ctypes.c_uint64),
                 ("bytes_written", ctypes.c_uint64), ("device", ctypes.c_int32), ("kind", ctypes.c_int32),
                 ("host_copy_bytes", ctypes.c_uint64), ("host_copies", ctypes.c_int64)]
+
+
+class PkvPagedCache(ctypes.Structure):
+    _fields_ = [("tag", ctypes.c_int32), ("layer", ctypes.c_int32), ("k_cache", ctypes.c_void_p),
+                ("v_cache", ctypes.c_void_p), ("cache_bytes", ctypes.c_uint64), ("codes", ctypes.c_void_p),
+                ("code_bytes", ctypes.c_uint64), ("scales", ctypes.c_void_p), ("scale_bytes", ctypes.c_uint64)]
+
+
+class PkvBatch(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_tokens", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+                ("pages_per_seq", ctypes.c_int32), ("max_kv_len", ctypes.c_int64), ("token_start", ctypes.c_void_p),
+                ("kv_lens", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
+class PkvAttention(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("q", ctypes.c_void_p), ("q_token_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("out", ctypes.c_void_p), ("out_token_stride", ctypes.c_int64),
+                ("out_head_stride", ctypes.c_int64), ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_uint64)]
 
 
 class PkvError(RuntimeError):
@@ -102,6 +123,17 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pkv_restore_from_host_noalloc.restype = i32
     lib.pkv_plan_payload_bytes.argtypes = [vp, i32, ctypes.POINTER(u64)]
     lib.pkv_plan_payload_bytes.restype = i32
+    model, cache, batch = ctypes.POINTER(PkvModel), ctypes.POINTER(PkvPagedCache), ctypes.POINTER(PkvBatch)
+    attention, i64 = ctypes.POINTER(PkvAttention), ctypes.c_int64
+    lib.pkv_cache_size.argtypes = [model, i32, ctypes.POINTER(u64), ctypes.POINTER(u64)]
+    lib.pkv_cache_size.restype = i32
+    for f in (lib.pkv_cache_append, lib.pkv_cache_read):
+        f.argtypes = [model, cache, batch, vp, vp, i64, i64, vp]
+        f.restype = i32
+    lib.pkv_attention_workspace.argtypes = [model, cache, batch, attention, ctypes.POINTER(u64)]
+    lib.pkv_attention_workspace.restype = i32
+    lib.pkv_attention.argtypes = [model, cache, batch, attention, vp]
+    lib.pkv_attention.restype = i32
     _lib = lib
     return lib
 
@@ -387,3 +419,37 @@ def restore_tensors(plan: Plan, payload, scales, k_cache, v_cache, stream=None) 
     nbytes = lambda t: t.numel() * t.element_size()
     pkv_restore(plan, payload.data_ptr(), nbytes(payload), scales.data_ptr(), nbytes(scales), k_cache.data_ptr(),
                 v_cache.data_ptr(), cache_nbytes(k_cache, v_cache), stream.cuda_stream)
+
+
+def pkv_cache_size(shape, tag: int):
+    """(code bytes, scale bytes) of a quantised paged cache, all layers."""
+    cb, sb = ctypes.c_uint64(), ctypes.c_uint64()
+    st = load().pkv_cache_size(ctypes.byref(make_model(shape)), int(tag), ctypes.byref(cb), ctypes.byref(sb))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_cache_size")
+    return cb.value, sb.value
+
+
+# The serving calls take the structures as they are; serving.py fills them from tensors.
+
+def pkv_cache_append_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, k, v, token_stride: int,
+                            head_stride: int, stream=0) -> int:
+    return load().pkv_cache_append(model, cache, batch, k, v, token_stride, head_stride, stream or None)
+
+
+def pkv_cache_read_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, k, v, token_stride: int,
+                          head_stride: int, stream=0) -> int:
+    return load().pkv_cache_read(model, cache, batch, k, v, token_stride, head_stride, stream or None)
+
+
+def pkv_attention_workspace(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, attention: PkvAttention) -> int:
+    out = ctypes.c_uint64()
+    st = load().pkv_attention_workspace(model, cache, batch, attention, ctypes.byref(out))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_attention_workspace")
+    return out.value
+
+
+def pkv_attention_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, attention: PkvAttention,
+                         stream=0) -> int:
+    return load().pkv_attention(model, cache, batch, attention, stream or None)

@@ -1,4 +1,4 @@
-"""Build libpkv.so in-tree: host plan code with g++, the HIP kernel with hipcc
+"""Build libpkv.so in-tree: host code with g++, the HIP kernels with hipcc
 for gfx950, linked into one shared library next to this file."""
 from __future__ import annotations
 
@@ -6,6 +6,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -20,6 +21,10 @@ ARCH = "gfx950"
 HIP_FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC", "-Wall",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", f"-I{INCLUDE}", f"-I{CSRC}"]
 CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra", f"-I{INCLUDE}", f"-I{CSRC}"]
+HOST_SRC = ("plan.cpp", "serve_plan.cpp")
+# The attention kernels are built once for each head_dim.
+HIP_SRC = (("restore.hip", ()), ("gather.hip", ()), ("serve.hip", ()),
+           *(("attend.hip", (f"-DPKV_HEAD_DIM={d}",)) for d in (64, 128, 256)))
 
 
 def _run(cmd, verbose):
@@ -36,13 +41,13 @@ def build(verbose: bool = False) -> str:
     """Compile and link libpkv.so; returns its path.  Always rebuilds."""
     os.makedirs(BUILD, exist_ok=True)
     cxx = shutil.which("g++") or "g++"
-    plan_o = os.path.join(BUILD, "plan.o")
-    _run([cxx, *CXX_FLAGS, "-c", os.path.join(CSRC, "plan.cpp"), "-o", plan_o], verbose)
-    objs = [plan_o]
-    for src in ("restore.hip", "gather.hip"):
-        obj = os.path.join(BUILD, src.replace(".hip", ".o"))
-        _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
-        objs.append(obj)
+    steps = [(src.replace(".cpp", ".o"), [cxx, *CXX_FLAGS, "-c", os.path.join(CSRC, src)]) for src in HOST_SRC]
+    for src, flags in HIP_SRC:
+        obj = src.replace(".hip", "".join("_" + f.split("=")[1] for f in flags) + ".o")
+        steps.append((obj, [HIPCC, *HIP_FLAGS, *flags, "-c", os.path.join(CSRC, src)]))
+    objs = [os.path.join(BUILD, obj) for obj, _ in steps]
+    with ThreadPoolExecutor(min(len(steps), os.cpu_count() or 1)) as pool:
+        list(pool.map(lambda s: _run([*s[1], "-o", os.path.join(BUILD, s[0])], verbose), steps))
     tmp = LIB + ".tmp"
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp], verbose)
     os.replace(tmp, LIB)

@@ -429,6 +429,9 @@ int32_t page_shift(const pkv_model_t& m);
 int64_t layer_elems(const pkv_model_t& m);
 uint64_t cache_bytes(const pkv_model_t& m);  // of each separate cache, or of the paired one
 
+// The constraints of pkv_model_t.
+pkv_status_t check_model(const pkv_model_t* m);
+
 // The cache pointers of a call against the model's layout: both 16-byte
 // aligned; separate caches of cache_bytes each must not overlap; a paired
 // cache has v_cache = k_cache + P*H*D elements.  `ranges` receives the byte

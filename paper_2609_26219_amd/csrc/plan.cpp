@@ -27,6 +27,8 @@ int ilog2(int64_t x) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+}  // namespace
+
 pkv_status_t check_model(const pkv_model_t* m) {
   if (!m) return PKV_ERR_INVALID_ARGUMENT;
   if (m->num_layers < 1 || m->num_kv_heads < 1) return PKV_ERR_INVALID_ARGUMENT;
@@ -55,6 +57,8 @@ pkv_status_t check_model(const pkv_model_t* m) {
   if (elems > 1e18) return PKV_ERR_INVALID_ARGUMENT;
   return PKV_OK;
 }
+
+namespace {
 
 // RoPE helpers: rotated channels per head, the frequency of pair i, and the
 // pair that element e of key piece j rotates (k = 8j + e; -1 = none).

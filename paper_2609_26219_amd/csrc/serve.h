@@ -1,0 +1,83 @@
+// The serving calls (pkv_cache_append, pkv_cache_read, pkv_attention): what
+// their host checks hand to the kernels.
+#ifndef PKV_SERVE_H
+#define PKV_SERVE_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "pkv.h"
+#include "pkv_internal.h"
+
+namespace pkv {
+
+// One layer's cache and the rows of a call, as the kernels see them.
+struct ServeArgs {
+  const int32_t* token_start;
+  const int32_t* kv_lens;
+  const int32_t* positions;
+  const int32_t* page_table;
+  // FP16 tag: the layer's first slot of K and of V, in 16-bit elements; a page
+  // is page_stride elements after the one before, a slot H * D.
+  uint16_t* k_cache;
+  uint16_t* v_cache;
+  // Quantised tags: the layer's codes (bytes) and (scale, zero) words; a page
+  // is page_stride bytes / scale_stride words after the one before, a head
+  // head_stride bytes / 2 * P words, the V tile v_offset bytes after the K tile.
+  uint8_t* codes;
+  uint32_t* scales;
+  int64_t page_stride;
+  int64_t scale_stride;
+  int64_t head_stride;
+  int64_t v_offset;
+  int64_t pool_pages;
+  int32_t num_seqs, num_tokens, max_tokens, pages_per_seq;
+  int32_t max_kv;  // bound of kv_lens, at most pages_per_seq * P
+  int32_t log2P;
+  int32_t H, D;
+  int32_t tag, bf16;
+};
+
+struct RowArgs {
+  uint16_t* k;
+  uint16_t* v;
+  int64_t token_stride, head_stride;
+};
+
+struct AttendArgs {
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;         // or null
+  float* part;        // [num_tokens * Hq][splits][D] sums of one split, relative to its maximum
+  float* part_ml;     // [num_tokens * Hq][splits][2] its maximum (base 2) and sum
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+  int32_t Hq, group;  // query heads, query heads per KV head
+  int32_t window, sinks;
+  float scale;        // scale * log2(e)
+  int32_t row_tiles;  // of one sequence and KV head
+  int32_t splits;     // pieces that a sequence's tokens are dealt to
+  int32_t chunk;      // least tiles of tokens in a piece
+};
+
+// How an attention call is launched.
+struct AttendLaunch {
+  int32_t row_tiles, splits, chunk;
+  int64_t groups;           // workgroups
+  uint64_t part_bytes;      // of AttendArgs::part, then part_ml
+  uint64_t workspace_bytes; // both
+};
+
+constexpr int kRowTile = 16;   // rows (token, query head of one KV head) of a workgroup
+constexpr int kTokenTile = 32; // cached tokens a wave takes at a time
+
+// Host checks that need no GPU; they fill the arguments.
+pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                        bool pointers, ServeArgs* out);
+pkv_status_t row_args(const ServeArgs& s, const void* k, const void* v, int64_t token_stride, int64_t head_stride,
+                      RowArgs* out);
+pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool pointers, AttendArgs* out);
+AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a);
+
+}  // namespace pkv
+
+#endif  // PKV_SERVE_H

@@ -1,0 +1,362 @@
+// The paged cache written and read back (pkv_cache_append, pkv_cache_read), and
+// the entry points of the serving calls.
+//
+// Both kernels move rows (one token, one head, K and V): a workgroup takes
+// `tokens` consecutive rows of the call's buffers and all heads.  It first
+// finds their places in the cache (sequence, position, page), one thread per
+// token, and leaves them in LDS; then groups of D/8 lanes (rounded up to a
+// power of two) take one row each, 8 channels per lane, with neighbouring
+// groups on neighbouring tokens of one head, so that the codes they store or
+// load are one run of the head's tile.  What bounds both is memory: a row of
+// 128 channels is 256 bytes in 16 bits against 68 in 4.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "pkv.h"
+#include "pkv_internal.h"
+#include "serve.h"
+
+namespace pkv {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMostTokens = 64;    // of a workgroup
+constexpr int kStartsInLds = 1024; // sequences whose starts are searched in LDS
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float f16_float(uint32_t bits) {
+  return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(bits)));
+}
+__device__ __forceinline__ uint32_t f16_bits(float f) {
+  return __builtin_bit_cast(uint16_t, static_cast<_Float16>(f));
+}
+
+// Element e of 8 16-bit cache values.
+template <bool BF16>
+__device__ __forceinline__ float value(const u32x4& w, int e) {
+  const uint32_t word = w[e >> 1];
+  if constexpr (BF16) return __uint_as_float(e & 1 ? word & 0xFFFF0000u : word << 16);
+  return f16_float(e & 1 ? word >> 16 : word);
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  if constexpr (BF16) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+  } else {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+  }
+}
+
+// Where row i of the call lies: its slot in the cache (page * P + slot in the
+// page), -1 where there is none, -2 for a row of no sequence.  `starts` is token_start, in LDS if it fits there.
+__device__ __forceinline__ int64_t place_of(const ServeArgs& a, const int32_t* starts, int32_t i) {
+  int32_t s = 0;
+  for (int32_t end = a.num_seqs; end - s > 1;) {
+    const int32_t mid = s + (end - s) / 2;
+    if (starts[mid] <= i) s = mid; else end = mid;
+  }
+  const int32_t end = starts[s + 1];
+  if (i < starts[s] || i >= end) return -2;
+  int64_t pos;
+  if (a.positions) {
+    pos = a.positions[i];
+  } else {
+    const int32_t len = a.kv_lens[s];
+    pos = int64_t(len < a.max_kv ? len : a.max_kv) - (end - i);
+  }
+  const int64_t page_at = pos >> a.log2P;
+  if (pos < 0 || page_at >= a.pages_per_seq) return -1;
+  const int64_t page = a.page_table[int64_t(s) * a.pages_per_seq + page_at];
+  if (page < 0 || page >= a.pool_pages) return -1;
+  return (page << a.log2P) | (pos & ((int64_t(1) << a.log2P) - 1));
+}
+
+// The places of tokens [i0, i0 + n) into `place`, by the whole workgroup.
+__device__ __forceinline__ void find_places(const ServeArgs& a, int32_t i0, int32_t n, int32_t* starts, int64_t* place) {
+  const int tid = threadIdx.x;
+  const bool in_lds = a.num_seqs < kStartsInLds;
+  if (in_lds)
+    for (int32_t j = tid; j <= a.num_seqs; j += kThreads) starts[j] = a.token_start[j];
+  __syncthreads();
+  if (tid < n) place[tid] = place_of(a, in_lds ? starts : a.token_start, i0 + tid);
+  __syncthreads();
+}
+
+// Zero and scale of a row from its range, and its codes.  The zero is exact in
+// single precision; the scale's first guess (a product by 1 / (2^bits - 1)) is
+// off by at most one binary16 step and is set right by the definition itself,
+// scale * (2^bits - 1) >= max - zero, whose two sides are exact in double.
+struct RowQuant {
+  float zero, inv;
+  uint32_t scale_bits, zero_bits;
+};
+
+__device__ __forceinline__ uint32_t f16_down(uint32_t b) {
+  if (b & 0x8000) return b + 1;
+  return b == 0 ? 0x8001u : b - 1;
+}
+
+template <int BITS>
+__device__ __forceinline__ RowQuant row_quant(float mn, float mx) {
+  constexpr double kMost = (1 << BITS) - 1;
+  RowQuant q;
+  mn += 0.0f;  // -0 counts as +0
+  q.zero_bits = f16_bits(mn);
+  if (f16_float(q.zero_bits) > mn) q.zero_bits = f16_down(q.zero_bits);
+  q.zero = f16_float(q.zero_bits);
+  const double span = static_cast<double>(mx) - static_cast<double>(q.zero);
+  uint32_t s = span > 0.0 ? f16_bits(static_cast<float>(span) * static_cast<float>(1.0 / kMost)) : 0;
+  if (static_cast<double>(f16_float(s)) * kMost < span) ++s;
+  else if (s && static_cast<double>(f16_float(s - 1)) * kMost >= span) --s;
+  q.scale_bits = s;
+  q.inv = s ? __builtin_amdgcn_rcpf(f16_float(s)) : 0.0f;
+  return q;
+}
+
+// Codes of N values (8 of 4 bits or 4 of 8 bits) in one word.  t is within
+// 6.1e-5 of the quotient (x - zero) / scale (roundings of 2^-24, 2^-23 and 2^-24
+// relative on at most 255), and the hardware's float to byte conversion rounds
+// it half to even; a word with a t within 1e-4 of a half-integer is computed
+// again in double with a true division.
+template <bool BF16, int BITS>
+__device__ __forceinline__ uint32_t row_codes(const u32x4& w, int first, const RowQuant& q) {
+  constexpr int N = 32 / BITS;
+  uint32_t lo = 0, hi = 0;
+  float dist = 1.0f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float t = (value<BF16>(w, first + e) - q.zero) * q.inv;
+    if (BITS == 8 || !(e & 1))
+      lo = __builtin_amdgcn_cvt_pk_u8_f32(t, BITS == 8 ? e : e >> 1, lo);
+    else
+      hi = __builtin_amdgcn_cvt_pk_u8_f32(t, e >> 1, hi);
+    dist = __builtin_fminf(dist, __builtin_fabsf(__builtin_amdgcn_fractf(t) - 0.5f));
+  }
+  uint32_t packed = BITS == 8 ? lo : lo | (hi << 4);
+  if (dist < 1e-4f && q.scale_bits) {
+    const double scale = f16_float(q.scale_bits);
+    packed = 0;
+    for (int e = 0; e < N; ++e) {
+      double c = __builtin_rint((static_cast<double>(value<BF16>(w, first + e)) - static_cast<double>(q.zero)) / scale);
+      c = c < 0.0 ? 0.0 : c > double((1 << BITS) - 1) ? double((1 << BITS) - 1) : c;
+      packed |= static_cast<uint32_t>(c) << (BITS * e);
+    }
+  }
+  return packed;
+}
+
+// One row piece (8 channels) into the cache.
+template <bool BF16, int BITS>
+__device__ __forceinline__ void put(const ServeArgs& a, const u32x4& w, int which, int64_t place, int32_t head,
+                                    int32_t piece, int32_t lanes, bool on) {
+  if constexpr (BITS == 16) {
+    if (on) {
+      uint16_t* base = which ? a.v_cache : a.k_cache;
+      const int64_t page = place >> a.log2P, slot = place & ((int64_t(1) << a.log2P) - 1);
+      *reinterpret_cast<u32x4*>(base + page * a.page_stride + slot * a.H * a.D + head * a.D + 8 * piece) = w;
+    }
+  } else {
+    float mn = __builtin_inff(), mx = -__builtin_inff();
+    if (8 * piece < a.D) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = value<BF16>(w, e);
+        mn = __builtin_fminf(mn, x);
+        mx = __builtin_fmaxf(mx, x);
+      }
+    }
+    for (int off = 1; off < lanes; off <<= 1) {
+      mn = __builtin_fminf(mn, __shfl_xor(mn, off));
+      mx = __builtin_fmaxf(mx, __shfl_xor(mx, off));
+    }
+    const RowQuant q = row_quant<BITS>(mn, mx);
+    if (!on) return;
+    const int64_t page = place >> a.log2P, slot = place & ((int64_t(1) << a.log2P) - 1);
+    uint8_t* row = a.codes + page * a.page_stride + head * a.head_stride + (which ? a.v_offset : 0) +
+                   slot * (a.D * BITS / 8) + piece * BITS;
+    if constexpr (BITS == 8)
+      *reinterpret_cast<u32x2*>(row) = u32x2{row_codes<BF16, 8>(w, 0, q), row_codes<BF16, 8>(w, 4, q)};
+    else
+      *reinterpret_cast<uint32_t*>(row) = row_codes<BF16, 4>(w, 0, q);
+    if (piece == 0)
+      a.scales[page * a.scale_stride + ((int64_t(head) * 2 + which) << a.log2P) + slot] =
+          q.scale_bits | (q.zero_bits << 16);
+  }
+}
+
+// One row piece from the cache, as 8 16-bit values.
+template <bool BF16, int BITS>
+__device__ __forceinline__ u32x4 get(const ServeArgs& a, int which, int64_t place, int32_t head, int32_t piece) {
+  const int64_t page = place >> a.log2P, slot = place & ((int64_t(1) << a.log2P) - 1);
+  if constexpr (BITS == 16) {
+    const uint16_t* base = which ? a.v_cache : a.k_cache;
+    return *reinterpret_cast<const u32x4*>(base + page * a.page_stride + slot * a.H * a.D + head * a.D + 8 * piece);
+  } else {
+    const uint8_t* row = a.codes + page * a.page_stride + head * a.head_stride + (which ? a.v_offset : 0) +
+                         slot * (a.D * BITS / 8) + piece * BITS;
+    const uint32_t sz = a.scales[page * a.scale_stride + ((int64_t(head) * 2 + which) << a.log2P) + slot];
+    const float s = f16_float(sz), z = f16_float(sz >> 16);
+    float x[8];
+    if constexpr (BITS == 8) {
+      const u32x2 c = *reinterpret_cast<const u32x2*>(row);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(static_cast<float>((c[e >> 2] >> (8 * (e & 3))) & 0xFF), s, z);
+    } else {
+      const uint32_t c = *reinterpret_cast<const uint32_t*>(row);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(static_cast<float>((c >> (4 * e)) & 0xF), s, z);
+    }
+    return u32x4{pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3]), pack2<BF16>(x[4], x[5]), pack2<BF16>(x[6], x[7])};
+  }
+}
+
+struct RowWork {
+  int32_t log2_tokens;  // of a workgroup
+  int32_t log2_lanes;   // of a row
+};
+
+template <bool BF16, int KB, int VB, bool WRITE>
+__global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, RowWork w) {
+  __shared__ int32_t starts[kStartsInLds];
+  __shared__ int64_t place[kMostTokens];
+  const int32_t tokens = 1 << w.log2_tokens, lanes = 1 << w.log2_lanes;
+  const int32_t i0 = int32_t(blockIdx.x) << w.log2_tokens;
+  const int32_t n = tokens < a.num_tokens - i0 ? tokens : a.num_tokens - i0;
+  find_places(a, i0, n, starts, place);
+  const int32_t piece = threadIdx.x & (lanes - 1);
+  const int32_t rows = a.H << w.log2_tokens, step = kThreads >> w.log2_lanes;
+  // Every lane of a row's group runs the same passes, so the exchange in put() is between live lanes.
+  for (int32_t row = threadIdx.x >> w.log2_lanes; row < rows; row += step) {
+    const int32_t head = row >> w.log2_tokens, t = row & (tokens - 1);
+    const bool mine = t < n && 8 * piece < a.D;
+    const int64_t at = t < n ? place[t] : -2;
+    const int64_t off = int64_t(i0 + t) * r.token_stride + head * r.head_stride + 8 * piece;
+    if constexpr (WRITE) {
+      u32x4 k{}, v{};
+      if (mine) {
+        k = *reinterpret_cast<const u32x4*>(r.k + off);
+        v = *reinterpret_cast<const u32x4*>(r.v + off);
+      }
+      put<BF16, KB>(a, k, 0, at, head, piece, lanes, mine && at >= 0);
+      put<BF16, VB>(a, v, 1, at, head, piece, lanes, mine && at >= 0);
+    } else if (mine && at != -2) {
+      u32x4 k{}, v{};
+      if (at >= 0) {
+        k = get<BF16, KB>(a, 0, at, head, piece);
+        v = get<BF16, VB>(a, 1, at, head, piece);
+      }
+      *reinterpret_cast<u32x4*>(r.k + off) = k;
+      *reinterpret_cast<u32x4*>(r.v + off) = v;
+    }
+  }
+}
+
+template <bool WRITE>
+pkv_status_t launch_rows(const ServeArgs& s, const RowArgs& r, hipStream_t stream) {
+  RowWork w{0, 0};
+  while ((8 << w.log2_lanes) < s.D) ++w.log2_lanes;
+  // Enough rows for one pass of a workgroup; more while that leaves four workgroups to a compute unit.
+  const int32_t pass = kThreads >> w.log2_lanes;
+  while ((1 << w.log2_tokens) < kMostTokens &&
+         ((s.H << w.log2_tokens) < pass || (s.num_tokens >> w.log2_tokens) >= 2048))
+    ++w.log2_tokens;
+  const dim3 grid((uint32_t(s.num_tokens) + (1u << w.log2_tokens) - 1) >> w.log2_tokens);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, s, r, w); };
+  const int which = s.tag * 2 + (s.bf16 ? 1 : 0);
+  switch (which) {
+    case 0:  // 16-bit rows are copied as they are
+    case 1: go(rows_kernel<false, 16, 16, WRITE>); break;
+    case 2: go(rows_kernel<false, 8, 8, WRITE>); break;
+    case 3: go(rows_kernel<true, 8, 8, WRITE>); break;
+    case 4: go(rows_kernel<false, 8, 4, WRITE>); break;
+    case 5: go(rows_kernel<true, 8, 4, WRITE>); break;
+    case 6: go(rows_kernel<false, 4, 4, WRITE>); break;
+    default: go(rows_kernel<true, 4, 4, WRITE>); break;
+  }
+  return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_DEVICE;
+}
+
+// Whether every buffer of a call is memory of the current device.
+struct OnDevice {
+  int dev = -1;
+  bool ok = false;
+  OnDevice() { ok = hipGetDevice(&dev) == hipSuccess; }
+  bool has(const void* p) const {
+    if (!p) return true;
+    hipPointerAttribute_t a;
+    if (hipPointerGetAttributes(&a, p) != hipSuccess) {
+      (void)hipGetLastError();
+      return false;
+    }
+    return (a.type == hipMemoryTypeDevice || a.type == hipMemoryTypeManaged) && a.device == dev;
+  }
+  bool has(const ServeArgs& s) const {
+    return has(s.token_start) && has(s.kv_lens) && has(s.positions) && has(s.page_table) && has(s.k_cache) &&
+           has(s.v_cache) && has(s.codes) && has(s.scales);
+  }
+};
+
+template <bool WRITE>
+pkv_status_t rows_call(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch, const void* k,
+                       const void* v, int64_t token_stride, int64_t head_stride, void* hip_stream) {
+  ServeArgs s;
+  RowArgs r;
+  pkv_status_t st = serve_args(model, cache, batch, true, &s);
+  if (st == PKV_OK) st = row_args(s, k, v, token_stride, head_stride, &r);
+  if (st != PKV_OK || s.num_seqs == 0 || s.num_tokens == 0) return st;
+  const OnDevice here;
+  if (!here.ok) return PKV_ERR_DEVICE;
+  if (!here.has(s) || !here.has(r.k) || !here.has(r.v)) return PKV_ERR_INVALID_ARGUMENT;
+  return launch_rows<WRITE>(s, r, static_cast<hipStream_t>(hip_stream));
+}
+
+}  // namespace
+
+// One per head_dim, in objects of their own (attend.hip).
+pkv_status_t launch_attend_64(const ServeArgs& s, const AttendArgs& a, int64_t groups, hipStream_t stream);
+pkv_status_t launch_attend_128(const ServeArgs& s, const AttendArgs& a, int64_t groups, hipStream_t stream);
+pkv_status_t launch_attend_256(const ServeArgs& s, const AttendArgs& a, int64_t groups, hipStream_t stream);
+
+}  // namespace pkv
+
+extern "C" {
+
+pkv_status_t pkv_cache_append(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                              const void* k, const void* v, int64_t token_stride, int64_t head_stride,
+                              void* hip_stream) {
+  return pkv::rows_call<true>(model, cache, batch, k, v, token_stride, head_stride, hip_stream);
+}
+
+pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch, void* k,
+                            void* v, int64_t token_stride, int64_t head_stride, void* hip_stream) {
+  return pkv::rows_call<false>(model, cache, batch, k, v, token_stride, head_stride, hip_stream);
+}
+
+pkv_status_t pkv_attention(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                           const pkv_attention_t* attention, void* hip_stream) {
+  pkv::ServeArgs s;
+  pkv::AttendArgs a;
+  pkv_status_t st = pkv::serve_args(model, cache, batch, true, &s);
+  if (st == PKV_OK) st = pkv::attend_args(s, attention, true, &a);
+  if (st != PKV_OK || s.num_seqs == 0 || s.num_tokens == 0) return st;
+  const pkv::AttendLaunch l = pkv::attend_launch(s, a);
+  if (l.groups >= (int64_t(1) << 31)) return PKV_ERR_INVALID_ARGUMENT;
+  const pkv::OnDevice here;
+  if (!here.ok) return PKV_ERR_DEVICE;
+  if (!here.has(s) || !here.has(a.q) || !here.has(a.out) || !here.has(a.lse) || !here.has(a.part))
+    return PKV_ERR_INVALID_ARGUMENT;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (s.D == 64) return pkv::launch_attend_64(s, a, l.groups, stream);
+  if (s.D == 128) return pkv::launch_attend_128(s, a, l.groups, stream);
+  return pkv::launch_attend_256(s, a, l.groups, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,198 @@
+"""Serving from a paged cache: append rows, read them back, attend over them.
+
+Torch tensors in, torch tensors out; every step runs in libpkv
+(``include/pkv.h``), on the current stream.  A program keeps one
+:class:`PagedCache` per cache and one :class:`Batch` per set of buffers that it
+fills anew each step, and calls
+
+* :func:`append`     write new rows (quantised, where the cache holds codes);
+* :func:`read`       read rows back;
+* :func:`attention`  attention of new or recomputed rows over the cache, with an
+  optional sliding window and sinks.
+
+Nothing here waits for the device or copies from it.
+"""
+from __future__ import annotations
+
+import dataclasses
+from typing import Optional
+
+import torch
+
+from . import binding
+from .workloads import KEY_BITS, KV_PAIRED, KV_SEPARATE, OUT_BF16, OUT_FP16, TAG_FP16, VALUE_BITS
+
+_DTYPES = {torch.float16: OUT_FP16, torch.bfloat16: OUT_BF16}
+
+
+def _check(status: int, where: str) -> None:
+    if status != binding.PKV_OK:
+        raise binding.PkvError(status, where)
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+@dataclasses.dataclass
+class _Geometry:
+    num_layers: int
+    num_kv_heads: int
+    head_dim: int
+    page_size: int
+    pool_pages: int
+    out_dtype: int
+    kv_layout: int
+    block_tokens: int = 32  # of checkpoints; the serving calls have no use for it
+    rope_theta: float = 10000.0
+
+
+class PagedCache:
+    """A paged cache of all layers.
+
+    ``tag`` FP16: ``k_cache`` and ``v_cache`` of ``dtype``,
+    ``[L, pool_pages, P, H, D]`` (or without L for one layer), two tensors or
+    the K and V views of one paired cache (``device.alloc_caches``).  Other
+    tags: ``codes`` uint8 ``[L, pool_pages, H, bytes]`` and ``scales``
+    float16 ``[L, pool_pages, H, 2, P, 2]`` (or without L), allocated here when
+    not given (``pool_pages`` and ``device`` then say how many and where)."""
+
+    def __init__(self, num_kv_heads: int, head_dim: int, page_size: int, dtype, tag: int, codes=None, scales=None,
+                 k_cache=None, v_cache=None, num_layers: int = 1, pool_pages: Optional[int] = None, device="cuda"):
+        _need(dtype in _DTYPES, "dtype is float16 or bfloat16")
+        _need(0 <= tag < 4, "tag is a TAG_* value")
+        layout = KV_SEPARATE
+        if tag == TAG_FP16:
+            _need(k_cache is not None and v_cache is not None, "16-bit pages need k_cache and v_cache")
+            k = k_cache if k_cache.dim() == 5 else k_cache[None]
+            v = v_cache if v_cache.dim() == 5 else v_cache[None]
+            num_layers, pool_pages = k.shape[0], k.shape[1]
+            rows = (page_size, num_kv_heads, head_dim)
+            _need(k.shape == v.shape and tuple(k.shape[2:]) == rows, "caches are [L, pool_pages, P, H, D]")
+            _need(k.element_size() == 2 and v.element_size() == 2, "caches hold 16-bit values")
+            page = page_size * num_kv_heads * head_dim
+            inner = (num_kv_heads * head_dim, head_dim, 1)
+            if k.untyped_storage().data_ptr() == v.untyped_storage().data_ptr() and \
+                    v.data_ptr() == k.data_ptr() + 2 * page:
+                layout = KV_PAIRED
+            each = page * (2 if layout == KV_PAIRED else 1)
+            for t in (k, v):
+                _need(t.stride()[2:] == inner and (pool_pages == 1 or t.stride(1) == each) and
+                      (num_layers == 1 or t.stride(0) == pool_pages * each), "caches are whole or paired")
+            k_bytes = binding.cache_nbytes(k, v) if layout == KV_PAIRED else 2 * k.numel()
+            self.struct = binding.PkvPagedCache(tag, 0, k.data_ptr(), v.data_ptr(), k_bytes, None, 0, None, 0)
+        else:
+            size = page_size * head_dim * (KEY_BITS[tag] + VALUE_BITS[tag]) // 8
+            if codes is None and scales is None:
+                _need(pool_pages is not None, "pool_pages of a new cache")
+                codes = torch.zeros((num_layers, pool_pages, num_kv_heads, size), dtype=torch.uint8, device=device)
+                scales = torch.zeros((num_layers, pool_pages, num_kv_heads, 2, page_size, 2), dtype=torch.float16,
+                                     device=device)
+            _need(codes is not None and scales is not None, "codes and scales come together")
+            c = codes if codes.dim() == 4 else codes[None]
+            s = scales if scales.dim() == 6 else scales[None]
+            num_layers, pool_pages = c.shape[0], c.shape[1]
+            _need(c.dtype == torch.uint8 and s.dtype == torch.float16, "codes are uint8, scales float16")
+            _need(tuple(c.shape[2:]) == (num_kv_heads, size), f"codes are [L, pool_pages, H, {size}]")
+            _need(tuple(s.shape) == (num_layers, pool_pages, num_kv_heads, 2, page_size, 2),
+                  "scales are [L, pool_pages, H, 2, P, 2]")
+            _need(c.is_contiguous() and s.is_contiguous(), "codes and scales are contiguous")
+            self.struct = binding.PkvPagedCache(tag, 0, None, None, 0, c.data_ptr(), c.numel(), s.data_ptr(),
+                                                2 * s.numel())
+        self.codes, self.scales, self.k_cache, self.v_cache = codes, scales, k_cache, v_cache
+        self.tag, self.dtype, self.head_dim, self.num_kv_heads = tag, dtype, head_dim, num_kv_heads
+        self.num_layers, self.pool_pages, self.page_size = num_layers, pool_pages, page_size
+        self.device = (k_cache if tag == TAG_FP16 else codes).device
+        self.model = binding.make_model(_Geometry(num_layers, num_kv_heads, head_dim, page_size, pool_pages,
+                                                  _DTYPES[dtype], layout))
+        self._workspace = {}
+
+    def _at(self, layer: int) -> binding.PkvPagedCache:
+        self.struct.layer = layer
+        return self.struct
+
+    def workspace(self, nbytes: int, stream: int):
+        """Scratch memory of attention calls on one stream, grown as needed; calls on one stream follow each other."""
+        w = self._workspace.get(stream)
+        if w is None or w.numel() < nbytes:
+            w = self._workspace[stream] = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return w
+
+
+class Batch:
+    """The rows of a call (``pkv_batch_t``): int32 device tensors ``token_start`` ``[S + 1]``, ``kv_lens`` ``[S]``,
+    ``page_table`` ``[S, pages]`` and, for rows that are not the last ones, ``positions`` ``[num_tokens]``.  Their
+    contents may change from call to call; ``max_tokens`` and ``max_kv_len`` bound them (0: no bound known)."""
+
+    def __init__(self, token_start, kv_lens, page_table, num_tokens: int, positions=None, max_tokens: int = 0,
+                 max_kv_len: int = 0):
+        for t in (token_start, kv_lens, page_table, positions):
+            _need(t is None or (t.dtype == torch.int32 and t.is_contiguous()), "batch arrays are contiguous int32")
+        _need(page_table.dim() == 2 and page_table.shape[0] == kv_lens.numel(), "page_table is [S, pages]")
+        _need(token_start.numel() == kv_lens.numel() + 1, "token_start is [S + 1]")
+        _need(positions is None or positions.numel() == num_tokens, "positions is [num_tokens]")
+        self.keep = (token_start, kv_lens, page_table, positions)
+        self.num_tokens = num_tokens
+        self.struct = binding.PkvBatch(kv_lens.numel(), num_tokens, max_tokens, page_table.shape[1], max_kv_len,
+                                       token_start.data_ptr(), kv_lens.data_ptr(),
+                                       None if positions is None else positions.data_ptr(), page_table.data_ptr())
+
+
+def _rows(cache: PagedCache, batch: Batch, heads: int, *tensors) -> None:
+    """Rows of a call: [num_tokens, heads, D] of the cache's dtype, channels together, one stride for all."""
+    for t in tensors:
+        _need(t.dtype == cache.dtype and tuple(t.shape) == (batch.num_tokens, heads, cache.head_dim),
+              f"rows are [{batch.num_tokens}, {heads}, {cache.head_dim}] of {cache.dtype}")
+        _need(t.stride(2) == 1, "the channels of a row are consecutive")
+
+
+def _strides(t) -> tuple:
+    """Token and head stride; where a dimension has one element its stride says nothing."""
+    head = t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    return (t.stride(0) if t.shape[0] > 1 else t.shape[1] * head), head
+
+
+def append(cache: PagedCache, batch: Batch, k, v, layer: int = 0) -> None:
+    """Write rows ``k``, ``v`` ``[num_tokens, H, D]`` into the cache at the batch's positions."""
+    _rows(cache, batch, cache.num_kv_heads, k, v)
+    _need(_strides(k) == _strides(v), "k and v have the same strides")
+    _check(binding.pkv_cache_append_status(cache.model, cache._at(layer), batch.struct, k.data_ptr(), v.data_ptr(),
+                                           *_strides(k), torch.cuda.current_stream(cache.device).cuda_stream),
+           "pkv_cache_append")
+
+
+def read(cache: PagedCache, batch: Batch, layer: int = 0, out=None):
+    """The batch's rows of the cache, ``(k, v)`` of ``[num_tokens, H, D]`` (into ``out`` if given); a row that is not
+    there is zero, rows of no sequence are left as they are."""
+    shape = (batch.num_tokens, cache.num_kv_heads, cache.head_dim)
+    k, v = out if out is not None else (torch.empty(shape, dtype=cache.dtype, device=cache.device) for _ in range(2))
+    _rows(cache, batch, cache.num_kv_heads, k, v)
+    _need(_strides(k) == _strides(v), "k and v have the same strides")
+    _check(binding.pkv_cache_read_status(cache.model, cache._at(layer), batch.struct, k.data_ptr(), v.data_ptr(),
+                                         *_strides(k), torch.cuda.current_stream(cache.device).cuda_stream),
+           "pkv_cache_read")
+    return k, v
+
+
+def attention(cache: PagedCache, batch: Batch, q, scale: Optional[float] = None, window: int = 0, sinks: int = 0,
+              layer: int = 0, out=None, return_lse: bool = False):
+    """Attention of rows ``q`` ``[num_tokens, Hq, D]`` over the cache, causal by position: a row at position p sees
+    tokens t <= p and, with a window, those with p - t < window or t < sinks.  ``scale`` defaults to D ** -0.5.
+    Returns ``out`` ``[num_tokens, Hq, D]``, with ``return_lse`` also the rows' log-sum-exp, float32
+    ``[num_tokens, Hq]``.  A row that sees nothing gives 0 and -inf."""
+    heads = q.shape[1]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _rows(cache, batch, heads, q, out)
+    lse = torch.empty((batch.num_tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
+    a = binding.PkvAttention(heads, window, sinks, cache.head_dim ** -0.5 if scale is None else scale, q.data_ptr(),
+                             *_strides(q), out.data_ptr(), *_strides(out), lse.data_ptr() if return_lse else None,
+                             None, 0)
+    stream = torch.cuda.current_stream(cache.device).cuda_stream
+    struct = cache._at(layer)
+    nbytes = binding.pkv_attention_workspace(cache.model, struct, batch.struct, a)
+    if nbytes:
+        a.workspace, a.workspace_bytes = cache.workspace(nbytes, stream).data_ptr(), nbytes
+    _check(binding.pkv_attention_status(cache.model, struct, batch.struct, a, stream), "pkv_attention")
+    return (out, lse) if return_lse else out

@@ -1,0 +1,405 @@
+"""The serving calls on the GPU against the fp64 oracle: rows written into a paged cache (codes and scales bit for
+bit), read back, and attention over it at the sizes, masks and layouts where such kernels go wrong."""
+import numpy as np
+import pytest
+
+from paper_2609_26219_amd import binding as pb
+from paper_2609_26219_amd import workloads as wl
+from serving_cases import Case, check_attention, check_read
+
+pytestmark = pytest.mark.gpu
+
+FP16, K8V8, K8V4, K4V4 = range(4)
+HALF, BF16 = 0, 1
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as _t
+    if not _t.cuda.is_available():
+        pytest.skip("no GPU")
+    pb.load()
+    return _t
+
+
+def _dtype(torch, case):
+    return torch.bfloat16 if case.dtype else torch.float16
+
+
+def _up(torch, bits, case):
+    return torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).cuda().view(_dtype(torch, case))
+
+
+def _down(t):
+    import torch
+    return t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def _cache(torch, case):
+    """The case's cache on the device, other layers filled with 0x5A."""
+    from paper_2609_26219_amd import serving
+
+    def layered(a):
+        t = torch.full((case.layers, *a.shape), 0x5A, dtype=torch.uint8 if a.dtype == np.uint8 else torch.int16,
+                       device="cuda")
+        t[case.layer] = torch.from_numpy(a if a.dtype == np.uint8 else a.view(np.int16)).cuda()
+        return t
+
+    kw = dict(num_kv_heads=case.H, head_dim=case.D, page_size=case.P, dtype=_dtype(torch, case), tag=case.tag)
+    if case.tag == FP16:
+        k, v = (layered(a) for a in case.cache["kv"])
+        if case.paired:
+            both = torch.stack([k, v], 2)
+            k, v = both[:, :, 0], both[:, :, 1]
+        return serving.PagedCache(k_cache=k, v_cache=v, **kw)
+    return serving.PagedCache(codes=layered(case.cache["codes"]),
+                              scales=layered(case.cache["scales"]).view(torch.float16), **kw)
+
+
+def _batch(torch, case, bounds=True):
+    from paper_2609_26219_amd import serving
+    dev = lambda a: None if a is None else torch.from_numpy(a).cuda()  # noqa: E731
+    return serving.Batch(dev(case.start), dev(case.lens), dev(case.table), case.tokens, dev(case.positions),
+                         case.most_new if bounds else 0, case.most_kv if bounds else 0)
+
+
+def _state(torch, cache, case):
+    """The layer of the case as host arrays, and whether every other layer is untouched."""
+    if case.tag == FP16:
+        ts = [cache.k_cache, cache.v_cache]
+    else:
+        ts = [cache.codes, cache.scales]
+    host = [t.contiguous().view(torch.int16 if t.element_size() == 2 else torch.uint8).cpu().numpy() for t in ts]
+    others = all((np.delete(h, case.layer, 0) == 0x5A).all() for h in host)
+    return [h[case.layer] for h in host], others
+
+
+APPEND = [
+    # tag, dtype, H, D, P, lens, new
+    (K4V4, BF16, 2, 64, 16, (40, 3, 0, 17), (5, 3, 1, 17)),
+    (K8V4, HALF, 3, 128, 1, (9,), (9,)),
+    (K8V8, BF16, 1, 256, 4, (33, 1), (33, 1)),
+    (K4V4, HALF, 5, 96, 8, (21, 8), (7,)),
+    (K8V4, BF16, 2, 16, 2, (13,), (13,)),
+    (K4V4, HALF, 8, 512, 32, (70,), (70,)),
+    (FP16, BF16, 2, 128, 16, (31, 2), (9, 2)),
+    (FP16, HALF, 3, 48, 1, (5,), (5,)),
+    (K4V4, BF16, 8, 128, 64, tuple(range(1, 41)), (1,)),
+]
+
+
+@pytest.mark.parametrize("tag,dtype,H,D,P,lens,new", APPEND)
+@pytest.mark.parametrize("scattered", [False, True])
+def test_append_is_the_definition_bit_for_bit(torch, tag, dtype, H, D, P, lens, new, scattered):
+    from oracle import serving as os_
+    from paper_2609_26219_amd import serving
+
+    case = Case(11 + D, tag, dtype, H, 1, D, P, lens, new, scattered=scattered, holes=1, layers=3, layer=1)
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    serving.append(cache, batch, _up(torch, case.k, case), _up(torch, case.v, case), layer=1)
+    want = case.copy_of_cache()
+    os_.append(want, tag, P, case.where(), case.k, case.v, dtype)
+    got, others = _state(torch, cache, case)
+    names = want["kv"] if tag == FP16 else [want["codes"], want["scales"]]
+    for g, w in zip(got, names):
+        assert np.array_equal(g.view(w.dtype), w)
+    assert others
+
+
+def _special_rows(dtype):
+    """Rows whose range or codes sit where roundings go wrong: constants, signed zeros, extremes, ties, subnormals."""
+    rng = np.random.default_rng(5)
+    rows = [np.zeros(64), -np.zeros(64), np.full(64, 1.5), np.full(64, -2.0 ** -14), np.full(64, 65504.0 if not dtype else 65280.0)]
+    ramp = np.arange(64) / 4.0
+    rows += [ramp, -ramp, ramp * 2.0 ** -20, np.where(np.arange(64) % 2, 65280.0, -65280.0)]
+    rows += [np.concatenate([[-1.0, 6.5], rng.integers(0, 16, 62) * 0.5 - 0.75])]  # quotients at half-integers
+    rows += [np.concatenate([[0.0, 15.0], rng.integers(0, 30, 62) * 0.5])]
+    rows += [np.concatenate([[0.0, 255.0], rng.integers(0, 510, 62) * 0.5])]
+    rows += [rng.standard_normal(64) * 10.0 ** e for e in (-7, -5, -3, 2, 4)]
+    rows += [np.where(np.arange(64) % 3 == 0, -0.0, 2.0 ** -24)]
+    return np.clip(np.stack(rows), -65280, 65504 if not dtype else 65280)
+
+
+@pytest.mark.parametrize("tag", [K8V8, K4V4])
+@pytest.mark.parametrize("dtype", [HALF, BF16])
+def test_append_rows_at_the_edges_of_the_rule(torch, tag, dtype):
+    from oracle import serving as os_
+    from paper_2609_26219_amd import serving
+
+    rows = _special_rows(dtype)
+    n = len(rows)
+    case = Case(3, tag, dtype, 1, 1, 64, 16, (n,), (n,))
+    case.k, case.v = case.bits(rows)[:, None], case.bits(rows[::-1])[:, None]
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    serving.append(cache, batch, _up(torch, case.k, case), _up(torch, case.v, case))
+    want = case.copy_of_cache()
+    os_.append(want, tag, 16, case.where(), case.k, case.v, dtype)
+    (codes, scales), _ = _state(torch, cache, case)
+    assert np.array_equal(scales.view(np.uint16), want["scales"])
+    assert np.array_equal(codes, want["codes"])
+
+
+@pytest.mark.parametrize("tag,dtype,H,D,P,lens,new", APPEND)
+def test_read_back(torch, tag, dtype, H, D, P, lens, new):
+    from paper_2609_26219_amd import serving
+
+    case = Case(21 + D, tag, dtype, H, 1, D, P, lens, new, holes=1, layers=2, layer=1)
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    k, v = serving.read(cache, batch, layer=1)
+    for which, t in enumerate((k, v)):
+        check_read(case, _down(t), which)
+
+
+def test_rows_at_strides(torch):
+    """k and v as slices of one fused buffer, in and out; bytes between the rows stay."""
+    from oracle import serving as os_
+    from paper_2609_26219_amd import serving
+
+    case = Case(77, K8V4, BF16, 2, 1, 64, 16, (40, 9), (11, 9))
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    fused = torch.full((case.tokens, 7, 80), -3.0, dtype=torch.bfloat16, device="cuda")
+    k, v = fused[:, 1:3, :64], fused[:, 4:6, :64]
+    k.copy_(_up(torch, case.k, case))
+    v.copy_(_up(torch, case.v, case))
+    serving.append(cache, batch, k, v)
+    want = case.copy_of_cache()
+    os_.append(want, K8V4, 16, case.where(), case.k, case.v, BF16)
+    (codes, scales), _ = _state(torch, cache, case)
+    assert np.array_equal(codes, want["codes"]) and np.array_equal(scales.view(np.uint16), want["scales"])
+    case.cache = want
+    fused.fill_(-3.0)
+    serving.read(cache, batch, out=(k, v))
+    check_read(case, _down(k), 0)
+    check_read(case, _down(v), 1)
+    mask = torch.ones_like(fused, dtype=torch.bool)
+    mask[:, 1:3, :64] = False
+    mask[:, 4:6, :64] = False
+    assert (fused[mask] == -3.0).all()
+
+
+def test_rows_of_no_sequence_are_left_alone(torch):
+    from paper_2609_26219_amd import serving
+
+    case = Case(78, K4V4, HALF, 2, 2, 64, 16, (20, 30), (4, 6))
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    batch.keep[0].copy_(torch.tensor([2, 5, 8], dtype=torch.int32))  # rows 0, 1, 8 and 9 belong to nobody
+    before = [t.clone() for t in (cache.codes, cache.scales)]
+    k = torch.full((10, 2, 64), 7.0, dtype=torch.float16, device="cuda")
+    v = k.clone()
+    serving.read(cache, batch, out=(k, v))
+    out = torch.full((10, 4, 64), 7.0, dtype=torch.float16, device="cuda")
+    serving.attention(cache, batch, _up(torch, case.q, case), out=out)
+    for t in (k, v, out):
+        assert (t[[0, 1, 8, 9]] == 7.0).all() and (t[2:8] != 7.0).any()
+    case.start = np.array([2, 5, 8], np.int32)
+    check_read(case, _down(k), 0)
+    serving.append(cache, batch, k, v)  # nothing but the six rows
+    changed = (cache.scales.view(torch.int16) != before[1].view(torch.int16)).any(-1).any(3).any(2)[0]
+    assert {tuple(at) for at in changed.nonzero().tolist()} == {(p, slot) for _, _, p, slot in case.where() if p >= 0}
+
+
+ATTEND = [
+    # tag, dtype, H, group, D, P, lens, new, scattered, window, sinks
+    (K4V4, HALF, 2, 4, 64, 16, (1,), (1,), False, 0, 0),
+    (K4V4, BF16, 2, 4, 128, 16, (77, 0, 5, 32, 33, 31), (1,), False, 0, 0),
+    (K4V4, BF16, 1, 1, 256, 32, (65, 130), (2, 3), False, 0, 0),
+    (K8V4, HALF, 2, 3, 128, 16, (50, 200), (17, 40), False, 0, 0),
+    (K8V8, BF16, 1, 5, 64, 64, (100,), (100,), False, 0, 0),
+    (K4V4, HALF, 2, 2, 128, 1, (45, 3), (3, 3), False, 0, 0),
+    (K8V4, BF16, 1, 8, 64, 2, (39,), (5,), False, 9, 2),
+    (K4V4, HALF, 1, 2, 256, 8, (70, 12), (12,), False, 16, 4),
+    (K4V4, BF16, 2, 4, 128, 16, (300, 40), (1,), False, 64, 4),
+    (K8V8, HALF, 2, 1, 128, 16, (150,), (33,), True, 0, 0),
+    (FP16, BF16, 2, 4, 128, 16, (77, 0, 5, 32), (1,), False, 0, 0),
+    (FP16, HALF, 1, 4, 64, 16, (300, 17), (40, 17), False, 50, 3),
+    (FP16, BF16, 2, 2, 256, 4, (40, 90), (8, 1), False, 0, 0),
+    (FP16, BF16, 1, 16, 128, 32, (200,), (20,), True, 30, 40),
+    (FP16, HALF, 2, 1, 128, 1, (33,), (33,), False, 5, 0),
+    (FP16, BF16, 1, 1, 64, 64, (513,), (1,), False, 1, 0),
+    (FP16, HALF, 1, 2, 128, 16, (290,), (290,), False, 0, 0),
+    (K4V4, BF16, 1, 4, 128, 16, (1500, 700), (1,), False, 0, 0),
+    (FP16, BF16, 1, 4, 128, 16, (1500, 10), (1,), False, 200, 1000),
+    (K8V4, BF16, 1, 2, 128, 16, (400,), (130,), True, 40, 5),
+]
+
+
+@pytest.mark.parametrize("tag,dtype,H,group,D,P,lens,new,scattered,window,sinks", ATTEND)
+@pytest.mark.parametrize("holes", [0, 2])
+def test_attention(torch, tag, dtype, H, group, D, P, lens, new, scattered, window, sinks, holes):
+    from paper_2609_26219_amd import serving
+
+    case = Case(31 + D + window, tag, dtype, H, group, D, P, lens, new, scattered=scattered, holes=holes, layers=2,
+                layer=1, paired=tag == FP16 and P == 16, wide=holes)
+    cache = _cache(torch, case)
+    for bounds in (True, False):
+        out, lse = serving.attention(cache, _batch(torch, case, bounds), _up(torch, case.q, case), window=window,
+                                     sinks=sinks, layer=1, return_lse=True)
+        check_attention(case, _down(out), lse.cpu().numpy(), window, sinks)
+
+
+@pytest.mark.parametrize("tag,values", [(K4V4, 1e-3), (K4V4, 300.0), (K8V4, 1e-5), (FP16, 1e-4)])
+@pytest.mark.parametrize("dtype", [HALF, BF16])
+def test_attention_of_small_and_large_values(torch, tag, values, dtype):
+    """Scales near binary16's ends, scores far apart or all alike."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(41, tag, dtype, 1, 4, 128, 16, (90, 400), (3, 1), scale_of_values=values)
+    scale = 0.1 / values ** 2 if values < 1 else 1e-5
+    out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), scale=scale,
+                                 return_lse=True)
+    check_attention(case, _down(out), lse.cpu().numpy(), scale=scale)
+
+
+def test_attention_at_positions_past_the_cache(torch):
+    """Positions beyond kv_lens: only what is cached and in the window counts, so some rows keep their sinks alone or
+    see nothing; negative positions see nothing."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(43, FP16, BF16, 1, 2, 64, 16, (40, 70), (5, 4))
+    case.positions = np.array([39, 100, 45, -1, 0, 500, 69, -2 ** 31, 2 ** 31 - 1], np.int32)
+    for window, sinks in ((0, 0), (20, 3), (20, 0), (7, 100)):
+        out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), window=window,
+                                     sinks=sinks, return_lse=True)
+        check_attention(case, _down(out), lse.cpu().numpy(), window, sinks)
+
+
+def test_attention_at_strides_and_into_out(torch):
+    from paper_2609_26219_amd import serving
+
+    case = Case(47, K4V4, BF16, 2, 2, 128, 16, (60, 9), (2, 9))
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    fused = torch.full((case.tokens, 9, 136), 2.0, dtype=torch.bfloat16, device="cuda")
+    q, out = fused[:, :4, :128], fused[:, 5:, :128]
+    q.copy_(_up(torch, case.q, case))
+    got, lse = serving.attention(cache, batch, q, out=out, return_lse=True)
+    assert got is out
+    check_attention(case, _down(out), lse.cpu().numpy())
+    assert (fused[:, 4] == 2.0).all() and (fused[:, :, 128:] == 2.0).all()
+
+
+def test_infinities_and_nans_in_unseen_places_do_not_matter(torch):
+    """Values that no row sees, in pages that rows do see: past the end, before the window, behind the sinks."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(53, FP16, HALF, 1, 4, 64, 16, (100,), (1,))
+    clean = case.copy_of_cache()
+    for t in list(range(5, 60)):
+        p, s = case.table[0, t // 16], t % 16
+        for a in case.cache["kv"]:
+            a[p, s] = [0x7E00, 0x7C00, 0xFC00][t % 3]
+    dirty, case.cache = case.cache, clean
+    window, sinks = 40, 5
+    batch = _batch(torch, case)
+    case.cache = dirty
+    out, lse = serving.attention(_cache(torch, case), batch, _up(torch, case.q, case), window=window, sinks=sinks,
+                                 return_lse=True)
+    case.cache = clean
+    check_attention(case, _down(out), lse.cpu().numpy(), window, sinks)
+
+
+def test_cache_past_four_gibibytes(torch):
+    """Pages whose byte offsets pass 32 bits, quantised and 16-bit."""
+    from paper_2609_26219_amd import serving
+
+    for tag in (K4V4, FP16):
+        case = Case(59, tag, BF16, 8, 2, 128, 16, (50, 20), (1,))
+        far = 700_000 if tag != FP16 else 300_000  # 16 KiB of codes, 64 KiB of K and V a page
+        kw = dict(num_kv_heads=8, head_dim=128, page_size=16, dtype=torch.bfloat16, tag=tag)
+        up = lambda a: torch.from_numpy(a if a.dtype == np.uint8 else a.view(np.int16)).cuda()  # noqa: E731
+        if tag == FP16:
+            kv = torch.empty((far + case.pool, 2, 16, 8, 128), dtype=torch.bfloat16, device="cuda")
+            for which in range(2):
+                kv[far:, which] = up(case.cache["kv"][which]).view(torch.bfloat16)
+            cache = serving.PagedCache(k_cache=kv[:, 0], v_cache=kv[:, 1], **kw)
+        else:
+            codes = torch.empty((far + case.pool, 8, 16 * 128), dtype=torch.uint8, device="cuda")
+            scales = torch.empty((far + case.pool, 8, 2, 16, 2), dtype=torch.float16, device="cuda")
+            codes[far:], scales[far:] = up(case.cache["codes"]), up(case.cache["scales"]).view(torch.float16)
+            cache = serving.PagedCache(codes=codes, scales=scales, **kw)
+        batch = _batch(torch, case)
+        table = batch.keep[2]
+        table.copy_(torch.where(table >= 0, table + far, table))
+        out, lse = serving.attention(cache, batch, _up(torch, case.q, case), return_lse=True)
+        check_attention(case, _down(out), lse.cpu().numpy())
+        k, v = serving.read(cache, batch)
+        check_read(case, _down(k), 0)
+        check_read(case, _down(v), 1)
+        serving.append(cache, batch, k, v)
+        again, _ = serving.read(cache, batch)
+        assert (again.float() - k.float()).abs().max() <= 0.6  # one more quantisation: within a 4-bit step
+        del cache
+        torch.cuda.empty_cache()
+
+
+def test_other_stream_and_graph(torch):
+    """On a side stream, and replayed from a graph while lengths, tables and rows change in place."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(61, K4V4, BF16, 2, 4, 128, 16, (900, 300), (1,))
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    q, k, v = (_up(torch, b, case) for b in (case.q, case.k, case.v))
+
+    def step(out):
+        serving.append(cache, batch, k, v)
+        return serving.attention(cache, batch, q, out=out)
+
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(out)
+    side.synchronize()
+    from oracle import serving as os_
+    os_.append(case.cache, K4V4, 16, case.where(), case.k, case.v, BF16)
+    exact = case.attend()
+    check = lambda: check_attention(case, _down(out), exact[1].astype(np.float32))  # noqa: E731
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(out)
+    for lens in ((900, 300), (37, 299), (512, 1)):
+        out.zero_()
+        case.lens = np.array(lens, np.int32)
+        batch.keep[1].copy_(torch.tensor(lens, dtype=torch.int32))
+        rng = np.random.default_rng(lens[0])
+        case.q = case.bits(rng.standard_normal(case.q.shape))
+        case.k = case.bits(rng.standard_normal(case.k.shape))
+        q.copy_(_up(torch, case.q, case))
+        k.copy_(_up(torch, case.k, case))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        os_.append(case.cache, K4V4, 16, case.where(), case.k, case.v, BF16)
+        exact = case.attend()
+        check()
+
+
+def test_same_inputs_same_bits(torch):
+    from paper_2609_26219_amd import serving
+
+    case = Case(67, K8V4, BF16, 2, 4, 128, 16, (1400, 90), (1,))
+    cache, batch, q = _cache(torch, case), _batch(torch, case), _up(torch, case.q, case)
+    first, lse = serving.attention(cache, batch, q, return_lse=True)
+    for _ in range(3):
+        again, lse2 = serving.attention(cache, batch, q, return_lse=True)
+        assert torch.equal(first, again) and torch.equal(lse, lse2)
+
+
+def test_refusals_on_the_device(torch):
+    """Host memory, another tag's buffers and short buffers are refused before anything is enqueued."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(71, K4V4, BF16, 2, 2, 64, 16, (20,), (2,))
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    q = _up(torch, case.q, case)
+    with pytest.raises(pb.PkvError) as e:
+        serving.attention(cache, batch, q, out=torch.empty(q.shape, dtype=q.dtype))
+    assert e.value.status == pb.PKV_ERR_INVALID_ARGUMENT
+    host = torch.from_numpy(case.lens)
+    batch.struct.kv_lens = host.data_ptr()
+    with pytest.raises(pb.PkvError):
+        serving.attention(cache, batch, q)
+    with pytest.raises(ValueError):
+        serving.attention(cache, batch, q.float())
+    with pytest.raises(ValueError):
+        serving.append(cache, batch, q, q)

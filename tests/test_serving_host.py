@@ -1,0 +1,167 @@
+"""Host half of the serving calls, without a GPU: sizes, refusals before any HIP call, and the oracle's attention against
+a dense computation."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2609_26219_amd import binding as pb
+from paper_2609_26219_amd import workloads as wl
+from serving_cases import Case
+
+OK, BAD, TAG = pb.PKV_OK, pb.PKV_ERR_INVALID_ARGUMENT, pb.PKV_ERR_BAD_TAG
+
+
+def _gpu_present():
+    try:
+        import torch
+        return torch.cuda.is_available()
+    except Exception:  # pragma: no cover
+        return False
+
+
+def _shape(**kw):
+    base = dict(num_layers=2, num_kv_heads=4, head_dim=128, block_tokens=32, page_size=16, pool_pages=10,
+                rope_theta=1e4, out_dtype=1)
+    return wl.Shape(**{**base, **kw})
+
+
+A = 1 << 20  # an aligned address that no call gets to use: every call below fails or has nothing to do
+
+
+def _call(shape=None, cache=None, batch=None, attention=None, rows=None, which="attention"):
+    s = shape or _shape()
+    cb, sb = pb.pkv_cache_size(s, 3) if pb.load().pkv_cache_size(
+        ctypes.byref(pb.make_model(s)), 3, ctypes.byref(ctypes.c_uint64()), ctypes.byref(ctypes.c_uint64())) == OK else (0, 0)
+    c = dict(tag=3, layer=1, k_cache=None, v_cache=None, cache_bytes=0, codes=A, code_bytes=cb, scales=A, scale_bytes=sb)
+    c.update(cache or {})
+    b = dict(num_seqs=2, num_tokens=0, max_tokens=0, pages_per_seq=4, max_kv_len=0, token_start=A, kv_lens=A,
+             positions=None, page_table=A)
+    b.update(batch or {})
+    m, c, b = pb.make_model(s), pb.PkvPagedCache(**c), pb.PkvBatch(**b)
+    if which == "attention":
+        a = dict(num_q_heads=8, window=0, sinks=0, scale=0.1, q=A, q_token_stride=1024, q_head_stride=128, out=A,
+                 out_token_stride=1024, out_head_stride=128, lse=None, workspace=A, workspace_bytes=1 << 40)
+        a.update(attention or {})
+        return pb.pkv_attention_status(m, c, b, pb.PkvAttention(**a))
+    r = dict(k=A, v=A, token_stride=512, head_stride=128)
+    r.update(rows or {})
+    f = pb.pkv_cache_append_status if which == "append" else pb.pkv_cache_read_status
+    return f(m, c, b, r["k"], r["v"], r["token_stride"], r["head_stride"])
+
+
+@pytest.mark.parametrize("which", ["attention", "append", "read"])
+def test_nothing_to_do_is_ok(which):
+    assert _call(which=which) == OK
+    assert _call(which=which, batch=dict(num_seqs=0, num_tokens=5)) == OK
+
+
+CACHE = [
+    (dict(cache=dict(tag=4)), TAG), (dict(cache=dict(tag=-1)), TAG), (dict(cache=dict(layer=2)), BAD),
+    (dict(cache=dict(layer=-1)), BAD), (dict(cache=dict(codes=None)), BAD), (dict(cache=dict(scales=None)), BAD),
+    (dict(cache=dict(codes=A + 8)), BAD), (dict(cache=dict(scales=A + 4)), BAD), (dict(cache=dict(code_bytes=100)), BAD),
+    (dict(cache=dict(scale_bytes=100)), BAD), (dict(cache=dict(tag=2)), BAD), (dict(cache=dict(tag=0)), BAD),
+    (dict(cache=dict(tag=0, k_cache=A, v_cache=A + (1 << 30), cache_bytes=8)), BAD),
+    (dict(cache=dict(tag=0, k_cache=A, v_cache=A, cache_bytes=1 << 30)), BAD),
+    (dict(batch=dict(num_seqs=-1)), BAD), (dict(batch=dict(num_tokens=-1)), BAD), (dict(batch=dict(max_tokens=-1)), BAD),
+    (dict(batch=dict(pages_per_seq=0)), BAD), (dict(batch=dict(max_kv_len=-1)), BAD),
+    (dict(batch=dict(pages_per_seq=(1 << 26) + 1)), BAD),
+    (dict(batch=dict(num_tokens=3, token_start=None)), BAD), (dict(batch=dict(num_tokens=3, kv_lens=None)), BAD),
+    (dict(batch=dict(num_tokens=3, page_table=None)), BAD), (dict(batch=dict(num_tokens=3, kv_lens=A + 2)), BAD),
+    (dict(batch=dict(num_tokens=3, positions=A + 1)), BAD),
+    (dict(shape=_shape(page_size=12)), BAD), (dict(shape=_shape(num_layers=0)), BAD),
+]
+
+
+@pytest.mark.parametrize("kw,status", CACHE)
+@pytest.mark.parametrize("which", ["attention", "append", "read"])
+def test_cache_and_batch_refusals(kw, status, which):
+    assert _call(which=which, **kw) == status
+
+
+@pytest.mark.parametrize("rows", [dict(token_stride=4), dict(head_stride=64), dict(head_stride=132), dict(token_stride=-8),
+                                  dict(k=A + 8), dict(v=A + 2), dict(k=None), dict(v=None)])
+@pytest.mark.parametrize("which", ["append", "read"])
+def test_row_refusals(rows, which):
+    assert _call(which=which, batch=dict(num_tokens=1), rows=rows) == BAD
+
+
+@pytest.mark.parametrize("attention", [dict(num_q_heads=6), dict(num_q_heads=0), dict(window=-1), dict(sinks=-1),
+                                       dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+                                       dict(scale=float("inf")), dict(q=None), dict(out=None), dict(q=A + 8),
+                                       dict(out=A + 2), dict(lse=A + 1), dict(q_token_stride=3), dict(out_head_stride=64),
+                                       dict(workspace=None), dict(workspace_bytes=8), dict(workspace=A + 8)])
+def test_attention_refusals(attention):
+    kw = dict(batch=dict(num_tokens=2, max_tokens=1, pages_per_seq=1000), attention=attention)
+    assert _call(**kw) == BAD
+
+
+@pytest.mark.parametrize("dim", [16, 32, 96, 192, 512])
+def test_attention_head_dims(dim):
+    assert _call(shape=_shape(head_dim=dim)) == BAD
+
+
+def test_too_many_rows_are_refused():
+    assert _call(batch=dict(num_tokens=(1 << 28))) == BAD
+
+
+@pytest.mark.parametrize("tag", range(4))
+def test_sizes(tag):
+    s = _shape(num_layers=3, head_dim=96, page_size=8, pool_pages=7)
+    cb, sb = pb.pkv_cache_size(s, tag)
+    rows = 3 * 7 * 8 * 4
+    assert cb == (0 if tag == 0 else rows * 96 * (wl.KEY_BITS[tag] + wl.VALUE_BITS[tag]) // 8)
+    assert sb == (0 if tag == 0 else rows * 8)
+    lib = pb.load()
+    out = ctypes.c_uint64()
+    assert lib.pkv_cache_size(ctypes.byref(pb.make_model(s)), tag, None, ctypes.byref(out)) == BAD
+    assert lib.pkv_cache_size(ctypes.byref(pb.make_model(s)), 9, ctypes.byref(out), ctypes.byref(out)) == TAG
+
+
+def test_workspace_covers_few_rows_and_none_where_rows_fill_the_gpu():
+    s = _shape(pool_pages=4096)
+    m = pb.make_model(s)
+    c = pb.PkvPagedCache(tag=3)
+    a = pb.PkvAttention(num_q_heads=8, scale=0.1)
+    few = pb.PkvBatch(num_seqs=1, num_tokens=1, max_tokens=1, pages_per_seq=4096)
+    nbytes = pb.pkv_attention_workspace(m, c, few, a)
+    per = 8 * (128 + 2) * 4
+    assert nbytes > 0 and nbytes % per == 0 and nbytes // per <= 4096 * 16 // 32
+    many = pb.PkvBatch(num_seqs=512, num_tokens=512 * 64, max_tokens=64, pages_per_seq=4096)
+    assert pb.pkv_attention_workspace(m, c, many, a) == 0
+
+
+def test_oracle_against_a_dense_computation():
+    """The oracle's attention against softmax over whole rows built another way (16-bit cache, no unmapped pages)."""
+    case = Case(5, 0, 0, 2, 3, 64, 8, (37, 9), (6, 9))
+    out, lse, *_ = case.attend(window=11, sinks=2)
+    at = 0
+    for s, (n, m) in enumerate(zip((37, 9), (6, 9))):
+        k, v = (np.stack([a[case.table[s, t // 8], t % 8] for t in range(n)]).view(np.float16).astype(np.float64)
+                for a in case.cache["kv"])
+        q = case.q[at:at + m].view(np.float16).astype(np.float64)
+        score = np.einsum("ihd,thd->iht", q, np.repeat(k, 3, 1)) / 8.0
+        pos, tok = np.arange(n - m, n)[:, None], np.arange(n)[None]
+        ok = (tok <= pos) & ((pos - tok < 11) | (tok < 2))
+        score[~np.broadcast_to(ok[:, None], score.shape)] = -np.inf
+        w = np.exp(score)
+        assert np.allclose(np.log(w.sum(-1)), lse[at:at + m], atol=1e-12)
+        assert np.allclose(np.einsum("iht,thd->ihd", w / w.sum(-1, keepdims=True), np.repeat(v, 3, 1)), out[at:at + m],
+                           atol=1e-12)
+        at += m
+
+
+def test_oracle_rows_by_hand():
+    """A row 0, 1, .. 15 in 4 bits: zero 0, scale 1, codes the values; nibbles low first."""
+    from oracle import serving as os_
+    codes, scale, zero = os_.quantise_row(np.arange(16.0), 4)
+    assert (scale, zero) == (1.0, 0.0) and list(codes) == list(range(16))
+    cache = {"codes": np.zeros((1, 1, 32), np.uint8), "scales": np.zeros((1, 1, 2, 2, 2), np.uint16)}
+    bits = np.arange(16, dtype=np.float16).view(np.uint16)[None, None]
+    os_.append(cache, 3, 2, [(0, 1, 0, 1)], bits, bits, 0)
+    assert list(cache["codes"][0, 0, 8:16]) == [0x10, 0x32, 0x54, 0x76, 0x98, 0xBA, 0xDC, 0xFE]
+    assert list(cache["codes"][0, 0, 24:32]) == [0x10, 0x32, 0x54, 0x76, 0x98, 0xBA, 0xDC, 0xFE]
+    assert not cache["codes"][0, 0, :8].any() and not cache["codes"][0, 0, 16:24].any()
+    assert cache["scales"][0, 0, 0, 1, 0] == 0x3C00 and cache["scales"][0, 0, 0, 0, 0] == 0
+    x, free, mid = os_.row(cache, 3, 2, 0, 0, 0, 1, 0)
+    assert list(x) == list(range(16)) and list(free) == [abs(i - 8) for i in range(16)] and mid == 8.0
