@@ -54,6 +54,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kQkSteps = D / 32;  // matrix instructions of one S^T
 constexpr int kChannels = D / 16; // channels of a lane in V, matrix instructions of one O^T update
+constexpr int kMostRowTiles = most_row_tiles(D);
 constexpr float kInf = __builtin_inff();
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -153,10 +154,13 @@ __device__ __forceinline__ uint32_t v_pair(const uint32_t* a, const uint32_t* b,
   }
 }
 
-// Sums and maxima over the four lanes (c) of a column.
+// Sums and maxima over the four lanes (c) of a column: the halves of the wave
+// exchanged, then the neighbouring rows of 16 lanes.
 __device__ __forceinline__ float over_c_max(float v) {
-  v = __builtin_fmaxf(v, __shfl_xor(v, 16));
-  return __builtin_fmaxf(v, __shfl_xor(v, 32));
+  u32x2 w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __builtin_fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __builtin_fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 }
 __device__ __forceinline__ float over_c_sum(float v) {
   v += __shfl_xor(v, 16);
@@ -173,75 +177,110 @@ __device__ __forceinline__ int over_x_min(int v) {
 
 // What a tile's lane holds of the cache: for each half of 16 tokens its piece of one
 // token's keys, of four tokens' values, and those four tokens' (scale, zero).
-template <int KB, int VB>
-struct Piece {
-  static constexpr int kKBytes = D / 4 * KB / 8, kVBytes = kChannels * VB / 8;
-  static constexpr int kKWords = kKBytes / 4, kVWords = (kVBytes + 3) / 4;
-  uint32_t k[2][kKWords];
-  uint32_t v[2][4][kVWords];
-  uint32_t ks[2][4], vs[2][4];
+template <int BITS>
+struct Keys {
+  static constexpr int kBytes = D / 4 * BITS / 8;
+  uint32_t w[2][kBytes / 4];
+  uint32_t scale[2][4];
+};
+template <int BITS>
+struct Values {
+  static constexpr int kBytes = kChannels * BITS / 8, kWords = (kBytes + 3) / 4;
+  uint32_t w[2][4][kWords];
+  uint32_t scale[2][4];
 };
 
 // Physical page of a logical one, or -1.
-__device__ __forceinline__ int64_t page_of(const ServeArgs& s, const int32_t* table, int64_t at) {
+__device__ __forceinline__ int32_t page_of(const ServeArgs& s, const int32_t* table, int32_t at) {
   if (at >= s.pages_per_seq) return -1;
   const int32_t p = table[at];
   return p >= 0 && p < s.pool_pages ? p : -1;
 }
 
-// Loads the tile of tokens [t0, t0 + 32).  Returns a mask of the lane's tokens that are
-// there (bit 4u + i: token t0 + 16u + 4c + i); the others are loaded from page
-// 0, which exists.  WHOLE: pages hold 16 slots or more, so each half of the
-// tile lies on one page.
-template <int KB, int VB, bool WHOLE>
-__device__ __forceinline__ uint32_t load_tile(const ServeArgs& s, const int32_t* table, int head, int32_t t0, int c,
-                                              int x, Piece<KB, VB>& p) {
-  uint32_t there = 0;
+// Bytes into a lane's piece from a base that the wave shares.
+template <int BYTES>
+__device__ __forceinline__ void load_at(uint32_t* to, const void* base, uint32_t off) {
+  load_bytes<BYTES>(to, static_cast<const char*>(base) + off);
+}
+
+// Load the keys or values of the tile of tokens [t0, t0 + 32); tokens that are not
+// there are loaded from page 0, which exists.  WHOLE: pages hold 16 slots or more, so
+// each half of the tile lies on one page (`pages`, or -1).
+template <int BITS, bool WHOLE>
+__device__ __forceinline__ void load_keys(const ServeArgs& s, const int32_t* table, int head, int32_t t0,
+                                          const int32_t (&pages)[2], int c, int x, Keys<BITS>& p) {
   const int32_t slots = (1 << s.log2P) - 1;
-  auto k_at = [&](int64_t page, int32_t slot) -> const void* {
-    if constexpr (KB == 16)
-      return s.k_cache + page * s.page_stride + int64_t(slot) * s.H * D + head * D + c * (D / 4);
-    else
-      return s.codes + page * s.page_stride + head * s.head_stride + int64_t(slot) * (D * KB / 8) + c * (D / 4 * KB / 8);
+  const uint32_t row = BITS == 16 ? uint32_t(s.H) * D * 2 : D * BITS / 8, mine = c * Keys<BITS>::kBytes;
+  auto first_of = [&](int64_t page) -> const char* {
+    if constexpr (BITS == 16) return reinterpret_cast<const char*>(s.k_cache + page * s.page_stride + head * D);
+    return reinterpret_cast<const char*>(s.codes + page * s.page_stride + head * s.head_stride);
   };
-  auto v_at = [&](int64_t page, int32_t slot) -> const void* {
-    if constexpr (VB == 16)
-      return s.v_cache + page * s.page_stride + int64_t(slot) * s.H * D + head * D + x * kChannels;
-    else
-      return s.codes + page * s.page_stride + head * s.head_stride + s.v_offset + int64_t(slot) * (D * VB / 8) +
-             x * (kChannels * VB / 8);
-  };
-  auto scale_at = [&](int64_t page, int which, int32_t slot) -> const uint32_t* {
-    return s.scales + page * s.scale_stride + ((int64_t(head) * 2 + which) << s.log2P) + slot;
-  };
+  auto scales_of = [&](int64_t page) { return s.scales + page * s.scale_stride + ((int64_t(head) * 2) << s.log2P); };
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int32_t t = t0 + 16 * u;
     if constexpr (WHOLE) {
-      int64_t page = page_of(s, table, t >> s.log2P);
-      there |= (page >= 0 ? 0xFu : 0u) << (4 * u);
-      page = page >= 0 ? page : 0;
-      const int32_t slot = t & slots;
-      load_bytes<Piece<KB, VB>::kKBytes>(p.k[u], k_at(page, slot + x));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) load_bytes<Piece<KB, VB>::kVBytes>(p.v[u][i], v_at(page, slot + 4 * c + i));
-      if constexpr (KB != 16) load_bytes<16>(p.ks[u], scale_at(page, 0, slot + 4 * c));
-      if constexpr (VB != 16) load_bytes<16>(p.vs[u], scale_at(page, 1, slot + 4 * c));
+      const int32_t page = pages[u] >= 0 ? pages[u] : 0;
+      const int64_t slot = t & slots;
+      load_at<Keys<BITS>::kBytes>(p.w[u], first_of(page) + slot * row, x * row + mine);
+      if constexpr (BITS != 16) load_at<16>(p.scale[u], scales_of(page) + slot, 16 * c);
     } else {
-      const int64_t kp = page_of(s, table, (t + x) >> s.log2P);
-      load_bytes<Piece<KB, VB>::kKBytes>(p.k[u], k_at(kp >= 0 ? kp : 0, (t + x) & slots));
+      const int32_t page = page_of(s, table, (t + x) >> s.log2P);
+      load_bytes<Keys<BITS>::kBytes>(p.w[u], first_of(page >= 0 ? page : 0) + int64_t((t + x) & slots) * row + mine);
+      if constexpr (BITS != 16) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int32_t tok = t + 4 * c + i, slot = tok & slots;
-        int64_t page = page_of(s, table, tok >> s.log2P);
-        there |= (page >= 0 ? 1u : 0u) << (4 * u + i);
-        page = page >= 0 ? page : 0;
-        load_bytes<Piece<KB, VB>::kVBytes>(p.v[u][i], v_at(page, slot));
-        if constexpr (KB != 16) p.ks[u][i] = *scale_at(page, 0, slot);
-        if constexpr (VB != 16) p.vs[u][i] = *scale_at(page, 1, slot);
+        for (int i = 0; i < 4; ++i) {
+          const int32_t tok = t + 4 * c + i, at = page_of(s, table, tok >> s.log2P);
+          p.scale[u][i] = scales_of(at >= 0 ? at : 0)[tok & slots];
+        }
       }
     }
   }
+}
+
+template <int BITS, bool WHOLE>
+__device__ __forceinline__ void load_values(const ServeArgs& s, const int32_t* table, int head, int32_t t0,
+                                            const int32_t (&pages)[2], int c, int x, Values<BITS>& p) {
+  const int32_t slots = (1 << s.log2P) - 1;
+  const uint32_t row = BITS == 16 ? uint32_t(s.H) * D * 2 : D * BITS / 8, mine = x * Values<BITS>::kBytes;
+  auto first_of = [&](int64_t page) -> const char* {
+    if constexpr (BITS == 16) return reinterpret_cast<const char*>(s.v_cache + page * s.page_stride + head * D);
+    return reinterpret_cast<const char*>(s.codes + page * s.page_stride + head * s.head_stride + s.v_offset);
+  };
+  auto scales_of = [&](int64_t page) { return s.scales + page * s.scale_stride + ((int64_t(head) * 2 + 1) << s.log2P); };
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int32_t t = t0 + 16 * u;
+    if constexpr (WHOLE) {
+      const int32_t page = pages[u] >= 0 ? pages[u] : 0;
+      const int64_t slot = t & slots;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        load_at<Values<BITS>::kBytes>(p.w[u][i], first_of(page) + (slot + i) * row, 4 * c * row + mine);
+      if constexpr (BITS != 16) load_at<16>(p.scale[u], scales_of(page) + slot, 16 * c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int32_t tok = t + 4 * c + i, at = page_of(s, table, tok >> s.log2P);
+        const int64_t slot = tok & slots, page = at >= 0 ? at : 0;
+        load_bytes<Values<BITS>::kBytes>(p.w[u][i], first_of(page) + slot * row + mine);
+        if constexpr (BITS != 16) p.scale[u][i] = scales_of(page)[slot];
+      }
+    }
+  }
+}
+
+// Which of the lane's tokens are there: bit 4u + i for token t0 + 16u + 4c + i.
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t tokens_there(const ServeArgs& s, const int32_t* table, int32_t t0,
+                                                 const int32_t (&pages)[2], int c) {
+  if constexpr (WHOLE) return (pages[0] >= 0 ? 0x0Fu : 0u) | (pages[1] >= 0 ? 0xF0u : 0u);
+  uint32_t there = 0;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      there |= (page_of(s, table, (t0 + 16 * u + 4 * c + i) >> s.log2P) >= 0 ? 1u : 0u) << (4 * u + i);
   return there;
 }
 
@@ -255,51 +294,286 @@ struct Span {  // of a row tile, over its rows
   int32_t sink_tiles, first, tiles;  // tiles of tokens to look at: the sinks', then those from token `first` on
 };
 
-template <bool BF16, int KB, int VB, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void attend_kernel(ServeArgs s, AttendArgs a) {
+// The running softmax of a wave over its rows (lane: row x of each of RT row tiles).
+template <int RT>
+struct Running {
+  f32x4 o[RT][kChannels];
+  float ref[RT];   // exponents are taken relative to it (base 2): within kSlack of the largest so far; -inf at first
+  float l[RT], o_zero[RT];
+  float fac;       // codes: O counts in units of 1 / fac
+  float most_scale;
+};
+
+// P is stored as 2^kShift p where the operands are binary16, which keeps small
+// probabilities clear of its subnormals; the reference of the exponents is moved only
+// when a score passes it by kSlack, so that O is rescaled once or twice a row and not
+// at every new maximum (with 64 rows in a wave nearly every tile has one).  2^(kShift + kSlack) is
+// in binary16's range.
+constexpr float kSlack = 8.0f;
+constexpr float kShiftOfHalf = 6.0f;
+
+// One tile: `there` of its tokens exist; more_keys and more_values load the next
+// tile's over this one's as soon as those have been used.
+template <bool BF16, int KB, int VB, int RT, typename MoreKeys, typename MoreValues>
+__device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& span, const Sight (&see)[RT],
+                                            const u32x4 (&q)[RT][kQkSteps], const float (&q_sum)[RT],
+                                            const float (&f)[RT], int c, int32_t t0, uint32_t there, Keys<KB>& keys,
+                                            Values<VB>& values, Running<RT>& st, MoreKeys more_keys,
+                                            MoreValues more_values) {
   constexpr bool kCodes = KB != 16;
   constexpr bool kHalf = kCodes || !BF16;  // operands in binary16
-  // P is scaled by 2^kShift, which keeps small probabilities clear of binary16's subnormals.
-  constexpr float kShift = kHalf ? 14.0f : 0.0f;
+  const bool all = t0 + kTokenTile - 1 <= span.hi_least && (span.lo_most < t0 || t0 + kTokenTile <= a.sinks) &&
+                   __all(there == 0xFFu);
+  // S^T, in units of 1 / f.
+  f32x4 t[RT][2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) t[r][u] = f32x4{};
+#pragma unroll
+    for (int i = 0; i < kQkSteps; ++i) {
+      const u32x4 k = k_operand<KB>(keys.w[u], i);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        if constexpr (kHalf)
+          t[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k),
+                                                           __builtin_bit_cast(f16x8, q[r][i]), t[r][u], 0, 0, 0);
+        else
+          t[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k),
+                                                            __builtin_bit_cast(bf16x8, q[r][i]), t[r][u], 0, 0, 0);
+      }
+    }
+  }
+  float vs[2][4], vz[2][4];
+  if constexpr (kCodes) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float sc = f16_float(keys.scale[u][i]);
+        const float zc = __builtin_fmaf(sc, float(1 << (KB - 1)), f16_float(keys.scale[u][i] >> 16));
+#pragma unroll
+        for (int r = 0; r < RT; ++r) t[r][u][i] = __builtin_fmaf(sc, t[r][u][i], zc * q_sum[r]);
+        vs[u][i] = f16_float(values.scale[u][i]);
+        vz[u][i] = __builtin_fmaf(vs[u][i], float(1 << (VB - 1)), f16_float(values.scale[u][i] >> 16));
+      }
+  }
+  more_keys();
+  if (!all) {
+    // A row's score where it does not see; the values of tokens that no row sees, whatever lies there.
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int32_t tok = t0 + 16 * u + 4 * c + i;
+        const bool is = (there >> (4 * u + i)) & 1;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          t[r][u][i] = is && tok <= see[r].hi && (tok > see[r].lo || tok < a.sinks) ? t[r][u][i] : -kInf;
+        const bool any = is && tok <= span.hi_most && (tok > span.lo_least || tok < a.sinks);
+        if constexpr (kCodes) {
+          vs[u][i] = any ? vs[u][i] : 0.0f;
+          vz[u][i] = any ? vz[u][i] : 0.0f;
+        } else {
+#pragma unroll
+          for (int w = 0; w < Values<VB>::kWords; ++w) values.w[u][i][w] = any ? values.w[u][i][w] : 0;
+        }
+      }
+  }
+  // The reference of the exponents.
+  float top[RT];
+  bool move = false;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    top[r] = t[r][0][0];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top[r] = __builtin_fmaxf(top[r], t[r][u][i]);
+    top[r] *= f[r];
+    move |= top[r] > st.ref[r] + kSlack;
+  }
+  if (__any(move)) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      float next = over_c_max(top[r]);
+      next = next > st.ref[r] ? next : st.ref[r];
+      const float shrink = st.ref[r] == -kInf ? 0.0f : exp2_of(st.ref[r] - next);
+      st.ref[r] = next;
+      st.l[r] *= shrink;
+      st.o_zero[r] *= shrink;
+#pragma unroll
+      for (int j = 0; j < kChannels; ++j) st.o[r][j] *= shrink;
+    }
+  }
+  if constexpr (kCodes) {
+    float tile_most = vs[0][0];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tile_most = __builtin_fmaxf(tile_most, vs[u][i]);
+    if (__any(tile_most > st.most_scale)) {
+      st.most_scale = __builtin_fmaxf(st.most_scale, over_c_max(tile_most));
+      // 2^e > the largest scale so far: scales times fac stay below 2^kShift.
+      const int e = int(__float_as_uint(st.most_scale) >> 23) - 126;
+      const float next = __uint_as_float(uint32_t(127 + int(kShiftOfHalf) - e) << 23);
+      if (next != st.fac) {
+        const float ratio = next / st.fac;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int j = 0; j < kChannels; ++j) st.o[r][j] *= ratio;
+        st.fac = next;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vs[u][i] *= st.fac;
+  }
+  // The probabilities and their sum.
+  u32x4 pt[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const float base = (kCodes || !kHalf ? 0.0f : kShiftOfHalf) - (st.ref[r] == -kInf ? 0.0f : st.ref[r]);
+    float pr[2][4];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pr[u][i] = exp2_of(__builtin_fmaf(t[r][u][i], f[r], base));
+        st.l[r] += pr[u][i];
+        if constexpr (kCodes) {
+          st.o_zero[r] = __builtin_fmaf(pr[u][i], vz[u][i], st.o_zero[r]);
+          pr[u][i] *= vs[u][i];
+        }
+      }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        pt[r][2 * u + i] = kHalf ? pack_f16(pr[u][2 * i], pr[u][2 * i + 1]) : pack_bf16(pr[u][2 * i], pr[u][2 * i + 1]);
+  }
+#pragma unroll
+  for (int j = 0; j < kChannels; ++j) {
+    u32x4 v;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) v[2 * u + i] = v_pair<VB>(values.w[u][2 * i], values.w[u][2 * i + 1], j);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      if constexpr (kHalf)
+        st.o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, pt[r]),
+                                                            st.o[r][j], 0, 0, 0);
+      else
+        st.o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v),
+                                                             __builtin_bit_cast(bf16x8, pt[r]), st.o[r][j], 0, 0, 0);
+    }
+  }
+  more_values();
+}
+
+// Entry `at` of a table that the wave shares, by a scalar load.
+__device__ __forceinline__ int32_t scalar_entry(const int32_t* table, int32_t at) {
+  const auto* t = (const __attribute__((address_space(4))) int32_t*)(reinterpret_cast<uintptr_t>(table));
+  return t[__builtin_amdgcn_readfirstlane(at)];
+}
+
+template <bool BF16, int KB, int VB, bool WHOLE, int RT>
+__global__ __launch_bounds__(kThreads, RT * D > 256 ? 1 : 2) void attend_kernel(ServeArgs s, AttendArgs a) {
+  constexpr bool kCodes = KB != 16;
+  constexpr int kRows = kRowTile * RT;
   __shared__ float join_ml[kWaves][kRowTile][2];
   __shared__ float join[kWaves][kRowTile][D + 4];
 
-  int64_t b = blockIdx.x;
-  const int32_t head = int32_t(b % s.H);
-  b /= s.H;
-  const int32_t split = int32_t(b % a.splits);
-  b /= a.splits;
-  const int32_t tile = int32_t(b % a.row_tiles);
-  const int32_t seq = int32_t(b / a.row_tiles);
+  uint32_t b = blockIdx.x;
+  const int32_t head = int32_t(b % uint32_t(s.H));
+  b /= uint32_t(s.H);
+  const int32_t split = int32_t(b % uint32_t(a.splits));
+  b /= uint32_t(a.splits);
+  const int32_t tile = int32_t(b % uint32_t(a.row_tiles));
+  const int32_t seq = int32_t(b / uint32_t(a.row_tiles));
 
   const int lane = threadIdx.x & 63, c = lane >> 4, x = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // The tile's rows.
-  int32_t start = s.token_start[seq], end = s.token_start[seq + 1];
+  int32_t start = scalar_entry(s.token_start, seq), end = scalar_entry(s.token_start, seq + 1);
+  int32_t kv_len = scalar_entry(s.kv_lens, seq);
   start = start < 0 ? 0 : start;
   end = end < s.num_tokens ? end : s.num_tokens;
   const int32_t count = end - start < s.max_tokens ? end - start : s.max_tokens;
-  const int64_t row0 = int64_t(tile) * kRowTile;
+  const int64_t row0 = int64_t(tile) * kRows;
   if (row0 >= int64_t(count) * a.group) return;  // the whole workgroup
-  int32_t kv_len = s.kv_lens[seq];
   kv_len = kv_len < 0 ? 0 : kv_len < s.max_kv ? kv_len : s.max_kv;
-  const int64_t row = row0 + x;
-  const int32_t token = int32_t(row / a.group), sub = int32_t(row % a.group);
-  const bool on = token < count;
-  Sight see{-1, -1};
-  if (on) {
-    const int32_t pos = s.positions ? s.positions[start + token] : kv_len - (end - start) + token;
-    see.hi = pos < kv_len ? pos : kv_len - 1;
-    see.hi = see.hi < -1 ? -1 : see.hi;
-    see.lo = a.window > 0 && pos >= a.window ? pos - a.window : -1;
+  Sight see[RT];
+  Span span{-1, 0x7FFFFFFF, -1, 0x7FFFFFFF, 0, 0, 0};
+  u32x4 q[RT][kQkSteps];
+  float q_sum[RT], f[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const uint32_t row = uint32_t(row0) + kRowTile * r + x;
+    const int32_t token = int32_t(row / uint32_t(a.group)), sub = int32_t(row % uint32_t(a.group));
+    const bool on = token < count;
+    see[r] = Sight{-1, -1};
+    if (on) {
+      const int32_t pos = s.positions ? s.positions[start + token] : kv_len - (end - start) + token;
+      see[r].hi = pos < kv_len ? pos : kv_len - 1;
+      see[r].hi = see[r].hi < -1 ? -1 : see[r].hi;
+      see[r].lo = a.window > 0 && pos >= a.window ? pos - a.window : -1;
+      span.hi_least = span.hi_least < see[r].hi ? span.hi_least : see[r].hi;
+      if (see[r].hi >= 0 && see[r].lo < span.lo_least) span.lo_least = see[r].lo;
+    }
+    span.hi_most = span.hi_most > see[r].hi ? span.hi_most : see[r].hi;
+    span.lo_most = span.lo_most > see[r].lo ? span.lo_most : see[r].lo;
+
+    // The queries, in the operands' order, and their sum.
+    q_sum[r] = 0.0f;
+    f[r] = a.scale;
+    const uint16_t* from_q = a.q + int64_t(start + token) * a.q_token_stride +
+                             int64_t(head * a.group + sub) * a.q_head_stride + c * (D / 4);
+    float v[kQkSteps][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kQkSteps; ++i) {
+      u32x4 w{};
+      if (on) w = *reinterpret_cast<const u32x4*>(from_q + 8 * i);
+      if constexpr (!kCodes) {
+        q[r][i] = w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t bits = e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xFFFF;
+          v[i][e] = s.bf16 ? bf16_float(bits) : f16_float(bits);
+          const uint32_t mag = __float_as_uint(v[i][e]) & 0x7FFFFFFF;
+          top = top > mag ? top : mag;
+        }
+      }
+    }
+    if constexpr (kCodes) {
+      top = max(top, uint32_t(__shfl_xor(int(top), 16)));
+      top = max(top, uint32_t(__shfl_xor(int(top), 32)));
+      // 2^-e with 2^e <= |q| < 2^(e + 1): the largest becomes 1..2 and S is scaled back by 2^e in f.
+      int e = int(top >> 23) - 127;
+      e = e < -60 ? -60 : e > 120 ? 120 : e;  // f stays a normal number
+      const float down = __uint_as_float(uint32_t(127 - e) << 23);
+      f[r] *= __uint_as_float(uint32_t(127 + e) << 23);
+#pragma unroll
+      for (int i = 0; i < kQkSteps; ++i) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+          q[r][i][p] = pack_f16(v[i][k_channel<KB>(p, 0)] * down, v[i][k_channel<KB>(p, 1)] * down);
+#pragma unroll
+        for (int e2 = 0; e2 < 8; ++e2) q_sum[r] += v[i][e2] * down;
+      }
+      q_sum[r] = over_c_sum(q_sum[r]);
+    }
   }
-  Span span;
-  span.hi_most = over_x_max(see.hi);
-  span.hi_least = over_x_min(on ? see.hi : 0x7FFFFFFF);
-  span.lo_most = over_x_max(see.lo);
-  span.lo_least = over_x_min(see.hi >= 0 ? see.lo : 0x7FFFFFFF);
-  span.first = span.sink_tiles = span.tiles = 0;
+  span.hi_most = __builtin_amdgcn_readfirstlane(over_x_max(span.hi_most));
+  span.hi_least = __builtin_amdgcn_readfirstlane(over_x_min(span.hi_least));
+  span.lo_most = __builtin_amdgcn_readfirstlane(over_x_max(span.lo_most));
+  span.lo_least = __builtin_amdgcn_readfirstlane(over_x_min(span.lo_least));
   if (span.hi_most >= 0) {
     span.first = (span.lo_least + 1) & ~(kTokenTile - 1);
     const int32_t sinks = a.sinks < span.hi_most + 1 ? a.sinks : span.hi_most + 1;
@@ -314,240 +588,121 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(ServeArgs s, AttendArg
   const int64_t from = int64_t(split) * share;
   const int32_t upto = int32_t(from + share < span.tiles ? from + share : span.tiles);
 
-  // The queries, in the operands' order, and their sum.
-  u32x4 q[kQkSteps];
-  float q_sum = 0.0f, f = a.scale;
-  {
-    float v[kQkSteps][8];
-    const uint16_t* from_q = a.q + int64_t(start + token) * a.q_token_stride +
-                             int64_t(head * a.group + sub) * a.q_head_stride + c * (D / 4);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < kQkSteps; ++i) {
-      u32x4 w{};
-      if (on) w = *reinterpret_cast<const u32x4*>(from_q + 8 * i);
-      if constexpr (!kCodes) q[i] = w;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t bits = e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xFFFF;
-        v[i][e] = s.bf16 ? bf16_float(bits) : f16_float(bits);
-        const uint32_t mag = __float_as_uint(v[i][e]) & 0x7FFFFFFF;
-        top = top > mag ? top : mag;
-      }
-    }
-    if constexpr (kCodes) {
-      top = max(top, uint32_t(__shfl_xor(int(top), 16)));
-      top = max(top, uint32_t(__shfl_xor(int(top), 32)));
-      // 2^-e with 2^e <= |q| < 2^(e + 1): the largest becomes 1..2 and S is scaled back by 2^e in f.
-      int e = int(top >> 23) - 127;
-      e = e < -60 ? -60 : e > 120 ? 120 : e;  // f stays a normal number
-      const float down = __uint_as_float(uint32_t(127 - e) << 23);
-      f *= __uint_as_float(uint32_t(127 + e) << 23);
-#pragma unroll
-      for (int i = 0; i < kQkSteps; ++i) {
-#pragma unroll
-        for (int p = 0; p < 4; ++p)
-          q[i][p] = pack_f16(v[i][k_channel<KB>(p, 0)] * down, v[i][k_channel<KB>(p, 1)] * down);
-#pragma unroll
-        for (int e2 = 0; e2 < 8; ++e2) q_sum += v[i][e2] * down;
-      }
-      q_sum = over_c_sum(q_sum);
-    }
-  }
-
   const int32_t* table = s.page_table + int64_t(seq) * s.pages_per_seq;
-  f32x4 o[kChannels] = {};
-  float m = -kInf, l = 0.0f, o_zero = 0.0f;
-  float fac = 1.0f;  // codes: O counts in units of 1 / fac, the same in every lane
-  float most_scale = 0.0f;
+  Running<RT> st;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    st.ref[r] = -kInf;
+    st.l[r] = st.o_zero[r] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kChannels; ++j) st.o[r][j] = f32x4{};
+  }
+  st.fac = 1.0f;
+  st.most_scale = 0.0f;
 
-  for (int32_t it = int32_t(from) + wave; it < upto; it += kWaves) {
-    const int32_t t0 = it < span.sink_tiles ? it * kTokenTile : span.first + (it - span.sink_tiles) * kTokenTile;
-    Piece<KB, VB> p;
-    const uint32_t there = load_tile<KB, VB, WHOLE>(s, table, head, t0, c, x, p);
-    const bool all = t0 + kTokenTile - 1 <= span.hi_least &&
-                     (span.lo_most < t0 || t0 + kTokenTile <= a.sinks) && __all(there == 0xFFu);
-    // S^T, in units of 1 / f.
-    float t[2][4];
+  auto tile_at = [&](int32_t it) {
+    return it < span.sink_tiles ? it * kTokenTile : span.first + (it - span.sink_tiles) * kTokenTile;
+  };
+  auto pages_at = [&](int32_t it, int32_t (&pages)[2]) {  // of a tile that exists, else -1
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      f32x4 acc{};
-#pragma unroll
-      for (int i = 0; i < kQkSteps; ++i) {
-        const u32x4 k = k_operand<KB>(p.k[u], i);
-        if constexpr (kHalf)
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k), __builtin_bit_cast(f16x8, q[i]),
-                                                       acc, 0, 0, 0);
-        else
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[i]),
-                                                        acc, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        t[u][i] = acc[i];
-        if constexpr (kCodes) {
-          const float sc = f16_float(p.ks[u][i]);
-          const float zc = __builtin_fmaf(sc, float(1 << (KB - 1)), f16_float(p.ks[u][i] >> 16));
-          t[u][i] = __builtin_fmaf(sc, acc[i], zc * q_sum);
-        }
-      }
+      const int32_t at = (tile_at(it) + 16 * u) >> s.log2P;
+      pages[u] = WHOLE && it < upto && at < s.pages_per_seq ? scalar_entry(table, at) : -1;
+      pages[u] = pages[u] < s.pool_pages ? pages[u] : -1;
     }
-    float vs[2][4], vz[2][4];
-    if constexpr (kCodes) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          vs[u][i] = f16_float(p.vs[u][i]);
-          vz[u][i] = __builtin_fmaf(vs[u][i], float(1 << (VB - 1)), f16_float(p.vs[u][i] >> 16));
-        }
-    }
-    if (!all) {
-      // A row's score where it does not see; the values of tokens that no row sees, whatever lies there.
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int32_t tok = t0 + 16 * u + 4 * c + i;
-          const bool is = (there >> (4 * u + i)) & 1;
-          const bool sees = is && tok <= see.hi && (tok > see.lo || tok < a.sinks);
-          t[u][i] = sees ? t[u][i] : -kInf;
-          const bool any = is && tok <= span.hi_most && (tok > span.lo_least || tok < a.sinks);
-          if constexpr (kCodes) {
-            vs[u][i] = any ? vs[u][i] : 0.0f;
-            vz[u][i] = any ? vz[u][i] : 0.0f;
-          } else {
-#pragma unroll
-            for (int w = 0; w < Piece<KB, VB>::kVWords; ++w) p.v[u][i][w] = any ? p.v[u][i][w] : 0;
-          }
-        }
-    }
-    // The running maximum (base 2), the probabilities and their sum.
-    float top = t[0][0];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = __builtin_fmaxf(top, t[u][i]);
-    float m_new = over_c_max(top) * f;
-    m_new = m_new > m ? m_new : m;
-    const float base = m_new == -kInf ? 0.0f : m_new;
-    const float shrink = exp2_of(m - base);
-    m = m_new;
-    l *= shrink;
-    o_zero *= shrink;
-    float keep = shrink;
-    float pr[2][4];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        pr[u][i] = exp2_of(__builtin_fmaf(t[u][i], f, (kCodes ? 0.0f : kShift) - base));
-        l += pr[u][i];
-      }
-    if constexpr (kCodes) {
-      float tile_most = vs[0][0];
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tile_most = __builtin_fmaxf(tile_most, vs[u][i]);
-      if (__any(tile_most > most_scale)) {
-        most_scale = __builtin_fmaxf(most_scale, over_c_max(tile_most));
-        // 2^e > the largest scale so far; p s 2^(14 - e) < 2^14.
-        const int e = int(__float_as_uint(most_scale) >> 23) - 126;
-        const float next = __uint_as_float(uint32_t(127 + 14 - e) << 23);
-        keep *= next / fac;
-        fac = next;
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          o_zero = __builtin_fmaf(pr[u][i], vz[u][i], o_zero);
-          pr[u][i] *= vs[u][i] * fac;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < kChannels; ++j) o[j] *= keep;
-    u32x4 pt;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        pt[2 * u + i] = kHalf ? pack_f16(pr[u][2 * i], pr[u][2 * i + 1]) : pack_bf16(pr[u][2 * i], pr[u][2 * i + 1]);
-#pragma unroll
-    for (int j = 0; j < kChannels; ++j) {
-      u32x4 v;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) v[2 * u + i] = v_pair<VB>(p.v[u][2 * i], p.v[u][2 * i + 1], j);
-      if constexpr (kHalf)
-        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, pt), o[j],
-                                                      0, 0, 0);
-      else
-        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pt),
-                                                       o[j], 0, 0, 0);
+  };
+  // A tile's keys are loaded while the softmax and the sums of the one before run, its values while its own
+  // scores are computed, its pages one tile earlier.
+  int32_t it = int32_t(from) + wave;
+  if (it < upto) {
+    Keys<KB> keys;
+    Values<VB> values;
+    int32_t pages[2], next[2];
+    pages_at(it, pages);
+    load_keys<KB, WHOLE>(s, table, head, tile_at(it), pages, c, x, keys);
+    load_values<VB, WHOLE>(s, table, head, tile_at(it), pages, c, x, values);
+    pages_at(it + kWaves, next);
+    for (; it < upto; it += kWaves) {
+      const int32_t t0 = tile_at(it), t1 = tile_at(it + kWaves);
+      const bool more = it + kWaves < upto;
+      const uint32_t there = tokens_there<WHOLE>(s, table, t0, pages, c);
+      attend_tile<BF16, KB, VB, RT>(
+          a, span, see, q, q_sum, f, c, t0, there, keys, values, st,
+          [&] {
+            if (more) load_keys<KB, WHOLE>(s, table, head, t1, next, c, x, keys);
+          },
+          [&] {
+            if (more) load_values<VB, WHOLE>(s, table, head, t1, next, c, x, values);
+          });
+      pages[0] = next[0];
+      pages[1] = next[1];
+      pages_at(it + 2 * kWaves, next);
     }
   }
 
-  // Join the waves: every one's sums relative to the largest maximum.
-  l = over_c_sum(l);
-  if constexpr (kCodes) o_zero = over_c_sum(o_zero);
-  if (c == 0) {
-    join_ml[wave][x][0] = m;
-    join_ml[wave][x][1] = l;
+  // Join the waves, a row tile at a time: every one's sums relative to the largest reference.
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const float l = over_c_sum(st.l[r]), m = st.ref[r];
+    const float o_zero = kCodes ? over_c_sum(st.o_zero[r]) : 0.0f;
+    if (r) __syncthreads();
+    if (c == 0) {
+      join_ml[wave][x][0] = m;
+      join_ml[wave][x][1] = l;
+    }
+    __syncthreads();
+    float m_all = -kInf;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m_all = __builtin_fmaxf(m_all, join_ml[w][x][0]);
+    const float part = m == -kInf ? 0.0f : exp2_of(m - m_all);
+    const float unit = kCodes ? part / st.fac : part;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < kChannels; ++j)
+        join[wave][x][(4 * c + i) * kChannels + j] =
+            m == -kInf ? 0.0f : kCodes ? __builtin_fmaf(o_zero, part, st.o[r][j][i] * unit) : st.o[r][j][i] * part;
+    __syncthreads();
+    constexpr int kPerRow = kThreads / kRowTile, kPer = D / kPerRow;  // 16 threads to a row
+    const int y = threadIdx.x / kPerRow, at = (threadIdx.x % kPerRow) * kPer;
+    const uint32_t out_row = uint32_t(row0) + kRowTile * r + y;
+    const int32_t out_token = int32_t(out_row / uint32_t(a.group));
+    if (out_token >= count) continue;
+    const int32_t out_head = head * a.group + int32_t(out_row % uint32_t(a.group));
+    float mm = -kInf, ll = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mm = __builtin_fmaxf(mm, join_ml[w][y][0]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      ll += join_ml[w][y][0] == -kInf ? 0.0f : join_ml[w][y][1] * exp2_of(join_ml[w][y][0] - mm);
+    float sum[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      sum[e] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) sum[e] += join[w][y][at + e];
+    }
+    const int64_t flat = int64_t(start + out_token) * a.Hq + out_head;
+    if (a.splits > 1) {
+      const int64_t slot = flat * a.splits + split;
+#pragma unroll
+      for (int e = 0; e < kPer; e += 4)
+        *reinterpret_cast<f32x4*>(a.part + slot * D + at + e) = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+      if (at == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * slot) = f32x2{mm, ll};
+      continue;
+    }
+    const float inv = ll > 0.0f ? 1.0f / ll : ll == 0.0f ? 0.0f : ll;
+    uint32_t word[kPer / 2];
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2)
+      word[e / 2] = s.bf16 ? pack_bf16(sum[e] * inv, sum[e + 1] * inv) : pack_f16(sum[e] * inv, sum[e + 1] * inv);
+    uint16_t* to = a.out + int64_t(start + out_token) * a.out_token_stride + int64_t(out_head) * a.out_head_stride + at;
+#pragma unroll
+    for (int e = 0; e < kPer / 2; e += 2) *reinterpret_cast<u32x2*>(to + 2 * e) = u32x2{word[e], word[e + 1]};
+    constexpr float kUp = kCodes || BF16 ? 1.0f : 1.0f / 64.0f;  // l counts 2^kShift to one where p does
+    if (a.lse && at == 0)
+      a.lse[flat] = ll == 0.0f ? -kInf : (mm + __builtin_amdgcn_logf(ll * kUp)) * 0.69314718055994531f;
   }
-  __syncthreads();
-  float m_all = -kInf;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) m_all = __builtin_fmaxf(m_all, join_ml[w][x][0]);
-  const float part = m == -kInf ? 0.0f : exp2_of(m - m_all);
-  const float unit = kCodes ? part / fac : part;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < kChannels; ++j)
-      join[wave][x][(4 * c + i) * kChannels + j] =
-          m == -kInf ? 0.0f : kCodes ? __builtin_fmaf(o_zero, part, o[j][i] * unit) : o[j][i] * part;
-  __syncthreads();
-  constexpr int kPerRow = kThreads / kRowTile, kPer = D / kPerRow;  // 16 threads to a row
-  const int r = threadIdx.x / kPerRow, at = (threadIdx.x % kPerRow) * kPer;
-  const int64_t out_row = row0 + r;
-  const int32_t out_token = int32_t(out_row / a.group);
-  if (out_token >= count) return;
-  const int32_t out_head = head * a.group + int32_t(out_row % a.group);
-  float mm = -kInf, ll = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) mm = __builtin_fmaxf(mm, join_ml[w][r][0]);
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w)
-    ll += join_ml[w][r][0] == -kInf ? 0.0f : join_ml[w][r][1] * exp2_of(join_ml[w][r][0] - mm);
-  float sum[kPer];
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    sum[e] = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum[e] += join[w][r][at + e];
-  }
-  const int64_t flat = int64_t(start + out_token) * a.Hq + out_head;
-  constexpr float kUp = kCodes || BF16 ? 1.0f : 1.0f / 16384.0f;  // l counts 2^kShift to one where p does
-  if (a.splits > 1) {
-    const int64_t slot = flat * a.splits + split;
-#pragma unroll
-    for (int e = 0; e < kPer; e += 4)
-      *reinterpret_cast<f32x4*>(a.part + slot * D + at + e) = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
-    if (at == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * slot) = f32x2{mm, ll};
-    return;
-  }
-  const float inv = ll > 0.0f ? 1.0f / ll : ll == 0.0f ? 0.0f : ll;
-  uint32_t word[kPer / 2];
-#pragma unroll
-  for (int e = 0; e < kPer; e += 2)
-    word[e / 2] = s.bf16 ? pack_bf16(sum[e] * inv, sum[e + 1] * inv) : pack_f16(sum[e] * inv, sum[e + 1] * inv);
-  uint16_t* to = a.out + int64_t(start + out_token) * a.out_token_stride + int64_t(out_head) * a.out_head_stride + at;
-#pragma unroll
-  for (int e = 0; e < kPer / 2; e += 2) *reinterpret_cast<u32x2*>(to + 2 * e) = u32x2{word[e], word[e + 1]};
-  if (a.lse && at == 0) a.lse[flat] = ll == 0.0f ? -kInf : (mm + __builtin_amdgcn_logf(ll * kUp)) * 0.69314718055994531f;
 }
 
 // Joins the splits of each row: one wave per row.
@@ -593,20 +748,28 @@ __global__ __launch_bounds__(kThreads) void join_kernel(ServeArgs s, AttendArgs 
 pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const AttendArgs& a, int64_t groups,
                                                       hipStream_t stream) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(uint32_t(groups)), dim3(kThreads), 0, stream, s, a); };
-  auto by_tag = [&](auto whole) {
+  auto by_tag = [&](auto whole, auto tiles) {
     constexpr bool kWhole = decltype(whole)::value;
+    constexpr int kTiles = decltype(tiles)::value;
     switch (s.tag) {
-      case PKV_TAG_FP16: s.bf16 ? go(attend_kernel<true, 16, 16, kWhole>) : go(attend_kernel<false, 16, 16, kWhole>); break;
-      case PKV_TAG_K8V8: go(attend_kernel<false, 8, 8, kWhole>); break;
-      case PKV_TAG_K8V4: go(attend_kernel<false, 8, 4, kWhole>); break;
-      default: go(attend_kernel<false, 4, 4, kWhole>); break;
+      case PKV_TAG_FP16:
+        s.bf16 ? go(attend_kernel<true, 16, 16, kWhole, kTiles>) : go(attend_kernel<false, 16, 16, kWhole, kTiles>);
+        break;
+      case PKV_TAG_K8V8: go(attend_kernel<false, 8, 8, kWhole, kTiles>); break;
+      case PKV_TAG_K8V4: go(attend_kernel<false, 8, 4, kWhole, kTiles>); break;
+      default: go(attend_kernel<false, 4, 4, kWhole, kTiles>); break;
     }
   };
-  s.log2P >= 4 ? by_tag(std::true_type{}) : by_tag(std::false_type{});
+  auto by_tiles = [&](auto whole) {
+    if constexpr (kMostRowTiles >= 4)
+      if (a.tiles == 4) return by_tag(whole, std::integral_constant<int, 4>{});
+    a.tiles == 2 ? by_tag(whole, std::integral_constant<int, 2>{}) : by_tag(whole, std::integral_constant<int, 1>{});
+  };
+  s.log2P >= 4 ? by_tiles(std::true_type{}) : by_tiles(std::false_type{});
   if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
   if (a.splits > 1) {
     const int64_t rows = int64_t(s.num_tokens) * a.Hq;
-    const float up = s.tag == PKV_TAG_FP16 && !s.bf16 ? 1.0f / 16384.0f : 1.0f;
+    const float up = s.tag == PKV_TAG_FP16 && !s.bf16 ? 1.0f / 64.0f : 1.0f;
     hipLaunchKernelGGL(join_kernel, dim3(uint32_t((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, stream, s, a, up);
     if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
   }

@@ -54,21 +54,25 @@ struct AttendArgs {
   int32_t Hq, group;  // query heads, query heads per KV head
   int32_t window, sinks;
   float scale;        // scale * log2(e)
-  int32_t row_tiles;  // of one sequence and KV head
+  int32_t tiles;      // row tiles of a workgroup
+  int32_t row_tiles;  // workgroups' shares of the rows of one sequence and KV head
   int32_t splits;     // pieces that a sequence's tokens are dealt to
   int32_t chunk;      // least tiles of tokens in a piece
 };
 
 // How an attention call is launched.
 struct AttendLaunch {
-  int32_t row_tiles, splits, chunk;
+  int32_t tiles, row_tiles, splits, chunk;
   int64_t groups;           // workgroups
   uint64_t part_bytes;      // of AttendArgs::part, then part_ml
   uint64_t workspace_bytes; // both
 };
 
-constexpr int kRowTile = 16;   // rows (token, query head of one KV head) of a workgroup
+constexpr int kRowTile = 16;   // rows (token, query head of one KV head) of a matrix instruction
 constexpr int kTokenTile = 32; // cached tokens a wave takes at a time
+
+// Row tiles that a wave can hold: queries and sums of 64 rows of 128 channels take 192 registers.
+constexpr int most_row_tiles(int head_dim) { return head_dim > 128 ? 2 : 4; }
 
 // Host checks that need no GPU; they fill the arguments.
 pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,

@@ -131,6 +131,7 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
     r.out_head_stride = a->out_head_stride;
   }
   const AttendLaunch l = attend_launch(s, r);
+  r.tiles = l.tiles;
   r.row_tiles = l.row_tiles;
   r.splits = l.splits;
   r.chunk = l.chunk;
@@ -145,7 +146,10 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
 
 AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   AttendLaunch l{};
-  l.row_tiles = int32_t((int64_t(s.max_tokens) * a.group + kRowTile - 1) / kRowTile);
+  const int64_t rows = int64_t(s.max_tokens) * a.group;
+  l.tiles = 1;
+  while (l.tiles < most_row_tiles(s.D) && rows > kRowTile * l.tiles) l.tiles *= 2;
+  l.row_tiles = int32_t((rows + kRowTile * l.tiles - 1) / (kRowTile * l.tiles));
   const int64_t base = int64_t(s.num_seqs) * s.H * l.row_tiles;
   // tokens that a row tile may have to look at
   int64_t seen = s.max_kv;
@@ -158,9 +162,9 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   l.chunk = int32_t((tiles + splits - 1) / splits);
   l.groups = base * splits;
   if (splits > 1) {
-    const uint64_t rows = uint64_t(s.num_tokens) * a.Hq;
-    l.part_bytes = rows * splits * s.D * 4;
-    l.workspace_bytes = l.part_bytes + rows * splits * 8;
+    const uint64_t parts = uint64_t(s.num_tokens) * a.Hq * splits;
+    l.part_bytes = parts * s.D * 4;
+    l.workspace_bytes = l.part_bytes + parts * 8;
   }
   return l;
 }
