@@ -54,7 +54,6 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kQkSteps = D / 32;  // matrix instructions of one S^T
 constexpr int kChannels = D / 16; // channels of a lane in V, matrix instructions of one O^T update
-constexpr int kMostRowTiles = most_row_tiles(D);
 constexpr float kInf = __builtin_inff();
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -127,6 +126,15 @@ __device__ __forceinline__ u32x4 k_operand(const uint32_t* w, int step) {
     return u32x4{add_f16((b & 0x000F000Fu) | 0x64006400u, -1032.0f), add_f16((b & 0x00F000F0u) | 0x54005400u, -72.0f),
                  add_f16((h & 0x000F000Fu) | 0x64006400u, -1032.0f), add_f16((h & 0x00F000F0u) | 0x54005400u, -72.0f)};
   }
+}
+
+// First channel of the 8 that lane group c has in instruction `step`, where a
+// lane loads its part of a row in pieces of up to 16 bytes and the four lanes of a row lie next
+// to each other, so that they take 64 bytes of a line together.
+template <int BITS>
+__device__ __forceinline__ constexpr int k_first(int step, int c) {
+  constexpr int kBytes = D / 4 * BITS / 8 < 16 ? D / 4 * BITS / 8 : 16, kPer = kBytes * 8 / BITS, kSteps = kPer / 8;
+  return step / kSteps * 4 * kPer + c * kPer + step % kSteps * 8;
 }
 
 // Channel e (0..7) of register pair position p in the order above.
@@ -210,7 +218,8 @@ template <int BITS, bool WHOLE>
 __device__ __forceinline__ void load_keys(const ServeArgs& s, const int32_t* table, int head, int32_t t0,
                                           const int32_t (&pages)[2], int c, int x, Keys<BITS>& p) {
   const int32_t slots = (1 << s.log2P) - 1;
-  const uint32_t row = BITS == 16 ? uint32_t(s.H) * D * 2 : D * BITS / 8, mine = c * Keys<BITS>::kBytes;
+  constexpr int kPiece = Keys<BITS>::kBytes < 16 ? Keys<BITS>::kBytes : 16;
+  const uint32_t row = BITS == 16 ? uint32_t(s.H) * D * 2 : D * BITS / 8, mine = c * kPiece;
   auto first_of = [&](int64_t page) -> const char* {
     if constexpr (BITS == 16) return reinterpret_cast<const char*>(s.k_cache + page * s.page_stride + head * D);
     return reinterpret_cast<const char*>(s.codes + page * s.page_stride + head * s.head_stride);
@@ -222,11 +231,16 @@ __device__ __forceinline__ void load_keys(const ServeArgs& s, const int32_t* tab
     if constexpr (WHOLE) {
       const int32_t page = pages[u] >= 0 ? pages[u] : 0;
       const int64_t slot = t & slots;
-      load_at<Keys<BITS>::kBytes>(p.w[u], first_of(page) + slot * row, x * row + mine);
+#pragma unroll
+      for (int n = 0; n < Keys<BITS>::kBytes / kPiece; ++n)
+        load_at<kPiece>(p.w[u] + n * (kPiece / 4), first_of(page) + slot * row + n * (4 * kPiece), x * row + mine);
       if constexpr (BITS != 16) load_at<16>(p.scale[u], scales_of(page) + slot, 16 * c);
     } else {
       const int32_t page = page_of(s, table, (t + x) >> s.log2P);
-      load_bytes<Keys<BITS>::kBytes>(p.w[u], first_of(page >= 0 ? page : 0) + int64_t((t + x) & slots) * row + mine);
+      const char* from = first_of(page >= 0 ? page : 0) + int64_t((t + x) & slots) * row + mine;
+#pragma unroll
+      for (int n = 0; n < Keys<BITS>::kBytes / kPiece; ++n)
+        load_bytes<kPiece>(p.w[u] + n * (kPiece / 4), from + n * (4 * kPiece));
       if constexpr (BITS != 16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -312,18 +326,36 @@ struct Running {
 constexpr float kSlack = 8.0f;
 constexpr float kShiftOfHalf = 6.0f;
 
-// One tile: `there` of its tokens exist; more_keys and more_values load the next
-// tile's over this one's as soon as those have been used.
-template <bool BF16, int KB, int VB, int RT, typename MoreKeys, typename MoreValues>
-__device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& span, const Sight (&see)[RT],
-                                            const u32x4 (&q)[RT][kQkSteps], const float (&q_sum)[RT],
-                                            const float (&f)[RT], int c, int32_t t0, uint32_t there, Keys<KB>& keys,
-                                            Values<VB>& values, Running<RT>& st, MoreKeys more_keys,
-                                            MoreValues more_values) {
+// What stands for a token beside its codes: key scale and zero, value scale and zero, both zeros at mid-code.
+struct Scales {
+  float ks[2][4], kz[2][4], vs[2][4], vz[2][4];
+};
+
+// The first row x of each of a wave's RT row tiles: what it sees and its queries.
+template <int RT>
+struct Rows {
+  Sight see[RT];
+  u32x4 q[RT][kQkSteps];
+  float q_sum[RT], f[RT];
+};
+
+// One tile of 32 tokens from t0 on, of which the lane's are `there` (bit 4u + i: t0 + 16u + 4c + i).
+// key(u, i) and value(j) give the operands, after_keys() runs when the last key has been used, hide(keep) leaves of
+// 16-bit values only the halves of operand words that `keep` has.
+template <bool BF16, int KB, int VB, int RT, typename Key, typename Value, typename After, typename Hide>
+__device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& span, const Rows<RT>& rows, int c,
+                                            int32_t t0, uint32_t there, Scales& sc, Running<RT>& st, Key key,
+                                            Value value, After after_keys, Hide hide) {
   constexpr bool kCodes = KB != 16;
   constexpr bool kHalf = kCodes || !BF16;  // operands in binary16
   const bool all = t0 + kTokenTile - 1 <= span.hi_least && (span.lo_most < t0 || t0 + kTokenTile <= a.sinks) &&
                    __all(there == 0xFFu);
+  auto mfma = [](const u32x4& x, const u32x4& y, const f32x4& z) {
+    if constexpr (kHalf)
+      return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), z, 0, 0, 0);
+    else
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), z, 0, 0, 0);
+  };
   // S^T, in units of 1 / f.
   f32x4 t[RT][2];
 #pragma unroll
@@ -332,53 +364,46 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     for (int r = 0; r < RT; ++r) t[r][u] = f32x4{};
 #pragma unroll
     for (int i = 0; i < kQkSteps; ++i) {
-      const u32x4 k = k_operand<KB>(keys.w[u], i);
+      const u32x4 k = key(u, i);
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        if constexpr (kHalf)
-          t[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k),
-                                                           __builtin_bit_cast(f16x8, q[r][i]), t[r][u], 0, 0, 0);
-        else
-          t[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k),
-                                                            __builtin_bit_cast(bf16x8, q[r][i]), t[r][u], 0, 0, 0);
-      }
+      for (int r = 0; r < RT; ++r) t[r][u] = mfma(k, rows.q[r][i], t[r][u]);
     }
   }
-  float vs[2][4], vz[2][4];
   if constexpr (kCodes) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float sc = f16_float(keys.scale[u][i]);
-        const float zc = __builtin_fmaf(sc, float(1 << (KB - 1)), f16_float(keys.scale[u][i] >> 16));
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) t[r][u][i] = __builtin_fmaf(sc, t[r][u][i], zc * q_sum[r]);
-        vs[u][i] = f16_float(values.scale[u][i]);
-        vz[u][i] = __builtin_fmaf(vs[u][i], float(1 << (VB - 1)), f16_float(values.scale[u][i] >> 16));
-      }
+        for (int r = 0; r < RT; ++r)
+          t[r][u][i] = __builtin_fmaf(sc.ks[u][i], t[r][u][i], sc.kz[u][i] * rows.q_sum[r]);
   }
-  more_keys();
+  after_keys();
   if (!all) {
-    // A row's score where it does not see; the values of tokens that no row sees, whatever lies there.
+    u32x4 keep{};
+    // A row's score where it does not see; the values of tokens that no row of the wave sees, whatever lies there.
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int32_t tok = t0 + 16 * u + 4 * c + i;
         const bool is = (there >> (4 * u + i)) & 1;
+        bool any = false;
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-          t[r][u][i] = is && tok <= see[r].hi && (tok > see[r].lo || tok < a.sinks) ? t[r][u][i] : -kInf;
-        const bool any = is && tok <= span.hi_most && (tok > span.lo_least || tok < a.sinks);
+        for (int r = 0; r < RT; ++r) {
+          const bool sees = is && tok <= rows.see[r].hi && (tok > rows.see[r].lo || tok < a.sinks);
+          t[r][u][i] = sees ? t[r][u][i] : -kInf;
+          any |= sees;
+        }
+        any = (__ballot(any) >> (16 * c)) & 0xFFFF;
         if constexpr (kCodes) {
-          vs[u][i] = any ? vs[u][i] : 0.0f;
-          vz[u][i] = any ? vz[u][i] : 0.0f;
+          sc.vs[u][i] = any ? sc.vs[u][i] : 0.0f;
+          sc.vz[u][i] = any ? sc.vz[u][i] : 0.0f;
         } else {
-#pragma unroll
-          for (int w = 0; w < Values<VB>::kWords; ++w) values.w[u][i][w] = any ? values.w[u][i][w] : 0;
+          keep[2 * u + i / 2] |= any ? 0xFFFFu << (16 * (i & 1)) : 0;
         }
       }
+    if constexpr (!kCodes) hide(keep);
   }
   // The reference of the exponents.
   float top[RT];
@@ -390,7 +415,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top[r] = __builtin_fmaxf(top[r], t[r][u][i]);
-    top[r] *= f[r];
+    top[r] *= rows.f[r];
     move |= top[r] > st.ref[r] + kSlack;
   }
   if (__any(move)) {
@@ -407,11 +432,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     }
   }
   if constexpr (kCodes) {
-    float tile_most = vs[0][0];
+    float tile_most = sc.vs[0][0];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tile_most = __builtin_fmaxf(tile_most, vs[u][i]);
+      for (int i = 0; i < 4; ++i) tile_most = __builtin_fmaxf(tile_most, sc.vs[u][i]);
     if (__any(tile_most > st.most_scale)) {
       st.most_scale = __builtin_fmaxf(st.most_scale, over_c_max(tile_most));
       // 2^e > the largest scale so far: scales times fac stay below 2^kShift.
@@ -429,7 +454,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vs[u][i] *= st.fac;
+      for (int i = 0; i < 4; ++i) sc.vs[u][i] *= st.fac;
   }
   // The probabilities and their sum.
   u32x4 pt[RT];
@@ -441,11 +466,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        pr[u][i] = exp2_of(__builtin_fmaf(t[r][u][i], f[r], base));
+        pr[u][i] = exp2_of(__builtin_fmaf(t[r][u][i], rows.f[r], base));
         st.l[r] += pr[u][i];
         if constexpr (kCodes) {
-          st.o_zero[r] = __builtin_fmaf(pr[u][i], vz[u][i], st.o_zero[r]);
-          pr[u][i] *= vs[u][i];
+          st.o_zero[r] = __builtin_fmaf(pr[u][i], sc.vz[u][i], st.o_zero[r]);
+          pr[u][i] *= sc.vs[u][i];
         }
       }
 #pragma unroll
@@ -456,22 +481,10 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
   }
 #pragma unroll
   for (int j = 0; j < kChannels; ++j) {
-    u32x4 v;
+    const u32x4 v = value(j);
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) v[2 * u + i] = v_pair<VB>(values.w[u][2 * i], values.w[u][2 * i + 1], j);
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      if constexpr (kHalf)
-        st.o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, pt[r]),
-                                                            st.o[r][j], 0, 0, 0);
-      else
-        st.o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v),
-                                                             __builtin_bit_cast(bf16x8, pt[r]), st.o[r][j], 0, 0, 0);
-    }
+    for (int r = 0; r < RT; ++r) st.o[r][j] = mfma(v, pt[r], st.o[r][j]);
   }
-  more_values();
 }
 
 // Entry `at` of a table that the wave shares, by a scalar load.
@@ -480,67 +493,69 @@ __device__ __forceinline__ int32_t scalar_entry(const int32_t* table, int32_t at
   return t[__builtin_amdgcn_readfirstlane(at)];
 }
 
-template <bool BF16, int KB, int VB, bool WHOLE, int RT>
-__global__ __launch_bounds__(kThreads, RT * D > 256 ? 1 : 2) void attend_kernel(ServeArgs s, AttendArgs a) {
-  constexpr bool kCodes = KB != 16;
-  constexpr int kRows = kRowTile * RT;
-  __shared__ float join_ml[kWaves][kRowTile][2];
-  __shared__ float join[kWaves][kRowTile][D + 4];
+// The rows of a call that a workgroup shares: one sequence's, of one KV head.
+struct Group {
+  int32_t head, split, tile, seq;
+  int32_t start, count, kv_len, trail;  // rows [start, start + count); the last row of the sequence is `trail` rows on
+};
 
+__device__ __forceinline__ Group group_of(const ServeArgs& s, const AttendArgs& a) {
+  Group g;
   uint32_t b = blockIdx.x;
-  const int32_t head = int32_t(b % uint32_t(s.H));
+  g.head = int32_t(b % uint32_t(s.H));
   b /= uint32_t(s.H);
-  const int32_t split = int32_t(b % uint32_t(a.splits));
+  g.split = int32_t(b % uint32_t(a.splits));
   b /= uint32_t(a.splits);
-  const int32_t tile = int32_t(b % uint32_t(a.row_tiles));
-  const int32_t seq = int32_t(b / uint32_t(a.row_tiles));
-
-  const int lane = threadIdx.x & 63, c = lane >> 4, x = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-  // The tile's rows.
-  int32_t start = scalar_entry(s.token_start, seq), end = scalar_entry(s.token_start, seq + 1);
-  int32_t kv_len = scalar_entry(s.kv_lens, seq);
-  start = start < 0 ? 0 : start;
+  g.tile = a.row_tiles - 1 - int32_t(b % uint32_t(a.row_tiles));  // the rows that see the most start first
+  g.seq = int32_t(b / uint32_t(a.row_tiles));
+  int32_t end = scalar_entry(s.token_start, g.seq + 1);
+  g.start = scalar_entry(s.token_start, g.seq);
+  g.kv_len = scalar_entry(s.kv_lens, g.seq);
+  g.start = g.start < 0 ? 0 : g.start;
   end = end < s.num_tokens ? end : s.num_tokens;
-  const int32_t count = end - start < s.max_tokens ? end - start : s.max_tokens;
-  const int64_t row0 = int64_t(tile) * kRows;
-  if (row0 >= int64_t(count) * a.group) return;  // the whole workgroup
-  kv_len = kv_len < 0 ? 0 : kv_len < s.max_kv ? kv_len : s.max_kv;
-  Sight see[RT];
-  Span span{-1, 0x7FFFFFFF, -1, 0x7FFFFFFF, 0, 0, 0};
-  u32x4 q[RT][kQkSteps];
-  float q_sum[RT], f[RT];
+  g.trail = end - g.start;
+  g.count = g.trail < s.max_tokens ? g.trail : s.max_tokens;
+  g.kv_len = g.kv_len < 0 ? 0 : g.kv_len < s.max_kv ? g.kv_len : s.max_kv;
+  return g;
+}
+
+// Rows row0 + 16 r + x of the group: what they see (and the lane's part of the span) and their queries in the
+// operands' order, 8 channels from first(i) on in instruction i.
+template <int KB, int RT, typename First>
+__device__ __forceinline__ void load_rows(const ServeArgs& s, const AttendArgs& a, const Group& g, uint32_t row0, int x,
+                                          First first, Rows<RT>& rows, Span& span) {
+  constexpr bool kCodes = KB != 16;
+  span = Span{-1, 0x7FFFFFFF, -1, 0x7FFFFFFF, 0, 0, 0};
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const uint32_t row = uint32_t(row0) + kRowTile * r + x;
+    const uint32_t row = row0 + kRowTile * r + x;
     const int32_t token = int32_t(row / uint32_t(a.group)), sub = int32_t(row % uint32_t(a.group));
-    const bool on = token < count;
-    see[r] = Sight{-1, -1};
+    const bool on = token < g.count;
+    Sight see{-1, -1};
     if (on) {
-      const int32_t pos = s.positions ? s.positions[start + token] : kv_len - (end - start) + token;
-      see[r].hi = pos < kv_len ? pos : kv_len - 1;
-      see[r].hi = see[r].hi < -1 ? -1 : see[r].hi;
-      see[r].lo = a.window > 0 && pos >= a.window ? pos - a.window : -1;
-      span.hi_least = span.hi_least < see[r].hi ? span.hi_least : see[r].hi;
-      if (see[r].hi >= 0 && see[r].lo < span.lo_least) span.lo_least = see[r].lo;
+      const int32_t pos = s.positions ? s.positions[g.start + token] : g.kv_len - g.trail + token;
+      see.hi = pos < g.kv_len ? pos : g.kv_len - 1;
+      see.hi = see.hi < -1 ? -1 : see.hi;
+      see.lo = a.window > 0 && pos >= a.window ? pos - a.window : -1;
+      span.hi_least = span.hi_least < see.hi ? span.hi_least : see.hi;
+      if (see.hi >= 0 && see.lo < span.lo_least) span.lo_least = see.lo;
     }
-    span.hi_most = span.hi_most > see[r].hi ? span.hi_most : see[r].hi;
-    span.lo_most = span.lo_most > see[r].lo ? span.lo_most : see[r].lo;
+    span.hi_most = span.hi_most > see.hi ? span.hi_most : see.hi;
+    span.lo_most = span.lo_most > see.lo ? span.lo_most : see.lo;
+    rows.see[r] = see;
 
-    // The queries, in the operands' order, and their sum.
-    q_sum[r] = 0.0f;
-    f[r] = a.scale;
-    const uint16_t* from_q = a.q + int64_t(start + token) * a.q_token_stride +
-                             int64_t(head * a.group + sub) * a.q_head_stride + c * (D / 4);
+    rows.q_sum[r] = 0.0f;
+    rows.f[r] = a.scale;
+    const uint16_t* from = a.q + int64_t(g.start + token) * a.q_token_stride +
+                           int64_t(g.head * a.group + sub) * a.q_head_stride;
     float v[kQkSteps][8];
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < kQkSteps; ++i) {
       u32x4 w{};
-      if (on) w = *reinterpret_cast<const u32x4*>(from_q + 8 * i);
+      if (on) w = *reinterpret_cast<const u32x4*>(from + first(i));
       if constexpr (!kCodes) {
-        q[r][i] = w;
+        rows.q[r][i] = w;
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -558,38 +573,50 @@ __global__ __launch_bounds__(kThreads, RT * D > 256 ? 1 : 2) void attend_kernel(
       int e = int(top >> 23) - 127;
       e = e < -60 ? -60 : e > 120 ? 120 : e;  // f stays a normal number
       const float down = __uint_as_float(uint32_t(127 - e) << 23);
-      f[r] *= __uint_as_float(uint32_t(127 + e) << 23);
+      rows.f[r] *= __uint_as_float(uint32_t(127 + e) << 23);
 #pragma unroll
       for (int i = 0; i < kQkSteps; ++i) {
 #pragma unroll
         for (int p = 0; p < 4; ++p)
-          q[r][i][p] = pack_f16(v[i][k_channel<KB>(p, 0)] * down, v[i][k_channel<KB>(p, 1)] * down);
+          rows.q[r][i][p] = pack_f16(v[i][k_channel<KB>(p, 0)] * down, v[i][k_channel<KB>(p, 1)] * down);
 #pragma unroll
-        for (int e2 = 0; e2 < 8; ++e2) q_sum[r] += v[i][e2] * down;
+        for (int e2 = 0; e2 < 8; ++e2) rows.q_sum[r] += v[i][e2] * down;
       }
-      q_sum[r] = over_c_sum(q_sum[r]);
+      rows.q_sum[r] = over_c_sum(rows.q_sum[r]);
     }
   }
   span.hi_most = __builtin_amdgcn_readfirstlane(over_x_max(span.hi_most));
   span.hi_least = __builtin_amdgcn_readfirstlane(over_x_min(span.hi_least));
   span.lo_most = __builtin_amdgcn_readfirstlane(over_x_max(span.lo_most));
   span.lo_least = __builtin_amdgcn_readfirstlane(over_x_min(span.lo_least));
+}
+
+// The tiles of TOKENS tokens that some row of a span sees, and the first and the end of a split's share.
+template <int TOKENS>
+__device__ __forceinline__ void tiles_of(const AttendArgs& a, int32_t split, Span& span, int32_t& from, int32_t& upto) {
+  span.first = span.sink_tiles = span.tiles = 0;
   if (span.hi_most >= 0) {
-    span.first = (span.lo_least + 1) & ~(kTokenTile - 1);
+    span.first = (span.lo_least + 1) & ~(TOKENS - 1);
     const int32_t sinks = a.sinks < span.hi_most + 1 ? a.sinks : span.hi_most + 1;
-    span.sink_tiles = (sinks + kTokenTile - 1) / kTokenTile;
-    span.sink_tiles = span.sink_tiles < span.first / kTokenTile ? span.sink_tiles : span.first / kTokenTile;
+    span.sink_tiles = (sinks + TOKENS - 1) / TOKENS;
+    span.sink_tiles = span.sink_tiles < span.first / TOKENS ? span.sink_tiles : span.first / TOKENS;
     // (a position past kv_lens may leave a row its sinks alone)
-    span.tiles = span.sink_tiles + (span.hi_most >= span.first ? (span.hi_most - span.first) / kTokenTile + 1 : 0);
+    span.tiles = span.sink_tiles + (span.hi_most >= span.first ? (span.hi_most - span.first) / TOKENS + 1 : 0);
   }
-  // This workgroup's share of them.
   int32_t share = (span.tiles + a.splits - 1) / a.splits;
   share = share > a.chunk ? share : a.chunk;
-  const int64_t from = int64_t(split) * share;
-  const int32_t upto = int32_t(from + share < span.tiles ? from + share : span.tiles);
+  const int64_t begin = int64_t(split) * share;
+  from = int32_t(begin < span.tiles ? begin : span.tiles);
+  upto = int32_t(begin + share < span.tiles ? begin + share : span.tiles);
+}
 
-  const int32_t* table = s.page_table + int64_t(seq) * s.pages_per_seq;
-  Running<RT> st;
+template <int TOKENS>
+__device__ __forceinline__ int32_t tile_at(const Span& span, int32_t it) {
+  return it < span.sink_tiles ? it * TOKENS : span.first + (it - span.sink_tiles) * TOKENS;
+}
+
+template <int RT>
+__device__ __forceinline__ void begin(Running<RT>& st) {
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     st.ref[r] = -kInf;
@@ -599,41 +626,98 @@ __global__ __launch_bounds__(kThreads, RT * D > 256 ? 1 : 2) void attend_kernel(
   }
   st.fac = 1.0f;
   st.most_scale = 0.0f;
+}
 
-  auto tile_at = [&](int32_t it) {
-    return it < span.sink_tiles ? it * kTokenTile : span.first + (it - span.sink_tiles) * kTokenTile;
-  };
+__device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
+// Log-sum-exp from the reference (base 2) and the sum, which counts `up` of what it stands for.
+__device__ __forceinline__ float lse_of(float ref, float l, float up) {
+  return l == 0.0f ? -kInf : (ref + __builtin_amdgcn_logf(l * up)) * 0.69314718055994531f;
+}
+template <bool BF16, int KB>
+constexpr float kUp = KB != 16 || BF16 ? 1.0f : 1.0f / 64.0f;  // 2^-kShift where p carries it into the sum
+
+// Few rows (kRowTile * RT): the four waves of a workgroup share them and deal the tiles of tokens among
+// themselves.  Each lane's pieces of the cache go from memory to its registers and, decoded, straight
+// into the matrix instructions.
+template <bool BF16, int KB, int VB, bool WHOLE, int RT>
+__global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, AttendArgs a) {
+  constexpr bool kCodes = KB != 16;
+  constexpr int kRows = kRowTile * RT;
+  __shared__ float join_ml[kWaves][kRowTile][2];
+  __shared__ float join[kWaves][kRowTile][D + 4];
+
+  const Group g = group_of(s, a);
+  const int lane = threadIdx.x & 63, c = lane >> 4, x = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row0 = int64_t(g.tile) * kRows;
+  if (row0 >= int64_t(g.count) * a.group) return;  // the whole workgroup
+  Rows<RT> rows;
+  Span span;
+  load_rows<KB, RT>(s, a, g, uint32_t(row0), x, [&](int i) { return k_first<KB>(i, c); }, rows, span);
+  int32_t from, upto;
+  tiles_of<kTokenTile>(a, g.split, span, from, upto);
+
+  const int32_t* table = s.page_table + int64_t(g.seq) * s.pages_per_seq;
+  Running<RT> st;
+  begin(st);
   auto pages_at = [&](int32_t it, int32_t (&pages)[2]) {  // of a tile that exists, else -1
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int32_t at = (tile_at(it) + 16 * u) >> s.log2P;
+      const int32_t at = (tile_at<kTokenTile>(span, it) + 16 * u) >> s.log2P;
       pages[u] = WHOLE && it < upto && at < s.pages_per_seq ? scalar_entry(table, at) : -1;
       pages[u] = pages[u] < s.pool_pages ? pages[u] : -1;
     }
   };
   // A tile's keys are loaded while the softmax and the sums of the one before run, its values while its own
   // scores are computed, its pages one tile earlier.
-  int32_t it = int32_t(from) + wave;
+  int32_t it = from + wave;
   if (it < upto) {
     Keys<KB> keys;
     Values<VB> values;
     int32_t pages[2], next[2];
     pages_at(it, pages);
-    load_keys<KB, WHOLE>(s, table, head, tile_at(it), pages, c, x, keys);
-    load_values<VB, WHOLE>(s, table, head, tile_at(it), pages, c, x, values);
+    load_keys<KB, WHOLE>(s, table, g.head, tile_at<kTokenTile>(span, it), pages, c, x, keys);
+    load_values<VB, WHOLE>(s, table, g.head, tile_at<kTokenTile>(span, it), pages, c, x, values);
     pages_at(it + kWaves, next);
     for (; it < upto; it += kWaves) {
-      const int32_t t0 = tile_at(it), t1 = tile_at(it + kWaves);
+      const int32_t t0 = tile_at<kTokenTile>(span, it), t1 = tile_at<kTokenTile>(span, it + kWaves);
       const bool more = it + kWaves < upto;
       const uint32_t there = tokens_there<WHOLE>(s, table, t0, pages, c);
+      Scales sc;
+      if constexpr (kCodes) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sc.ks[u][i] = f16_float(keys.scale[u][i]);
+            sc.kz[u][i] = __builtin_fmaf(sc.ks[u][i], float(1 << (KB - 1)), f16_float(keys.scale[u][i] >> 16));
+            sc.vs[u][i] = f16_float(values.scale[u][i]);
+            sc.vz[u][i] = __builtin_fmaf(sc.vs[u][i], float(1 << (VB - 1)), f16_float(values.scale[u][i] >> 16));
+          }
+      }
       attend_tile<BF16, KB, VB, RT>(
-          a, span, see, q, q_sum, f, c, t0, there, keys, values, st,
-          [&] {
-            if (more) load_keys<KB, WHOLE>(s, table, head, t1, next, c, x, keys);
+          a, span, rows, c, t0, there, sc, st, [&](int u, int i) { return k_operand<KB>(keys.w[u], i); },
+          [&](int j) {
+            u32x4 v;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) v[2 * u + i] = v_pair<VB>(values.w[u][2 * i], values.w[u][2 * i + 1], j);
+            return v;
           },
           [&] {
-            if (more) load_values<VB, WHOLE>(s, table, head, t1, next, c, x, values);
+            if (more) load_keys<KB, WHOLE>(s, table, g.head, t1, next, c, x, keys);
+          },
+          [&](const u32x4& keep) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int w = 0; w < Values<VB>::kWords; ++w)
+                  values.w[u][i][w] = (keep[2 * u + i / 2] >> (16 * (i & 1))) & 1 ? values.w[u][i][w] : 0;
           });
+      if (more) load_values<VB, WHOLE>(s, table, g.head, t1, next, c, x, values);
       pages[0] = next[0];
       pages[1] = next[1];
       pages_at(it + 2 * kWaves, next);
@@ -667,8 +751,8 @@ __global__ __launch_bounds__(kThreads, RT * D > 256 ? 1 : 2) void attend_kernel(
     const int y = threadIdx.x / kPerRow, at = (threadIdx.x % kPerRow) * kPer;
     const uint32_t out_row = uint32_t(row0) + kRowTile * r + y;
     const int32_t out_token = int32_t(out_row / uint32_t(a.group));
-    if (out_token >= count) continue;
-    const int32_t out_head = head * a.group + int32_t(out_row % uint32_t(a.group));
+    if (out_token >= g.count) continue;
+    const int32_t out_head = g.head * a.group + int32_t(out_row % uint32_t(a.group));
     float mm = -kInf, ll = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) mm = __builtin_fmaxf(mm, join_ml[w][y][0]);
@@ -682,62 +766,322 @@ __global__ __launch_bounds__(kThreads, RT * D > 256 ? 1 : 2) void attend_kernel(
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) sum[e] += join[w][y][at + e];
     }
-    const int64_t flat = int64_t(start + out_token) * a.Hq + out_head;
+    const int64_t flat = int64_t(g.start + out_token) * a.Hq + out_head;
     if (a.splits > 1) {
-      const int64_t slot = flat * a.splits + split;
+      const int64_t slot = flat * a.splits + g.split;
 #pragma unroll
       for (int e = 0; e < kPer; e += 4)
         *reinterpret_cast<f32x4*>(a.part + slot * D + at + e) = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
       if (at == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * slot) = f32x2{mm, ll};
       continue;
     }
-    const float inv = ll > 0.0f ? 1.0f / ll : ll == 0.0f ? 0.0f : ll;
+    const float inv = inverse(ll);
     uint32_t word[kPer / 2];
 #pragma unroll
     for (int e = 0; e < kPer; e += 2)
       word[e / 2] = s.bf16 ? pack_bf16(sum[e] * inv, sum[e + 1] * inv) : pack_f16(sum[e] * inv, sum[e + 1] * inv);
-    uint16_t* to = a.out + int64_t(start + out_token) * a.out_token_stride + int64_t(out_head) * a.out_head_stride + at;
+    uint16_t* to = a.out + int64_t(g.start + out_token) * a.out_token_stride + int64_t(out_head) * a.out_head_stride + at;
 #pragma unroll
     for (int e = 0; e < kPer / 2; e += 2) *reinterpret_cast<u32x2*>(to + 2 * e) = u32x2{word[e], word[e + 1]};
-    constexpr float kUp = kCodes || BF16 ? 1.0f : 1.0f / 64.0f;  // l counts 2^kShift to one where p does
-    if (a.lse && at == 0)
-      a.lse[flat] = ll == 0.0f ? -kInf : (mm + __builtin_amdgcn_logf(ll * kUp)) * 0.69314718055994531f;
+    if (a.lse && at == 0) a.lse[flat] = lse_of(mm, ll, kUp<BF16, KB>);
   }
 }
 
-// Joins the splits of each row: one wave per row.
+// Many rows: each wave has 32 of its own (16 at 256 channels), and the workgroup's four share the cache through LDS.  A tile of
+// kManyTokens tokens (64 at 128 channels: 16 KiB of keys, 16 of values, in binary16 or the cache's type) is decoded
+// once for all of them and lies in LDS as the matrix operands want it, 16 bytes to a lane; two tiles take
+// turns, the next one's loads in flight while one is computed, with one barrier to a tile.  Waves 0 and 1
+// bring the values, waves 2 and 3 the keys.
+constexpr int kManyTokens = kManyElems / D;
+constexpr int kManyRows = kRowTile * many_tiles(D) / kWaves;  // of a wave
+constexpr int kOperand = 64 * 4;  // words of one operand of a wave
+
+template <int KB, int VB>
+struct ManyLds {
+  uint32_t k[2][kManyElems / 2];
+  uint32_t v[2][kManyElems / 2];
+  float scale[2][4][KB != 16 ? kManyTokens : 1];  // ks, kz, vs, vz
+  int64_t k_off[2][kManyTokens];                  // bytes from the layer's first key (code) to the token's row of this head
+  int64_t v_off[2][KB != 16 ? kManyTokens : 1];
+  int64_t s_off[2][KB != 16 ? kManyTokens : 1];   // words to its key scale
+  uint64_t there[4][2];                           // (written two tiles ahead, while a tile's own is read)
+  int32_t span[kWaves][4];
+};
+
+template <bool BF16, int KB, int VB>
+__global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, AttendArgs a) {
+  constexpr bool kCodes = KB != 16;
+  constexpr int RT = kManyRows / kRowTile;
+  __shared__ __attribute__((aligned(16))) ManyLds<KB, VB> m;
+
+  const Group g = group_of(s, a);
+  const int tid = threadIdx.x, lane = tid & 63, c = lane >> 4, x = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t group_row0 = int64_t(g.tile) * (kManyRows * kWaves);
+  if (group_row0 >= int64_t(g.count) * a.group) return;  // the whole workgroup
+  const uint32_t row0 = uint32_t(group_row0) + wave * kManyRows;
+  Rows<RT> rows;
+  Span mine;
+  load_rows<KB, RT>(s, a, g, row0, x, [&](int i) { return 32 * i + 8 * c; }, rows, mine);
+  if (lane == 0) {
+    m.span[wave][0] = mine.hi_most;
+    m.span[wave][1] = mine.lo_least;
+  }
+  __syncthreads();
+  Span span = mine;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    span.hi_most = span.hi_most > m.span[w][0] ? span.hi_most : m.span[w][0];
+    span.lo_least = span.lo_least < m.span[w][1] ? span.lo_least : m.span[w][1];
+  }
+  int32_t from, upto;
+  tiles_of<kManyTokens>(a, g.split, span, from, upto);
+  from = __builtin_amdgcn_readfirstlane(from);
+  upto = __builtin_amdgcn_readfirstlane(upto);
+
+  const int32_t* table = s.page_table + int64_t(g.seq) * s.pages_per_seq;
+  // Where the tokens of a tile lie, one thread to a token; a token that is not there is read from page 0.
+  auto entry_of = [&](int32_t it) -> int32_t {
+    return tid < kManyTokens ? page_of(s, table, (tile_at<kManyTokens>(span, it) + tid) >> s.log2P) : -1;
+  };
+  auto put_places = [&](int32_t it, int32_t entry) {
+    if (wave * 64 >= kManyTokens) return;
+    const int b = it & 1;
+    const uint64_t there = __ballot(entry >= 0);
+    if (lane == 0) m.there[it & 3][wave] = there;
+    if (tid >= kManyTokens) return;
+    const int64_t slot = (tile_at<kManyTokens>(span, it) + tid) & ((1 << s.log2P) - 1), page = entry >= 0 ? entry : 0;
+    if constexpr (kCodes) {
+      const int64_t at = page * s.page_stride + g.head * s.head_stride;
+      m.k_off[b][tid] = at + slot * (D * KB / 8);
+      m.v_off[b][tid] = at + s.v_offset + slot * (D * VB / 8);
+      m.s_off[b][tid] = page * s.scale_stride + ((int64_t(g.head) * 2) << s.log2P) + slot;
+    } else {
+      m.k_off[b][tid] = 2 * (page * s.page_stride + slot * s.H * D + g.head * D);
+    }
+  };
+  // A thread's share of a tile: 64 values (8 tokens x 8 channels), or 64 keys (two pieces of 32 channels of a token, or
+  // eight of 8), and the scales of a token.
+  constexpr int kPairs = D / 32;
+  uint32_t raw[2 * (KB > VB ? KB : VB)];
+  uint32_t raw_scale[2];
+  const int kt = tid - 128;
+  auto bring = [&](int32_t it) {
+    const int b = it & 1;
+    if (wave < 2) {
+      const int piece = tid % (D / 8), tokens = tid / (D / 8) * 8;  // tokens: 32 p + {4c.., 16 + 4c..}
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const int tok = tokens / 32 * 32 + (n >> 2) * 16 + (tokens % 32) / 2 + (n & 3);
+        if constexpr (kCodes)
+          load_bytes<VB>(raw + n * (VB / 4), s.codes + m.v_off[b][tok] + piece * VB);
+        else
+          load_bytes<16>(raw + 4 * n, reinterpret_cast<const char*>(s.v_cache) + m.k_off[b][tok] + piece * 16);
+      }
+    } else if constexpr (kCodes) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int id = kt + 128 * n, tok = id / 16 / kPairs * 16 + id % 16, i = id / 16 % kPairs;
+        load_bytes<4 * KB>(raw + n * KB, s.codes + m.k_off[b][tok] + i * (4 * KB));
+      }
+      if (kt < kManyTokens) {
+        raw_scale[0] = s.scales[m.s_off[b][kt]];
+        raw_scale[1] = s.scales[m.s_off[b][kt] + (int64_t(1) << s.log2P)];
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const int id = kt + 128 * n, tok = id / (D / 8), piece = id % (D / 8);
+        load_bytes<16>(raw + 4 * n, reinterpret_cast<const char*>(s.k_cache) + m.k_off[b][tok] + piece * 16);
+      }
+    }
+  };
+  // Into LDS.  The 16 tokens of a key operand are permuted by its channels, so that threads that hold one token's channels
+  // write to all banks.
+  auto put_key = [&](int b, int tok, int i, int cc, const u32x4& w) {
+    const int at = ((tok / 16) * kPairs + i) * kOperand + (cc * 16 + ((tok % 16) ^ ((4 * i + cc) & 15))) * 4;
+    *reinterpret_cast<u32x4*>(&m.k[b][at]) = w;
+  };
+  auto put_tile = [&](int32_t it) {
+    const int b = it & 1;
+    if (wave < 2) {
+      const int piece = tid % (D / 8), tokens = tid / (D / 8) * 8, cc = tokens % 32 / 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int channel = 8 * piece + e, row = channel / kChannels, j = channel % kChannels;
+        u32x4 w;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          constexpr int kStep = VB == 16 ? 4 : VB / 4;
+          w[n] = v_pair<VB>(raw + 2 * n * kStep, raw + (2 * n + 1) * kStep, e);
+        }
+        *reinterpret_cast<u32x4*>(&m.v[b][(tokens / 32 * kChannels + j) * kOperand + (cc * 16 + row) * 4]) = w;
+      }
+    } else if constexpr (kCodes) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int id = kt + 128 * n, tok = id / 16 / kPairs * 16 + id % 16, i = id / 16 % kPairs;
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc) put_key(b, tok, i, cc, k_operand<KB>(raw + n * KB, cc));
+      }
+      if (kt < kManyTokens) {
+        const float ks = f16_float(raw_scale[0]), vs = f16_float(raw_scale[1]);
+        m.scale[b][0][kt] = ks;
+        m.scale[b][1][kt] = __builtin_fmaf(ks, float(1 << (KB - 1)), f16_float(raw_scale[0] >> 16));
+        m.scale[b][2][kt] = vs;
+        m.scale[b][3][kt] = __builtin_fmaf(vs, float(1 << (VB - 1)), f16_float(raw_scale[1] >> 16));
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const int id = kt + 128 * n, tok = id / (D / 8), piece = id % (D / 8);
+        put_key(b, tok, piece / 4, piece % 4, u32x4{raw[4 * n], raw[4 * n + 1], raw[4 * n + 2], raw[4 * n + 3]});
+      }
+    }
+  };
+
+  Running<RT> st;
+  begin(st);
+  if (from < upto) {
+    put_places(from, entry_of(from));
+    __syncthreads();
+    bring(from);
+    if (from + 1 < upto) put_places(from + 1, entry_of(from + 1));
+    put_tile(from);
+    __syncthreads();
+    for (int32_t it = from; it < upto; ++it) {
+      const int b = it & 1;
+      const bool more = it + 1 < upto, later = it + 2 < upto;
+      if (more) bring(it + 1);
+      const int32_t entry = later ? entry_of(it + 2) : -1;
+      const int32_t t0 = tile_at<kManyTokens>(span, it);
+#pragma unroll
+      for (int p = 0; p < kManyTokens / 32; ++p) {
+        const int32_t t = t0 + 32 * p;
+        if (t > mine.hi_most || (t + 31 <= mine.lo_least && t >= a.sinks)) continue;  // no row of this wave sees it
+        const uint32_t word = uint32_t(m.there[it & 3][p >> 1] >> (32 * (p & 1)));
+        const uint32_t there = ((word >> (4 * c)) & 0xF) | (((word >> (16 + 4 * c)) & 0xF) << 4);
+        Scales sc;
+        u32x4 keep = {~0u, ~0u, ~0u, ~0u};
+        if constexpr (kCodes) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int at = 32 * p + 16 * u + 4 * c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              sc.ks[u][i] = m.scale[b][0][at + i];
+              sc.kz[u][i] = m.scale[b][1][at + i];
+              sc.vs[u][i] = m.scale[b][2][at + i];
+              sc.vz[u][i] = m.scale[b][3][at + i];
+            }
+          }
+        }
+        attend_tile<BF16, KB, VB, RT>(
+            a, mine, rows, c, t, there, sc, st,
+            [&](int u, int i) {
+              return *reinterpret_cast<const u32x4*>(
+                  &m.k[b][((2 * p + u) * kPairs + i) * kOperand + (c * 16 + (x ^ ((4 * i + c) & 15))) * 4]);
+            },
+            [&](int j) { return *reinterpret_cast<const u32x4*>(&m.v[b][(p * kChannels + j) * kOperand + lane * 4]) & keep; },
+            [] {}, [&](const u32x4& seen) { keep = seen; });
+      }
+      if (more) put_tile(it + 1);
+      if (later) put_places(it + 2, entry);
+      __syncthreads();
+    }
+  }
+
+  // Every row's sums are one wave's.
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const float l = over_c_sum(st.l[r]);
+    const float o_zero = kCodes ? over_c_sum(st.o_zero[r]) : 0.0f;
+    const uint32_t row = row0 + kRowTile * r + x;
+    const int32_t token = int32_t(row / uint32_t(a.group)), out_head = g.head * a.group + int32_t(row % uint32_t(a.group));
+    if (token >= g.count) continue;
+    const int64_t flat = int64_t(g.start + token) * a.Hq + out_head;
+    const float unit = kCodes ? 1.0f / st.fac : 1.0f;
+    if (a.splits > 1) {
+      const int64_t slot = flat * a.splits + g.split;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < kChannels; j += 4) {
+          f32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = kCodes ? __builtin_fmaf(st.o[r][j + e][i], unit, o_zero) : st.o[r][j + e][i];
+          *reinterpret_cast<f32x4*>(a.part + slot * D + (4 * c + i) * kChannels + j) = w;
+        }
+      if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * slot) = f32x2{st.ref[r], l};
+      continue;
+    }
+    const float inv = inverse(l);
+    uint16_t* to = a.out + int64_t(g.start + token) * a.out_token_stride + int64_t(out_head) * a.out_head_stride;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < kChannels; j += 4) {
+        float w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = (kCodes ? __builtin_fmaf(st.o[r][j + e][i], unit, o_zero) : st.o[r][j + e][i]) * inv;
+        *reinterpret_cast<u32x2*>(to + (4 * c + i) * kChannels + j) =
+            s.bf16 ? u32x2{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])} : u32x2{pack_f16(w[0], w[1]), pack_f16(w[2], w[3])};
+      }
+    if (a.lse && c == 0) a.lse[flat] = lse_of(st.ref[r], l, kUp<BF16, KB>);
+  }
+}
+
+// Joins the splits of each row, one workgroup to a row: D / 4 threads to a split's sums, the splits dealt to
+// the groups of so many threads.
 __global__ __launch_bounds__(kThreads) void join_kernel(ServeArgs s, AttendArgs a, float up) {
-  const int lane = threadIdx.x & 63;
-  const int64_t flat = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-  if (flat >= int64_t(s.num_tokens) * a.Hq) return;
-  const int32_t token = int32_t(flat / a.Hq), head = int32_t(flat % a.Hq);
+  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
+  __shared__ float wave_most[kWaves];
+  __shared__ f32x4 sums[kGroups][kLanes];
+  __shared__ float parts[kGroups];
+  const int64_t flat = blockIdx.x;
+  const int32_t token = int32_t(uint32_t(flat) / uint32_t(a.Hq)), head = int32_t(uint32_t(flat) % uint32_t(a.Hq));
   // Rows of no sequence have no parts.
-  const int32_t first = s.token_start[0], last = s.token_start[s.num_seqs];
-  if (token < first || token >= last) return;
+  if (token < scalar_entry(s.token_start, 0) || token >= scalar_entry(s.token_start, s.num_seqs)) return;
   const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + flat * a.splits;
+  const f32x4* part = reinterpret_cast<const f32x4*>(a.part + flat * a.splits * D);
   float m = -kInf;
-  for (int i = lane; i < a.splits; i += 64) m = __builtin_fmaxf(m, ml[i][0]);
+  for (int i = threadIdx.x; i < a.splits; i += kThreads) m = __builtin_fmaxf(m, ml[i][0]);
   for (int off = 1; off < 64; off <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
+  if ((threadIdx.x & 63) == 0) wave_most[threadIdx.x >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) m = __builtin_fmaxf(m, wave_most[w]);
+  const int group = threadIdx.x / kLanes, at = threadIdx.x % kLanes;
   float l = 0.0f;
-  constexpr int kPer = D / 64;
-  float sum[kPer] = {};
-  for (int i = 0; i < a.splits; ++i) {
+  f32x4 sum{};
+#pragma unroll 4
+  for (int i = group; i < a.splits; i += kGroups) {
     const f32x2 w = ml[i];
-    if (w[1] == 0.0f) continue;
-    const float scale = exp2_of(w[0] - m);
+    const f32x4 p = part[int64_t(i) * kLanes + at];
+    // A split that saw nothing has sums of nothing in particular.
+    const float scale = w[1] == 0.0f ? 0.0f : exp2_of(w[0] - m);
     l += w[1] * scale;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e)
-      sum[e] = __builtin_fmaf(a.part[(flat * a.splits + i) * D + lane * kPer + e], scale, sum[e]);
+    for (int e = 0; e < 4; ++e) sum[e] += w[1] == 0.0f ? 0.0f : p[e] * scale;
   }
-  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-  uint16_t* to = a.out + token * a.out_token_stride + head * a.out_head_stride + lane * kPer;
+  sums[group][at] = sum;
+  if (at == 0) parts[group] = l;
+  __syncthreads();
+  if (group) return;
+  l = 0.0f;
+  sum = f32x4{};
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    const uint32_t w = s.bf16 ? pack_bf16(sum[e] * inv, 0.0f) : pack_f16(sum[e] * inv, 0.0f);
-    to[e] = uint16_t(w);
+  for (int i = 0; i < kGroups; ++i) {
+    l += parts[i];
+    sum += sums[i][at];
   }
-  if (a.lse && lane == 0) a.lse[flat] = l == 0.0f ? -kInf : (m + __builtin_amdgcn_logf(l * up)) * 0.69314718055994531f;
+  const float inv = inverse(l);
+  uint16_t* to = a.out + token * a.out_token_stride + head * a.out_head_stride + 4 * at;
+  sum *= inv;
+  *reinterpret_cast<u32x2*>(to) = s.bf16 ? u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])}
+                                         : u32x2{pack_f16(sum[0], sum[1]), pack_f16(sum[2], sum[3])};
+  if (a.lse && at == 0) a.lse[flat] = lse_of(m, l, up);
 }
 
 }  // namespace
@@ -748,29 +1092,36 @@ __global__ __launch_bounds__(kThreads) void join_kernel(ServeArgs s, AttendArgs 
 pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const AttendArgs& a, int64_t groups,
                                                       hipStream_t stream) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(uint32_t(groups)), dim3(kThreads), 0, stream, s, a); };
-  auto by_tag = [&](auto whole, auto tiles) {
+  auto few = [&](auto whole, auto tiles) {
     constexpr bool kWhole = decltype(whole)::value;
     constexpr int kTiles = decltype(tiles)::value;
     switch (s.tag) {
       case PKV_TAG_FP16:
-        s.bf16 ? go(attend_kernel<true, 16, 16, kWhole, kTiles>) : go(attend_kernel<false, 16, 16, kWhole, kTiles>);
+        s.bf16 ? go(attend_few_kernel<true, 16, 16, kWhole, kTiles>) : go(attend_few_kernel<false, 16, 16, kWhole, kTiles>);
         break;
-      case PKV_TAG_K8V8: go(attend_kernel<false, 8, 8, kWhole, kTiles>); break;
-      case PKV_TAG_K8V4: go(attend_kernel<false, 8, 4, kWhole, kTiles>); break;
-      default: go(attend_kernel<false, 4, 4, kWhole, kTiles>); break;
+      case PKV_TAG_K8V8: go(attend_few_kernel<false, 8, 8, kWhole, kTiles>); break;
+      case PKV_TAG_K8V4: go(attend_few_kernel<false, 8, 4, kWhole, kTiles>); break;
+      default: go(attend_few_kernel<false, 4, 4, kWhole, kTiles>); break;
     }
   };
-  auto by_tiles = [&](auto whole) {
-    if constexpr (kMostRowTiles >= 4)
-      if (a.tiles == 4) return by_tag(whole, std::integral_constant<int, 4>{});
-    a.tiles == 2 ? by_tag(whole, std::integral_constant<int, 2>{}) : by_tag(whole, std::integral_constant<int, 1>{});
+  auto few_of = [&](auto whole) {
+    a.tiles == 1 ? few(whole, std::integral_constant<int, 1>{}) : few(whole, std::integral_constant<int, few_tiles(D)>{});
   };
-  s.log2P >= 4 ? by_tiles(std::true_type{}) : by_tiles(std::false_type{});
+  if (a.tiles > few_tiles(D)) {
+    switch (s.tag) {
+      case PKV_TAG_FP16: s.bf16 ? go(attend_many_kernel<true, 16, 16>) : go(attend_many_kernel<false, 16, 16>); break;
+      case PKV_TAG_K8V8: go(attend_many_kernel<false, 8, 8>); break;
+      case PKV_TAG_K8V4: go(attend_many_kernel<false, 8, 4>); break;
+      default: go(attend_many_kernel<false, 4, 4>); break;
+    }
+  } else {
+    s.log2P >= 4 ? few_of(std::true_type{}) : few_of(std::false_type{});
+  }
   if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
   if (a.splits > 1) {
     const int64_t rows = int64_t(s.num_tokens) * a.Hq;
     const float up = s.tag == PKV_TAG_FP16 && !s.bf16 ? 1.0f / 64.0f : 1.0f;
-    hipLaunchKernelGGL(join_kernel, dim3(uint32_t((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, stream, s, a, up);
+    hipLaunchKernelGGL(join_kernel, dim3(uint32_t(rows)), dim3(kThreads), 0, stream, s, a, up);
     if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
   }
   return PKV_OK;

@@ -71,8 +71,12 @@ struct AttendLaunch {
 constexpr int kRowTile = 16;   // rows (token, query head of one KV head) of a matrix instruction
 constexpr int kTokenTile = 32; // cached tokens a wave takes at a time
 
-// Row tiles that a wave can hold: queries and sums of 64 rows of 128 channels take 192 registers.
-constexpr int most_row_tiles(int head_dim) { return head_dim > 128 ? 2 : 4; }
+// Up to few_tiles row tiles are shared by a workgroup's waves, which deal the tokens among themselves; more rows are
+// dealt to them, many_tiles row tiles to a workgroup, and the tokens shared: kManyElems keys and as many values at a
+// time.  (A wave's queries and sums take 6 registers a row of 128 channels: two row tiles leave room for two waves a SIMD.)
+constexpr int few_tiles(int head_dim) { return head_dim > 128 ? 1 : 2; }
+constexpr int many_tiles(int head_dim) { return 4 * few_tiles(head_dim); }
+constexpr int kManyElems = 8192;
 
 // Host checks that need no GPU; they fill the arguments.
 pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,

@@ -147,15 +147,16 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
 AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   AttendLaunch l{};
   const int64_t rows = int64_t(s.max_tokens) * a.group;
-  l.tiles = 1;
-  while (l.tiles < most_row_tiles(s.D) && rows > kRowTile * l.tiles) l.tiles *= 2;
+  const bool many = rows > kRowTile * few_tiles(s.D);
+  l.tiles = many ? many_tiles(s.D) : rows <= kRowTile ? 1 : few_tiles(s.D);
   l.row_tiles = int32_t((rows + kRowTile * l.tiles - 1) / (kRowTile * l.tiles));
   const int64_t base = int64_t(s.num_seqs) * s.H * l.row_tiles;
   // tokens that a row tile may have to look at
   int64_t seen = s.max_kv;
   if (a.window > 0 && !s.positions) seen = std::min<int64_t>(seen, int64_t(a.sinks) + a.window + s.max_tokens);
-  const int64_t tiles = std::max<int64_t>(1, (seen + kTokenTile - 1) / kTokenTile + 1);
-  const int64_t want = 4 * 256;
+  const int64_t tokens = many ? kManyElems / s.D : kTokenTile;
+  const int64_t tiles = std::max<int64_t>(1, (seen + tokens - 1) / tokens + 1);
+  const int64_t want = many ? 2 * 256 : 4 * 256;
   int64_t splits = base > 0 ? std::min(want / base, tiles / 4) : 1;
   splits = std::max<int64_t>(1, splits);
   l.splits = int32_t(splits);

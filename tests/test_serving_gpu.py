@@ -220,6 +220,13 @@ ATTEND = [
     (K4V4, BF16, 1, 4, 128, 16, (1500, 700), (1,), False, 0, 0),
     (FP16, BF16, 1, 4, 128, 16, (1500, 10), (1,), False, 200, 1000),
     (K8V4, BF16, 1, 2, 128, 16, (400,), (130,), True, 40, 5),
+    (FP16, HALF, 1, 3, 256, 16, (70, 200), (23, 31), False, 0, 0),
+    (FP16, BF16, 1, 1, 256, 2, (90,), (60,), True, 11, 3),
+    (K4V4, BF16, 2, 8, 64, 16, (33, 170), (4,), False, 0, 0),
+    (K8V8, HALF, 1, 8, 128, 16, (400, 9, 31), (4, 2, 4), False, 100, 7),
+    (FP16, BF16, 2, 8, 128, 8, (33, 170), (4,), False, 0, 0),
+    (K8V4, HALF, 1, 1, 64, 1, (260, 5), (140, 5), False, 128, 1),
+    (K4V4, BF16, 1, 4, 128, 16, (700,), (65,), True, 33, 70),
 ]
 
 
