@@ -790,8 +790,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, At
 // Many rows: each wave has 32 of its own (16 at 256 channels), and the workgroup's four share the cache through LDS.  A tile of
 // kManyTokens tokens (64 at 128 channels: 16 KiB of keys, 16 of values, in binary16 or the cache's type) is decoded
 // once for all of them and lies in LDS as the matrix operands want it, 16 bytes to a lane; two tiles take
-// turns, the next one's loads in flight while one is computed, with one barrier to a tile.  Waves 0 and 1
-// bring the values, waves 2 and 3 the keys.
+// turns, the next one's loads in flight while one is computed, with one barrier to a tile.
 constexpr int kManyTokens = kManyElems / D;
 constexpr int kManyRows = kRowTile * many_tiles(D) / kWaves;  // of a wave
 constexpr int kOperand = 64 * 4;  // words of one operand of a wave
@@ -840,103 +839,89 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
   upto = __builtin_amdgcn_readfirstlane(upto);
 
   const int32_t* table = s.page_table + int64_t(g.seq) * s.pages_per_seq;
-  // Where the tokens of a tile lie, one thread to a token; a token that is not there is read from page 0.
+  // Where the tokens of a tile lie; a token that is not there is read from page 0.  (More threads than tokens: the
+  // others repeat them.)
+  const int own = tid & (kManyTokens - 1);
   auto entry_of = [&](int32_t it) -> int32_t {
-    return tid < kManyTokens ? page_of(s, table, (tile_at<kManyTokens>(span, it) + tid) >> s.log2P) : -1;
+    const int32_t at = (tile_at<kManyTokens>(span, it) + own) >> s.log2P;
+    return table[at < s.pages_per_seq ? at : s.pages_per_seq - 1];
   };
   auto put_places = [&](int32_t it, int32_t entry) {
-    if (wave * 64 >= kManyTokens) return;
     const int b = it & 1;
-    const uint64_t there = __ballot(entry >= 0);
-    if (lane == 0) m.there[it & 3][wave] = there;
-    if (tid >= kManyTokens) return;
-    const int64_t slot = (tile_at<kManyTokens>(span, it) + tid) & ((1 << s.log2P) - 1), page = entry >= 0 ? entry : 0;
+    const int32_t t = tile_at<kManyTokens>(span, it) + own;
+    const bool is = entry >= 0 && entry < s.pool_pages && (t >> s.log2P) < s.pages_per_seq;
+    const uint64_t there = __ballot(is);
+    m.there[it & 3][wave & (sizeof(m.there[0]) / 8 - 1)] = there;
+    const int64_t slot = t & ((1 << s.log2P) - 1), page = is ? entry : 0;
     if constexpr (kCodes) {
       const int64_t at = page * s.page_stride + g.head * s.head_stride;
-      m.k_off[b][tid] = at + slot * (D * KB / 8);
-      m.v_off[b][tid] = at + s.v_offset + slot * (D * VB / 8);
-      m.s_off[b][tid] = page * s.scale_stride + ((int64_t(g.head) * 2) << s.log2P) + slot;
+      m.k_off[b][own] = at + slot * (D * KB / 8);
+      m.v_off[b][own] = at + s.v_offset + slot * (D * VB / 8);
+      m.s_off[b][own] = page * s.scale_stride + ((int64_t(g.head) * 2) << s.log2P) + slot;
     } else {
-      m.k_off[b][tid] = 2 * (page * s.page_stride + slot * s.H * D + g.head * D);
+      m.k_off[b][own] = 2 * (page * s.page_stride + slot * s.H * D + g.head * D);
     }
   };
-  // A thread's share of a tile: 64 values (8 tokens x 8 channels), or 64 keys (two pieces of 32 channels of a token, or
-  // eight of 8), and the scales of a token.
-  constexpr int kPairs = D / 32;
-  uint32_t raw[2 * (KB > VB ? KB : VB)];
-  uint32_t raw_scale[2];
-  const int kt = tid - 128;
+  // A thread's share of a tile: 32 values (8 tokens x 4 channels), 32 keys (32 channels of a token in codes, four times 8 in
+  // 16 bits) and, in codes, the scales of a token.
+  constexpr int kPairs = D / 32, kVPiece = VB / 2, kVWords = (kVPiece + 3) / 4;
+  uint32_t raw_k[kCodes ? KB : 16], raw_v[8][kVWords], raw_scale[2];
+  const int v_piece = tid % (D / 4), v_tokens = tid / (D / 4);  // tokens 32 (v_tokens / 4) + {0, 16} + 4 (v_tokens % 4) + 0..3
+  const int k_token = tid / 16 / kPairs * 16 + tid % 16, k_step = tid / 16 % kPairs;  // of codes
   auto bring = [&](int32_t it) {
     const int b = it & 1;
-    if (wave < 2) {
-      const int piece = tid % (D / 8), tokens = tid / (D / 8) * 8;  // tokens: 32 p + {4c.., 16 + 4c..}
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const int tok = tokens / 32 * 32 + (n >> 2) * 16 + (tokens % 32) / 2 + (n & 3);
-        if constexpr (kCodes)
-          load_bytes<VB>(raw + n * (VB / 4), s.codes + m.v_off[b][tok] + piece * VB);
-        else
-          load_bytes<16>(raw + 4 * n, reinterpret_cast<const char*>(s.v_cache) + m.k_off[b][tok] + piece * 16);
-      }
-    } else if constexpr (kCodes) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int id = kt + 128 * n, tok = id / 16 / kPairs * 16 + id % 16, i = id / 16 % kPairs;
-        load_bytes<4 * KB>(raw + n * KB, s.codes + m.k_off[b][tok] + i * (4 * KB));
-      }
-      if (kt < kManyTokens) {
-        raw_scale[0] = s.scales[m.s_off[b][kt]];
-        raw_scale[1] = s.scales[m.s_off[b][kt] + (int64_t(1) << s.log2P)];
-      }
+    if constexpr (kCodes) {
+      load_bytes<4 * KB>(raw_k, s.codes + m.k_off[b][k_token] + k_step * (4 * KB));
+      raw_scale[0] = s.scales[m.s_off[b][own]];
+      raw_scale[1] = s.scales[m.s_off[b][own] + (int64_t(1) << s.log2P)];
     } else {
 #pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const int id = kt + 128 * n, tok = id / (D / 8), piece = id % (D / 8);
-        load_bytes<16>(raw + 4 * n, reinterpret_cast<const char*>(s.k_cache) + m.k_off[b][tok] + piece * 16);
+      for (int n = 0; n < 4; ++n) {
+        const int id = tid + kThreads * n, tok = id / (D / 8), piece = id % (D / 8);
+        load_bytes<16>(raw_k + 4 * n, reinterpret_cast<const char*>(s.k_cache) + m.k_off[b][tok] + piece * 16);
       }
     }
+    const char* values = kCodes ? reinterpret_cast<const char*>(s.codes) : reinterpret_cast<const char*>(s.v_cache);
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const int tok = v_tokens / 4 * 32 + (n >> 2) * 16 + v_tokens % 4 * 4 + (n & 3);
+      load_bytes<kVPiece>(raw_v[n], values + (kCodes ? m.v_off[b][tok] : m.k_off[b][tok]) + v_piece * kVPiece);
+    }
   };
-  // Into LDS.  The 16 tokens of a key operand are permuted by its channels, so that threads that hold one token's channels
-  // write to all banks.
-  auto put_key = [&](int b, int tok, int i, int cc, const u32x4& w) {
-    const int at = ((tok / 16) * kPairs + i) * kOperand + (cc * 16 + ((tok % 16) ^ ((4 * i + cc) & 15))) * 4;
-    *reinterpret_cast<u32x4*>(&m.k[b][at]) = w;
+  // Into LDS.  The 16 tokens of a key operand and the 16 rows of a value operand are permuted so that the threads of a
+  // write, which hold one token's channels or neighbouring channels, reach all banks.
+  auto k_place = [](int u, int i, int cc, int token) {
+    return (u * kPairs + i) * kOperand + (cc * 16 + (token ^ ((4 * i + cc) & 15))) * 4;
+  };
+  auto v_place = [](int p, int j, int cc, int row) {
+    return (p * kChannels + j) * kOperand + (cc * 16 + (row ^ (j / 4 * (64 / kChannels) & 15))) * 4;
   };
   auto put_tile = [&](int32_t it) {
     const int b = it & 1;
-    if (wave < 2) {
-      const int piece = tid % (D / 8), tokens = tid / (D / 8) * 8, cc = tokens % 32 / 8;
+    if constexpr (kCodes) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int channel = 8 * piece + e, row = channel / kChannels, j = channel % kChannels;
-        u32x4 w;
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          constexpr int kStep = VB == 16 ? 4 : VB / 4;
-          w[n] = v_pair<VB>(raw + 2 * n * kStep, raw + (2 * n + 1) * kStep, e);
-        }
-        *reinterpret_cast<u32x4*>(&m.v[b][(tokens / 32 * kChannels + j) * kOperand + (cc * 16 + row) * 4]) = w;
-      }
-    } else if constexpr (kCodes) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int id = kt + 128 * n, tok = id / 16 / kPairs * 16 + id % 16, i = id / 16 % kPairs;
-#pragma unroll
-        for (int cc = 0; cc < 4; ++cc) put_key(b, tok, i, cc, k_operand<KB>(raw + n * KB, cc));
-      }
-      if (kt < kManyTokens) {
-        const float ks = f16_float(raw_scale[0]), vs = f16_float(raw_scale[1]);
-        m.scale[b][0][kt] = ks;
-        m.scale[b][1][kt] = __builtin_fmaf(ks, float(1 << (KB - 1)), f16_float(raw_scale[0] >> 16));
-        m.scale[b][2][kt] = vs;
-        m.scale[b][3][kt] = __builtin_fmaf(vs, float(1 << (VB - 1)), f16_float(raw_scale[1] >> 16));
-      }
+      for (int cc = 0; cc < 4; ++cc)
+        *reinterpret_cast<u32x4*>(&m.k[b][k_place(k_token / 16, k_step, cc, k_token % 16)]) = k_operand<KB>(raw_k, cc);
+      const float ks = f16_float(raw_scale[0]), vs = f16_float(raw_scale[1]);
+      m.scale[b][0][own] = ks;
+      m.scale[b][1][own] = __builtin_fmaf(ks, float(1 << (KB - 1)), f16_float(raw_scale[0] >> 16));
+      m.scale[b][2][own] = vs;
+      m.scale[b][3][own] = __builtin_fmaf(vs, float(1 << (VB - 1)), f16_float(raw_scale[1] >> 16));
     } else {
 #pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const int id = kt + 128 * n, tok = id / (D / 8), piece = id % (D / 8);
-        put_key(b, tok, piece / 4, piece % 4, u32x4{raw[4 * n], raw[4 * n + 1], raw[4 * n + 2], raw[4 * n + 3]});
+      for (int n = 0; n < 4; ++n) {
+        const int id = tid + kThreads * n, tok = id / (D / 8), piece = id % (D / 8);
+        *reinterpret_cast<u32x4*>(&m.k[b][k_place(tok / 16, piece / 4, piece % 4, tok % 16)]) =
+            u32x4{raw_k[4 * n], raw_k[4 * n + 1], raw_k[4 * n + 2], raw_k[4 * n + 3]};
       }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int channel = 4 * v_piece + e;
+      u32x4 w;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) w[n] = v_pair<VB>(raw_v[2 * n], raw_v[2 * n + 1], e);
+      *reinterpret_cast<u32x4*>(&m.v[b][v_place(v_tokens / 4, channel % kChannels, v_tokens % 4, channel / kChannels)]) = w;
     }
   };
 
@@ -953,7 +938,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       const int b = it & 1;
       const bool more = it + 1 < upto, later = it + 2 < upto;
       if (more) bring(it + 1);
-      const int32_t entry = later ? entry_of(it + 2) : -1;
+      int32_t entry = later ? entry_of(it + 2) : -1;
       const int32_t t0 = tile_at<kManyTokens>(span, it);
 #pragma unroll
       for (int p = 0; p < kManyTokens / 32; ++p) {
@@ -979,12 +964,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
         attend_tile<BF16, KB, VB, RT>(
             a, mine, rows, c, t, there, sc, st,
             [&](int u, int i) {
-              return *reinterpret_cast<const u32x4*>(
-                  &m.k[b][((2 * p + u) * kPairs + i) * kOperand + (c * 16 + (x ^ ((4 * i + c) & 15))) * 4]);
+              return *reinterpret_cast<const u32x4*>(&m.k[b][k_place(2 * p + u, i, c, x)]);
             },
-            [&](int j) { return *reinterpret_cast<const u32x4*>(&m.v[b][(p * kChannels + j) * kOperand + lane * 4]) & keep; },
+            [&](int j) { return *reinterpret_cast<const u32x4*>(&m.v[b][v_place(p, j, c, x)]) & keep; },
             [] {}, [&](const u32x4& seen) { keep = seen; });
       }
+      // What was loaded is first looked at here, behind the whole tile's work.
+#pragma unroll
+      for (uint32_t& w : raw_k) asm volatile("" : "+v"(w));
+#pragma unroll
+      for (auto& row : raw_v)
+#pragma unroll
+        for (uint32_t& w : row) asm volatile("" : "+v"(w));
+      if constexpr (kCodes) asm volatile("" : "+v"(raw_scale[0]), "+v"(raw_scale[1]));
+      asm volatile("" : "+v"(entry));
       if (more) put_tile(it + 1);
       if (later) put_places(it + 2, entry);
       __syncthreads();
