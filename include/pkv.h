@@ -481,8 +481,9 @@ pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* c
  * exact products (codes and queries are exact in the matrix instructions'
  * binary16 operands, queries scaled by a power of two), probabilities are rounded
  * to binary16; 16-bit caches: probabilities are rounded to out_dtype.  What a
- * cache holds at places that no row of the call sees (NaN, infinities) does
- * not matter; a place that some row of a sequence sees should hold finite values.
+ * cache holds past kv_lens, on pages that are not there, before every row's window and behind
+ * the sinks (NaN, infinities) does not matter; what lies between places that
+ * rows of a sequence see should be finite.
  * At most two kernels on `hip_stream`.  Errors as pkv_cache_append. */
 typedef struct {
   int32_t num_q_heads; /* a multiple of num_kv_heads */

@@ -369,6 +369,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
       for (int r = 0; r < RT; ++r) t[r][u] = mfma(k, rows.q[r][i], t[r][u]);
     }
   }
+  after_keys();
   if constexpr (kCodes) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -378,7 +379,6 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
         for (int r = 0; r < RT; ++r)
           t[r][u][i] = __builtin_fmaf(sc.ks[u][i], t[r][u][i], sc.kz[u][i] * rows.q_sum[r]);
   }
-  after_keys();
   if (!all) {
     u32x4 keep{};
     // A row's score where it does not see; the values of tokens that no row of the wave sees, whatever lies there.
@@ -793,13 +793,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, At
 // turns, the next one's loads in flight while one is computed, with one barrier to a tile.
 constexpr int kManyTokens = kManyElems / D;
 constexpr int kManyRows = kRowTile * many_tiles(D) / kWaves;  // of a wave
-constexpr int kOperand = 64 * 4;  // words of one operand of a wave
+constexpr int kOperand = 64;  // 16-byte pieces of one operand of a wave
 
 template <int KB, int VB>
 struct ManyLds {
-  uint32_t k[2][kManyElems / 2];
-  uint32_t v[2][kManyElems / 2];
-  float scale[2][4][KB != 16 ? kManyTokens : 1];  // ks, kz, vs, vz
+  u32x4 k[2][kManyElems / 8];
+  u32x4 v[2][kManyElems / 8];
+  f32x4 scale[2][4][KB != 16 ? kManyTokens / 4 : 1];  // ks, kz, vs, vz
   int64_t k_off[2][kManyTokens];                  // bytes from the layer's first key (code) to the token's row of this head
   int64_t v_off[2][KB != 16 ? kManyTokens : 1];
   int64_t s_off[2][KB != 16 ? kManyTokens : 1];   // words to its key scale
@@ -851,7 +851,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
     const int32_t t = tile_at<kManyTokens>(span, it) + own;
     const bool is = entry >= 0 && entry < s.pool_pages && (t >> s.log2P) < s.pages_per_seq;
     const uint64_t there = __ballot(is);
-    m.there[it & 3][wave & (sizeof(m.there[0]) / 8 - 1)] = there;
+    if (lane == 0) m.there[it & 3][wave & 1] = there;  // (one lane: 64 writes to one place take 64 turns)
     const int64_t slot = t & ((1 << s.log2P) - 1), page = is ? entry : 0;
     if constexpr (kCodes) {
       const int64_t at = page * s.page_stride + g.head * s.head_stride;
@@ -888,31 +888,49 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       load_bytes<kVPiece>(raw_v[n], values + (kCodes ? m.v_off[b][tok] : m.k_off[b][tok]) + v_piece * kVPiece);
     }
   };
-  // Into LDS.  The 16 tokens of a key operand and the 16 rows of a value operand are permuted so that the threads of a
-  // write, which hold one token's channels or neighbouring channels, reach all banks.
+  // Into LDS.  The 16 tokens of a 16-bit key operand and the 16 rows of a value operand are permuted so that the threads
+  // of a write, which hold one token's channels or neighbouring channels, reach all banks.
   auto k_place = [](int u, int i, int cc, int token) {
-    return (u * kPairs + i) * kOperand + (cc * 16 + (token ^ ((4 * i + cc) & 15))) * 4;
+    return (u * kPairs + i) * kOperand + cc * 16 + (token ^ (kCodes ? 0 : (4 * i + cc) & 15));
   };
   auto v_place = [](int p, int j, int cc, int row) {
-    return (p * kChannels + j) * kOperand + (cc * 16 + (row ^ (j / 4 * (64 / kChannels) & 15))) * 4;
+    return (p * kChannels + j) * kOperand + cc * 16 + (row ^ (j / 4 * (32 / kChannels)));
   };
+  auto seen = [&](int32_t t, bool is) { return is && t <= span.hi_most && (t > span.lo_least || t < a.sinks); };
   auto put_tile = [&](int32_t it) {
     const int b = it & 1;
+    // Values (scales) of tokens that no row of the workgroup sees are zero, whatever lies there.
+    const int32_t t0 = tile_at<kManyTokens>(span, it);
+    const uint64_t there[2] = {m.there[it & 3][0], m.there[it & 3][1]};
     if constexpr (kCodes) {
 #pragma unroll
       for (int cc = 0; cc < 4; ++cc)
-        *reinterpret_cast<u32x4*>(&m.k[b][k_place(k_token / 16, k_step, cc, k_token % 16)]) = k_operand<KB>(raw_k, cc);
+        m.k[b][k_place(k_token / 16, k_step, cc, k_token % 16)] = k_operand<KB>(raw_k, cc);
+      if (!seen(t0 + own, (there[own >> 6] >> (own & 63)) & 1)) raw_scale[1] = 0;
       const float ks = f16_float(raw_scale[0]), vs = f16_float(raw_scale[1]);
-      m.scale[b][0][own] = ks;
-      m.scale[b][1][own] = __builtin_fmaf(ks, float(1 << (KB - 1)), f16_float(raw_scale[0] >> 16));
-      m.scale[b][2][own] = vs;
-      m.scale[b][3][own] = __builtin_fmaf(vs, float(1 << (VB - 1)), f16_float(raw_scale[1] >> 16));
+      m.scale[b][0][own / 4][own % 4] = ks;
+      m.scale[b][1][own / 4][own % 4] = __builtin_fmaf(ks, float(1 << (KB - 1)), f16_float(raw_scale[0] >> 16));
+      m.scale[b][2][own / 4][own % 4] = vs;
+      m.scale[b][3][own / 4][own % 4] = __builtin_fmaf(vs, float(1 << (VB - 1)), f16_float(raw_scale[1] >> 16));
     } else {
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         const int id = tid + kThreads * n, tok = id / (D / 8), piece = id % (D / 8);
-        *reinterpret_cast<u32x4*>(&m.k[b][k_place(tok / 16, piece / 4, piece % 4, tok % 16)]) =
-            u32x4{raw_k[4 * n], raw_k[4 * n + 1], raw_k[4 * n + 2], raw_k[4 * n + 3]};
+        m.k[b][k_place(tok / 16, piece / 4, piece % 4, tok % 16)] = u32x4{raw_k[4 * n], raw_k[4 * n + 1], raw_k[4 * n + 2], raw_k[4 * n + 3]};
+      }
+    }
+    if constexpr (!kCodes) {
+      constexpr uint64_t kAll = kManyTokens < 64 ? (uint64_t(1) << (kManyTokens & 63)) - 1 : ~uint64_t(0);
+      const bool whole = t0 + kManyTokens - 1 <= span.hi_most && (t0 > span.lo_least || t0 + kManyTokens <= a.sinks) &&
+                         (there[0] & there[1] & kAll) == kAll;
+      if (!__builtin_amdgcn_readfirstlane(whole)) {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          const int tok = v_tokens / 4 * 32 + (n >> 2) * 16 + v_tokens % 4 * 4 + (n & 3);
+          const bool keep = seen(t0 + tok, (there[tok >> 6] >> (tok & 63)) & 1);
+#pragma unroll
+          for (uint32_t& w : raw_v[n]) w = keep ? w : 0;
+        }
       }
     }
 #pragma unroll
@@ -921,7 +939,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       u32x4 w;
 #pragma unroll
       for (int n = 0; n < 4; ++n) w[n] = v_pair<VB>(raw_v[2 * n], raw_v[2 * n + 1], e);
-      *reinterpret_cast<u32x4*>(&m.v[b][v_place(v_tokens / 4, channel % kChannels, v_tokens % 4, channel / kChannels)]) = w;
+      m.v[b][v_place(v_tokens / 4, channel % kChannels, v_tokens % 4, channel / kChannels)] = w;
     }
   };
 
@@ -934,8 +952,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
     if (from + 1 < upto) put_places(from + 1, entry_of(from + 1));
     put_tile(from);
     __syncthreads();
+    uint64_t there[2] = {m.there[from & 3][0], m.there[from & 3][1]};
     for (int32_t it = from; it < upto; ++it) {
       const int b = it & 1;
+      const uint64_t there_next[2] = {m.there[(it + 1) & 3][0], m.there[(it + 1) & 3][1]};  // (of nothing behind the last)
       const bool more = it + 1 < upto, later = it + 2 < upto;
       if (more) bring(it + 1);
       int32_t entry = later ? entry_of(it + 2) : -1;
@@ -944,30 +964,37 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       for (int p = 0; p < kManyTokens / 32; ++p) {
         const int32_t t = t0 + 32 * p;
         if (t > mine.hi_most || (t + 31 <= mine.lo_least && t >= a.sinks)) continue;  // no row of this wave sees it
-        const uint32_t word = uint32_t(m.there[it & 3][p >> 1] >> (32 * (p & 1)));
+        const uint32_t word = uint32_t(there[p >> 1] >> (32 * (p & 1)));
         const uint32_t there = ((word >> (4 * c)) & 0xF) | (((word >> (16 + 4 * c)) & 0xF) << 4);
         Scales sc;
-        u32x4 keep = {~0u, ~0u, ~0u, ~0u};
         if constexpr (kCodes) {
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const int at = 32 * p + 16 * u + 4 * c;
+            const int at = 8 * p + 4 * u + c;
+            const f32x4 ks = m.scale[b][0][at], kz = m.scale[b][1][at], vs = m.scale[b][2][at], vz = m.scale[b][3][at];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              sc.ks[u][i] = m.scale[b][0][at + i];
-              sc.kz[u][i] = m.scale[b][1][at + i];
-              sc.vs[u][i] = m.scale[b][2][at + i];
-              sc.vz[u][i] = m.scale[b][3][at + i];
+              sc.ks[u][i] = ks[i];
+              sc.kz[u][i] = kz[i];
+              sc.vs[u][i] = vs[i];
+              sc.vz[u][i] = vz[i];
             }
           }
         }
+        // All of a phase's operands are asked for before its first instruction.
+        u32x4 k[2][kQkSteps], v[kChannels];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < kQkSteps; ++i)
+            k[u][i] = m.k[b][k_place(2 * p + u, i, c, x)];
         attend_tile<BF16, KB, VB, RT>(
-            a, mine, rows, c, t, there, sc, st,
-            [&](int u, int i) {
-              return *reinterpret_cast<const u32x4*>(&m.k[b][k_place(2 * p + u, i, c, x)]);
+            a, mine, rows, c, t, there, sc, st, [&](int u, int i) { return k[u][i]; }, [&](int j) { return v[j]; },
+            [&] {
+#pragma unroll
+              for (int j = 0; j < kChannels; ++j) v[j] = m.v[b][v_place(p, j, c, x)];
             },
-            [&](int j) { return *reinterpret_cast<const u32x4*>(&m.v[b][v_place(p, j, c, x)]) & keep; },
-            [] {}, [&](const u32x4& seen) { keep = seen; });
+            [](const u32x4&) {});
       }
       // What was loaded is first looked at here, behind the whole tile's work.
 #pragma unroll
@@ -980,6 +1007,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       asm volatile("" : "+v"(entry));
       if (more) put_tile(it + 1);
       if (later) put_places(it + 2, entry);
+      there[0] = there_next[0];
+      there[1] = there_next[1];
       __syncthreads();
     }
   }

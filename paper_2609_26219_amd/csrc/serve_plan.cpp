@@ -156,8 +156,8 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   if (a.window > 0 && !s.positions) seen = std::min<int64_t>(seen, int64_t(a.sinks) + a.window + s.max_tokens);
   const int64_t tokens = many ? kManyElems / s.D : kTokenTile;
   const int64_t tiles = std::max<int64_t>(1, (seen + tokens - 1) / tokens + 1);
-  const int64_t want = many ? 2 * 256 : 4 * 256;
-  int64_t splits = base > 0 ? std::min(want / base, tiles / 4) : 1;
+  const int64_t want = many ? 6 * 256 : 4 * 256;
+  int64_t splits = base > 0 ? std::min(want / base, tiles / (many ? 16 : 4)) : 1;
   splits = std::max<int64_t>(1, splits);
   l.splits = int32_t(splits);
   l.chunk = int32_t((tiles + splits - 1) / splits);
