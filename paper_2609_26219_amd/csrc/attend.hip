@@ -103,28 +103,41 @@ __device__ __forceinline__ void load_bytes(uint32_t* to, const void* from) {
   }
 }
 
+// A nibble or byte becomes a binary16 value by being put into the mantissa of 1024 (units of 1; a nibble four
+// bits up into that of 64), and the offset is taken off again with the centre: both exact.  The constants sit
+// in registers, where one instruction masks and merges (with literals it takes two).
+struct Magic {
+  uint32_t low, high, k1024, k64;  // nibble masks, 1024 and 64 in both halves
+};
+__device__ __forceinline__ Magic magic() {
+  Magic m{0x000F000Fu, 0x00F000F0u, 0x64006400u, 0x54005400u};
+  asm volatile("" : "+v"(m.low), "+v"(m.high), "+v"(m.k1024), "+v"(m.k64));
+  return m;
+}
+__device__ __forceinline__ uint32_t low_nibbles(const Magic& m, uint32_t w) {
+  return add_f16((w & m.low) | m.k1024, -1032.0f);
+}
+__device__ __forceinline__ uint32_t high_nibbles(const Magic& m, uint32_t w) {
+  return add_f16((w & m.high) | m.k64, -72.0f);
+}
+// Bytes `at` and `at` + 2 of w.
+__device__ __forceinline__ uint32_t two_bytes(const Magic& m, uint32_t w, int at) {
+  return add_f16(__builtin_amdgcn_perm(w, m.k1024, at ? 0x03070105u : 0x03060104u), -1152.0f);
+}
+
 // The K operand of instruction `step` from a lane's words: 8 channels, codes
 // centred.  Order of the 8 channels within the operand: 4 bits (0,4)(1,5)(2,6)(3,7), 8 bits
-// (0,2)(1,3)(4,6)(5,7), 16 bits as they lie.  A nibble or byte becomes a binary16
-// value by or-ing it into the mantissa of 1024 (units of 1; a nibble four bits
-// up into that of 64), and the offset is taken off again with the centre: both exact.
+// (0,2)(1,3)(4,6)(5,7), 16 bits as they lie.
 template <int BITS>
-__device__ __forceinline__ u32x4 k_operand(const uint32_t* w, int step) {
+__device__ __forceinline__ u32x4 k_operand(const Magic& m, const uint32_t* w, int step) {
   if constexpr (BITS == 16) {
     return u32x4{w[4 * step], w[4 * step + 1], w[4 * step + 2], w[4 * step + 3]};
   } else if constexpr (BITS == 8) {
-    u32x4 r;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t b = w[2 * step + i];
-      r[2 * i] = add_f16((b & 0x00FF00FFu) | 0x64006400u, -1152.0f);
-      r[2 * i + 1] = add_f16(((b >> 8) & 0x00FF00FFu) | 0x64006400u, -1152.0f);
-    }
-    return r;
+    return u32x4{two_bytes(m, w[2 * step], 0), two_bytes(m, w[2 * step], 1), two_bytes(m, w[2 * step + 1], 0),
+                 two_bytes(m, w[2 * step + 1], 1)};
   } else {
     const uint32_t b = w[step], h = b >> 8;
-    return u32x4{add_f16((b & 0x000F000Fu) | 0x64006400u, -1032.0f), add_f16((b & 0x00F000F0u) | 0x54005400u, -72.0f),
-                 add_f16((h & 0x000F000Fu) | 0x64006400u, -1032.0f), add_f16((h & 0x00F000F0u) | 0x54005400u, -72.0f)};
+    return u32x4{low_nibbles(m, b), high_nibbles(m, b), low_nibbles(m, h), high_nibbles(m, h)};
   }
 }
 
@@ -148,17 +161,15 @@ __device__ __forceinline__ constexpr int k_channel(int p, int half) {
 // One channel of two tokens as a packed pair, from the tokens' words a and b of the
 // lane's V pieces; j counts the lane's channels.
 template <int BITS>
-__device__ __forceinline__ uint32_t v_pair(const uint32_t* a, const uint32_t* b, int j) {
+__device__ __forceinline__ uint32_t v_pair(const Magic& m, const uint32_t* a, const uint32_t* b, int j) {
   if constexpr (BITS == 16) {
     return __builtin_amdgcn_perm(b[j / 2], a[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
   } else if constexpr (BITS == 8) {
-    const uint32_t w = __builtin_amdgcn_perm(b[j / 4], a[j / 4], j & 2 ? 0x07060302u : 0x05040100u);
-    return add_f16(((j & 1 ? w >> 8 : w) & 0x00FF00FFu) | 0x64006400u, -1152.0f);
+    return two_bytes(m, __builtin_amdgcn_perm(b[j / 4], a[j / 4], j & 2 ? 0x07060302u : 0x05040100u), j & 1);
   } else {
     uint32_t w = __builtin_amdgcn_perm(b[j / 8], a[j / 8], j & 4 ? 0x07060302u : 0x05040100u);
     if (j & 2) w >>= 8;
-    return j & 1 ? add_f16((w & 0x00F000F0u) | 0x54005400u, -72.0f)
-                 : add_f16((w & 0x000F000Fu) | 0x64006400u, -1032.0f);
+    return j & 1 ? high_nibbles(m, w) : low_nibbles(m, w);
   }
 }
 
@@ -658,6 +669,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, At
   tiles_of<kTokenTile>(a, g.split, span, from, upto);
 
   const int32_t* table = s.page_table + int64_t(g.seq) * s.pages_per_seq;
+  const Magic code = magic();
   Running<RT> st;
   begin(st);
   auto pages_at = [&](int32_t it, int32_t (&pages)[2]) {  // of a tile that exists, else -1
@@ -696,13 +708,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, At
           }
       }
       attend_tile<BF16, KB, VB, RT>(
-          a, span, rows, c, t0, there, sc, st, [&](int u, int i) { return k_operand<KB>(keys.w[u], i); },
+          a, span, rows, c, t0, there, sc, st, [&](int u, int i) { return k_operand<KB>(code, keys.w[u], i); },
           [&](int j) {
             u32x4 v;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int i = 0; i < 2; ++i) v[2 * u + i] = v_pair<VB>(values.w[u][2 * i], values.w[u][2 * i + 1], j);
+              for (int i = 0; i < 2; ++i) v[2 * u + i] = v_pair<VB>(code, values.w[u][2 * i], values.w[u][2 * i + 1], j);
             return v;
           },
           [&] {
@@ -862,6 +874,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       m.k_off[b][own] = 2 * (page * s.page_stride + slot * s.H * D + g.head * D);
     }
   };
+  const Magic code = magic();
   // A thread's share of a tile: 32 values (8 tokens x 4 channels), 32 keys (32 channels of a token in codes, four times 8 in
   // 16 bits) and, in codes, the scales of a token.
   constexpr int kPairs = D / 32, kVPiece = VB / 2, kVWords = (kVPiece + 3) / 4;
@@ -905,7 +918,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
     if constexpr (kCodes) {
 #pragma unroll
       for (int cc = 0; cc < 4; ++cc)
-        m.k[b][k_place(k_token / 16, k_step, cc, k_token % 16)] = k_operand<KB>(raw_k, cc);
+        m.k[b][k_place(k_token / 16, k_step, cc, k_token % 16)] = k_operand<KB>(code, raw_k, cc);
       if (!seen(t0 + own, (there[own >> 6] >> (own & 63)) & 1)) raw_scale[1] = 0;
       const float ks = f16_float(raw_scale[0]), vs = f16_float(raw_scale[1]);
       m.scale[b][0][own / 4][own % 4] = ks;
@@ -938,7 +951,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       const int channel = 4 * v_piece + e;
       u32x4 w;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) w[n] = v_pair<VB>(raw_v[2 * n], raw_v[2 * n + 1], e);
+      for (int n = 0; n < 4; ++n) w[n] = v_pair<VB>(code, raw_v[2 * n], raw_v[2 * n + 1], e);
       m.v[b][v_place(v_tokens / 4, channel % kChannels, v_tokens % 4, channel / kChannels)] = w;
     }
   };
