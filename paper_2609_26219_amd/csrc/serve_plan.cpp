@@ -160,7 +160,7 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   int64_t splits = base > 0 ? std::min(want / base, tiles / (many ? 16 : 4)) : 1;
   splits = std::max<int64_t>(1, splits);
   l.splits = int32_t(splits);
-  l.chunk = int32_t((tiles + splits - 1) / splits);
+  l.chunk = many ? 16 : int32_t((tiles + splits - 1) / splits);
   l.groups = base * splits;
   if (splits > 1) {
     const uint64_t parts = uint64_t(s.num_tokens) * a.Hq * splits;
