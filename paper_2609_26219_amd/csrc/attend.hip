@@ -195,18 +195,16 @@ __device__ __forceinline__ int over_x_min(int v) {
 }
 
 // What a tile's lane holds of the cache: for each half of 16 tokens its piece of one
-// token's keys, of four tokens' values, and those four tokens' (scale, zero).
+// token's keys and of four tokens' values.
 template <int BITS>
 struct Keys {
   static constexpr int kBytes = D / 4 * BITS / 8;
   uint32_t w[2][kBytes / 4];
-  uint32_t scale[2][4];
 };
 template <int BITS>
 struct Values {
   static constexpr int kBytes = kChannels * BITS / 8, kWords = (kBytes + 3) / 4;
   uint32_t w[2][4][kWords];
-  uint32_t scale[2][4];
 };
 
 // Physical page of a logical one, or -1.
@@ -222,90 +220,106 @@ __device__ __forceinline__ void load_at(uint32_t* to, const void* base, uint32_t
   load_bytes<BYTES>(to, static_cast<const char*>(base) + off);
 }
 
-// Load the keys or values of the tile of tokens [t0, t0 + 32); tokens that are not
-// there are loaded from page 0, which exists.  WHOLE: pages hold 16 slots or more, so
-// each half of the tile lies on one page (`pages`, or -1).
+// Where a segment's cache begins, and where a tile's tokens lie in it.  WHOLE: pages hold 16 slots or more, so each
+// half of a tile lies on one page, whose number the wave shares (-1: not there); else every lane looks its tokens up.
+// Tokens that are not there are read from page 0, which exists.
+struct Source {
+  const char* k;           // page 0, slot 0 of the head
+  const char* v;
+  const uint32_t* scales;  // keys'
+  const int32_t* table;
+};
+template <int KB>
+__device__ __forceinline__ Source source_of(const ServeArgs& s, int32_t seq, int32_t head) {
+  Source f;
+  if constexpr (KB == 16) {
+    f.k = reinterpret_cast<const char*>(s.k_cache + head * D);
+    f.v = reinterpret_cast<const char*>(s.v_cache + head * D);
+    f.scales = nullptr;
+  } else {
+    f.k = reinterpret_cast<const char*>(s.codes + head * s.head_stride);
+    f.v = f.k + s.v_offset;
+    f.scales = s.scales + ((int64_t(head) * 2) << s.log2P);
+  }
+  f.table = s.page_table + int64_t(seq) * s.pages_per_seq;
+  return f;
+}
+struct Tile {
+  int32_t t0;
+  int32_t page[2];  // WHOLE: of each half, or -1
+};
+// Byte offset of a slot's row, of `row` bytes, on a page (a page is at most 2 GiB, its number 32 bits).
+template <int BITS>
+__device__ __forceinline__ uint64_t row_at(const ServeArgs& s, int32_t page, uint32_t slot, uint32_t row) {
+  const uint32_t stride = uint32_t(s.page_stride) * (BITS == 16 ? 2 : 1);
+  return uint64_t(uint32_t(page < 0 ? 0 : page)) * stride + uint64_t(slot) * row;
+}
+
 template <int BITS, bool WHOLE>
-__device__ __forceinline__ void load_keys(const ServeArgs& s, const int32_t* table, int head, int32_t t0,
-                                          const int32_t (&pages)[2], int c, int x, Keys<BITS>& p) {
-  const int32_t slots = (1 << s.log2P) - 1;
+__device__ __forceinline__ void load_keys(const ServeArgs& s, const Source& f, const Tile& tile, int c, int x,
+                                          Keys<BITS>& p) {
   constexpr int kPiece = Keys<BITS>::kBytes < 16 ? Keys<BITS>::kBytes : 16;
+  const int32_t slots = (1 << s.log2P) - 1;
   const uint32_t row = BITS == 16 ? uint32_t(s.H) * D * 2 : D * BITS / 8, mine = c * kPiece;
-  auto first_of = [&](int64_t page) -> const char* {
-    if constexpr (BITS == 16) return reinterpret_cast<const char*>(s.k_cache + page * s.page_stride + head * D);
-    return reinterpret_cast<const char*>(s.codes + page * s.page_stride + head * s.head_stride);
-  };
-  auto scales_of = [&](int64_t page) { return s.scales + page * s.scale_stride + ((int64_t(head) * 2) << s.log2P); };
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const int32_t t = t0 + 16 * u;
+    const int32_t t = tile.t0 + 16 * u;
     if constexpr (WHOLE) {
-      const int32_t page = pages[u] >= 0 ? pages[u] : 0;
-      const int64_t slot = t & slots;
+      const char* from = f.k + row_at<BITS>(s, tile.page[u], t & slots, row);
 #pragma unroll
       for (int n = 0; n < Keys<BITS>::kBytes / kPiece; ++n)
-        load_at<kPiece>(p.w[u] + n * (kPiece / 4), first_of(page) + slot * row + n * (4 * kPiece), x * row + mine);
-      if constexpr (BITS != 16) load_at<16>(p.scale[u], scales_of(page) + slot, 16 * c);
+        load_at<kPiece>(p.w[u] + n * (kPiece / 4), from + n * (4 * kPiece), x * row + mine);
     } else {
-      const int32_t page = page_of(s, table, (t + x) >> s.log2P);
-      const char* from = first_of(page >= 0 ? page : 0) + int64_t((t + x) & slots) * row + mine;
+      const char* from = f.k + row_at<BITS>(s, page_of(s, f.table, (t + x) >> s.log2P), (t + x) & slots, row) + mine;
 #pragma unroll
       for (int n = 0; n < Keys<BITS>::kBytes / kPiece; ++n)
         load_bytes<kPiece>(p.w[u] + n * (kPiece / 4), from + n * (4 * kPiece));
-      if constexpr (BITS != 16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int32_t tok = t + 4 * c + i, at = page_of(s, table, tok >> s.log2P);
-          p.scale[u][i] = scales_of(at >= 0 ? at : 0)[tok & slots];
-        }
-      }
     }
   }
 }
 
 template <int BITS, bool WHOLE>
-__device__ __forceinline__ void load_values(const ServeArgs& s, const int32_t* table, int head, int32_t t0,
-                                            const int32_t (&pages)[2], int c, int x, Values<BITS>& p) {
+__device__ __forceinline__ void load_values(const ServeArgs& s, const Source& f, const Tile& tile, int c, int x,
+                                            Values<BITS>& p) {
   const int32_t slots = (1 << s.log2P) - 1;
   const uint32_t row = BITS == 16 ? uint32_t(s.H) * D * 2 : D * BITS / 8, mine = x * Values<BITS>::kBytes;
-  auto first_of = [&](int64_t page) -> const char* {
-    if constexpr (BITS == 16) return reinterpret_cast<const char*>(s.v_cache + page * s.page_stride + head * D);
-    return reinterpret_cast<const char*>(s.codes + page * s.page_stride + head * s.head_stride + s.v_offset);
-  };
-  auto scales_of = [&](int64_t page) { return s.scales + page * s.scale_stride + ((int64_t(head) * 2 + 1) << s.log2P); };
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const int32_t t = t0 + 16 * u;
+    const int32_t t = tile.t0 + 16 * u;
     if constexpr (WHOLE) {
-      const int32_t page = pages[u] >= 0 ? pages[u] : 0;
-      const int64_t slot = t & slots;
+      const char* from = f.v + row_at<BITS>(s, tile.page[u], t & slots, row);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        load_at<Values<BITS>::kBytes>(p.w[u][i], first_of(page) + (slot + i) * row, 4 * c * row + mine);
-      if constexpr (BITS != 16) load_at<16>(p.scale[u], scales_of(page) + slot, 16 * c);
+      for (int i = 0; i < 4; ++i) load_at<Values<BITS>::kBytes>(p.w[u][i], from + i * row, 4 * c * row + mine);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int32_t tok = t + 4 * c + i, at = page_of(s, table, tok >> s.log2P);
-        const int64_t slot = tok & slots, page = at >= 0 ? at : 0;
-        load_bytes<Values<BITS>::kBytes>(p.w[u][i], first_of(page) + slot * row + mine);
-        if constexpr (BITS != 16) p.scale[u][i] = scales_of(page)[slot];
+        const int32_t tok = t + 4 * c + i;
+        load_bytes<Values<BITS>::kBytes>(
+            p.w[u][i], f.v + row_at<BITS>(s, page_of(s, f.table, tok >> s.log2P), tok & slots, row) + mine);
       }
     }
   }
+}
+
+// The tile's 64 (scale, zero) words, one to a lane: keys' of its 32 tokens, then values'.
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t load_scale(const ServeArgs& s, const Source& f, const Tile& tile, int lane) {
+  const int32_t slots = (1 << s.log2P) - 1, t = tile.t0 + (lane & 31);
+  const int32_t page = WHOLE ? (lane & 16 ? tile.page[1] : tile.page[0]) : page_of(s, f.table, t >> s.log2P);
+  return f.scales[uint64_t(uint32_t(page < 0 ? 0 : page)) * uint32_t(s.scale_stride) +
+                  ((uint32_t(lane >> 5) << s.log2P) + uint32_t(t & slots))];
 }
 
 // Which of the lane's tokens are there: bit 4u + i for token t0 + 16u + 4c + i.
 template <bool WHOLE>
-__device__ __forceinline__ uint32_t tokens_there(const ServeArgs& s, const int32_t* table, int32_t t0,
-                                                 const int32_t (&pages)[2], int c) {
-  if constexpr (WHOLE) return (pages[0] >= 0 ? 0x0Fu : 0u) | (pages[1] >= 0 ? 0xF0u : 0u);
+__device__ __forceinline__ uint32_t tokens_there(const ServeArgs& s, const Source& f, const Tile& tile, int c) {
+  if constexpr (WHOLE) return (tile.page[0] >= 0 ? 0x0Fu : 0u) | (tile.page[1] >= 0 ? 0xF0u : 0u);
   uint32_t there = 0;
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      there |= (page_of(s, table, (t0 + 16 * u + 4 * c + i) >> s.log2P) >= 0 ? 1u : 0u) << (4 * u + i);
+      there |= (page_of(s, f.table, (tile.t0 + 16 * u + 4 * c + i) >> s.log2P) >= 0 ? 1u : 0u) << (4 * u + i);
   return there;
 }
 
@@ -323,23 +337,39 @@ struct Span {  // of a row tile, over its rows
 template <int RT>
 struct Running {
   f32x4 o[RT][kChannels];
-  float ref[RT];   // exponents are taken relative to it (base 2): within kSlack of the largest so far; -inf at first
+  float ref[RT];  // exponents (base 2) are taken relative to it; -inf at first
   float l[RT], o_zero[RT];
-  float fac;       // codes: O counts in units of 1 / fac
-  float most_scale;
 };
 
-// P is stored as 2^kShift p where the operands are binary16, which keeps small
-// probabilities clear of its subnormals; the reference of the exponents is moved only
-// when a score passes it by kSlack, so that O is rescaled once or twice a row and not
-// at every new maximum (with 64 rows in a wave nearly every tile has one).  2^(kShift + kSlack) is
-// in binary16's range.
+// The operand P (times the token's value scale, where the cache holds codes) has to fit
+// binary16 with room below, so the reference is chosen that the largest p (times scale) so far is
+// 2^kTop, and moved only when one passes that by kSlack (binary16 ends at 2^16): O is then rescaled once or
+// twice a row and not at every new maximum, of which 32 rows have one in nearly every tile.  A
+// scale counts as at least 2^-24, binary16's least.  bfloat16 needs no room: kTop = 0.
 constexpr float kSlack = 8.0f;
-constexpr float kShiftOfHalf = 6.0f;
+template <bool HALF>
+constexpr float kTop = HALF ? 6.0f : 0.0f;
 
-// What stands for a token beside its codes: key scale and zero, value scale and zero, both zeros at mid-code.
-struct Scales {
-  float ks[2][4], kz[2][4], vs[2][4], vz[2][4];
+// What stands for a token beside its codes, for the lane's 4 tokens of each half of a tile: key scale and zero, value
+// scale and zero at mid-code.  As the cache has it, or as numbers.
+template <int VB>
+struct WordScales {
+  u32x4 k[2], v[2];
+  __device__ float ks(int u, int i) const { return f16_float(k[u][i]); }
+  __device__ float kz(int u, int i) const { return f16_float(k[u][i] >> 16); }
+  __device__ float vs(int u, int i) const { return f16_float(v[u][i]); }
+  __device__ float vz(int u, int i) const {
+    return __builtin_fmaf(f16_float(v[u][i]), float(1 << (VB - 1)), f16_float(v[u][i] >> 16));
+  }
+  __device__ void hide(int u, int i) { v[u][i] = 0; }
+};
+struct FloatScales {
+  f32x4 ks_[2], kz_[2], vs_[2], vz_[2];
+  __device__ float ks(int u, int i) const { return ks_[u][i]; }
+  __device__ float kz(int u, int i) const { return kz_[u][i]; }
+  __device__ float vs(int u, int i) const { return vs_[u][i]; }
+  __device__ float vz(int u, int i) const { return vz_[u][i]; }
+  __device__ void hide(int u, int i) { vs_[u][i] = vz_[u][i] = 0.0f; }
 };
 
 // The first row x of each of a wave's RT row tiles: what it sees and its queries.
@@ -353,7 +383,7 @@ struct Rows {
 // One tile of 32 tokens from t0 on, of which the lane's are `there` (bit 4u + i: t0 + 16u + 4c + i).
 // key(u, i) and value(j) give the operands, after_keys() runs when the last key has been used, hide(keep) leaves of
 // 16-bit values only the halves of operand words that `keep` has.
-template <bool BF16, int KB, int VB, int RT, typename Key, typename Value, typename After, typename Hide>
+template <bool BF16, int KB, int VB, int RT, typename Scales, typename Key, typename Value, typename After, typename Hide>
 __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& span, const Rows<RT>& rows, int c,
                                             int32_t t0, uint32_t there, Scales& sc, Running<RT>& st, Key key,
                                             Value value, After after_keys, Hide hide) {
@@ -367,12 +397,15 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     else
       return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), z, 0, 0, 0);
   };
-  // S^T, in units of 1 / f.
+  // S^T, in units of 1 / f.  (Codes: their centre times sum(q) to begin with, so that it is of the codes themselves.)
   f32x4 t[RT][2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r) t[r][u] = f32x4{};
+    for (int r = 0; r < RT; ++r) {
+      const float first = kCodes ? rows.q_sum[r] * float(1 << (KB - 1)) : 0.0f;
+      t[r][u] = f32x4{first, first, first, first};
+    }
 #pragma unroll
     for (int i = 0; i < kQkSteps; ++i) {
       const u32x4 k = key(u, i);
@@ -388,7 +421,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int r = 0; r < RT; ++r)
-          t[r][u][i] = __builtin_fmaf(sc.ks[u][i], t[r][u][i], sc.kz[u][i] * rows.q_sum[r]);
+          t[r][u][i] = __builtin_fmaf(sc.ks(u, i), t[r][u][i], sc.kz(u, i) * rows.q_sum[r]);
   }
   if (!all) {
     u32x4 keep{};
@@ -408,8 +441,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
         }
         any = (__ballot(any) >> (16 * c)) & 0xFFFF;
         if constexpr (kCodes) {
-          sc.vs[u][i] = any ? sc.vs[u][i] : 0.0f;
-          sc.vz[u][i] = any ? sc.vz[u][i] : 0.0f;
+          if (!any) sc.hide(u, i);
         } else {
           keep[2 * u + i / 2] |= any ? 0xFFFFu << (16 * (i & 1)) : 0;
         }
@@ -417,6 +449,15 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     if constexpr (!kCodes) hide(keep);
   }
   // The reference of the exponents.
+  float above = -kTop<kHalf>;
+  if constexpr (kCodes) {
+    float most = 0x1p-24f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = __builtin_fmaxf(most, sc.vs(u, i));
+    above += __builtin_amdgcn_logf(most);
+  }
   float top[RT];
   bool move = false;
 #pragma unroll
@@ -426,7 +467,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top[r] = __builtin_fmaxf(top[r], t[r][u][i]);
-    top[r] *= rows.f[r];
+    top[r] = __builtin_fmaf(top[r], rows.f[r], above);
     move |= top[r] > st.ref[r] + kSlack;
   }
   if (__any(move)) {
@@ -442,36 +483,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
       for (int j = 0; j < kChannels; ++j) st.o[r][j] *= shrink;
     }
   }
-  if constexpr (kCodes) {
-    float tile_most = sc.vs[0][0];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tile_most = __builtin_fmaxf(tile_most, sc.vs[u][i]);
-    if (__any(tile_most > st.most_scale)) {
-      st.most_scale = __builtin_fmaxf(st.most_scale, over_c_max(tile_most));
-      // 2^e > the largest scale so far: scales times fac stay below 2^kShift.
-      const int e = int(__float_as_uint(st.most_scale) >> 23) - 126;
-      const float next = __uint_as_float(uint32_t(127 + int(kShiftOfHalf) - e) << 23);
-      if (next != st.fac) {
-        const float ratio = next / st.fac;
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-          for (int j = 0; j < kChannels; ++j) st.o[r][j] *= ratio;
-        st.fac = next;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sc.vs[u][i] *= st.fac;
-  }
   // The probabilities and their sum.
   u32x4 pt[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const float base = (kCodes || !kHalf ? 0.0f : kShiftOfHalf) - (st.ref[r] == -kInf ? 0.0f : st.ref[r]);
+    const float base = st.ref[r] == -kInf ? 0.0f : -st.ref[r];
     float pr[2][4];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -480,8 +496,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
         pr[u][i] = exp2_of(__builtin_fmaf(t[r][u][i], rows.f[r], base));
         st.l[r] += pr[u][i];
         if constexpr (kCodes) {
-          st.o_zero[r] = __builtin_fmaf(pr[u][i], sc.vz[u][i], st.o_zero[r]);
-          pr[u][i] *= sc.vs[u][i];
+          st.o_zero[r] = __builtin_fmaf(pr[u][i], sc.vz(u, i), st.o_zero[r]);
+          pr[u][i] *= sc.vs(u, i);
         }
       }
 #pragma unroll
@@ -510,23 +526,34 @@ struct Group {
   int32_t start, count, kv_len, trail;  // rows [start, start + count); the last row of the sequence is `trail` rows on
 };
 
-__device__ __forceinline__ Group group_of(const ServeArgs& s, const AttendArgs& a) {
-  Group g;
-  uint32_t b = blockIdx.x;
-  g.head = int32_t(b % uint32_t(s.H));
-  b /= uint32_t(s.H);
-  g.split = int32_t(b % uint32_t(a.splits));
-  b /= uint32_t(a.splits);
-  g.tile = a.row_tiles - 1 - int32_t(b % uint32_t(a.row_tiles));  // the rows that see the most start first
-  g.seq = int32_t(b / uint32_t(a.row_tiles));
-  int32_t end = scalar_entry(s.token_start, g.seq + 1);
-  g.start = scalar_entry(s.token_start, g.seq);
-  g.kv_len = scalar_entry(s.kv_lens, g.seq);
-  g.start = g.start < 0 ? 0 : g.start;
+__device__ __forceinline__ Group group_from(const ServeArgs& s, int32_t start, int32_t end, int32_t kv_len) {
+  Group g{};
+  g.start = start < 0 ? 0 : start;
   end = end < s.num_tokens ? end : s.num_tokens;
   g.trail = end - g.start;
   g.count = g.trail < s.max_tokens ? g.trail : s.max_tokens;
-  g.kv_len = g.kv_len < 0 ? 0 : g.kv_len < s.max_kv ? g.kv_len : s.max_kv;
+  g.kv_len = kv_len < 0 ? 0 : kv_len < s.max_kv ? kv_len : s.max_kv;
+  return g;
+}
+
+__device__ __forceinline__ Group group_of_sequence(const ServeArgs& s, int32_t seq) {
+  Group g = group_from(s, scalar_entry(s.token_start, seq), scalar_entry(s.token_start, seq + 1),
+                       scalar_entry(s.kv_lens, seq));
+  g.seq = seq;
+  return g;
+}
+
+// Of a launch of splits x row tiles x heads for each sequence.
+__device__ __forceinline__ Group group_of(const ServeArgs& s, const AttendArgs& a) {
+  uint32_t b = blockIdx.x;
+  const int32_t head = int32_t(b % uint32_t(s.H));
+  b /= uint32_t(s.H);
+  const int32_t split = int32_t(b % uint32_t(a.splits));
+  b /= uint32_t(a.splits);
+  Group g = group_of_sequence(s, int32_t(b / uint32_t(a.row_tiles)));
+  g.head = head;
+  g.split = split;
+  g.tile = a.row_tiles - 1 - int32_t(b % uint32_t(a.row_tiles));  // the rows that see the most start first
   return g;
 }
 
@@ -635,90 +662,160 @@ __device__ __forceinline__ void begin(Running<RT>& st) {
 #pragma unroll
     for (int j = 0; j < kChannels; ++j) st.o[r][j] = f32x4{};
   }
-  st.fac = 1.0f;
-  st.most_scale = 0.0f;
 }
 
 __device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
-// Log-sum-exp from the reference (base 2) and the sum, which counts `up` of what it stands for.
-__device__ __forceinline__ float lse_of(float ref, float l, float up) {
-  return l == 0.0f ? -kInf : (ref + __builtin_amdgcn_logf(l * up)) * 0.69314718055994531f;
+// Log-sum-exp from the reference (base 2) and the sum relative to it.
+__device__ __forceinline__ float lse_of(float ref, float l) {
+  return l == 0.0f ? -kInf : (ref + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
-template <bool BF16, int KB>
-constexpr float kUp = KB != 16 || BF16 ? 1.0f : 1.0f / 64.0f;  // 2^-kShift where p carries it into the sum
 
-// Few rows (kRowTile * RT): the four waves of a workgroup share them and deal the tiles of tokens among
-// themselves.  Each lane's pieces of the cache go from memory to its registers and, decoded, straight
-// into the matrix instructions.
+// ---- Few rows ----
+//
+// A sequence's rows of one KV head (a segment) fit one row tile or two.  The segments' tiles of tokens, all put end to
+// end, are cut into equal ranges, one to a workgroup, so that sequences of any lengths keep the whole GPU busy to the
+// end: a workgroup takes the last part of one segment, some whole ones, the first part of another.  A
+// segment counts kSegmentCost tiles more than it has, for its start and its join.
+
+// What the rows of sequence `seq` look at when nothing but lengths is known: a span without the rows' own bounds.
+__device__ __forceinline__ Span few_span(const ServeArgs& s, const AttendArgs& a, const Group& g) {
+  Span span{-1, 0, -1, -1, 0, 0, 0};
+  if (s.positions) {
+    span.hi_most = g.kv_len - 1;
+  } else {
+    const int32_t pos0 = g.kv_len - g.trail;
+    span.hi_most = pos0 + g.count - 1;
+    const int32_t first = pos0 > 0 ? pos0 : 0;
+    span.lo_least = a.window > 0 && first >= a.window ? first - a.window : -1;
+  }
+  int32_t from, upto;
+  tiles_of<kTokenTile>(a, 0, span, from, upto);
+  return span;
+}
+
+__device__ __forceinline__ int64_t units_of(const ServeArgs& s, const AttendArgs& a, int32_t start, int32_t end,
+                                            int32_t kv_len) {
+  const Group g = group_from(s, start, end, kv_len);
+  return g.count > 0 ? int64_t(s.H) * (few_span(s, a, g).tiles + kSegmentCost) : 0;
+}
+
+// Inclusive sums over the lanes of a wave.
+__device__ __forceinline__ int64_t wave_sums(int64_t v, int lane) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int64_t other = __shfl_up(v, off);
+    v += lane >= off ? other : 0;
+  }
+  return v;
+}
+
+// The units of all sequences, by every wave for itself, 64 sequences at a time: calls each(first, inclusive sums of the
+// lanes with all before, own units) and returns the total.
+template <typename Each>
+__device__ __forceinline__ int64_t over_sequences(const ServeArgs& s, const AttendArgs& a, int lane, Each each) {
+  int64_t before = 0;
+  for (int32_t first = 0; first < s.num_seqs; first += 64) {
+    const int32_t seq = first + lane;
+    int64_t units = 0;
+    if (seq < s.num_seqs) units = units_of(s, a, s.token_start[seq], s.token_start[seq + 1], s.kv_lens[seq]);
+    const int64_t sums = before + wave_sums(units, lane);
+    each(first, sums, units);
+    before = __shfl(sums, 63);
+  }
+  return before;
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return int64_t(uint32_t(__builtin_amdgcn_readfirstlane(int32_t(v)))) |
+         int64_t(__builtin_amdgcn_readfirstlane(int32_t(v >> 32))) << 32;
+}
+
+// Units of a workgroup's range.
+__device__ __forceinline__ int64_t range_of(const AttendArgs& a, int64_t total) {
+  const int64_t even = (total + a.ranges - 1) / a.ranges;
+  return even > a.chunk ? even : a.chunk;
+}
+
+template <int RT>
+struct FewLds {
+  float join_ml[kWaves][kRowTile][2];
+  float join[kWaves][kRowTile][D + 4];
+  u32x4 words[kWaves][16];
+};
+
+// Tiles [from, upto) of a segment, into `out` and `lse` if they are all of them, else as a part.
 template <bool BF16, int KB, int VB, bool WHOLE, int RT>
-__global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, AttendArgs a) {
+__device__ __forceinline__ void few_segment(const ServeArgs& s, const AttendArgs& a, const Group& g, int32_t from,
+                                            int32_t upto, int64_t part_slot, const Magic& code, FewLds<RT>& m) {
   constexpr bool kCodes = KB != 16;
-  constexpr int kRows = kRowTile * RT;
-  __shared__ float join_ml[kWaves][kRowTile][2];
-  __shared__ float join[kWaves][kRowTile][D + 4];
-
-  const Group g = group_of(s, a);
   const int lane = threadIdx.x & 63, c = lane >> 4, x = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row0 = int64_t(g.tile) * kRows;
-  if (row0 >= int64_t(g.count) * a.group) return;  // the whole workgroup
   Rows<RT> rows;
   Span span;
-  load_rows<KB, RT>(s, a, g, uint32_t(row0), x, [&](int i) { return k_first<KB>(i, c); }, rows, span);
-  int32_t from, upto;
-  tiles_of<kTokenTile>(a, g.split, span, from, upto);
+  load_rows<KB, RT>(s, a, g, 0, x, [&](int i) { return k_first<KB>(i, c); }, rows, span);
+  {
+    const Span all = few_span(s, a, g);
+    span.first = all.first;
+    span.sink_tiles = all.sink_tiles;
+    span.tiles = all.tiles;
+  }
 
-  const int32_t* table = s.page_table + int64_t(g.seq) * s.pages_per_seq;
-  const Magic code = magic();
+  const Source f = source_of<KB>(s, g.seq, g.head);
   Running<RT> st;
   begin(st);
-  auto pages_at = [&](int32_t it, int32_t (&pages)[2]) {  // of a tile that exists, else -1
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int32_t at = (tile_at<kTokenTile>(span, it) + 16 * u) >> s.log2P;
-      pages[u] = WHOLE && it < upto && at < s.pages_per_seq ? scalar_entry(table, at) : -1;
-      pages[u] = pages[u] < s.pool_pages ? pages[u] : -1;
-    }
+  // The wave's tiles are `from` + wave + kWaves n.  Their pages are looked up 32 tiles at a time, a half of a tile to
+  // a lane, and read from there: a scalar load for each tile would have every wait for LDS wait for it too.
+  const int32_t first = from + wave, count = first < upto ? (upto - first + kWaves - 1) / kWaves : 0;
+  auto pages_from = [&](int32_t n) -> int32_t {
+    if constexpr (!WHOLE) return -1;
+    const int32_t it = first + (n + (lane >> 1)) * kWaves;
+    return it < upto ? page_of(s, f.table, (tile_at<kTokenTile>(span, it) + 16 * (lane & 1)) >> s.log2P) : -1;
   };
-  // A tile's keys are loaded while the softmax and the sums of the one before run, its values while its own
-  // scores are computed, its pages one tile earlier.
-  int32_t it = from + wave;
-  if (it < upto) {
+  auto tile_of = [&](int32_t n, int32_t pages) {
+    const int at = (n & 31) * 2;
+    return Tile{tile_at<kTokenTile>(span, first + n * kWaves),
+                {__builtin_amdgcn_readlane(pages, at), __builtin_amdgcn_readlane(pages, at + 1)}};
+  };
+  if (count > 0) {
+    // A tile's registers are filled again, keys and then values, as soon as its own have been used.
     Keys<KB> keys;
     Values<VB> values;
-    int32_t pages[2], next[2];
-    pages_at(it, pages);
-    load_keys<KB, WHOLE>(s, table, g.head, tile_at<kTokenTile>(span, it), pages, c, x, keys);
-    load_values<VB, WHOLE>(s, table, g.head, tile_at<kTokenTile>(span, it), pages, c, x, values);
-    pages_at(it + kWaves, next);
-    for (; it < upto; it += kWaves) {
-      const int32_t t0 = tile_at<kTokenTile>(span, it), t1 = tile_at<kTokenTile>(span, it + kWaves);
-      const bool more = it + kWaves < upto;
-      const uint32_t there = tokens_there<WHOLE>(s, table, t0, pages, c);
-      Scales sc;
+    uint32_t scale = 0;
+    int32_t pages = pages_from(0);
+    Tile tile = tile_of(0, pages);
+    load_keys<KB, WHOLE>(s, f, tile, c, x, keys);
+    load_values<VB, WHOLE>(s, f, tile, c, x, values);
+    if constexpr (kCodes) scale = load_scale<WHOLE>(s, f, tile, lane);
+    for (int32_t n = 0; n < count; ++n) {
+      const bool more = n + 1 < count;
+      if (((n + 1) & 31) == 0) pages = pages_from(n + 1);
+      const Tile next = tile_of(n + 1, pages);
+      const uint32_t there = tokens_there<WHOLE>(s, f, tile, c);
+      // Through LDS, where each lane finds the words of its 4 tokens of each half (the wave's own: no barrier).
+      WordScales<VB> sc;
       if constexpr (kCodes) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            sc.ks[u][i] = f16_float(keys.scale[u][i]);
-            sc.kz[u][i] = __builtin_fmaf(sc.ks[u][i], float(1 << (KB - 1)), f16_float(keys.scale[u][i] >> 16));
-            sc.vs[u][i] = f16_float(values.scale[u][i]);
-            sc.vz[u][i] = __builtin_fmaf(sc.vs[u][i], float(1 << (VB - 1)), f16_float(values.scale[u][i] >> 16));
-          }
+        reinterpret_cast<uint32_t*>(m.words[wave])[lane] = scale;
+        sc.k[0] = m.words[wave][c];
+        sc.k[1] = m.words[wave][4 + c];
       }
       attend_tile<BF16, KB, VB, RT>(
-          a, span, rows, c, t0, there, sc, st, [&](int u, int i) { return k_operand<KB>(code, keys.w[u], i); },
+          a, span, rows, c, tile.t0, there, sc, st, [&](int u, int i) { return k_operand<KB>(code, keys.w[u], i); },
           [&](int j) {
             u32x4 v;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int i = 0; i < 2; ++i) v[2 * u + i] = v_pair<VB>(code, values.w[u][2 * i], values.w[u][2 * i + 1], j);
+              for (int i = 0; i < 2; ++i)
+                v[2 * u + i] = v_pair<VB>(code, values.w[u][2 * i], values.w[u][2 * i + 1], j);
             return v;
           },
           [&] {
-            if (more) load_keys<KB, WHOLE>(s, table, g.head, t1, next, c, x, keys);
+            if (more) load_keys<KB, WHOLE>(s, f, next, c, x, keys);
+            if constexpr (kCodes) {
+              sc.v[0] = m.words[wave][8 + c];
+              sc.v[1] = m.words[wave][12 + c];
+              if (more) scale = load_scale<WHOLE>(s, f, next, lane);
+            }
           },
           [&](const u32x4& keep) {
 #pragma unroll
@@ -729,58 +826,53 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, At
                 for (int w = 0; w < Values<VB>::kWords; ++w)
                   values.w[u][i][w] = (keep[2 * u + i / 2] >> (16 * (i & 1))) & 1 ? values.w[u][i][w] : 0;
           });
-      if (more) load_values<VB, WHOLE>(s, table, g.head, t1, next, c, x, values);
-      pages[0] = next[0];
-      pages[1] = next[1];
-      pages_at(it + 2 * kWaves, next);
+      if (more) load_values<VB, WHOLE>(s, f, next, c, x, values);
+      tile = next;
     }
   }
 
   // Join the waves, a row tile at a time: every one's sums relative to the largest reference.
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const float l = over_c_sum(st.l[r]), m = st.ref[r];
+    const float l = over_c_sum(st.l[r]), ref = st.ref[r];
     const float o_zero = kCodes ? over_c_sum(st.o_zero[r]) : 0.0f;
-    if (r) __syncthreads();
+    __syncthreads();
     if (c == 0) {
-      join_ml[wave][x][0] = m;
-      join_ml[wave][x][1] = l;
+      m.join_ml[wave][x][0] = ref;
+      m.join_ml[wave][x][1] = l;
     }
     __syncthreads();
-    float m_all = -kInf;
+    float all = -kInf;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m_all = __builtin_fmaxf(m_all, join_ml[w][x][0]);
-    const float part = m == -kInf ? 0.0f : exp2_of(m - m_all);
-    const float unit = kCodes ? part / st.fac : part;
+    for (int w = 0; w < kWaves; ++w) all = __builtin_fmaxf(all, m.join_ml[w][x][0]);
+    const float part = ref == -kInf ? 0.0f : exp2_of(ref - all);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < kChannels; ++j)
-        join[wave][x][(4 * c + i) * kChannels + j] =
-            m == -kInf ? 0.0f : kCodes ? __builtin_fmaf(o_zero, part, st.o[r][j][i] * unit) : st.o[r][j][i] * part;
+        m.join[wave][x][(4 * c + i) * kChannels + j] = ref == -kInf ? 0.0f : (st.o[r][j][i] + o_zero) * part;
     __syncthreads();
     constexpr int kPerRow = kThreads / kRowTile, kPer = D / kPerRow;  // 16 threads to a row
     const int y = threadIdx.x / kPerRow, at = (threadIdx.x % kPerRow) * kPer;
-    const uint32_t out_row = uint32_t(row0) + kRowTile * r + y;
-    const int32_t out_token = int32_t(out_row / uint32_t(a.group));
-    if (out_token >= g.count) continue;
-    const int32_t out_head = g.head * a.group + int32_t(out_row % uint32_t(a.group));
+    const uint32_t row = kRowTile * r + y;
+    const int32_t token = int32_t(row / uint32_t(a.group));
+    if (token >= g.count) continue;
+    const int32_t out_head = g.head * a.group + int32_t(row % uint32_t(a.group));
     float mm = -kInf, ll = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) mm = __builtin_fmaxf(mm, join_ml[w][y][0]);
+    for (int w = 0; w < kWaves; ++w) mm = __builtin_fmaxf(mm, m.join_ml[w][y][0]);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
-      ll += join_ml[w][y][0] == -kInf ? 0.0f : join_ml[w][y][1] * exp2_of(join_ml[w][y][0] - mm);
+      ll += m.join_ml[w][y][0] == -kInf ? 0.0f : m.join_ml[w][y][1] * exp2_of(m.join_ml[w][y][0] - mm);
     float sum[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
       sum[e] = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) sum[e] += join[w][y][at + e];
+      for (int w = 0; w < kWaves; ++w) sum[e] += m.join[w][y][at + e];
     }
-    const int64_t flat = int64_t(g.start + out_token) * a.Hq + out_head;
-    if (a.splits > 1) {
-      const int64_t slot = flat * a.splits + g.split;
+    if (part_slot >= 0) {
+      const int64_t slot = part_slot * a.part_rows + row;
 #pragma unroll
       for (int e = 0; e < kPer; e += 4)
         *reinterpret_cast<f32x4*>(a.part + slot * D + at + e) = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
@@ -792,10 +884,66 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, At
 #pragma unroll
     for (int e = 0; e < kPer; e += 2)
       word[e / 2] = s.bf16 ? pack_bf16(sum[e] * inv, sum[e + 1] * inv) : pack_f16(sum[e] * inv, sum[e + 1] * inv);
-    uint16_t* to = a.out + int64_t(g.start + out_token) * a.out_token_stride + int64_t(out_head) * a.out_head_stride + at;
+    uint16_t* to = a.out + int64_t(g.start + token) * a.out_token_stride + int64_t(out_head) * a.out_head_stride + at;
 #pragma unroll
     for (int e = 0; e < kPer / 2; e += 2) *reinterpret_cast<u32x2*>(to + 2 * e) = u32x2{word[e], word[e + 1]};
-    if (a.lse && at == 0) a.lse[flat] = lse_of(mm, ll, kUp<BF16, KB>);
+    if (a.lse && at == 0) a.lse[int64_t(g.start + token) * a.Hq + out_head] = lse_of(mm, ll);
+  }
+}
+
+// The four waves of a workgroup share a segment's rows and deal its tiles among themselves.  Each lane's pieces of the cache
+// go from memory to its registers and, decoded, straight into the matrix instructions.
+template <bool BF16, int KB, int VB, bool WHOLE, int RT>
+__global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) FewLds<RT> m;
+  const int lane = threadIdx.x & 63;
+  const Magic code = magic();
+  if (a.ranges == 0) {  // one segment to a workgroup
+    Group g = group_of_sequence(s, int32_t(blockIdx.x / uint32_t(s.H)));
+    g.head = int32_t(blockIdx.x % uint32_t(s.H));
+    if (g.count > 0) few_segment<BF16, KB, VB, WHOLE, RT>(s, a, g, 0, few_span(s, a, g).tiles, -1, code, m);
+    return;
+  }
+  // The range, and the sequence that it starts in.
+  const int64_t total = uniform(over_sequences(s, a, lane, [](int32_t, int64_t, int64_t) {}));
+  const int64_t per = range_of(a, total);
+  const int64_t begin_at = per * blockIdx.x, end_at = begin_at + per < total ? begin_at + per : total;
+  if (begin_at >= total) return;
+  int32_t seq = -1;
+  int64_t base = 0;
+  over_sequences(s, a, lane, [&](int32_t first, int64_t sums, int64_t units) {
+    const uint64_t past = __ballot(sums > begin_at);
+    if (seq >= 0 || !past) return;
+    const int at = __builtin_ctzll(past);
+    seq = first + at;
+    base = __shfl(sums - units, at);
+  });
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  base = uniform(base);
+  Group g = group_of_sequence(s, seq);
+  int32_t tiles = few_span(s, a, g).tiles;
+  for (int64_t at = begin_at; at < end_at;) {
+    const int64_t units = tiles + kSegmentCost;
+    if (g.count <= 0 || at >= base + units * s.H) {  // on to the next sequence that has rows
+      if (g.count > 0) base += units * s.H;
+      if (++seq >= s.num_seqs) return;
+      g = group_of_sequence(s, seq);
+      tiles = few_span(s, a, g).tiles;
+      continue;
+    }
+    g.head = int32_t((at - base) / units);
+    const int64_t segment = base + g.head * units;
+    const int32_t a0 = int32_t(at - segment), a1 = int32_t(end_at - segment < units ? end_at - segment : units);
+    const bool whole = a0 == 0 && a1 == units;
+    const int32_t from = a0 > kSegmentCost ? a0 - kSegmentCost : 0, upto = a1 > kSegmentCost ? a1 - kSegmentCost : 0;
+    const int64_t slot = whole ? -1 : 2 * int64_t(blockIdx.x) + (at == begin_at ? 0 : 1);
+    if (whole || from < upto) {
+      few_segment<BF16, KB, VB, WHOLE, RT>(s, a, g, from, upto, slot, code, m);
+    } else {  // a part with no tiles: only its rows' empty sums
+      for (int r = threadIdx.x; r < a.part_rows; r += kThreads)
+        *reinterpret_cast<f32x2*>(a.part_ml + 2 * (slot * a.part_rows + r)) = f32x2{-kInf, 0.0f};
+    }
+    at = segment + a1;
   }
 }
 
@@ -922,7 +1070,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       if (!seen(t0 + own, (there[own >> 6] >> (own & 63)) & 1)) raw_scale[1] = 0;
       const float ks = f16_float(raw_scale[0]), vs = f16_float(raw_scale[1]);
       m.scale[b][0][own / 4][own % 4] = ks;
-      m.scale[b][1][own / 4][own % 4] = __builtin_fmaf(ks, float(1 << (KB - 1)), f16_float(raw_scale[0] >> 16));
+      m.scale[b][1][own / 4][own % 4] = f16_float(raw_scale[0] >> 16);
       m.scale[b][2][own / 4][own % 4] = vs;
       m.scale[b][3][own / 4][own % 4] = __builtin_fmaf(vs, float(1 << (VB - 1)), f16_float(raw_scale[1] >> 16));
     } else {
@@ -979,19 +1127,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
         if (t > mine.hi_most || (t + 31 <= mine.lo_least && t >= a.sinks)) continue;  // no row of this wave sees it
         const uint32_t word = uint32_t(there[p >> 1] >> (32 * (p & 1)));
         const uint32_t there = ((word >> (4 * c)) & 0xF) | (((word >> (16 + 4 * c)) & 0xF) << 4);
-        Scales sc;
+        FloatScales sc;
         if constexpr (kCodes) {
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const int at = 8 * p + 4 * u + c;
-            const f32x4 ks = m.scale[b][0][at], kz = m.scale[b][1][at], vs = m.scale[b][2][at], vz = m.scale[b][3][at];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              sc.ks[u][i] = ks[i];
-              sc.kz[u][i] = kz[i];
-              sc.vs[u][i] = vs[i];
-              sc.vz[u][i] = vz[i];
-            }
+            sc.ks_[u] = m.scale[b][0][at];
+            sc.kz_[u] = m.scale[b][1][at];
           }
         }
         // All of a phase's operands are asked for before its first instruction.
@@ -1006,6 +1148,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
             [&] {
 #pragma unroll
               for (int j = 0; j < kChannels; ++j) v[j] = m.v[b][v_place(p, j, c, x)];
+              if constexpr (kCodes) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                  sc.vs_[u] = m.scale[b][2][8 * p + 4 * u + c];
+                  sc.vz_[u] = m.scale[b][3][8 * p + 4 * u + c];
+                }
+              }
             },
             [](const u32x4&) {});
       }
@@ -1035,7 +1184,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
     const int32_t token = int32_t(row / uint32_t(a.group)), out_head = g.head * a.group + int32_t(row % uint32_t(a.group));
     if (token >= g.count) continue;
     const int64_t flat = int64_t(g.start + token) * a.Hq + out_head;
-    const float unit = kCodes ? 1.0f / st.fac : 1.0f;
     if (a.splits > 1) {
       const int64_t slot = flat * a.splits + g.split;
 #pragma unroll
@@ -1044,7 +1192,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
         for (int j = 0; j < kChannels; j += 4) {
           f32x4 w;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = kCodes ? __builtin_fmaf(st.o[r][j + e][i], unit, o_zero) : st.o[r][j + e][i];
+          for (int e = 0; e < 4; ++e) w[e] = st.o[r][j + e][i] + o_zero;
           *reinterpret_cast<f32x4*>(a.part + slot * D + (4 * c + i) * kChannels + j) = w;
         }
       if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * slot) = f32x2{st.ref[r], l};
@@ -1058,30 +1206,27 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       for (int j = 0; j < kChannels; j += 4) {
         float w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          w[e] = (kCodes ? __builtin_fmaf(st.o[r][j + e][i], unit, o_zero) : st.o[r][j + e][i]) * inv;
+        for (int e = 0; e < 4; ++e) w[e] = (st.o[r][j + e][i] + o_zero) * inv;
         *reinterpret_cast<u32x2*>(to + (4 * c + i) * kChannels + j) =
             s.bf16 ? u32x2{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])} : u32x2{pack_f16(w[0], w[1]), pack_f16(w[2], w[3])};
       }
-    if (a.lse && c == 0) a.lse[flat] = lse_of(st.ref[r], l, kUp<BF16, KB>);
+    if (a.lse && c == 0) a.lse[flat] = lse_of(st.ref[r], l);
   }
 }
 
-// Joins the splits of each row, one workgroup to a row: D / 4 threads to a split's sums, the splits dealt to
-// the groups of so many threads.
-__global__ __launch_bounds__(kThreads) void join_kernel(ServeArgs s, AttendArgs a, float up) {
+// Joins the parts of a row, by a workgroup: D / 4 threads to a part's sums, the parts dealt to the groups of so many
+// threads; part i is at slot(i).
+template <typename Slot>
+__device__ __forceinline__ void join_parts(const ServeArgs& s, const AttendArgs& a, int32_t token, int32_t head,
+                                           int32_t parts, Slot slot) {
   constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
   __shared__ float wave_most[kWaves];
   __shared__ f32x4 sums[kGroups][kLanes];
-  __shared__ float parts[kGroups];
-  const int64_t flat = blockIdx.x;
-  const int32_t token = int32_t(uint32_t(flat) / uint32_t(a.Hq)), head = int32_t(uint32_t(flat) % uint32_t(a.Hq));
-  // Rows of no sequence have no parts.
-  if (token < scalar_entry(s.token_start, 0) || token >= scalar_entry(s.token_start, s.num_seqs)) return;
-  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + flat * a.splits;
-  const f32x4* part = reinterpret_cast<const f32x4*>(a.part + flat * a.splits * D);
+  __shared__ float totals[kGroups];
+  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml);
+  const f32x4* part = reinterpret_cast<const f32x4*>(a.part);
   float m = -kInf;
-  for (int i = threadIdx.x; i < a.splits; i += kThreads) m = __builtin_fmaxf(m, ml[i][0]);
+  for (int i = threadIdx.x; i < parts; i += kThreads) m = __builtin_fmaxf(m, ml[slot(i)][0]);
   for (int off = 1; off < 64; off <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
   if ((threadIdx.x & 63) == 0) wave_most[threadIdx.x >> 6] = m;
   __syncthreads();
@@ -1091,24 +1236,25 @@ __global__ __launch_bounds__(kThreads) void join_kernel(ServeArgs s, AttendArgs 
   float l = 0.0f;
   f32x4 sum{};
 #pragma unroll 4
-  for (int i = group; i < a.splits; i += kGroups) {
-    const f32x2 w = ml[i];
-    const f32x4 p = part[int64_t(i) * kLanes + at];
-    // A split that saw nothing has sums of nothing in particular.
+  for (int i = group; i < parts; i += kGroups) {
+    const int64_t from = slot(i);
+    const f32x2 w = ml[from];
+    const f32x4 p = part[from * kLanes + at];
+    // A part that saw nothing has sums of nothing in particular.
     const float scale = w[1] == 0.0f ? 0.0f : exp2_of(w[0] - m);
     l += w[1] * scale;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += w[1] == 0.0f ? 0.0f : p[e] * scale;
   }
   sums[group][at] = sum;
-  if (at == 0) parts[group] = l;
+  if (at == 0) totals[group] = l;
   __syncthreads();
   if (group) return;
   l = 0.0f;
   sum = f32x4{};
 #pragma unroll
   for (int i = 0; i < kGroups; ++i) {
-    l += parts[i];
+    l += totals[i];
     sum += sums[i][at];
   }
   const float inv = inverse(l);
@@ -1116,7 +1262,46 @@ __global__ __launch_bounds__(kThreads) void join_kernel(ServeArgs s, AttendArgs 
   sum *= inv;
   *reinterpret_cast<u32x2*>(to) = s.bf16 ? u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])}
                                          : u32x2{pack_f16(sum[0], sum[1]), pack_f16(sum[2], sum[3])};
-  if (a.lse && at == 0) a.lse[flat] = lse_of(m, l, up);
+  if (a.lse && at == 0) a.lse[int64_t(token) * a.Hq + head] = lse_of(m, l);
+}
+
+// The splits of each row of a call of many rows, one workgroup to a row.
+__global__ __launch_bounds__(kThreads) void join_splits_kernel(ServeArgs s, AttendArgs a) {
+  const int32_t token = int32_t(blockIdx.x / uint32_t(a.Hq)), head = int32_t(blockIdx.x % uint32_t(a.Hq));
+  // Rows of no sequence have no parts.
+  if (token < scalar_entry(s.token_start, 0) || token >= scalar_entry(s.token_start, s.num_seqs)) return;
+  const int64_t first = int64_t(blockIdx.x) * a.splits;
+  join_parts(s, a, token, head, a.splits, [&](int i) { return first + i; });
+}
+
+// The parts that the ranges' ends have cut a segment into, one workgroup to a row; whole segments are done.
+__global__ __launch_bounds__(kThreads) void join_ranges_kernel(ServeArgs s, AttendArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int32_t token = int32_t(blockIdx.x / uint32_t(a.Hq)), head = int32_t(blockIdx.x % uint32_t(a.Hq));
+  int64_t segment = 0, units = 0;
+  int32_t row = -1;
+  const int64_t total = uniform(over_sequences(s, a, lane, [&](int32_t first, int64_t sums, int64_t own) {
+    const int32_t seq = first + lane;
+    int32_t at = -1;
+    if (seq < s.num_seqs && own > 0) {
+      const Group g = group_from(s, s.token_start[seq], s.token_start[seq + 1], s.kv_lens[seq]);
+      if (token >= g.start && token < g.start + g.count) at = token - g.start;
+    }
+    const uint64_t mine = __ballot(at >= 0);
+    if (!mine) return;
+    const int from = __builtin_ctzll(mine);
+    units = __shfl(own, from) / s.H;
+    segment = __shfl(sums - own, from) + head / a.group * units;
+    row = __shfl(at, from) * a.group + head % a.group;
+  }));
+  if (row < 0) return;
+  const int64_t per = range_of(a, total);
+  const int64_t first = segment / per, last = (segment + units - 1) / per;
+  if (first == last) return;
+  const bool at_start = first * per == segment;
+  join_parts(s, a, token, head, int32_t(last - first + 1), [&](int i) {
+    return (2 * (first + i) + (i == 0 && !at_start ? 1 : 0)) * a.part_rows + row;
+  });
 }
 
 }  // namespace
@@ -1153,12 +1338,12 @@ pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const 
     s.log2P >= 4 ? few_of(std::true_type{}) : few_of(std::false_type{});
   }
   if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
-  if (a.splits > 1) {
-    const int64_t rows = int64_t(s.num_tokens) * a.Hq;
-    const float up = s.tag == PKV_TAG_FP16 && !s.bf16 ? 1.0f / 64.0f : 1.0f;
-    hipLaunchKernelGGL(join_kernel, dim3(uint32_t(rows)), dim3(kThreads), 0, stream, s, a, up);
-    if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
-  }
+  const dim3 rows(uint32_t(s.num_tokens) * uint32_t(a.Hq));
+  if (a.ranges)
+    hipLaunchKernelGGL(join_ranges_kernel, rows, dim3(kThreads), 0, stream, s, a);
+  else if (a.splits > 1)
+    hipLaunchKernelGGL(join_splits_kernel, rows, dim3(kThreads), 0, stream, s, a);
+  if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
   return PKV_OK;
 }
 

@@ -134,6 +134,8 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
   r.tiles = l.tiles;
   r.row_tiles = l.row_tiles;
   r.splits = l.splits;
+  r.ranges = l.ranges;
+  r.part_rows = l.part_rows;
   r.chunk = l.chunk;
   if (pointers && l.workspace_bytes) {
     if (!a->workspace || a->workspace_bytes < l.workspace_bytes) return PKV_ERR_INVALID_ARGUMENT;
@@ -150,23 +152,33 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   const bool many = rows > kRowTile * few_tiles(s.D);
   l.tiles = many ? many_tiles(s.D) : rows <= kRowTile ? 1 : few_tiles(s.D);
   l.row_tiles = int32_t((rows + kRowTile * l.tiles - 1) / (kRowTile * l.tiles));
+  l.part_rows = int32_t(rows);
   const int64_t base = int64_t(s.num_seqs) * s.H * l.row_tiles;
   // tokens that a row tile may have to look at
   int64_t seen = s.max_kv;
   if (a.window > 0 && !s.positions) seen = std::min<int64_t>(seen, int64_t(a.sinks) + a.window + s.max_tokens);
   const int64_t tokens = many ? kManyElems / s.D : kTokenTile;
   const int64_t tiles = std::max<int64_t>(1, (seen + tokens - 1) / tokens + 1);
-  const int64_t want = many ? 6 * 256 : 4 * 256;
-  int64_t splits = base > 0 ? std::min(want / base, tiles / (many ? 16 : 4)) : 1;
-  splits = std::max<int64_t>(1, splits);
-  l.splits = int32_t(splits);
-  l.chunk = many ? 16 : int32_t((tiles + splits - 1) / splits);
-  l.groups = base * splits;
-  if (splits > 1) {
-    const uint64_t parts = uint64_t(s.num_tokens) * a.Hq * splits;
-    l.part_bytes = parts * s.D * 4;
-    l.workspace_bytes = l.part_bytes + parts * 8;
+  uint64_t parts = 0;
+  l.splits = 1;
+  if (many) {
+    // Workgroups for six times the compute units, of 16 tiles at least.
+    l.chunk = 16;
+    if (base > 0) l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(6 * 256 / base, tiles / l.chunk)));
+    l.groups = base * l.splits;
+    if (l.splits > 1) parts = uint64_t(s.num_tokens) * a.Hq * l.splits;
+  } else if (tiles <= kSingleTiles) {
+    l.groups = base;
+  } else {
+    // As many workgroups as run at once; ranges of two tiles a wave at least.
+    const int64_t at_once = 256 * (s.D > 128 || l.tiles > 1 ? 2 : 3);
+    l.chunk = kSegmentCost + 8;
+    l.ranges = int32_t(std::min<int64_t>(at_once, base * (tiles + kSegmentCost) / l.chunk + 1));
+    l.groups = l.ranges;
+    parts = uint64_t(l.ranges) * 2 * l.part_rows;
   }
+  l.part_bytes = parts * s.D * 4;
+  l.workspace_bytes = l.part_bytes + parts * 8;
   return l;
 }
 
