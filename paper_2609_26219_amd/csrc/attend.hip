@@ -672,10 +672,10 @@ __device__ __forceinline__ float lse_of(float ref, float l) {
 
 // ---- Few rows ----
 //
-// A sequence's rows of one KV head (a segment) fit one row tile or two.  The segments' tiles of tokens, all put end to
-// end, are cut into equal ranges, one to a workgroup, so that sequences of any lengths keep the whole GPU busy to the
-// end: a workgroup takes the last part of one segment, some whole ones, the first part of another.  A
-// segment counts kSegmentCost tiles more than it has, for its start and its join.
+// A sequence's rows of one KV head fit one row tile or two.  Its tiles of tokens are cut into even pieces, one to a
+// workgroup and head: as many pieces for each sequence as make the longest piece of all shortest, with as many workgroups
+// as run at once, so that sequences of any lengths keep the whole GPU busy to the end.  Every workgroup
+// works the pieces out from the lengths, which only the device knows.
 
 // What the rows of sequence `seq` look at when nothing but lengths is known: a span without the rows' own bounds.
 __device__ __forceinline__ Span few_span(const ServeArgs& s, const AttendArgs& a, const Group& g) {
@@ -693,47 +693,80 @@ __device__ __forceinline__ Span few_span(const ServeArgs& s, const AttendArgs& a
   return span;
 }
 
-__device__ __forceinline__ int64_t units_of(const ServeArgs& s, const AttendArgs& a, int32_t start, int32_t end,
-                                            int32_t kv_len) {
-  const Group g = group_from(s, start, end, kv_len);
-  return g.count > 0 ? int64_t(s.H) * (few_span(s, a, g).tiles + kSegmentCost) : 0;
+// Tiles of a sequence, or -1 if it has no rows.
+__device__ __forceinline__ int32_t tiles_of_sequence(const ServeArgs& s, const AttendArgs& a, int32_t seq) {
+  if (seq >= s.num_seqs) return -1;
+  const Group g = group_from(s, s.token_start[seq], s.token_start[seq + 1], s.kv_lens[seq]);
+  return g.count > 0 ? few_span(s, a, g).tiles : -1;
+}
+__device__ __forceinline__ int32_t pieces_of(int32_t tiles, int32_t per) {
+  return tiles < 0 ? 0 : tiles == 0 ? 1 : (tiles - 1) / per + 1;
 }
 
-// Inclusive sums over the lanes of a wave.
-__device__ __forceinline__ int64_t wave_sums(int64_t v, int lane) {
+// Inclusive sums over the lanes of a wave, and the sum of all.
+template <typename T>
+__device__ __forceinline__ T wave_sums(T v, int lane) {
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
-    const int64_t other = __shfl_up(v, off);
+    const T other = __shfl_up(v, off);
     v += lane >= off ? other : 0;
   }
   return v;
 }
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) v += __shfl_xor(v, off);
+  return v;
+}
 
-// The units of all sequences, by every wave for itself, 64 sequences at a time: calls each(first, inclusive sums of the
-// lanes with all before, own units) and returns the total.
-template <typename Each>
-__device__ __forceinline__ int64_t over_sequences(const ServeArgs& s, const AttendArgs& a, int lane, Each each) {
-  int64_t before = 0;
+// Tiles of the longest piece, by every wave for itself.  `mine`: the tiles of sequence `lane`.  With p pieces wanted, total / p is
+// the least that could do and total / (p - sequences) surely does; up to 64 sequences the least that does is found
+// between them.
+__device__ __forceinline__ int32_t piece_tiles(const ServeArgs& s, const AttendArgs& a, int lane, int32_t mine) {
+  int64_t total = 0;
+  int32_t rows = 0;
   for (int32_t first = 0; first < s.num_seqs; first += 64) {
-    const int32_t seq = first + lane;
-    int64_t units = 0;
-    if (seq < s.num_seqs) units = units_of(s, a, s.token_start[seq], s.token_start[seq + 1], s.kv_lens[seq]);
-    const int64_t sums = before + wave_sums(units, lane);
-    each(first, sums, units);
-    before = __shfl(sums, 63);
+    const int32_t tiles = first ? tiles_of_sequence(s, a, first + lane) : mine;
+    total += tiles > 0 ? tiles : 0;
+    rows += __popcll(__ballot(tiles >= 0));
   }
-  return before;
+  total = wave_sum(total);
+  int64_t low = (total + a.pieces - 1) / a.pieces, high = (total + a.pieces - rows - 1) / (a.pieces - rows);
+  low = low > a.chunk ? low : a.chunk;
+  high = high > a.chunk ? high : a.chunk;
+  if (s.num_seqs <= 64) {
+    for (int step = 0; step < 6 && low < high; ++step) {
+      const int64_t middle = (low + high) / 2;
+      if (wave_sum(pieces_of(mine, int32_t(middle))) <= a.pieces)
+        high = middle;
+      else
+        low = middle + 1;
+    }
+  }
+  return __builtin_amdgcn_readfirstlane(int32_t(high));
 }
 
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  return int64_t(uint32_t(__builtin_amdgcn_readfirstlane(int32_t(v)))) |
-         int64_t(__builtin_amdgcn_readfirstlane(int32_t(v >> 32))) << 32;
-}
-
-// Units of a workgroup's range.
-__device__ __forceinline__ int64_t range_of(const AttendArgs& a, int64_t total) {
-  const int64_t even = (total + a.ranges - 1) / a.ranges;
-  return even > a.chunk ? even : a.chunk;
+// The first sequence, with sequence `first` + lane's tiles, for which found(lanes' inclusive sums of pieces, tiles) holds in
+// some lane: its number, the pieces before it and its tiles; -1 if there is none.
+struct Found {
+  int32_t seq, before, tiles;
+};
+template <typename Test>
+__device__ __forceinline__ Found find_sequence(const ServeArgs& s, const AttendArgs& a, int lane, int32_t mine, int32_t per,
+                                               Test test) {
+  int32_t before = 0;
+  for (int32_t first = 0; first < s.num_seqs; first += 64) {
+    const int32_t tiles = first ? tiles_of_sequence(s, a, first + lane) : mine;
+    const int32_t own = pieces_of(tiles, per), sums = before + wave_sums(own, lane);
+    const uint64_t hit = __ballot(test(first + lane, sums, own));
+    if (hit) {
+      const int at = __builtin_ctzll(hit);
+      return Found{first + at, __builtin_amdgcn_readlane(sums - own, at), __builtin_amdgcn_readlane(tiles, at)};
+    }
+    before = __builtin_amdgcn_readlane(sums, 63);
+  }
+  return Found{-1, 0, 0};
 }
 
 template <int RT>
@@ -743,49 +776,48 @@ struct FewLds {
   u32x4 words[kWaves][16];
 };
 
-// Tiles [from, upto) of a segment, into `out` and `lse` if they are all of them, else as a part.
+// Tiles [from, upto) of a sequence and head, into `out` and `lse` if they are all of them, else as part `part_slot`.
 template <bool BF16, int KB, int VB, bool WHOLE, int RT>
-__device__ __forceinline__ void few_segment(const ServeArgs& s, const AttendArgs& a, const Group& g, int32_t from,
+__device__ __forceinline__ void few_piece(const ServeArgs& s, const AttendArgs& a, const Group& g, int32_t from,
                                             int32_t upto, int64_t part_slot, const Magic& code, FewLds<RT>& m) {
   constexpr bool kCodes = KB != 16;
   const int lane = threadIdx.x & 63, c = lane >> 4, x = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Rows<RT> rows;
-  Span span;
-  load_rows<KB, RT>(s, a, g, 0, x, [&](int i) { return k_first<KB>(i, c); }, rows, span);
-  {
-    const Span all = few_span(s, a, g);
-    span.first = all.first;
-    span.sink_tiles = all.sink_tiles;
-    span.tiles = all.tiles;
-  }
-
+  const Span looks = few_span(s, a, g);
   const Source f = source_of<KB>(s, g.seq, g.head);
-  Running<RT> st;
-  begin(st);
   // The wave's tiles are `from` + wave + kWaves n.  Their pages are looked up 32 tiles at a time, a half of a tile to
   // a lane, and read from there: a scalar load for each tile would have every wait for LDS wait for it too.
   const int32_t first = from + wave, count = first < upto ? (upto - first + kWaves - 1) / kWaves : 0;
   auto pages_from = [&](int32_t n) -> int32_t {
     if constexpr (!WHOLE) return -1;
     const int32_t it = first + (n + (lane >> 1)) * kWaves;
-    return it < upto ? page_of(s, f.table, (tile_at<kTokenTile>(span, it) + 16 * (lane & 1)) >> s.log2P) : -1;
+    return it < upto ? page_of(s, f.table, (tile_at<kTokenTile>(looks, it) + 16 * (lane & 1)) >> s.log2P) : -1;
   };
   auto tile_of = [&](int32_t n, int32_t pages) {
     const int at = (n & 31) * 2;
-    return Tile{tile_at<kTokenTile>(span, first + n * kWaves),
+    return Tile{tile_at<kTokenTile>(looks, first + n * kWaves),
                 {__builtin_amdgcn_readlane(pages, at), __builtin_amdgcn_readlane(pages, at + 1)}};
   };
+  // The first tile is asked for before the queries are.
+  Keys<KB> keys;
+  Values<VB> values;
+  uint32_t scale = 0;
+  int32_t pages = -1;
+  Tile tile{};
   if (count > 0) {
-    // A tile's registers are filled again, keys and then values, as soon as its own have been used.
-    Keys<KB> keys;
-    Values<VB> values;
-    uint32_t scale = 0;
-    int32_t pages = pages_from(0);
-    Tile tile = tile_of(0, pages);
+    pages = pages_from(0);
+    tile = tile_of(0, pages);
     load_keys<KB, WHOLE>(s, f, tile, c, x, keys);
     load_values<VB, WHOLE>(s, f, tile, c, x, values);
     if constexpr (kCodes) scale = load_scale<WHOLE>(s, f, tile, lane);
+  }
+  Rows<RT> rows;
+  Span span;
+  load_rows<KB, RT>(s, a, g, 0, x, [&](int i) { return k_first<KB>(i, c); }, rows, span);
+  Running<RT> st;
+  begin(st);
+  if (count > 0) {
+    // A tile's registers are filled again, keys and then values, as soon as its own have been used.
     for (int32_t n = 0; n < count; ++n) {
       const bool more = n + 1 < count;
       if (((n + 1) & 31) == 0) pages = pages_from(n + 1);
@@ -891,60 +923,31 @@ __device__ __forceinline__ void few_segment(const ServeArgs& s, const AttendArgs
   }
 }
 
-// The four waves of a workgroup share a segment's rows and deal its tiles among themselves.  Each lane's pieces of the cache
+// The four waves of a workgroup share the rows and deal the piece's tiles among themselves.  Each lane's pieces of the cache
 // go from memory to its registers and, decoded, straight into the matrix instructions.
 template <bool BF16, int KB, int VB, bool WHOLE, int RT>
 __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, AttendArgs a) {
   __shared__ __attribute__((aligned(16))) FewLds<RT> m;
   const int lane = threadIdx.x & 63;
   const Magic code = magic();
-  if (a.ranges == 0) {  // one segment to a workgroup
-    Group g = group_of_sequence(s, int32_t(blockIdx.x / uint32_t(s.H)));
+  const uint32_t piece = blockIdx.x / uint32_t(s.H);
+  if (a.pieces == 0) {  // a sequence to a workgroup and head
+    Group g = group_of_sequence(s, int32_t(piece));
     g.head = int32_t(blockIdx.x % uint32_t(s.H));
-    if (g.count > 0) few_segment<BF16, KB, VB, WHOLE, RT>(s, a, g, 0, few_span(s, a, g).tiles, -1, code, m);
+    if (g.count > 0) few_piece<BF16, KB, VB, WHOLE, RT>(s, a, g, 0, few_span(s, a, g).tiles, -1, code, m);
     return;
   }
-  // The range, and the sequence that it starts in.
-  const int64_t total = uniform(over_sequences(s, a, lane, [](int32_t, int64_t, int64_t) {}));
-  const int64_t per = range_of(a, total);
-  const int64_t begin_at = per * blockIdx.x, end_at = begin_at + per < total ? begin_at + per : total;
-  if (begin_at >= total) return;
-  int32_t seq = -1;
-  int64_t base = 0;
-  over_sequences(s, a, lane, [&](int32_t first, int64_t sums, int64_t units) {
-    const uint64_t past = __ballot(sums > begin_at);
-    if (seq >= 0 || !past) return;
-    const int at = __builtin_ctzll(past);
-    seq = first + at;
-    base = __shfl(sums - units, at);
+  const int32_t mine = tiles_of_sequence(s, a, lane), per = piece_tiles(s, a, lane, mine);
+  const Found at = find_sequence(s, a, lane, mine, per, [&](int32_t, int32_t sums, int32_t own) {
+    return own > 0 && sums > int32_t(piece);
   });
-  seq = __builtin_amdgcn_readfirstlane(seq);
-  base = uniform(base);
-  Group g = group_of_sequence(s, seq);
-  int32_t tiles = few_span(s, a, g).tiles;
-  for (int64_t at = begin_at; at < end_at;) {
-    const int64_t units = tiles + kSegmentCost;
-    if (g.count <= 0 || at >= base + units * s.H) {  // on to the next sequence that has rows
-      if (g.count > 0) base += units * s.H;
-      if (++seq >= s.num_seqs) return;
-      g = group_of_sequence(s, seq);
-      tiles = few_span(s, a, g).tiles;
-      continue;
-    }
-    g.head = int32_t((at - base) / units);
-    const int64_t segment = base + g.head * units;
-    const int32_t a0 = int32_t(at - segment), a1 = int32_t(end_at - segment < units ? end_at - segment : units);
-    const bool whole = a0 == 0 && a1 == units;
-    const int32_t from = a0 > kSegmentCost ? a0 - kSegmentCost : 0, upto = a1 > kSegmentCost ? a1 - kSegmentCost : 0;
-    const int64_t slot = whole ? -1 : 2 * int64_t(blockIdx.x) + (at == begin_at ? 0 : 1);
-    if (whole || from < upto) {
-      few_segment<BF16, KB, VB, WHOLE, RT>(s, a, g, from, upto, slot, code, m);
-    } else {  // a part with no tiles: only its rows' empty sums
-      for (int r = threadIdx.x; r < a.part_rows; r += kThreads)
-        *reinterpret_cast<f32x2*>(a.part_ml + 2 * (slot * a.part_rows + r)) = f32x2{-kInf, 0.0f};
-    }
-    at = segment + a1;
-  }
+  if (at.seq < 0) return;
+  Group g = group_of_sequence(s, at.seq);
+  g.head = int32_t(blockIdx.x % uint32_t(s.H));
+  const int32_t pieces = pieces_of(at.tiles, per), share = (at.tiles + pieces - 1) / pieces;
+  const int32_t from = (int32_t(piece) - at.before) * share;
+  few_piece<BF16, KB, VB, WHOLE, RT>(s, a, g, from, from + share < at.tiles ? from + share : at.tiles,
+                                     pieces == 1 ? -1 : int64_t(blockIdx.x), code, m);
 }
 
 // Many rows: each wave has 32 of its own (16 at 256 channels), and the workgroup's four share the cache through LDS.  A tile of
@@ -1274,33 +1277,23 @@ __global__ __launch_bounds__(kThreads) void join_splits_kernel(ServeArgs s, Atte
   join_parts(s, a, token, head, a.splits, [&](int i) { return first + i; });
 }
 
-// The parts that the ranges' ends have cut a segment into, one workgroup to a row; whole segments are done.
-__global__ __launch_bounds__(kThreads) void join_ranges_kernel(ServeArgs s, AttendArgs a) {
+// The pieces of a sequence of few rows, one workgroup to a row; a sequence of one piece is done.
+__global__ __launch_bounds__(kThreads) void join_pieces_kernel(ServeArgs s, AttendArgs a) {
   const int lane = threadIdx.x & 63;
   const int32_t token = int32_t(blockIdx.x / uint32_t(a.Hq)), head = int32_t(blockIdx.x % uint32_t(a.Hq));
-  int64_t segment = 0, units = 0;
-  int32_t row = -1;
-  const int64_t total = uniform(over_sequences(s, a, lane, [&](int32_t first, int64_t sums, int64_t own) {
-    const int32_t seq = first + lane;
-    int32_t at = -1;
-    if (seq < s.num_seqs && own > 0) {
-      const Group g = group_from(s, s.token_start[seq], s.token_start[seq + 1], s.kv_lens[seq]);
-      if (token >= g.start && token < g.start + g.count) at = token - g.start;
-    }
-    const uint64_t mine = __ballot(at >= 0);
-    if (!mine) return;
-    const int from = __builtin_ctzll(mine);
-    units = __shfl(own, from) / s.H;
-    segment = __shfl(sums - own, from) + head / a.group * units;
-    row = __shfl(at, from) * a.group + head % a.group;
-  }));
-  if (row < 0) return;
-  const int64_t per = range_of(a, total);
-  const int64_t first = segment / per, last = (segment + units - 1) / per;
-  if (first == last) return;
-  const bool at_start = first * per == segment;
-  join_parts(s, a, token, head, int32_t(last - first + 1), [&](int i) {
-    return (2 * (first + i) + (i == 0 && !at_start ? 1 : 0)) * a.part_rows + row;
+  const int32_t mine = tiles_of_sequence(s, a, lane), per = piece_tiles(s, a, lane, mine);
+  const Found at = find_sequence(s, a, lane, mine, per, [&](int32_t seq, int32_t, int32_t own) {
+    if (own == 0) return false;
+    const Group g = group_from(s, s.token_start[seq], s.token_start[seq + 1], s.kv_lens[seq]);
+    return token >= g.start && token < g.start + g.count;
+  });
+  if (at.seq < 0) return;
+  const int32_t pieces = pieces_of(at.tiles, per);
+  if (pieces == 1) return;
+  const int32_t start = scalar_entry(s.token_start, at.seq);
+  const int32_t row = (token - (start < 0 ? 0 : start)) * a.group + head % a.group;
+  join_parts(s, a, token, head, pieces, [&](int i) {
+    return (int64_t(at.before + i) * s.H + head / a.group) * a.part_rows + row;
   });
 }
 
@@ -1339,8 +1332,8 @@ pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const 
   }
   if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
   const dim3 rows(uint32_t(s.num_tokens) * uint32_t(a.Hq));
-  if (a.ranges)
-    hipLaunchKernelGGL(join_ranges_kernel, rows, dim3(kThreads), 0, stream, s, a);
+  if (a.pieces)
+    hipLaunchKernelGGL(join_pieces_kernel, rows, dim3(kThreads), 0, stream, s, a);
   else if (a.splits > 1)
     hipLaunchKernelGGL(join_splits_kernel, rows, dim3(kThreads), 0, stream, s, a);
   if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;

@@ -49,7 +49,7 @@ struct AttendArgs {
   uint16_t* out;
   float* lse;         // or null
   // Parts of rows: [..][D] sums relative to a reference, and [..][2] the reference (base 2) and the sum of the
-  // probabilities.  Splits: [num_tokens * Hq][splits]; ranges: [ranges][2][part_rows].
+  // probabilities.  Splits: [num_tokens * Hq][splits]; pieces: [pieces][H][part_rows].
   float* part;
   float* part_ml;
   int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
@@ -59,14 +59,14 @@ struct AttendArgs {
   int32_t tiles;      // row tiles of a workgroup
   int32_t row_tiles;  // workgroups' shares of the rows of one sequence and KV head
   int32_t splits;     // many rows: workgroups that share the tokens of a row tile
-  int32_t ranges;     // few rows: workgroups that share all tiles of all sequences (0: one to each segment)
-  int32_t part_rows;  // rows of a segment
-  int32_t chunk;      // least tiles of tokens in a split, units in a range
+  int32_t pieces;     // few rows: most pieces of all sequences' tokens together (0: each sequence is whole)
+  int32_t part_rows;  // rows of a sequence and KV head
+  int32_t chunk;      // least tiles of tokens in a split or piece
 };
 
 // How an attention call is launched.
 struct AttendLaunch {
-  int32_t tiles, row_tiles, splits, ranges, part_rows, chunk;
+  int32_t tiles, row_tiles, splits, pieces, part_rows, chunk;
   int64_t groups;           // workgroups
   uint64_t part_bytes;      // of AttendArgs::part, then part_ml
   uint64_t workspace_bytes; // both
@@ -81,10 +81,8 @@ constexpr int kTokenTile = 32; // cached tokens a wave takes at a time
 constexpr int few_tiles(int head_dim) { return head_dim > 128 ? 1 : 2; }
 constexpr int many_tiles(int head_dim) { return 4 * few_tiles(head_dim); }
 constexpr int kManyElems = 8192;
-// Tiles that a segment of few rows counts more than it has (measured: a segment's start and join take about as long).
-constexpr int kSegmentCost = 4;
-// Segments of no more tiles go to a workgroup each, whole: no second kernel.
-constexpr int kSingleTiles = 12;
+// Sequences of no more tiles are not cut: no second kernel.
+constexpr int kWholeTiles = 12;
 
 // Host checks that need no GPU; they fill the arguments.
 pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,

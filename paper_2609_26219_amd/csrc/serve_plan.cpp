@@ -134,7 +134,7 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
   r.tiles = l.tiles;
   r.row_tiles = l.row_tiles;
   r.splits = l.splits;
-  r.ranges = l.ranges;
+  r.pieces = l.pieces;
   r.part_rows = l.part_rows;
   r.chunk = l.chunk;
   if (pointers && l.workspace_bytes) {
@@ -167,15 +167,19 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
     if (base > 0) l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(6 * 256 / base, tiles / l.chunk)));
     l.groups = base * l.splits;
     if (l.splits > 1) parts = uint64_t(s.num_tokens) * a.Hq * l.splits;
-  } else if (tiles <= kSingleTiles) {
+  } else if (tiles <= kWholeTiles) {
     l.groups = base;
   } else {
-    // As many workgroups as run at once; ranges of two tiles a wave at least.
-    const int64_t at_once = 256 * (s.D > 128 || l.tiles > 1 ? 2 : 3);
-    l.chunk = kSegmentCost + 8;
-    l.ranges = int32_t(std::min<int64_t>(at_once, base * (tiles + kSegmentCost) / l.chunk + 1));
-    l.groups = l.ranges;
-    parts = uint64_t(l.ranges) * 2 * l.part_rows;
+    // As many workgroups as run at once, of two tiles a wave at least; where the sequences alone are more than half of
+    // that, two rounds of them and half as many again as there are sequences.
+    const int64_t at_once = 256 * (s.D > 128 || l.tiles > 1 ? 2 : 3) / s.H;
+    l.chunk = 8;
+    int64_t pieces = at_once;
+    if (s.num_seqs > at_once / 2) pieces = std::max<int64_t>(2 * at_once, s.num_seqs + s.num_seqs / 2 + 1);
+    pieces = std::min<int64_t>(pieces, s.num_seqs * ((tiles - 1) / l.chunk + 1) + 1);
+    l.pieces = int32_t(std::max<int64_t>(pieces, s.num_seqs + 1));
+    l.groups = int64_t(l.pieces) * s.H;
+    parts = uint64_t(l.groups) * l.part_rows;
   }
   l.part_bytes = parts * s.D * 4;
   l.workspace_bytes = l.part_bytes + parts * 8;
