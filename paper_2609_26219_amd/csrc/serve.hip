@@ -79,15 +79,67 @@ __device__ __forceinline__ int64_t place_of(const ServeArgs& a, const int32_t* s
   return (page << a.log2P) | (pos & ((int64_t(1) << a.log2P) - 1));
 }
 
+// Where a token's rows of head 0 lie: bytes from the layer's first key (code) and value (code), words from its first scale; k < 0
+// as place_of.
+struct Place {
+  int64_t k, v, scale;
+};
+
 // The places of tokens [i0, i0 + n) into `place`, by the whole workgroup.
-__device__ __forceinline__ void find_places(const ServeArgs& a, int32_t i0, int32_t n, int32_t* starts, int64_t* place) {
+template <int KB, int VB>
+__device__ __forceinline__ void find_places(const ServeArgs& a, int32_t i0, int32_t n, int32_t* starts, Place* place) {
   const int tid = threadIdx.x;
   const bool in_lds = a.num_seqs < kStartsInLds;
   if (in_lds)
     for (int32_t j = tid; j <= a.num_seqs; j += kThreads) starts[j] = a.token_start[j];
   __syncthreads();
-  if (tid < n) place[tid] = place_of(a, in_lds ? starts : a.token_start, i0 + tid);
+  if (tid < n) {
+    const int64_t at = in_lds ? place_of(a, starts, i0 + tid) : place_of(a, a.token_start, i0 + tid);
+    Place p{at, at, at};
+    if (at >= 0) {
+      const int64_t page = at >> a.log2P, slot = at & ((int64_t(1) << a.log2P) - 1);
+      if constexpr (KB == 16) {
+        p.k = p.v = 2 * (page * a.page_stride + slot * a.H * a.D);
+      } else {
+        p.k = page * a.page_stride + slot * (a.D * KB / 8);
+        p.v = page * a.page_stride + a.v_offset + slot * (a.D * VB / 8);
+        p.scale = page * a.scale_stride + slot;
+      }
+    }
+    place[tid] = p;
+  }
   __syncthreads();
+}
+
+// Minimum and maximum over the 2, 4, .. 64 lanes of a row, which lie next to each other: exchanges within quads, halves of
+// 16 and 16 lanes by the operand path of the minimum itself, beyond by lane swaps.
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ void row_range(float& mn, float& mx, int32_t lanes) {
+  mn = __builtin_fminf(mn, moved<0xB1>(mn));  // quad_perm [1, 0, 3, 2]
+  mx = __builtin_fmaxf(mx, moved<0xB1>(mx));
+  if (lanes > 2) {
+    mn = __builtin_fminf(mn, moved<0x4E>(mn));  // quad_perm [2, 3, 0, 1]
+    mx = __builtin_fmaxf(mx, moved<0x4E>(mx));
+  }
+  if (lanes > 4) {
+    mn = __builtin_fminf(mn, moved<0x141>(mn));  // row_half_mirror
+    mx = __builtin_fmaxf(mx, moved<0x141>(mx));
+  }
+  if (lanes > 8) {
+    mn = __builtin_fminf(mn, moved<0x140>(mn));  // row_mirror
+    mx = __builtin_fmaxf(mx, moved<0x140>(mx));
+  }
+  if (lanes > 16) {
+    mn = __builtin_fminf(mn, __shfl_xor(mn, 16));
+    mx = __builtin_fmaxf(mx, __shfl_xor(mx, 16));
+  }
+  if (lanes > 32) {
+    mn = __builtin_fminf(mn, __shfl_xor(mn, 32));
+    mx = __builtin_fmaxf(mx, __shfl_xor(mx, 32));
+  }
 }
 
 // Zero and scale of a row from its range, and its codes.  The zero is exact in
@@ -124,10 +176,9 @@ __device__ __forceinline__ RowQuant row_quant(float mn, float mx) {
 // Codes of N values (8 of 4 bits or 4 of 8 bits) in one word.  t is within
 // 6.1e-5 of the quotient (x - zero) / scale (roundings of 2^-24, 2^-23 and 2^-24
 // relative on at most 255), and the hardware's float to byte conversion rounds
-// it half to even; a word with a t within 1e-4 of a half-integer is computed
-// again in double with a true division.
+// it half to even; `near` is set where a t is within 1e-4 of a half-integer, where that cannot decide.
 template <bool BF16, int BITS>
-__device__ __forceinline__ uint32_t row_codes(const u32x4& w, int first, const RowQuant& q) {
+__device__ __forceinline__ uint32_t row_codes(const u32x4& w, int first, const RowQuant& q, bool& near) {
   constexpr int N = 32 / BITS;
   uint32_t lo = 0, hi = 0;
   float dist = 1.0f;
@@ -140,82 +191,99 @@ __device__ __forceinline__ uint32_t row_codes(const u32x4& w, int first, const R
       hi = __builtin_amdgcn_cvt_pk_u8_f32(t, e >> 1, hi);
     dist = __builtin_fminf(dist, __builtin_fabsf(__builtin_amdgcn_fractf(t) - 0.5f));
   }
-  uint32_t packed = BITS == 8 ? lo : lo | (hi << 4);
-  if (dist < 1e-4f && q.scale_bits) {
-    const double scale = f16_float(q.scale_bits);
-    packed = 0;
-    for (int e = 0; e < N; ++e) {
-      double c = __builtin_rint((static_cast<double>(value<BF16>(w, first + e)) - static_cast<double>(q.zero)) / scale);
-      c = c < 0.0 ? 0.0 : c > double((1 << BITS) - 1) ? double((1 << BITS) - 1) : c;
-      packed |= static_cast<uint32_t>(c) << (BITS * e);
-    }
+  near |= dist < 1e-4f;
+  return BITS == 8 ? lo : lo | (hi << 4);
+}
+
+// The same codes with the rounding decided exactly: with b = floor(t), the code is b or b + 1 as x is below or above zero +
+// (b + 1/2) scale, and the even one where they are equal.  (b + 1/2) scale is exact in single precision (at most 20
+// bits), and so is its sum with zero as a pair of numbers, the rounded sum and its error.
+template <bool BF16, int BITS>
+__device__ __forceinline__ uint32_t row_codes_exact(const u32x4& w, int first, const RowQuant& q) {
+  constexpr int N = 32 / BITS;
+  const float scale = f16_float(q.scale_bits);
+  uint32_t packed = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float x = value<BF16>(w, first + e), b = __builtin_floorf((x - q.zero) * q.inv), h = (b + 0.5f) * scale;
+    const float sum = h + q.zero, back = sum - h, error = (h - (sum - back)) + (q.zero - back);
+    const float over = x - sum;  // (its sign is exact)
+    const bool above = over > 0.0f || (over == 0.0f && error < 0.0f), equal = over == 0.0f && error == 0.0f;
+    const int32_t low = static_cast<int32_t>(b);
+    packed |= static_cast<uint32_t>(low + ((above || (equal && (low & 1))) ? 1 : 0)) << (BITS * e);
   }
   return packed;
 }
 
-// One row piece (8 channels) into the cache.
-template <bool BF16, int BITS>
-__device__ __forceinline__ void put(const ServeArgs& a, const u32x4& w, int which, int64_t place, int32_t head,
+// A row's pieces (8 channels of K and of V) into the cache.
+template <bool BF16, int KB, int VB>
+__device__ __forceinline__ void put(const ServeArgs& a, const u32x4& k, const u32x4& v, const Place& at, int32_t head,
                                     int32_t piece, int32_t lanes, bool on) {
-  if constexpr (BITS == 16) {
-    if (on) {
-      uint16_t* base = which ? a.v_cache : a.k_cache;
-      const int64_t page = place >> a.log2P, slot = place & ((int64_t(1) << a.log2P) - 1);
-      *reinterpret_cast<u32x4*>(base + page * a.page_stride + slot * a.H * a.D + head * a.D + 8 * piece) = w;
-    }
+  if constexpr (KB == 16) {
+    if (!on) return;
+    const int64_t off = 2 * (head * a.D + 8 * piece);
+    *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(a.k_cache) + at.k + off) = k;
+    *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(a.v_cache) + at.v + off) = v;
   } else {
-    float mn = __builtin_inff(), mx = -__builtin_inff();
+    float mn[2] = {__builtin_inff(), __builtin_inff()}, mx[2] = {-__builtin_inff(), -__builtin_inff()};
     if (8 * piece < a.D) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = value<BF16>(w, e);
-        mn = __builtin_fminf(mn, x);
-        mx = __builtin_fmaxf(mx, x);
+        const float x = value<BF16>(k, e), y = value<BF16>(v, e);
+        mn[0] = __builtin_fminf(mn[0], x);
+        mx[0] = __builtin_fmaxf(mx[0], x);
+        mn[1] = __builtin_fminf(mn[1], y);
+        mx[1] = __builtin_fmaxf(mx[1], y);
       }
     }
-    for (int off = 1; off < lanes; off <<= 1) {
-      mn = __builtin_fminf(mn, __shfl_xor(mn, off));
-      mx = __builtin_fmaxf(mx, __shfl_xor(mx, off));
+    row_range(mn[0], mx[0], lanes);
+    row_range(mn[1], mx[1], lanes);
+    const RowQuant kq = row_quant<KB>(mn[0], mx[0]), vq = row_quant<VB>(mn[1], mx[1]);
+    constexpr int kKWords = KB / 4, kVWords = VB / 4;
+    uint32_t kc[kKWords], vc[kVWords];
+    bool near = false;
+#pragma unroll
+    for (int i = 0; i < kKWords; ++i) kc[i] = row_codes<BF16, KB>(k, 4 * i, kq, near);
+#pragma unroll
+    for (int i = 0; i < kVWords; ++i) vc[i] = row_codes<BF16, VB>(v, 4 * i, vq, near);
+    if (near) {
+#pragma unroll
+      for (int i = 0; i < kKWords; ++i) kc[i] = kq.scale_bits ? row_codes_exact<BF16, KB>(k, 4 * i, kq) : 0;
+#pragma unroll
+      for (int i = 0; i < kVWords; ++i) vc[i] = vq.scale_bits ? row_codes_exact<BF16, VB>(v, 4 * i, vq) : 0;
     }
-    const RowQuant q = row_quant<BITS>(mn, mx);
     if (!on) return;
-    const int64_t page = place >> a.log2P, slot = place & ((int64_t(1) << a.log2P) - 1);
-    uint8_t* row = a.codes + page * a.page_stride + head * a.head_stride + (which ? a.v_offset : 0) +
-                   slot * (a.D * BITS / 8) + piece * BITS;
-    if constexpr (BITS == 8)
-      *reinterpret_cast<u32x2*>(row) = u32x2{row_codes<BF16, 8>(w, 0, q), row_codes<BF16, 8>(w, 4, q)};
+    uint8_t* to = a.codes + head * a.head_stride;
+    if constexpr (KB == 8)
+      *reinterpret_cast<u32x2*>(to + at.k + 8 * piece) = u32x2{kc[0], kc[kKWords - 1]};
     else
-      *reinterpret_cast<uint32_t*>(row) = row_codes<BF16, 4>(w, 0, q);
-    if (piece == 0)
-      a.scales[page * a.scale_stride + ((int64_t(head) * 2 + which) << a.log2P) + slot] =
-          q.scale_bits | (q.zero_bits << 16);
+      *reinterpret_cast<uint32_t*>(to + at.k + 4 * piece) = kc[0];
+    if constexpr (VB == 8)
+      *reinterpret_cast<u32x2*>(to + at.v + 8 * piece) = u32x2{vc[0], vc[kVWords - 1]};
+    else
+      *reinterpret_cast<uint32_t*>(to + at.v + 4 * piece) = vc[0];
+    if (piece < 2) {
+      uint32_t* scales = a.scales + at.scale + ((int64_t(head) * 2 + piece) << a.log2P);
+      *scales = piece ? vq.scale_bits | (vq.zero_bits << 16) : kq.scale_bits | (kq.zero_bits << 16);
+    }
   }
 }
 
-// One row piece from the cache, as 8 16-bit values.
+// A row piece from the cache, as 8 16-bit values.
 template <bool BF16, int BITS>
-__device__ __forceinline__ u32x4 get(const ServeArgs& a, int which, int64_t place, int32_t head, int32_t piece) {
-  const int64_t page = place >> a.log2P, slot = place & ((int64_t(1) << a.log2P) - 1);
-  if constexpr (BITS == 16) {
-    const uint16_t* base = which ? a.v_cache : a.k_cache;
-    return *reinterpret_cast<const u32x4*>(base + page * a.page_stride + slot * a.H * a.D + head * a.D + 8 * piece);
+__device__ __forceinline__ u32x4 get(const uint8_t* row, uint32_t sz, int32_t piece) {
+  const float s = f16_float(sz), z = f16_float(sz >> 16);
+  float x[8];
+  if constexpr (BITS == 8) {
+    const u32x2 c = *reinterpret_cast<const u32x2*>(row + 8 * piece);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(static_cast<float>((c[e >> 2] >> (8 * (e & 3))) & 0xFF), s, z);
   } else {
-    const uint8_t* row = a.codes + page * a.page_stride + head * a.head_stride + (which ? a.v_offset : 0) +
-                         slot * (a.D * BITS / 8) + piece * BITS;
-    const uint32_t sz = a.scales[page * a.scale_stride + ((int64_t(head) * 2 + which) << a.log2P) + slot];
-    const float s = f16_float(sz), z = f16_float(sz >> 16);
-    float x[8];
-    if constexpr (BITS == 8) {
-      const u32x2 c = *reinterpret_cast<const u32x2*>(row);
+    const uint32_t c = *reinterpret_cast<const uint32_t*>(row + 4 * piece);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(static_cast<float>((c[e >> 2] >> (8 * (e & 3))) & 0xFF), s, z);
-    } else {
-      const uint32_t c = *reinterpret_cast<const uint32_t*>(row);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(static_cast<float>((c >> (4 * e)) & 0xF), s, z);
-    }
-    return u32x4{pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3]), pack2<BF16>(x[4], x[5]), pack2<BF16>(x[6], x[7])};
+    for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(static_cast<float>((c >> (4 * e)) & 0xF), s, z);
   }
+  return u32x4{pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3]), pack2<BF16>(x[4], x[5]), pack2<BF16>(x[6], x[7])};
 }
 
 struct RowWork {
@@ -226,35 +294,53 @@ struct RowWork {
 template <bool BF16, int KB, int VB, bool WRITE>
 __global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, RowWork w) {
   __shared__ int32_t starts[kStartsInLds];
-  __shared__ int64_t place[kMostTokens];
+  __shared__ Place place[kMostTokens];
   const int32_t tokens = 1 << w.log2_tokens, lanes = 1 << w.log2_lanes;
   const int32_t i0 = int32_t(blockIdx.x) << w.log2_tokens;
   const int32_t n = tokens < a.num_tokens - i0 ? tokens : a.num_tokens - i0;
-  find_places(a, i0, n, starts, place);
   const int32_t piece = threadIdx.x & (lanes - 1);
   const int32_t rows = a.H << w.log2_tokens, step = kThreads >> w.log2_lanes;
-  // Every lane of a row's group runs the same passes, so the exchange in put() is between live lanes.
-  for (int32_t row = threadIdx.x >> w.log2_lanes; row < rows; row += step) {
+  int32_t row = threadIdx.x >> w.log2_lanes;
+  auto off_of = [&](int32_t at) {
+    return int64_t(i0 + (at & (tokens - 1))) * r.token_stride + (at >> w.log2_tokens) * r.head_stride + 8 * piece;
+  };
+  auto mine = [&](int32_t at) { return at < rows && (at & (tokens - 1)) < n && 8 * piece < a.D; };
+  u32x4 k{}, v{};
+  if (WRITE && mine(row)) {  // on their way while the places are found
+    k = *reinterpret_cast<const u32x4*>(r.k + off_of(row));
+    v = *reinterpret_cast<const u32x4*>(r.v + off_of(row));
+  }
+  find_places<KB, VB>(a, i0, n, starts, place);
+  // Every lane of a row's group runs the same passes, so the exchanges in put() are between live lanes.
+  for (; row < rows; row += step) {
     const int32_t head = row >> w.log2_tokens, t = row & (tokens - 1);
-    const bool mine = t < n && 8 * piece < a.D;
-    const int64_t at = t < n ? place[t] : -2;
-    const int64_t off = int64_t(i0 + t) * r.token_stride + head * r.head_stride + 8 * piece;
+    const Place at = place[t < n ? t : 0];
+    const bool on = mine(row) && at.k >= 0;
     if constexpr (WRITE) {
-      u32x4 k{}, v{};
-      if (mine) {
-        k = *reinterpret_cast<const u32x4*>(r.k + off);
-        v = *reinterpret_cast<const u32x4*>(r.v + off);
+      const u32x4 k_now = k, v_now = v;
+      if (mine(row + step)) {
+        k = *reinterpret_cast<const u32x4*>(r.k + off_of(row + step));
+        v = *reinterpret_cast<const u32x4*>(r.v + off_of(row + step));
       }
-      put<BF16, KB>(a, k, 0, at, head, piece, lanes, mine && at >= 0);
-      put<BF16, VB>(a, v, 1, at, head, piece, lanes, mine && at >= 0);
-    } else if (mine && at != -2) {
-      u32x4 k{}, v{};
-      if (at >= 0) {
-        k = get<BF16, KB>(a, 0, at, head, piece);
-        v = get<BF16, VB>(a, 1, at, head, piece);
+      put<BF16, KB, VB>(a, k_now, v_now, at, head, piece, lanes, on);
+    } else if (mine(row) && at.k != -2) {
+      if (on) {
+        if constexpr (KB == 16) {
+          const int64_t off = 2 * (head * a.D + 8 * piece);
+          k = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.k_cache) + at.k + off);
+          v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.v_cache) + at.v + off);
+        } else {
+          const uint8_t* from = a.codes + head * a.head_stride;
+          const uint32_t* scales = a.scales + at.scale + ((int64_t(head) * 2) << a.log2P);
+          const uint32_t ks = scales[0], vs = scales[int64_t(1) << a.log2P];
+          k = get<BF16, KB>(from + at.k, ks, piece);
+          v = get<BF16, VB>(from + at.v, vs, piece);
+        }
+      } else {
+        k = v = u32x4{};
       }
-      *reinterpret_cast<u32x4*>(r.k + off) = k;
-      *reinterpret_cast<u32x4*>(r.v + off) = v;
+      *reinterpret_cast<u32x4*>(r.k + off_of(row)) = k;
+      *reinterpret_cast<u32x4*>(r.v + off_of(row)) = v;
     }
   }
 }
@@ -263,10 +349,10 @@ template <bool WRITE>
 pkv_status_t launch_rows(const ServeArgs& s, const RowArgs& r, hipStream_t stream) {
   RowWork w{0, 0};
   while ((8 << w.log2_lanes) < s.D) ++w.log2_lanes;
-  // Enough rows for one pass of a workgroup; more while that leaves four workgroups to a compute unit.
+  // Enough rows for one pass of a workgroup; more while that leaves 32 workgroups to a compute unit.
   const int32_t pass = kThreads >> w.log2_lanes;
   while ((1 << w.log2_tokens) < kMostTokens &&
-         ((s.H << w.log2_tokens) < pass || (s.num_tokens >> w.log2_tokens) >= 2048))
+         ((s.H << w.log2_tokens) < pass || (s.num_tokens >> w.log2_tokens) >= 8192))
     ++w.log2_tokens;
   const dim3 grid((uint32_t(s.num_tokens) + (1u << w.log2_tokens) - 1) >> w.log2_tokens);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, s, r, w); };
