@@ -22,7 +22,7 @@ namespace pkv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostTokens = 64;    // of a workgroup
+constexpr int kMostTokens = 128;   // of a workgroup (rows of 16 channels: two lanes each)
 constexpr int kStartsInLds = 1024; // sequences whose starts are searched in LDS
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -111,161 +111,140 @@ __device__ __forceinline__ void find_places(const ServeArgs& a, int32_t i0, int3
   __syncthreads();
 }
 
+template <bool BF16>
+__device__ __forceinline__ void piece_range(const u32x4& w, float& mn, float& mx) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = value<BF16>(w, e);
+    mn = __builtin_fminf(mn, x);
+    mx = __builtin_fmaxf(mx, x);
+  }
+}
+
+// The plain instructions: rows are finite (the quantiser's contract), and fminf's care for signalling NaN takes two more.
+__device__ __forceinline__ float least(float a, float b) {
+  asm("v_min_f32 %0, %1, %2" : "=v"(a) : "v"(a), "v"(b));
+  return a;
+}
+__device__ __forceinline__ float most(float a, float b) {
+  asm("v_max_f32 %0, %1, %2" : "=v"(a) : "v"(a), "v"(b));
+  return a;
+}
+
 // Minimum and maximum over the 2, 4, .. 64 lanes of a row, which lie next to each other: exchanges within quads, halves of
 // 16 and 16 lanes by the operand path of the minimum itself, beyond by lane swaps.
 template <int CTRL>
 __device__ __forceinline__ float moved(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
 }
-__device__ __forceinline__ void row_range(float& mn, float& mx, int32_t lanes) {
-  mn = __builtin_fminf(mn, moved<0xB1>(mn));  // quad_perm [1, 0, 3, 2]
-  mx = __builtin_fmaxf(mx, moved<0xB1>(mx));
-  if (lanes > 2) {
-    mn = __builtin_fminf(mn, moved<0x4E>(mn));  // quad_perm [2, 3, 0, 1]
-    mx = __builtin_fmaxf(mx, moved<0x4E>(mx));
+// (of K and of V)
+template <int CTRL>
+__device__ __forceinline__ void range_step(float (&mn)[2], float (&mx)[2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    mn[i] = least(mn[i], moved<CTRL>(mn[i]));
+    mx[i] = most(mx[i], moved<CTRL>(mx[i]));
   }
-  if (lanes > 4) {
-    mn = __builtin_fminf(mn, moved<0x141>(mn));  // row_half_mirror
-    mx = __builtin_fmaxf(mx, moved<0x141>(mx));
-  }
-  if (lanes > 8) {
-    mn = __builtin_fminf(mn, moved<0x140>(mn));  // row_mirror
-    mx = __builtin_fmaxf(mx, moved<0x140>(mx));
-  }
-  if (lanes > 16) {
-    mn = __builtin_fminf(mn, __shfl_xor(mn, 16));
-    mx = __builtin_fmaxf(mx, __shfl_xor(mx, 16));
-  }
-  if (lanes > 32) {
-    mn = __builtin_fminf(mn, __shfl_xor(mn, 32));
-    mx = __builtin_fmaxf(mx, __shfl_xor(mx, 32));
+}
+__device__ __forceinline__ void row_range(float (&mn)[2], float (&mx)[2], int32_t lanes) {
+  range_step<0xB1>(mn, mx);                  // quad_perm [1, 0, 3, 2]
+  if (lanes > 2) range_step<0x4E>(mn, mx);   // quad_perm [2, 3, 0, 1]
+  if (lanes > 4) range_step<0x141>(mn, mx);  // row_half_mirror
+  if (lanes > 8) range_step<0x140>(mn, mx);  // row_mirror
+  for (int off = 16; off < lanes; off <<= 1) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      mn[i] = least(mn[i], __shfl_xor(mn[i], off));
+      mx[i] = most(mx[i], __shfl_xor(mx[i], off));
+    }
   }
 }
 
-// Zero and scale of a row from its range, and its codes.  The zero is exact in
-// single precision; the scale's first guess (a product by 1 / (2^bits - 1)) is
-// off by at most one binary16 step and is set right by the definition itself,
-// scale * (2^bits - 1) >= max - zero, whose two sides are exact in double.
+// Zero and scale of a row from its range.  The zero is exact in single precision.  The scale is the least binary16 s with s *
+// (2^bits - 1) + zero >= max: the binary16 number at or next above the quotient, taken a little (2^-20) too
+// small so that it is never past s, and the one after it if the condition does not hold yet.  The condition is decided
+// exactly: the product has at most 19 bits, and its sum with zero is a pair of numbers, the rounded sum and its error.
 struct RowQuant {
-  float zero, inv;
-  uint32_t scale_bits, zero_bits;
+  float zero, inv, scale;
+  uint32_t word;  // scale, then zero
 };
 
-__device__ __forceinline__ uint32_t f16_down(uint32_t b) {
-  if (b & 0x8000) return b + 1;
-  return b == 0 ? 0x8001u : b - 1;
+// The sign of x - (a + b), exactly.
+__device__ __forceinline__ int compare_sum(float x, float a, float b) {
+  const float sum = a + b, back = sum - a, error = (a - (sum - back)) + (b - back);
+  const float over = x - sum;  // (its sign is exact)
+  return over > 0.0f ? 1 : over < 0.0f ? -1 : error < 0.0f ? 1 : error > 0.0f ? -1 : 0;
 }
 
 template <int BITS>
 __device__ __forceinline__ RowQuant row_quant(float mn, float mx) {
-  constexpr double kMost = (1 << BITS) - 1;
+  constexpr float kMost = float((1 << BITS) - 1);
   RowQuant q;
   mn += 0.0f;  // -0 counts as +0
-  q.zero_bits = f16_bits(mn);
-  if (f16_float(q.zero_bits) > mn) q.zero_bits = f16_down(q.zero_bits);
-  q.zero = f16_float(q.zero_bits);
-  const double span = static_cast<double>(mx) - static_cast<double>(q.zero);
-  uint32_t s = span > 0.0 ? f16_bits(static_cast<float>(span) * static_cast<float>(1.0 / kMost)) : 0;
-  if (static_cast<double>(f16_float(s)) * kMost < span) ++s;
-  else if (s && static_cast<double>(f16_float(s - 1)) * kMost >= span) --s;
-  q.scale_bits = s;
-  q.inv = s ? __builtin_amdgcn_rcpf(f16_float(s)) : 0.0f;
+  uint32_t z = f16_bits(mn);
+  if (f16_float(z) > mn) z = z & 0x8000 ? z + 1 : z == 0 ? 0x8001u : z - 1;
+  q.zero = f16_float(z);
+  const float low = (mx - q.zero) * ((1.0f - 0x1p-20f) / kMost);
+  uint32_t s = low > 0.0f ? f16_bits(low) : 0;
+  if (f16_float(s) < low) ++s;
+  if (compare_sum(mx, f16_float(s) * kMost, q.zero) > 0) ++s;
+  q.scale = f16_float(s);
+  q.inv = s ? __builtin_amdgcn_rcpf(q.scale) : 0.0f;
+  q.word = s | (z << 16);
   return q;
 }
 
-// Codes of N values (8 of 4 bits or 4 of 8 bits) in one word.  t is within
-// 6.1e-5 of the quotient (x - zero) / scale (roundings of 2^-24, 2^-23 and 2^-24
-// relative on at most 255), and the hardware's float to byte conversion rounds
-// it half to even; `near` is set where a t is within 1e-4 of a half-integer, where that cannot decide.
+// Codes of N values (8 of 4 bits or 4 of 8 bits) in one word.  t = (x - zero) * (1 / scale) is off the quotient by at most
+// 2.4e-7 of it (roundings of 2^-24, 2^-23 and 2^-24), is rounded half to even by adding 1.5 * 2^23, in whose low bits
+// the code then lies, and `far` keeps the largest distance of a t from its code: past 1/2 - kNear the rounding is in doubt.
+constexpr float kRound = 12582912.0f;
+template <int BITS>
+constexpr float kNear = BITS == 4 ? 5e-6f : 8e-5f;
+
 template <bool BF16, int BITS>
-__device__ __forceinline__ uint32_t row_codes(const u32x4& w, int first, const RowQuant& q, bool& near) {
+__device__ __forceinline__ uint32_t row_codes(const u32x4& w, int first, const RowQuant& q, float& far) {
   constexpr int N = 32 / BITS;
-  uint32_t lo = 0, hi = 0;
-  float dist = 1.0f;
+  uint32_t r[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    const float t = (value<BF16>(w, first + e) - q.zero) * q.inv;
-    if (BITS == 8 || !(e & 1))
-      lo = __builtin_amdgcn_cvt_pk_u8_f32(t, BITS == 8 ? e : e >> 1, lo);
-    else
-      hi = __builtin_amdgcn_cvt_pk_u8_f32(t, e >> 1, hi);
-    dist = __builtin_fminf(dist, __builtin_fabsf(__builtin_amdgcn_fractf(t) - 0.5f));
+    const float t = (value<BF16>(w, first + e) - q.zero) * q.inv, up = t + kRound;
+    far = __builtin_fmaxf(far, __builtin_fabsf(t - (up - kRound)));
+    r[e] = __float_as_uint(up);
   }
-  near |= dist < 1e-4f;
-  return BITS == 8 ? lo : lo | (hi << 4);
+  // Low bytes together; of 4-bit codes the even channels' and the odd ones', which go between.
+  auto bytes = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u),
+                                 0x05040100u);
+  };
+  if constexpr (BITS == 8) return bytes(r[0], r[1], r[2], r[3]);
+  else return bytes(r[0], r[2], r[4], r[6]) | (bytes(r[1], r[3], r[5], r[7]) << 4);
 }
 
 // The same codes with the rounding decided exactly: with b = floor(t), the code is b or b + 1 as x is below or above zero +
-// (b + 1/2) scale, and the even one where they are equal.  (b + 1/2) scale is exact in single precision (at most 20
-// bits), and so is its sum with zero as a pair of numbers, the rounded sum and its error.
+// (b + 1/2) scale, and the even one where they are equal.  (b + 1/2) scale is exact in single precision (at most 20 bits).
 template <bool BF16, int BITS>
 __device__ __forceinline__ uint32_t row_codes_exact(const u32x4& w, int first, const RowQuant& q) {
   constexpr int N = 32 / BITS;
-  const float scale = f16_float(q.scale_bits);
   uint32_t packed = 0;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    const float x = value<BF16>(w, first + e), b = __builtin_floorf((x - q.zero) * q.inv), h = (b + 0.5f) * scale;
-    const float sum = h + q.zero, back = sum - h, error = (h - (sum - back)) + (q.zero - back);
-    const float over = x - sum;  // (its sign is exact)
-    const bool above = over > 0.0f || (over == 0.0f && error < 0.0f), equal = over == 0.0f && error == 0.0f;
+    const float x = value<BF16>(w, first + e), b = __builtin_floorf((x - q.zero) * q.inv);
+    const int side = compare_sum(x, (b + 0.5f) * q.scale, q.zero);
     const int32_t low = static_cast<int32_t>(b);
-    packed |= static_cast<uint32_t>(low + ((above || (equal && (low & 1))) ? 1 : 0)) << (BITS * e);
+    packed |= static_cast<uint32_t>(low + (side > 0 || (side == 0 && (low & 1)) ? 1 : 0)) << (BITS * e);
   }
   return packed;
 }
 
-// A row's pieces (8 channels of K and of V) into the cache.
-template <bool BF16, int KB, int VB>
-__device__ __forceinline__ void put(const ServeArgs& a, const u32x4& k, const u32x4& v, const Place& at, int32_t head,
-                                    int32_t piece, int32_t lanes, bool on) {
-  if constexpr (KB == 16) {
-    if (!on) return;
-    const int64_t off = 2 * (head * a.D + 8 * piece);
-    *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(a.k_cache) + at.k + off) = k;
-    *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(a.v_cache) + at.v + off) = v;
-  } else {
-    float mn[2] = {__builtin_inff(), __builtin_inff()}, mx[2] = {-__builtin_inff(), -__builtin_inff()};
-    if (8 * piece < a.D) {
+// A row's pieces (8 channels of K and of V) as codes.
+template <bool BF16, int BITS>
+__device__ __forceinline__ void piece_codes(const u32x4& w, const RowQuant& q, uint32_t (&codes)[BITS / 4]) {
+  float far = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = value<BF16>(k, e), y = value<BF16>(v, e);
-        mn[0] = __builtin_fminf(mn[0], x);
-        mx[0] = __builtin_fmaxf(mx[0], x);
-        mn[1] = __builtin_fminf(mn[1], y);
-        mx[1] = __builtin_fmaxf(mx[1], y);
-      }
-    }
-    row_range(mn[0], mx[0], lanes);
-    row_range(mn[1], mx[1], lanes);
-    const RowQuant kq = row_quant<KB>(mn[0], mx[0]), vq = row_quant<VB>(mn[1], mx[1]);
-    constexpr int kKWords = KB / 4, kVWords = VB / 4;
-    uint32_t kc[kKWords], vc[kVWords];
-    bool near = false;
+  for (int i = 0; i < BITS / 4; ++i) codes[i] = row_codes<BF16, BITS>(w, 4 * i, q, far);
+  if (far > 0.5f - kNear<BITS>) {
 #pragma unroll
-    for (int i = 0; i < kKWords; ++i) kc[i] = row_codes<BF16, KB>(k, 4 * i, kq, near);
-#pragma unroll
-    for (int i = 0; i < kVWords; ++i) vc[i] = row_codes<BF16, VB>(v, 4 * i, vq, near);
-    if (near) {
-#pragma unroll
-      for (int i = 0; i < kKWords; ++i) kc[i] = kq.scale_bits ? row_codes_exact<BF16, KB>(k, 4 * i, kq) : 0;
-#pragma unroll
-      for (int i = 0; i < kVWords; ++i) vc[i] = vq.scale_bits ? row_codes_exact<BF16, VB>(v, 4 * i, vq) : 0;
-    }
-    if (!on) return;
-    uint8_t* to = a.codes + head * a.head_stride;
-    if constexpr (KB == 8)
-      *reinterpret_cast<u32x2*>(to + at.k + 8 * piece) = u32x2{kc[0], kc[kKWords - 1]};
-    else
-      *reinterpret_cast<uint32_t*>(to + at.k + 4 * piece) = kc[0];
-    if constexpr (VB == 8)
-      *reinterpret_cast<u32x2*>(to + at.v + 8 * piece) = u32x2{vc[0], vc[kVWords - 1]};
-    else
-      *reinterpret_cast<uint32_t*>(to + at.v + 4 * piece) = vc[0];
-    if (piece < 2) {
-      uint32_t* scales = a.scales + at.scale + ((int64_t(head) * 2 + piece) << a.log2P);
-      *scales = piece ? vq.scale_bits | (vq.zero_bits << 16) : kq.scale_bits | (kq.zero_bits << 16);
-    }
+    for (int i = 0; i < BITS / 4; ++i) codes[i] = row_codes_exact<BF16, BITS>(w, 4 * i, q);
   }
 }
 
@@ -295,53 +274,84 @@ template <bool BF16, int KB, int VB, bool WRITE>
 __global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, RowWork w) {
   __shared__ int32_t starts[kStartsInLds];
   __shared__ Place place[kMostTokens];
+  constexpr bool kCodes = KB != 16;
   const int32_t tokens = 1 << w.log2_tokens, lanes = 1 << w.log2_lanes;
   const int32_t i0 = int32_t(blockIdx.x) << w.log2_tokens;
   const int32_t n = tokens < a.num_tokens - i0 ? tokens : a.num_tokens - i0;
-  const int32_t piece = threadIdx.x & (lanes - 1);
-  const int32_t rows = a.H << w.log2_tokens, step = kThreads >> w.log2_lanes;
-  int32_t row = threadIdx.x >> w.log2_lanes;
-  auto off_of = [&](int32_t at) {
-    return int64_t(i0 + (at & (tokens - 1))) * r.token_stride + (at >> w.log2_tokens) * r.head_stride + 8 * piece;
-  };
-  auto mine = [&](int32_t at) { return at < rows && (at & (tokens - 1)) < n && 8 * piece < a.D; };
+  // A pass takes all of the workgroup's tokens and as many heads as there are groups of lanes for; a thread stays
+  // with its token.
+  const int32_t piece = threadIdx.x & (lanes - 1), group = threadIdx.x >> w.log2_lanes;
+  const int32_t t = group & (tokens - 1), head0 = group >> w.log2_tokens;
+  const int32_t heads = (kThreads >> w.log2_lanes) >> w.log2_tokens;
+  const bool mine = 8 * piece < a.D && t < n;
+  int64_t off = int64_t(i0 + t) * r.token_stride + head0 * r.head_stride + 8 * piece;
   u32x4 k{}, v{};
-  if (WRITE && mine(row)) {  // on their way while the places are found
-    k = *reinterpret_cast<const u32x4*>(r.k + off_of(row));
-    v = *reinterpret_cast<const u32x4*>(r.v + off_of(row));
+  if (WRITE && mine && head0 < a.H) {  // on their way while the places are found
+    k = *reinterpret_cast<const u32x4*>(r.k + off);
+    v = *reinterpret_cast<const u32x4*>(r.v + off);
   }
   find_places<KB, VB>(a, i0, n, starts, place);
-  // Every lane of a row's group runs the same passes, so the exchanges in put() are between live lanes.
-  for (; row < rows; row += step) {
-    const int32_t head = row >> w.log2_tokens, t = row & (tokens - 1);
-    const Place at = place[t < n ? t : 0];
-    const bool on = mine(row) && at.k >= 0;
+  const Place at = place[t < n ? t : 0];
+  const bool on = mine && at.k >= 0;
+  uint8_t* codes = a.codes + head0 * a.head_stride;
+  uint32_t* scales = a.scales + at.scale + ((int64_t(head0) * 2) << a.log2P);
+  char* k16 = reinterpret_cast<char*>(a.k_cache) + at.k + 2 * (head0 * a.D + 8 * piece);
+  char* v16 = reinterpret_cast<char*>(a.v_cache) + at.v + 2 * (head0 * a.D + 8 * piece);
+  // Every lane of a row's group runs the same passes, so the exchanges are between live lanes.
+  for (int32_t head = head0; head < a.H; head += heads) {
+    const int64_t next = off + heads * r.head_stride;
     if constexpr (WRITE) {
       const u32x4 k_now = k, v_now = v;
-      if (mine(row + step)) {
-        k = *reinterpret_cast<const u32x4*>(r.k + off_of(row + step));
-        v = *reinterpret_cast<const u32x4*>(r.v + off_of(row + step));
+      if (mine && head + heads < a.H) {
+        k = *reinterpret_cast<const u32x4*>(r.k + next);
+        v = *reinterpret_cast<const u32x4*>(r.v + next);
       }
-      put<BF16, KB, VB>(a, k_now, v_now, at, head, piece, lanes, on);
-    } else if (mine(row) && at.k != -2) {
-      if (on) {
-        if constexpr (KB == 16) {
-          const int64_t off = 2 * (head * a.D + 8 * piece);
-          k = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.k_cache) + at.k + off);
-          v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.v_cache) + at.v + off);
-        } else {
-          const uint8_t* from = a.codes + head * a.head_stride;
-          const uint32_t* scales = a.scales + at.scale + ((int64_t(head) * 2) << a.log2P);
-          const uint32_t ks = scales[0], vs = scales[int64_t(1) << a.log2P];
-          k = get<BF16, KB>(from + at.k, ks, piece);
-          v = get<BF16, VB>(from + at.v, vs, piece);
+      if constexpr (kCodes) {
+        float mn[2] = {__builtin_inff(), __builtin_inff()}, mx[2] = {-__builtin_inff(), -__builtin_inff()};
+        if (8 * piece < a.D) {
+          piece_range<BF16>(k_now, mn[0], mx[0]);
+          piece_range<BF16>(v_now, mn[1], mx[1]);
         }
-      } else {
-        k = v = u32x4{};
+        row_range(mn, mx, lanes);
+        const RowQuant kq = row_quant<KB>(mn[0], mx[0]), vq = row_quant<VB>(mn[1], mx[1]);
+        uint32_t kc[KB / 4], vc[VB / 4];
+        piece_codes<BF16, KB>(k_now, kq, kc);
+        piece_codes<BF16, VB>(v_now, vq, vc);
+        if (on) {
+          if constexpr (KB == 8)
+            *reinterpret_cast<u32x2*>(codes + at.k + 8 * piece) = u32x2{kc[0], kc[KB / 4 - 1]};
+          else
+            *reinterpret_cast<uint32_t*>(codes + at.k + 4 * piece) = kc[0];
+          if constexpr (VB == 8)
+            *reinterpret_cast<u32x2*>(codes + at.v + 8 * piece) = u32x2{vc[0], vc[VB / 4 - 1]};
+          else
+            *reinterpret_cast<uint32_t*>(codes + at.v + 4 * piece) = vc[0];
+          if (piece < 2) scales[int64_t(piece) << a.log2P] = piece ? vq.word : kq.word;
+        }
+      } else if (on) {
+        *reinterpret_cast<u32x4*>(k16) = k_now;
+        *reinterpret_cast<u32x4*>(v16) = v_now;
       }
-      *reinterpret_cast<u32x4*>(r.k + off_of(row)) = k;
-      *reinterpret_cast<u32x4*>(r.v + off_of(row)) = v;
+    } else if (mine && at.k != -2) {
+      k = v = u32x4{};
+      if (on) {
+        if constexpr (kCodes) {
+          const uint32_t ks = scales[0], vs = scales[int64_t(1) << a.log2P];
+          k = get<BF16, KB>(codes + at.k, ks, piece);
+          v = get<BF16, VB>(codes + at.v, vs, piece);
+        } else {
+          k = *reinterpret_cast<const u32x4*>(k16);
+          v = *reinterpret_cast<const u32x4*>(v16);
+        }
+      }
+      *reinterpret_cast<u32x4*>(r.k + off) = k;
+      *reinterpret_cast<u32x4*>(r.v + off) = v;
     }
+    off = next;
+    codes += heads * a.head_stride;
+    scales += (int64_t(heads) * 2) << a.log2P;
+    k16 += 2 * heads * a.D;
+    v16 += 2 * heads * a.D;
   }
 }
 
@@ -349,10 +359,10 @@ template <bool WRITE>
 pkv_status_t launch_rows(const ServeArgs& s, const RowArgs& r, hipStream_t stream) {
   RowWork w{0, 0};
   while ((8 << w.log2_lanes) < s.D) ++w.log2_lanes;
-  // Enough rows for one pass of a workgroup; more while that leaves 32 workgroups to a compute unit.
+  // Enough tokens for one pass of a workgroup; up to a pass of one head while that leaves four workgroups to a compute unit.
   const int32_t pass = kThreads >> w.log2_lanes;
-  while ((1 << w.log2_tokens) < kMostTokens &&
-         ((s.H << w.log2_tokens) < pass || (s.num_tokens >> w.log2_tokens) >= 8192))
+  while ((1 << w.log2_tokens) < pass &&
+         ((s.H << w.log2_tokens) < pass || (s.num_tokens >> w.log2_tokens) >= 2048))
     ++w.log2_tokens;
   const dim3 grid((uint32_t(s.num_tokens) + (1u << w.log2_tokens) - 1) >> w.log2_tokens);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, s, r, w); };
