@@ -1139,18 +1139,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
             sc.kz_[u] = m.scale[b][1][at];
           }
         }
-        // All of a phase's operands are asked for before its first instruction.
-        u32x4 k[2][kQkSteps], v[kChannels];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < kQkSteps; ++i)
-            k[u][i] = m.k[b][k_place(2 * p + u, i, c, x)];
         attend_tile<BF16, KB, VB, RT>(
-            a, mine, rows, c, t, there, sc, st, [&](int u, int i) { return k[u][i]; }, [&](int j) { return v[j]; },
+            a, mine, rows, c, t, there, sc, st, [&](int u, int i) { return m.k[b][k_place(2 * p + u, i, c, x)]; },
+            [&](int j) { return m.v[b][v_place(p, j, c, x)]; },
             [&] {
-#pragma unroll
-              for (int j = 0; j < kChannels; ++j) v[j] = m.v[b][v_place(p, j, c, x)];
               if constexpr (kCodes) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -1217,29 +1209,33 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
   }
 }
 
-// Joins the parts of a row, by a workgroup: D / 4 threads to a part's sums, the parts dealt to the groups of so many
-// threads; part i is at slot(i).
-template <typename Slot>
+// Joins the parts of a row, by GROUPS groups of D / 4 threads, each with every GROUPS-th part; part i is at slot(i).
+// (One group to a row needs no exchange; a workgroup of them takes as many rows as it has groups.)
+template <int GROUPS, typename Slot>
 __device__ __forceinline__ void join_parts(const ServeArgs& s, const AttendArgs& a, int32_t token, int32_t head,
                                            int32_t parts, Slot slot) {
-  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
-  __shared__ float wave_most[kWaves];
-  __shared__ f32x4 sums[kGroups][kLanes];
-  __shared__ float totals[kGroups];
+  constexpr int kLanes = D / 4;
+  static_assert(GROUPS == 1 || GROUPS * kLanes == kThreads, "a workgroup or a group");
   const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml);
   const f32x4* part = reinterpret_cast<const f32x4*>(a.part);
+  const int group = GROUPS == 1 ? 0 : threadIdx.x / kLanes, at = threadIdx.x % kLanes;
   float m = -kInf;
-  for (int i = threadIdx.x; i < parts; i += kThreads) m = __builtin_fmaxf(m, ml[slot(i)][0]);
-  for (int off = 1; off < 64; off <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
-  if ((threadIdx.x & 63) == 0) wave_most[threadIdx.x >> 6] = m;
-  __syncthreads();
+  if constexpr (GROUPS == 1) {
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) m = __builtin_fmaxf(m, ml[slot(i)][0]);
+  } else {
+    __shared__ float wave_most[kWaves];
+    for (int i = threadIdx.x; i < parts; i += kThreads) m = __builtin_fmaxf(m, ml[slot(i)][0]);
+    for (int off = 1; off < 64; off <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
+    if ((threadIdx.x & 63) == 0) wave_most[threadIdx.x >> 6] = m;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) m = __builtin_fmaxf(m, wave_most[w]);
-  const int group = threadIdx.x / kLanes, at = threadIdx.x % kLanes;
+    for (int w = 0; w < kWaves; ++w) m = __builtin_fmaxf(m, wave_most[w]);
+  }
   float l = 0.0f;
   f32x4 sum{};
 #pragma unroll 4
-  for (int i = group; i < parts; i += kGroups) {
+  for (int i = group; i < parts; i += GROUPS) {
     const int64_t from = slot(i);
     const f32x2 w = ml[from];
     const f32x4 p = part[from * kLanes + at];
@@ -1249,16 +1245,20 @@ __device__ __forceinline__ void join_parts(const ServeArgs& s, const AttendArgs&
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += w[1] == 0.0f ? 0.0f : p[e] * scale;
   }
-  sums[group][at] = sum;
-  if (at == 0) totals[group] = l;
-  __syncthreads();
-  if (group) return;
-  l = 0.0f;
-  sum = f32x4{};
+  if constexpr (GROUPS > 1) {
+    __shared__ f32x4 sums[GROUPS][kLanes];
+    __shared__ float totals[GROUPS];
+    sums[group][at] = sum;
+    if (at == 0) totals[group] = l;
+    __syncthreads();
+    if (group) return;
+    l = 0.0f;
+    sum = f32x4{};
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) {
-    l += totals[i];
-    sum += sums[i][at];
+    for (int i = 0; i < GROUPS; ++i) {
+      l += totals[i];
+      sum += sums[i][at];
+    }
   }
   const float inv = inverse(l);
   uint16_t* to = a.out + token * a.out_token_stride + head * a.out_head_stride + 4 * at;
@@ -1268,13 +1268,20 @@ __device__ __forceinline__ void join_parts(const ServeArgs& s, const AttendArgs&
   if (a.lse && at == 0) a.lse[int64_t(token) * a.Hq + head] = lse_of(m, l);
 }
 
-// The splits of each row of a call of many rows, one workgroup to a row.
+constexpr int kJoinGroups = kThreads / (D / 4);
+constexpr int kFewSplits = 16;
+
+// The splits of each row of a call of many rows: a row to a workgroup, or, where there are few splits (a workgroup to a
+// row then costs 1 ns of launching each and does little), to a group of its threads.
+template <int GROUPS>
 __global__ __launch_bounds__(kThreads) void join_splits_kernel(ServeArgs s, AttendArgs a) {
-  const int32_t token = int32_t(blockIdx.x / uint32_t(a.Hq)), head = int32_t(blockIdx.x % uint32_t(a.Hq));
+  const uint32_t row = GROUPS == 1 ? blockIdx.x * kJoinGroups + threadIdx.x / (D / 4) : blockIdx.x;
+  const int32_t token = int32_t(row / uint32_t(a.Hq)), head = int32_t(row % uint32_t(a.Hq));
   // Rows of no sequence have no parts.
   if (token < scalar_entry(s.token_start, 0) || token >= scalar_entry(s.token_start, s.num_seqs)) return;
-  const int64_t first = int64_t(blockIdx.x) * a.splits;
-  join_parts(s, a, token, head, a.splits, [&](int i) { return first + i; });
+  if (token >= s.num_tokens) return;
+  const int64_t first = int64_t(row) * a.splits;
+  join_parts<GROUPS>(s, a, token, head, a.splits, [&](int i) { return first + i; });
 }
 
 // The pieces of a sequence of few rows, one workgroup to a row; a sequence of one piece is done.
@@ -1292,7 +1299,7 @@ __global__ __launch_bounds__(kThreads) void join_pieces_kernel(ServeArgs s, Atte
   if (pieces == 1) return;
   const int32_t start = scalar_entry(s.token_start, at.seq);
   const int32_t row = (token - (start < 0 ? 0 : start)) * a.group + head % a.group;
-  join_parts(s, a, token, head, pieces, [&](int i) {
+  join_parts<kJoinGroups>(s, a, token, head, pieces, [&](int i) {
     return (int64_t(at.before + i) * s.H + head / a.group) * a.part_rows + row;
   });
 }
@@ -1334,8 +1341,11 @@ pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const 
   const dim3 rows(uint32_t(s.num_tokens) * uint32_t(a.Hq));
   if (a.pieces)
     hipLaunchKernelGGL(join_pieces_kernel, rows, dim3(kThreads), 0, stream, s, a);
+  else if (a.splits > kFewSplits)
+    hipLaunchKernelGGL(join_splits_kernel<kJoinGroups>, rows, dim3(kThreads), 0, stream, s, a);
   else if (a.splits > 1)
-    hipLaunchKernelGGL(join_splits_kernel, rows, dim3(kThreads), 0, stream, s, a);
+    hipLaunchKernelGGL(join_splits_kernel<1>, dim3((rows.x + kJoinGroups - 1) / kJoinGroups), dim3(kThreads), 0, stream, s,
+                       a);
   if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
   return PKV_OK;
 }
