@@ -426,10 +426,9 @@ typedef struct {
  * [token_start[s], token_start[s + 1]) of the call's row buffers belong to
  * sequence s.  Row i sits at logical position positions[i] of its sequence, or,
  * with positions == NULL, the rows are the last of the kv_lens[s] tokens; a
- * negative position has no row.  Rows of no sequence are neither read nor
- * written.  Arrays are device memory, 4-byte aligned; num_seqs, num_tokens >= 0,
- * num_tokens * num_q_heads < 2^31, pages_per_seq >= 1,
- * pages_per_seq * page_size <= 2^30. */
+ * negative position has no row.  Rows of no sequence take no part and are not
+ * written.  Arrays are device memory, 4-byte aligned; num_seqs and num_tokens
+ * from 0 to 2^24 - 1, pages_per_seq >= 1, pages_per_seq * page_size <= 2^30. */
 typedef struct {
   int32_t num_seqs;
   int32_t num_tokens;
@@ -484,6 +483,9 @@ pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* c
  * cache holds past kv_lens, on pages that are not there, before every row's window and behind
  * the sinks (NaN, infinities) does not matter; what lies between places that
  * rows of a sequence see should be finite.
+ * num_tokens * num_q_heads < 2^31, and < 2^24 where a workspace is needed; num_seqs *
+ * num_kv_heads * ceil(max_tokens * (num_q_heads / num_kv_heads) / 64) < 2^23 always
+ * suffices for the launch; a page of 16-bit K and V, or of codes, below 4 GiB.
  * At most two kernels on `hip_stream`.  Errors as pkv_cache_append. */
 typedef struct {
   int32_t num_q_heads; /* a multiple of num_kv_heads */

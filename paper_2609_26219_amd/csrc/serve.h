@@ -72,6 +72,9 @@ struct AttendLaunch {
   uint64_t workspace_bytes; // both
 };
 
+// A launch has fewer than 2^32 threads, in workgroups of 256.
+constexpr int64_t kMostGroups = int64_t(1) << 24;
+
 constexpr int kRowTile = 16;   // rows (token, query head of one KV head) of a matrix instruction
 constexpr int kTokenTile = 32; // cached tokens a wave takes at a time
 

@@ -444,7 +444,6 @@ pkv_status_t pkv_attention(const pkv_model_t* model, const pkv_paged_cache_t* ca
   if (st == PKV_OK) st = pkv::attend_args(s, attention, true, &a);
   if (st != PKV_OK || s.num_seqs == 0 || s.num_tokens == 0) return st;
   const pkv::AttendLaunch l = pkv::attend_launch(s, a);
-  if (l.groups >= (int64_t(1) << 31)) return PKV_ERR_INVALID_ARGUMENT;
   const pkv::OnDevice here;
   if (!here.ok) return PKV_ERR_DEVICE;
   if (!here.has(s) || !here.has(a.q) || !here.has(a.out) || !here.has(a.lse) || !here.has(a.part))

@@ -38,6 +38,7 @@ pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache
   if (cache->tag < PKV_TAG_FP16 || cache->tag > PKV_TAG_K4V4) return PKV_ERR_BAD_TAG;
   if (cache->layer < 0 || cache->layer >= m.num_layers) return PKV_ERR_INVALID_ARGUMENT;
   const pkv_batch_t& b = *batch;
+  if (b.num_seqs >= kMostGroups || b.num_tokens >= kMostGroups) return PKV_ERR_INVALID_ARGUMENT;
   if (b.num_seqs < 0 || b.num_tokens < 0 || b.max_tokens < 0 || b.pages_per_seq < 1 || b.max_kv_len < 0)
     return PKV_ERR_INVALID_ARGUMENT;
   const int64_t reach = int64_t(b.pages_per_seq) * m.page_size;
@@ -110,6 +111,9 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
   if (a->num_q_heads < 1 || a->num_q_heads % s.H || a->window < 0 || a->sinks < 0) return PKV_ERR_INVALID_ARGUMENT;
   if (!(isfinite(a->scale) && a->scale > 0.0f)) return PKV_ERR_INVALID_ARGUMENT;
   if (int64_t(s.num_tokens) * a->num_q_heads >= (int64_t(1) << 31)) return PKV_ERR_INVALID_ARGUMENT;
+  // The kernels multiply page numbers by 32-bit strides.
+  const int64_t most = (int64_t(1) << 32) - 1;
+  if (s.page_stride * (s.tag == PKV_TAG_FP16 ? 2 : 1) > most || s.scale_stride > most) return PKV_ERR_INVALID_ARGUMENT;
   AttendArgs r{};
   r.Hq = a->num_q_heads;
   r.group = r.Hq / s.H;
@@ -131,6 +135,8 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
     r.out_head_stride = a->out_head_stride;
   }
   const AttendLaunch l = attend_launch(s, r);
+  if (l.groups >= kMostGroups) return PKV_ERR_INVALID_ARGUMENT;
+  if (l.workspace_bytes && int64_t(s.num_tokens) * r.Hq >= kMostGroups) return PKV_ERR_INVALID_ARGUMENT;
   r.tiles = l.tiles;
   r.row_tiles = l.row_tiles;
   r.splits = l.splits;

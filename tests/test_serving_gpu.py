@@ -410,3 +410,50 @@ def test_refusals_on_the_device(torch):
         serving.attention(cache, batch, q.float())
     with pytest.raises(ValueError):
         serving.append(cache, batch, q, q)
+
+
+def _lengths(n, low, high, also=()):
+    rng = np.random.default_rng(n)
+    return (*also, *(int(x) for x in rng.integers(low, high, n)))
+
+
+SPREAD = [
+    # tag, dtype, H, group, D, P, lens, new, scattered, window, sinks: more sequences than a wave has lanes, cut into pieces and whole
+    (K4V4, BF16, 2, 4, 64, 16, _lengths(150, 0, 60, (900,)), (1,), False, 0, 0),
+    (FP16, HALF, 1, 2, 64, 16, _lengths(129, 0, 40, (700, 0, 0, 501)), (1, 2, 1), False, 0, 0),
+    (K8V4, HALF, 1, 1, 64, 8, _lengths(70, 1, 300), (1,), False, 0, 0),
+    (K4V4, BF16, 2, 7, 128, 16, (3000, 11, 2047), (3, 1, 4), False, 0, 0),
+    (K8V8, BF16, 3, 5, 128, 16, (1700,), (1,), False, 0, 0),
+    (FP16, BF16, 2, 3, 128, 32, (3000, 400), (2,), False, 1500, 40),
+    (K4V4, HALF, 1, 8, 256, 16, (1200, 33), (2, 1), False, 0, 0),
+    (FP16, HALF, 1, 2, 128, 16, (2000,), (4,), True, 700, 9),
+    # many rows whose tokens are split, between two to 16 workgroups and more
+    (FP16, BF16, 1, 1, 128, 64, (20001,), (40,), False, 0, 0),
+    (K4V4, HALF, 1, 2, 128, 32, (2500, 300), (33, 20), False, 0, 0),
+    (K8V4, BF16, 2, 5, 64, 16, (5003,), (9,), False, 0, 0),
+    (FP16, HALF, 1, 2, 256, 16, (1203, 0), (30,), False, 0, 0),
+    (K8V8, HALF, 1, 4, 256, 16, (9001,), (10,), True, 0, 0),
+]
+
+
+@pytest.mark.parametrize("tag,dtype,H,group,D,P,lens,new,scattered,window,sinks", SPREAD)
+def test_attention_spread_over_the_gpu(torch, tag, dtype, H, group, D, P, lens, new, scattered, window, sinks):
+    test_attention(torch, tag, dtype, H, group, D, P, lens, new, scattered, window, sinks, 1)
+
+
+@pytest.mark.parametrize("tag", [K4V4, FP16])
+def test_append_and_read_of_more_sequences_than_are_searched_in_lds(torch, tag):
+    from oracle import serving as os_
+    from paper_2609_26219_amd import serving
+
+    case = Case(61, tag, BF16, 1, 1, 64, 4, _lengths(1100, 0, 6), (1, 2, 1))
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    serving.append(cache, batch, _up(torch, case.k, case), _up(torch, case.v, case))
+    want = case.copy_of_cache()
+    os_.append(want, tag, 4, case.where(), case.k, case.v, BF16)
+    got, _ = _state(torch, cache, case)
+    for g, w in zip(got, want["kv"] if tag == FP16 else [want["codes"], want["scales"]]):
+        assert np.array_equal(g.view(w.dtype), w)
+    case.cache = want
+    for which, t in enumerate(serving.read(cache, batch)):
+        check_read(case, _down(t), which)

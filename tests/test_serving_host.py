@@ -165,3 +165,22 @@ def test_oracle_rows_by_hand():
     assert cache["scales"][0, 0, 0, 1, 0] == 0x3C00 and cache["scales"][0, 0, 0, 0, 0] == 0
     x, free, mid = os_.row(cache, 3, 2, 0, 0, 0, 1, 0)
     assert list(x) == list(range(16)) and list(free) == [abs(i - 8) for i in range(16)] and mid == 8.0
+
+
+def test_sizes_past_a_launch_are_refused():
+    """2^24 sequences, rows or workgroups, and pages whose stride passes 32 bits."""
+    for which in ("attention", "append", "read"):
+        assert _call(which=which, batch=dict(num_seqs=1 << 24)) == BAD
+        assert _call(which=which, batch=dict(num_tokens=1 << 24)) == BAD
+    assert _call(batch=dict(num_tokens=1 << 21, max_tokens=1, pages_per_seq=1000)) == BAD  # 2^24 rows to join
+    assert _call(batch=dict(num_seqs=1 << 20, num_tokens=1 << 20, max_tokens=1024)) == BAD  # 2^27 workgroups
+    s = _shape(num_layers=1, num_kv_heads=8, head_dim=128, page_size=1 << 20, pool_pages=2)
+    m, b, a = pb.make_model(s), pb.PkvBatch(num_seqs=1, num_tokens=1, pages_per_seq=1), pb.PkvAttention(num_q_heads=8, scale=1.0)
+    for paired, ok in ((0, True), (1, False)):  # 2 GiB of keys; keys and values on one page
+        m.kv_layout = paired
+        if ok:
+            pb.pkv_attention_workspace(m, pb.PkvPagedCache(tag=0), b, a)
+        else:
+            with pytest.raises(pb.PkvError):
+                pb.pkv_attention_workspace(m, pb.PkvPagedCache(tag=0), b, a)
+        pb.pkv_attention_workspace(m, pb.PkvPagedCache(tag=3), b, a)
