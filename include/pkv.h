@@ -477,12 +477,13 @@ pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* c
  *     NULL), 16-byte aligned, contents of no matter before and after; calls
  *     that may overlap need one each.
  * Sums, maxima and lse are single precision.  Quantised caches: q.code sums are
- * exact products (codes and queries are exact in the matrix instructions'
- * binary16 operands, queries scaled by a power of two), probabilities are rounded
- * to binary16; 16-bit caches: probabilities are rounded to out_dtype.  What a
- * cache holds past kv_lens, on pages that are not there, before every row's window and behind
- * the sinks (NaN, infinities) does not matter; what lies between places that
- * rows of a sequence see should be finite.
+ * of exact products (codes and queries are binary16 operands of the matrix
+ * instructions, queries scaled by a power of two); a probability times its token's
+ * scale is rounded to binary16 for BF16 results and to the sum of two
+ * binary16 numbers for FP16 ones.  16-bit caches: probabilities are rounded to
+ * out_dtype.  What a cache holds past kv_lens, on pages that are not there, before
+ * every row's window and behind the sinks (NaN, infinities) does not matter; what
+ * lies between places that rows of a sequence see should be finite.
  * num_tokens * num_q_heads < 2^31, and < 2^24 where a workspace is needed; num_seqs *
  * num_kv_heads * ceil(max_tokens * (num_q_heads / num_kv_heads) / 64) < 2^23 always
  * suffices for the launch; a page of 16-bit K and V, or of codes, below 4 GiB.

@@ -30,7 +30,10 @@
 //   q . k_t = s_t (q . codes_t) + z'_t sum(q),
 //   sum_t p_t v_t = sum_t (p_t s_t) codes_t + sum_t p_t z'_t,
 // so the one rounding on the way is p_t s_t to binary16 (scaled by a power of
-// two that keeps the largest near 2^14, so that small scales lose nothing).
+// two that keeps the largest near 2^14, so that small scales lose nothing).  Where a row's outliers put mid-code far
+// from its other channels, that rounding costs more than a binary16 result's own (4.5e-4 of a result in all, 2.0e-4
+// without it) and is lost in a bfloat16 one's (1.6e-3): for binary16 results p_t s_t goes in as two binary16 numbers, the
+// second what the first leaves.
 // Queries go in as binary16 too, each row scaled by a power of two.  16-bit caches use the
 // matrix instructions of their own type, p_t rounded to it.
 #include <hip/hip_runtime.h>
@@ -389,6 +392,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
                                             Value value, After after_keys, Hide hide) {
   constexpr bool kCodes = KB != 16;
   constexpr bool kHalf = kCodes || !BF16;  // operands in binary16
+  constexpr bool kFine = kCodes && !BF16;
   const bool all = t0 + kTokenTile - 1 <= span.hi_least && (span.lo_most < t0 || t0 + kTokenTile <= a.sinks) &&
                    __all(there == 0xFFu);
   auto mfma = [](const u32x4& x, const u32x4& y, const f32x4& z) {
@@ -484,7 +488,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     }
   }
   // The probabilities and their sum.
-  u32x4 pt[RT];
+  u32x4 pt[RT], rest[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const float base = st.ref[r] == -kInf ? 0.0f : -st.ref[r];
@@ -503,14 +507,20 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        pt[r][2 * u + i] = kHalf ? pack_f16(pr[u][2 * i], pr[u][2 * i + 1]) : pack_bf16(pr[u][2 * i], pr[u][2 * i + 1]);
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t w = kHalf ? pack_f16(pr[u][2 * i], pr[u][2 * i + 1]) : pack_bf16(pr[u][2 * i], pr[u][2 * i + 1]);
+        pt[r][2 * u + i] = w;
+        if constexpr (kFine) rest[r][2 * u + i] = pack_f16(pr[u][2 * i] - f16_float(w), pr[u][2 * i + 1] - f16_float(w >> 16));
+      }
   }
 #pragma unroll
   for (int j = 0; j < kChannels; ++j) {
     const u32x4 v = value(j);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) st.o[r][j] = mfma(v, pt[r], st.o[r][j]);
+    for (int r = 0; r < RT; ++r) {
+      st.o[r][j] = mfma(v, pt[r], st.o[r][j]);
+      if constexpr (kFine) st.o[r][j] = mfma(v, rest[r], st.o[r][j]);
+    }
   }
 }
 
@@ -1319,9 +1329,9 @@ pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const 
       case PKV_TAG_FP16:
         s.bf16 ? go(attend_few_kernel<true, 16, 16, kWhole, kTiles>) : go(attend_few_kernel<false, 16, 16, kWhole, kTiles>);
         break;
-      case PKV_TAG_K8V8: go(attend_few_kernel<false, 8, 8, kWhole, kTiles>); break;
-      case PKV_TAG_K8V4: go(attend_few_kernel<false, 8, 4, kWhole, kTiles>); break;
-      default: go(attend_few_kernel<false, 4, 4, kWhole, kTiles>); break;
+      case PKV_TAG_K8V8: s.bf16 ? go(attend_few_kernel<true, 8, 8, kWhole, kTiles>) : go(attend_few_kernel<false, 8, 8, kWhole, kTiles>); break;
+      case PKV_TAG_K8V4: s.bf16 ? go(attend_few_kernel<true, 8, 4, kWhole, kTiles>) : go(attend_few_kernel<false, 8, 4, kWhole, kTiles>); break;
+      default: s.bf16 ? go(attend_few_kernel<true, 4, 4, kWhole, kTiles>) : go(attend_few_kernel<false, 4, 4, kWhole, kTiles>); break;
     }
   };
   auto few_of = [&](auto whole) {
@@ -1330,9 +1340,9 @@ pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const 
   if (a.tiles > few_tiles(D)) {
     switch (s.tag) {
       case PKV_TAG_FP16: s.bf16 ? go(attend_many_kernel<true, 16, 16>) : go(attend_many_kernel<false, 16, 16>); break;
-      case PKV_TAG_K8V8: go(attend_many_kernel<false, 8, 8>); break;
-      case PKV_TAG_K8V4: go(attend_many_kernel<false, 8, 4>); break;
-      default: go(attend_many_kernel<false, 4, 4>); break;
+      case PKV_TAG_K8V8: s.bf16 ? go(attend_many_kernel<true, 8, 8>) : go(attend_many_kernel<false, 8, 8>); break;
+      case PKV_TAG_K8V4: s.bf16 ? go(attend_many_kernel<true, 8, 4>) : go(attend_many_kernel<false, 8, 4>); break;
+      default: s.bf16 ? go(attend_many_kernel<true, 4, 4>) : go(attend_many_kernel<false, 4, 4>); break;
     }
   } else {
     s.log2P >= 4 ? few_of(std::true_type{}) : few_of(std::false_type{});
