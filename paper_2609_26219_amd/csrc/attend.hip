@@ -789,10 +789,12 @@ struct FewLds {
 // Tiles [from, upto) of a sequence and head, into `out` and `lse` if they are all of them, else as part `part_slot`.
 template <bool BF16, int KB, int VB, bool WHOLE, int RT>
 __device__ __forceinline__ void few_piece(const ServeArgs& s, const AttendArgs& a, const Group& g, int32_t from,
-                                            int32_t upto, int64_t part_slot, const Magic& code, FewLds<RT>& m) {
+                                          int32_t upto, int64_t part_slot, const Magic& code, FewLds<RT>& m) {
   constexpr bool kCodes = KB != 16;
   const int lane = threadIdx.x & 63, c = lane >> 4, x = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t row0 = g.tile * (kRowTile * RT);
+  if (row0 >= g.count * a.group) return;  // the whole workgroup
   const Span looks = few_span(s, a, g);
   const Source f = source_of<KB>(s, g.seq, g.head);
   // The wave's tiles are `from` + wave + kWaves n.  Their pages are looked up 32 tiles at a time, a half of a tile to
@@ -823,7 +825,7 @@ __device__ __forceinline__ void few_piece(const ServeArgs& s, const AttendArgs& 
   }
   Rows<RT> rows;
   Span span;
-  load_rows<KB, RT>(s, a, g, 0, x, [&](int i) { return k_first<KB>(i, c); }, rows, span);
+  load_rows<KB, RT>(s, a, g, uint32_t(row0), x, [&](int i) { return k_first<KB>(i, c); }, rows, span);
   Running<RT> st;
   begin(st);
   if (count > 0) {
@@ -896,7 +898,7 @@ __device__ __forceinline__ void few_piece(const ServeArgs& s, const AttendArgs& 
     __syncthreads();
     constexpr int kPerRow = kThreads / kRowTile, kPer = D / kPerRow;  // 16 threads to a row
     const int y = threadIdx.x / kPerRow, at = (threadIdx.x % kPerRow) * kPer;
-    const uint32_t row = kRowTile * r + y;
+    const uint32_t row = row0 + kRowTile * r + y;
     const int32_t token = int32_t(row / uint32_t(a.group));
     if (token >= g.count) continue;
     const int32_t out_head = g.head * a.group + int32_t(row % uint32_t(a.group));
@@ -940,10 +942,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, At
   __shared__ __attribute__((aligned(16))) FewLds<RT> m;
   const int lane = threadIdx.x & 63;
   const Magic code = magic();
-  const uint32_t piece = blockIdx.x / uint32_t(s.H);
-  if (a.pieces == 0) {  // a sequence to a workgroup and head
+  uint32_t piece = blockIdx.x / uint32_t(s.H);
+  const int32_t head = int32_t(blockIdx.x % uint32_t(s.H)), tile = int32_t(piece % uint32_t(a.row_tiles));
+  piece /= uint32_t(a.row_tiles);
+  if (a.pieces == 0) {  // a sequence to a workgroup, head and row tile
     Group g = group_of_sequence(s, int32_t(piece));
-    g.head = int32_t(blockIdx.x % uint32_t(s.H));
+    g.head = head;
+    g.tile = tile;
     if (g.count > 0) few_piece<BF16, KB, VB, WHOLE, RT>(s, a, g, 0, few_span(s, a, g).tiles, -1, code, m);
     return;
   }
@@ -953,11 +958,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(ServeArgs s, At
   });
   if (at.seq < 0) return;
   Group g = group_of_sequence(s, at.seq);
-  g.head = int32_t(blockIdx.x % uint32_t(s.H));
+  g.head = head;
+  g.tile = tile;
   const int32_t pieces = pieces_of(at.tiles, per), share = (at.tiles + pieces - 1) / pieces;
   const int32_t from = (int32_t(piece) - at.before) * share;
   few_piece<BF16, KB, VB, WHOLE, RT>(s, a, g, from, from + share < at.tiles ? from + share : at.tiles,
-                                     pieces == 1 ? -1 : int64_t(blockIdx.x), code, m);
+                                     pieces == 1 ? -1 : int64_t(piece) * s.H + head, code, m);
 }
 
 // Many rows: each wave has 32 of its own (16 at 256 channels), and the workgroup's four share the cache through LDS.  A tile of
@@ -1280,6 +1286,7 @@ __device__ __forceinline__ void join_parts(const ServeArgs& s, const AttendArgs&
 
 constexpr int kJoinGroups = kThreads / (D / 4);
 constexpr int kFewSplits = 16;
+constexpr int kManyJoins = 1024;
 
 // The splits of each row of a call of many rows: a row to a workgroup, or, where there are few splits (a workgroup to a
 // row then costs 1 ns of launching each and does little), to a group of its threads.
@@ -1294,10 +1301,15 @@ __global__ __launch_bounds__(kThreads) void join_splits_kernel(ServeArgs s, Atte
   join_parts<GROUPS>(s, a, token, head, a.splits, [&](int i) { return first + i; });
 }
 
-// The pieces of a sequence of few rows, one workgroup to a row; a sequence of one piece is done.
+// The pieces of a sequence of few rows, a row to a workgroup or, where there are many rows, to a group of its threads (of
+// one token's heads); a sequence of one piece is done.
+template <int GROUPS>
 __global__ __launch_bounds__(kThreads) void join_pieces_kernel(ServeArgs s, AttendArgs a) {
   const int lane = threadIdx.x & 63;
-  const int32_t token = int32_t(blockIdx.x / uint32_t(a.Hq)), head = int32_t(blockIdx.x % uint32_t(a.Hq));
+  constexpr int kHeads = GROUPS == 1 ? kJoinGroups : 1;
+  const uint32_t shares = (uint32_t(a.Hq) + kHeads - 1) / kHeads;
+  const int32_t token = int32_t(blockIdx.x / shares);
+  const int32_t head = int32_t(blockIdx.x % shares) * kHeads + (GROUPS == 1 ? threadIdx.x / (D / 4) : 0);
   const int32_t mine = tiles_of_sequence(s, a, lane), per = piece_tiles(s, a, lane, mine);
   const Found at = find_sequence(s, a, lane, mine, per, [&](int32_t seq, int32_t, int32_t own) {
     if (own == 0) return false;
@@ -1306,10 +1318,10 @@ __global__ __launch_bounds__(kThreads) void join_pieces_kernel(ServeArgs s, Atte
   });
   if (at.seq < 0) return;
   const int32_t pieces = pieces_of(at.tiles, per);
-  if (pieces == 1) return;
+  if (pieces == 1 || head >= a.Hq) return;
   const int32_t start = scalar_entry(s.token_start, at.seq);
   const int32_t row = (token - (start < 0 ? 0 : start)) * a.group + head % a.group;
-  join_parts<kJoinGroups>(s, a, token, head, pieces, [&](int i) {
+  join_parts<GROUPS>(s, a, token, head, pieces, [&](int i) {
     return (int64_t(at.before + i) * s.H + head / a.group) * a.part_rows + row;
   });
 }
@@ -1349,8 +1361,11 @@ pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const 
   }
   if (hipGetLastError() != hipSuccess) return PKV_ERR_DEVICE;
   const dim3 rows(uint32_t(s.num_tokens) * uint32_t(a.Hq));
-  if (a.pieces)
-    hipLaunchKernelGGL(join_pieces_kernel, rows, dim3(kThreads), 0, stream, s, a);
+  if (a.pieces && int32_t(rows.x) >= kManyJoins && a.pieces <= int64_t(kFewSplits) * s.num_seqs)
+    hipLaunchKernelGGL(join_pieces_kernel<1>, dim3(uint32_t(s.num_tokens) * ((uint32_t(a.Hq) + kJoinGroups - 1) / kJoinGroups)),
+                       dim3(kThreads), 0, stream, s, a);
+  else if (a.pieces)
+    hipLaunchKernelGGL(join_pieces_kernel<kJoinGroups>, rows, dim3(kThreads), 0, stream, s, a);
   else if (a.splits > kFewSplits)
     hipLaunchKernelGGL(join_splits_kernel<kJoinGroups>, rows, dim3(kThreads), 0, stream, s, a);
   else if (a.splits > 1)

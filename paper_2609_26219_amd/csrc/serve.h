@@ -78,14 +78,21 @@ constexpr int64_t kMostGroups = int64_t(1) << 24;
 constexpr int kRowTile = 16;   // rows (token, query head of one KV head) of a matrix instruction
 constexpr int kTokenTile = 32; // cached tokens a wave takes at a time
 
-// Up to few_tiles row tiles are shared by a workgroup's waves, which deal the tokens among themselves; more rows are
-// dealt to them, many_tiles row tiles to a workgroup, and the tokens shared: kManyElems keys and as many values at a
-// time.  (A wave's queries and sums take 6 registers a row of 128 channels: two row tiles leave room for two waves a SIMD.)
+// Of few rows, up to few_tiles row tiles are shared by a workgroup's waves, which deal the tokens among themselves; many
+// rows are dealt to them, many_tiles row tiles to a workgroup, and the tokens shared: kManyElems keys and as many values
+// at a time.  (A wave's queries and sums take 6 registers a row of 128 channels: two row tiles leave room for two waves a SIMD.)
 constexpr int few_tiles(int head_dim) { return head_dim > 128 ? 1 : 2; }
 constexpr int many_tiles(int head_dim) { return 4 * few_tiles(head_dim); }
 constexpr int kManyElems = 8192;
-// Sequences of no more tiles are not cut: no second kernel.
-constexpr int kWholeTiles = 12;
+// Rows of a sequence and KV head, in workgroups' shares of few rows, above which they are many.  32 ragged sequences of up
+// to 16384 tokens, 8 heads of 128, 4 bits, us with few | many: 32 rows 115 | 270, 64 rows 207 | 311, 96 rows 289 | 327, and
+// 128 rows would be four shares of 97.  16-bit caches, 64 rows: 334 | 332.
+constexpr int few_shares(int key_bits) { return key_bits == 16 ? 1 : 3; }
+// Sequences of few rows and no more tiles of tokens are not cut, which saves the second kernel: 8 heads, a sequence
+// of 700 tokens 11.6 us against 9.6 + 4.4, of 1500 tokens 17.0 against 9.4 + 4.4.  Where the sequences alone give a
+// compute unit its workgroup, up to kWholeTilesOfMany: 32 of 2000 tokens 25.3 against 23.6 + 6.6.
+constexpr int kWholeTiles = 28;
+constexpr int kWholeTilesOfMany = 64;
 
 // Host checks that need no GPU; they fill the arguments.
 pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,

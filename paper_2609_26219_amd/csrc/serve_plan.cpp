@@ -155,7 +155,7 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
 AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   AttendLaunch l{};
   const int64_t rows = int64_t(s.max_tokens) * a.group;
-  const bool many = rows > kRowTile * few_tiles(s.D);
+  const bool many = rows > few_shares(kKeyBits[s.tag]) * kRowTile * few_tiles(s.D);
   l.tiles = many ? many_tiles(s.D) : rows <= kRowTile ? 1 : few_tiles(s.D);
   l.row_tiles = int32_t((rows + kRowTile * l.tiles - 1) / (kRowTile * l.tiles));
   l.part_rows = int32_t(rows);
@@ -173,19 +173,19 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
     if (base > 0) l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(6 * 256 / base, tiles / l.chunk)));
     l.groups = base * l.splits;
     if (l.splits > 1) parts = uint64_t(s.num_tokens) * a.Hq * l.splits;
-  } else if (tiles <= kWholeTiles) {
+  } else if (tiles <= (base >= 256 ? kWholeTilesOfMany : kWholeTiles)) {
     l.groups = base;
   } else {
     // As many workgroups as run at once, of two tiles a wave at least; where the sequences alone are more than half of
     // that, two rounds of them and half as many again as there are sequences.
-    const int64_t at_once = 256 * (s.D > 128 || l.tiles > 1 ? 2 : 3) / s.H;
+    const int64_t at_once = 256 * (s.D > 128 || l.tiles > 1 ? 2 : 3) / (int64_t(s.H) * l.row_tiles);
     l.chunk = 8;
     int64_t pieces = at_once;
     if (s.num_seqs > at_once / 2) pieces = std::max<int64_t>(2 * at_once, s.num_seqs + s.num_seqs / 2 + 1);
     pieces = std::min<int64_t>(pieces, s.num_seqs * ((tiles - 1) / l.chunk + 1) + 1);
     l.pieces = int32_t(std::max<int64_t>(pieces, s.num_seqs + 1));
-    l.groups = int64_t(l.pieces) * s.H;
-    parts = uint64_t(l.groups) * l.part_rows;
+    l.groups = int64_t(l.pieces) * s.H * l.row_tiles;
+    parts = uint64_t(l.pieces) * s.H * l.part_rows;
   }
   l.part_bytes = parts * s.D * 4;
   l.workspace_bytes = l.part_bytes + parts * 8;
