@@ -8,7 +8,7 @@
 // every wave rows of its own and shares the tokens in LDS.  A wave keeps the running maximum and
 // sum of the softmax, and what was cut is joined at the end: one pass over the cache.
 //
-// Few rows are bound by the cache's bytes and, in 4 bits, by decoding them: 32 ragged sequences (230 thousand tokens, 8
+// Few rows are bound by the cache's bytes and, in 4 bits, by decoding them: 32 ragged sequences (255 thousand tokens, 8
 // heads of 128, 4 query heads each) take 66 us, 4.2 TB/s, the vector units busy 51% of it; with a
 // window of 1024 over 16-bit pages 22.5 us, 5.0 TB/s.  Many rows are bound by the vector units (the softmax), which the
 // matrix units wait for: 2825 rows of 32 heads behind up to 10240 tokens in 8 and 4 bits run at 684 TFLOP/s,
