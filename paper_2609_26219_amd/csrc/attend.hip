@@ -694,10 +694,21 @@ __device__ __forceinline__ float lse_of(float ref, float l) {
 // as run at once, so that sequences of any lengths keep the whole GPU busy to the end.  Every workgroup
 // works the pieces out from the lengths, which only the device knows.
 
-// What the rows of sequence `seq` look at when nothing but lengths is known: a span without the rows' own bounds.
+// What a sequence's rows look at, without the queries: a span that bounds the rows' own.  (Positions are
+// read only where there is a window: 32 sequences, a window of 1024 over 16 bits, a row anywhere in each 24 + 7 us instead
+// of 203 + 8, two rows 97 + 10 instead of 210 + 9.)
 __device__ __forceinline__ Span few_span(const ServeArgs& s, const AttendArgs& a, const Group& g) {
   Span span{-1, 0, -1, -1, 0, 0, 0};
-  if (s.positions) {
+  if (s.positions && a.window > 0) {
+    span.lo_least = 0x7FFFFFFF;
+    for (int32_t i = 0; i < g.count; ++i) {
+      const int32_t pos = s.positions[g.start + i], hi = pos < g.kv_len ? pos : g.kv_len - 1;
+      if (hi < 0) continue;
+      const int32_t lo = pos >= a.window ? pos - a.window : -1;
+      span.hi_most = span.hi_most > hi ? span.hi_most : hi;
+      span.lo_least = span.lo_least < lo ? span.lo_least : lo;
+    }
+  } else if (s.positions) {
     span.hi_most = g.kv_len - 1;
   } else {
     const int32_t pos0 = g.kv_len - g.trail;

@@ -457,3 +457,9 @@ def test_append_and_read_of_more_sequences_than_are_searched_in_lds(torch, tag):
     case.cache = want
     for which, t in enumerate(serving.read(cache, batch)):
         check_read(case, _down(t), which)
+
+
+@pytest.mark.parametrize("tag,group,new", [(FP16, 4, 2), (K4V4, 2, 5), (K8V4, 8, 3)])
+def test_windows_at_scattered_positions_of_many_sequences(torch, tag, group, new):
+    """A window and positions: only the tokens between the rows' windows (and the sinks) are looked at, in pieces."""
+    test_attention(torch, tag, BF16, 2, group, 64, 16, _lengths(70, 0, 90, (1800, 1, 0, 950)), (new, 1, new), True, 60, 5, 1)
