@@ -463,3 +463,22 @@ def test_append_and_read_of_more_sequences_than_are_searched_in_lds(torch, tag):
 def test_windows_at_scattered_positions_of_many_sequences(torch, tag, group, new):
     """A window and positions: only the tokens between the rows' windows (and the sinks) are looked at, in pieces."""
     test_attention(torch, tag, BF16, 2, group, 64, 16, _lengths(70, 0, 90, (1800, 1, 0, 950)), (new, 1, new), True, 60, 5, 1)
+
+
+@pytest.mark.parametrize("tag", [K8V8, K8V4, K4V4])
+@pytest.mark.parametrize("new", [(1,), (130,)])
+def test_binary16_results_over_codes_carry_the_results_rounding_alone(torch, tag, new):
+    """Probabilities go in as two binary16 numbers, so what is left of their rounding is 2^-22 of each (2^-21 with the
+    second's own underflow at 2^-38 of the largest, which check_attention's bound has as 2^-24 a token): its bound with
+    that in the place of 2^-11.  Every row has an outlier 8 times its other channels."""
+    from oracle.restore import output_values
+    from paper_2609_26219_amd import serving
+
+    case = Case(83, tag, HALF, 2, 4, 128, 16, (300, 777, 130), new)
+    out, _ = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
+    exact, _, mass, whole, reach = case.attend()
+    have = output_values(_down(out), HALF)
+    delta = 2.0 ** -23 * (case.D / 8 + 16) * reach
+    tol = 2.0 ** -11 * np.abs(exact) * (1 + 2.0 ** -11) + (2.0 ** -21 + 2.0 ** -24 * case.most_kv) * mass + \
+        (4 * delta + 2.0 ** -18)[:, :, None] * whole + 2.0 ** -25
+    assert (np.abs(have - exact) <= tol).all(), float((np.abs(have - exact) / tol).max())
