@@ -1116,7 +1116,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         const int id = tid + kThreads * n, tok = id / (D / 8), piece = id % (D / 8);
-        m.k[b][k_place(tok / 16, piece / 4, piece % 4, tok % 16)] = u32x4{raw_k[4 * n], raw_k[4 * n + 1], raw_k[4 * n + 2], raw_k[4 * n + 3]};
+        m.k[b][k_place(tok / 16, piece / 4, piece % 4, tok % 16)] =
+            u32x4{raw_k[4 * n], raw_k[4 * n + 1], raw_k[4 * n + 2], raw_k[4 * n + 3]};
       }
     }
     if constexpr (!kCodes) {
@@ -1363,8 +1364,14 @@ pkv_status_t PKV_JOINED(launch_attend_, PKV_HEAD_DIM)(const ServeArgs& s, const 
       case PKV_TAG_FP16:
         s.bf16 ? go(attend_few_kernel<true, 16, 16, kWhole, kTiles>) : go(attend_few_kernel<false, 16, 16, kWhole, kTiles>);
         break;
-      case PKV_TAG_K8V8: s.bf16 ? go(attend_few_kernel<true, 8, 8, kWhole, kTiles>) : go(attend_few_kernel<false, 8, 8, kWhole, kTiles>); break;
-      case PKV_TAG_K8V4: s.bf16 ? go(attend_few_kernel<true, 8, 4, kWhole, kTiles>) : go(attend_few_kernel<false, 8, 4, kWhole, kTiles>); break;
+      case PKV_TAG_K8V8:
+        s.bf16 ? go(attend_few_kernel<true, 8, 8, kWhole, kTiles>)
+               : go(attend_few_kernel<false, 8, 8, kWhole, kTiles>);
+        break;
+      case PKV_TAG_K8V4:
+        s.bf16 ? go(attend_few_kernel<true, 8, 4, kWhole, kTiles>)
+               : go(attend_few_kernel<false, 8, 4, kWhole, kTiles>);
+        break;
       default: s.bf16 ? go(attend_few_kernel<true, 4, 4, kWhole, kTiles>) : go(attend_few_kernel<false, 4, 4, kWhole, kTiles>); break;
     }
   };
