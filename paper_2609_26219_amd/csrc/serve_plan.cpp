@@ -154,6 +154,7 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
 
 AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   AttendLaunch l{};
+  if (s.num_seqs == 0 || s.num_tokens == 0) return l;  // no workgroups, no workspace
   const int64_t rows = int64_t(s.max_tokens) * a.group;
   const bool many = rows > few_shares(kKeyBits[s.tag]) * kRowTile * few_tiles(s.D);
   l.tiles = many ? many_tiles(s.D) : rows <= kRowTile ? 1 : few_tiles(s.D);
@@ -172,7 +173,7 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
     // four times, 569 with six, 587 with eight; 2825 rows behind 10240 tokens: 598 with four and six, which leave them
     // uncut, 605 and 79 more to join with eight.)
     l.chunk = 16;
-    if (base > 0) l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(6 * 256 / base, tiles / l.chunk)));
+    l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(6 * 256 / base, tiles / l.chunk)));
     l.groups = base * l.splits;
     if (l.splits > 1) parts = uint64_t(s.num_tokens) * a.Hq * l.splits;
   } else if (tiles <= (base >= 256 ? kWholeTilesOfMany : kWholeTiles)) {

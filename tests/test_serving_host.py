@@ -184,3 +184,19 @@ def test_sizes_past_a_launch_are_refused():
             with pytest.raises(pb.PkvError):
                 pb.pkv_attention_workspace(m, pb.PkvPagedCache(tag=0), b, a)
         pb.pkv_attention_workspace(m, pb.PkvPagedCache(tag=3), b, a)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("tag", range(4))
+@pytest.mark.parametrize("empty", [dict(num_tokens=0), dict(num_seqs=0, num_tokens=3), dict(num_seqs=0, num_tokens=0)])
+def test_an_empty_batch_needs_nothing_however_long_its_sequences_may_be(dim, tag, empty):
+    """No row, or no sequence, over page tables of 16000 tokens: nothing to launch and no workspace."""
+    s = _shape(head_dim=dim)
+    m, c = pb.make_model(s), pb.PkvPagedCache(tag=tag)
+    for group in (1, 2, 40):
+        b = pb.PkvBatch(**{**dict(num_seqs=2, max_tokens=0, pages_per_seq=1000), **empty})
+        a = pb.PkvAttention(num_q_heads=4 * group, scale=0.1)
+        assert pb.pkv_attention_workspace(m, c, b, a) == 0
+    if tag == 3:  # (the codes that _call describes)
+        assert _call(shape=s, batch=dict(pages_per_seq=1000, **empty),
+                     attention=dict(q_head_stride=dim, out_head_stride=dim, workspace=None, workspace_bytes=0)) == OK
