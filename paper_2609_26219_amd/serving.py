@@ -108,11 +108,18 @@ class PagedCache:
         self._index = self.device.index
         self.model = binding.make_model(_Geometry(num_layers, num_kv_heads, head_dim, page_size, pool_pages,
                                                   _DTYPES[dtype], layout))
+        self._layers = [self._of_layer(layer) for layer in range(num_layers)]
         self._workspace = {}
 
+    def _of_layer(self, layer: int) -> binding.PkvPagedCache:
+        struct = binding.PkvPagedCache.from_buffer_copy(self.struct)
+        struct.layer = layer
+        return struct
+
     def _at(self, layer: int) -> binding.PkvPagedCache:
-        self.struct.layer = layer
-        return self.struct
+        """The cache of one layer as the library takes it.  No call writes to it: threads may be in calls of different
+        layers at once."""
+        return self._layers[layer] if 0 <= layer < self.num_layers else self._of_layer(layer)  # (the library refuses it)
 
     def workspace(self, nbytes: int, stream: int) -> int:
         """Address of scratch memory for attention calls on one stream (they follow each other), grown as needed.  A

@@ -1,0 +1,105 @@
+"""Several host threads on one paged cache, without a GPU: the library's calls are replaced by functions that note what
+they were given and hold a thread where another one can get in between.
+
+A cache lies in host memory here and says that it is on a device."""
+import threading
+
+import pytest
+import torch
+
+from paper_2609_26219_amd import binding as pb
+from paper_2609_26219_amd import serving
+from paper_2609_26219_amd import workloads as wl
+
+WAIT = 20.0  # seconds before a test gives up on a thread
+
+
+class Elsewhere(torch.Tensor):
+    @property
+    def device(self):
+        return torch.device("cuda", 0)
+
+
+def _zeros(shape, dtype):
+    return torch.zeros(shape, dtype=dtype).as_subclass(Elsewhere)
+
+
+def _cache(layers=3):
+    codes, scales = _zeros((layers, 4, 2, 16 * 64), torch.uint8), _zeros((layers, 4, 2, 2, 16, 2), torch.float16)
+    return serving.PagedCache(2, 64, 16, torch.bfloat16, wl.TAG_K4V4, codes=codes, scales=scales)
+
+
+def _batch(rows):
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    return serving.Batch(ints(0, rows), ints(40), ints(0, 1, 2).view(1, 3), rows)
+
+
+def _rows(heads, n=1):
+    return torch.zeros((n, heads, 64), dtype=torch.bfloat16)
+
+
+class Thread(threading.Thread):
+    """A thread whose error is raised by join."""
+
+    def __init__(self, work):
+        super().__init__(daemon=True)
+        self.work, self.error = work, None
+
+    def run(self):
+        try:
+            self.work()
+        except BaseException as e:  # noqa: BLE001
+            self.error = e
+
+    def join(self, timeout=WAIT):
+        super().join(timeout)
+        assert not self.is_alive()
+        if self.error:
+            raise self.error
+
+
+@pytest.fixture
+def one_stream(monkeypatch):
+    monkeypatch.setattr(serving, "_stream", lambda cache: 7)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+
+
+@pytest.mark.parametrize("other", ["append", "read", "attention"])
+def test_a_call_keeps_its_layer_while_another_thread_calls(monkeypatch, one_stream, other):
+    """Attention of layer 0 is held between its workspace query and its launch, while a call of layer 2 runs whole."""
+    cache, batch = _cache(), _batch(1)
+    inside, go, seen = threading.Event(), threading.Event(), []
+
+    def workspace(model, struct, b, a):
+        if not inside.is_set():
+            inside.set()
+            assert go.wait(WAIT)
+        return 0
+
+    def launched(model, struct, *rest):
+        seen.append(struct.layer)
+        return pb.PKV_OK
+
+    monkeypatch.setattr(pb, "pkv_attention_workspace", workspace)
+    for name in ("pkv_attention_status", "pkv_cache_append_status", "pkv_cache_read_status"):
+        monkeypatch.setattr(pb, name, launched)
+    first = Thread(lambda: serving.attention(cache, batch, _rows(4), layer=0))
+    first.start()
+    assert inside.wait(WAIT)
+    calls = {"append": lambda: serving.append(cache, batch, _rows(2), _rows(2), layer=2),
+             "read": lambda: serving.read(cache, batch, layer=2, out=(_rows(2), _rows(2))),
+             "attention": lambda: serving.attention(cache, batch, _rows(4), layer=2)}
+    calls[other]()
+    go.set()
+    first.join()
+    assert seen == [2, 0]
+
+
+def test_a_layer_that_is_not_there_is_the_librarys_to_refuse(one_stream):
+    cache, batch = _cache(), _batch(1)
+    for layer in (-1, 3, 1 << 20):
+        for call in (lambda: serving.append(cache, batch, _rows(2), _rows(2), layer=layer),
+                     lambda: serving.attention(cache, batch, _rows(4), layer=layer)):
+            with pytest.raises(pb.PkvError) as e:
+                call()
+            assert e.value.status == pb.PKV_ERR_INVALID_ARGUMENT
