@@ -10,11 +10,13 @@ fills anew each step, and calls
 * :func:`attention`  attention of new or recomputed rows over the cache, with an
   optional sliding window and sinks.
 
-Nothing here waits for the device or copies from it.
+Nothing here waits for the device or copies from it.  Several host threads may
+use one cache, on one stream or on streams of their own.
 """
 from __future__ import annotations
 
 import dataclasses
+import threading
 from typing import Optional
 
 import torch
@@ -110,6 +112,7 @@ class PagedCache:
                                                   _DTYPES[dtype], layout))
         self._layers = [self._of_layer(layer) for layer in range(num_layers)]
         self._workspace = {}
+        self._scratch = threading.Lock()  # held from taking scratch memory until the kernels that use it are enqueued
 
     def _of_layer(self, layer: int) -> binding.PkvPagedCache:
         struct = binding.PkvPagedCache.from_buffer_copy(self.struct)
@@ -123,7 +126,8 @@ class PagedCache:
 
     def workspace(self, nbytes: int, stream: int) -> int:
         """Address of scratch memory for attention calls on one stream (they follow each other), grown as needed.  A
-        captured call gets memory of its graph, so that replays share it with nothing else."""
+        captured call gets memory of its graph, so that replays share it with nothing else.  The caller holds
+        ``_scratch``: the kernels of two calls on one stream must not be enqueued in turn."""
         if torch.cuda.is_current_stream_capturing():
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device).data_ptr()
         held = self._workspace.get(stream)
@@ -220,6 +224,10 @@ def attention(cache: PagedCache, batch: Batch, q, scale: Optional[float] = None,
     struct = cache._at(layer)
     nbytes = binding.pkv_attention_workspace(cache.model, struct, batch.struct, a)
     if nbytes:
-        a.workspace, a.workspace_bytes = cache.workspace(nbytes, stream), nbytes
-    _check(binding.pkv_attention_status(cache.model, struct, batch.struct, a, stream), "pkv_attention")
+        with cache._scratch:
+            a.workspace, a.workspace_bytes = cache.workspace(nbytes, stream), nbytes
+            status = binding.pkv_attention_status(cache.model, struct, batch.struct, a, stream)
+    else:
+        status = binding.pkv_attention_status(cache.model, struct, batch.struct, a, stream)
+    _check(status, "pkv_attention")
     return (out, lse) if return_lse else out

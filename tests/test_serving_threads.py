@@ -103,3 +103,56 @@ def test_a_layer_that_is_not_there_is_the_librarys_to_refuse(one_stream):
             with pytest.raises(pb.PkvError) as e:
                 call()
             assert e.value.status == pb.PKV_ERR_INVALID_ARGUMENT
+
+
+def test_calls_that_share_scratch_memory_are_enqueued_one_after_the_other(monkeypatch, one_stream):
+    """Two threads on one stream use the same scratch memory, so the kernels of one call (attention, then the join of its
+    parts) have to be enqueued with none of the other's between them, and the memory has to stay the call's until then,
+    also where the other call wants more of it."""
+    cache, batch = _cache(), _batch(1)
+    sizes = {"first": 1 << 10, "second": 1 << 20}
+    inside, waiting, log = threading.Event(), threading.Event(), []
+
+    def workspace(model, struct, b, a):
+        return sizes[threading.current_thread().name]
+
+    def launched(model, struct, b, a, stream):
+        name = threading.current_thread().name
+        log.append((name, "begins"))
+        if name == "first":
+            inside.set()
+            waiting.wait(1.0)  # the second thread, if nothing holds it, is in here within that time
+            held = cache._workspace[stream]
+            assert held[1] == a.workspace and held[0] >= a.workspace_bytes
+        else:
+            waiting.set()
+        log.append((name, "ends"))
+        return pb.PKV_OK
+
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *size, device=None, **kw: empty(*size, **kw))
+    monkeypatch.setattr(pb, "pkv_attention_workspace", workspace)
+    monkeypatch.setattr(pb, "pkv_attention_status", launched)
+    threads = [Thread(lambda: serving.attention(cache, batch, _rows(4))) for _ in range(2)]
+    for t, name in zip(threads, sizes):
+        t.name = name
+    threads[0].start()
+    assert inside.wait(WAIT)
+    threads[1].start()
+    for t in threads:
+        t.join()
+    assert log == [("first", "begins"), ("first", "ends"), ("second", "begins"), ("second", "ends")]
+
+
+def test_scratch_memory_is_free_again_after_a_refused_call(monkeypatch, one_stream):
+    cache, batch = _cache(), _batch(1)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *size, device=None, **kw: empty(*size, **kw))
+    monkeypatch.setattr(pb, "pkv_attention_workspace", lambda *a: 64)
+    monkeypatch.setattr(pb, "pkv_attention_status", lambda *a: pb.PKV_ERR_DEVICE)
+    with pytest.raises(pb.PkvError):
+        serving.attention(cache, batch, _rows(4))
+    monkeypatch.setattr(pb, "pkv_attention_status", lambda *a: pb.PKV_OK)
+    again = Thread(lambda: serving.attention(cache, batch, _rows(4)))
+    again.start()
+    again.join()
