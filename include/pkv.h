@@ -432,7 +432,8 @@ typedef struct {
 typedef struct {
   int32_t num_seqs;
   int32_t num_tokens;
-  int32_t max_tokens;         /* bound of a sequence's rows: 1 for a decode step; 0 = num_tokens */
+  int32_t max_tokens;         /* bound of a sequence's rows: 1 for a decode step; 0 = num_tokens (attention leaves
+                               * the out and lse of a sequence's rows past it as they are) */
   int32_t pages_per_seq;      /* row length of page_table */
   int64_t max_kv_len;         /* bound of kv_lens, for the launch; 0 = pages_per_seq * page_size */
   const int32_t* token_start; /* [num_seqs + 1], ascending from 0 */

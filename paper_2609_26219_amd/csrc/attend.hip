@@ -1316,9 +1316,18 @@ template <int GROUPS>
 __global__ __launch_bounds__(kThreads) void join_splits_kernel(ServeArgs s, AttendArgs a) {
   const uint32_t row = GROUPS == 1 ? blockIdx.x * kJoinGroups + threadIdx.x / (D / 4) : blockIdx.x;
   const int32_t token = int32_t(row / uint32_t(a.Hq)), head = int32_t(row % uint32_t(a.Hq));
-  // Rows of no sequence have no parts.
+  // Rows of no sequence have no parts, and neither have a sequence's rows past max_tokens.
   if (token < scalar_entry(s.token_start, 0) || token >= scalar_entry(s.token_start, s.num_seqs)) return;
   if (token >= s.num_tokens) return;
+  if (s.max_tokens < s.num_tokens) {
+    int32_t seq = 0;
+    for (int32_t end = s.num_seqs; end - seq > 1;) {
+      const int32_t mid = seq + (end - seq) / 2;
+      if (s.token_start[mid] <= token) seq = mid; else end = mid;
+    }
+    const Group g = group_from(s, s.token_start[seq], s.token_start[seq + 1], 0);
+    if (token >= g.start + g.count) return;
+  }
   const int64_t first = int64_t(row) * a.splits;
   join_parts<GROUPS>(s, a, token, head, a.splits, [&](int i) { return first + i; });
 }

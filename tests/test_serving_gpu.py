@@ -482,3 +482,34 @@ def test_binary16_results_over_codes_carry_the_results_rounding_alone(torch, tag
     tol = 2.0 ** -11 * np.abs(exact) * (1 + 2.0 ** -11) + (2.0 ** -21 + 2.0 ** -24 * case.most_kv) * mass + \
         (4 * delta + 2.0 ** -18)[:, :, None] * whole + 2.0 ** -25
     assert (np.abs(have - exact) <= tol).all(), float((np.abs(have - exact) / tol).max())
+
+
+PAST = [
+    # tag, group, lens, rows, bound: the forms of few rows, whole and in pieces, and of many rows, whole, split and split often
+    (K4V4, 4, (300, 40), (5, 3), 2),
+    (K4V4, 4, (3000, 40), (5, 3), 2),
+    (FP16, 1, (200, 300), (90, 50), 45),
+    (FP16, 1, (5000, 300), (60, 45), 45),
+    (FP16, 1, (20001,), (60,), 45),
+    (K8V4, 4, (5000, 300, 7), (45, 30, 7), 30),
+]
+
+
+@pytest.mark.parametrize("tag,group,lens,rows,bound", PAST)
+def test_rows_past_the_bound_are_left_alone(torch, tag, group, lens, rows, bound):
+    """Sequences with more rows than max_tokens says (a replayed graph's, say): the first of each are attended, the others
+    keep what their places held."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(91, tag, BF16, 1, group, 128, 16, lens, rows)
+    cache, batch, q = _cache(torch, case), _batch(torch, case), _up(torch, case.q, case)
+    batch.struct.max_tokens = bound
+    past = np.concatenate([np.arange(n) >= bound for n in rows])
+    out = torch.full((case.tokens, group, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    _, lse = serving.attention(cache, batch, q, out=out, return_lse=True)
+    assert past.any() and (out[torch.from_numpy(past).cuda()] == 7.0).all()
+    # the rows within the bound, the others taken from a call that has them all
+    whole, whole_lse = serving.attention(cache, _batch(torch, case), q, return_lse=True)
+    out[torch.from_numpy(past).cuda()] = whole[torch.from_numpy(past).cuda()]
+    lse[torch.from_numpy(past).cuda()] = whole_lse[torch.from_numpy(past).cuda()]
+    check_attention(case, _down(out), lse.cpu().numpy())
