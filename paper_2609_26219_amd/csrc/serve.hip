@@ -68,7 +68,7 @@ __device__ __forceinline__ int64_t place_of(const ServeArgs& a, const int32_t* s
     const int32_t mid = s + (end - s) / 2;
     if (starts[mid] <= i) s = mid; else end = mid;
   }
-  const int32_t end = starts[s + 1];
+  const int32_t end = starts[s + 1] < a.num_tokens ? starts[s + 1] : a.num_tokens;
   if (i < starts[s] || i >= end) return -2;
   int64_t pos;
   if (a.positions) {

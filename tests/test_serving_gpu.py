@@ -513,3 +513,26 @@ def test_rows_past_the_bound_are_left_alone(torch, tag, group, lens, rows, bound
     out[torch.from_numpy(past).cuda()] = whole[torch.from_numpy(past).cuda()]
     lse[torch.from_numpy(past).cuda()] = whole_lse[torch.from_numpy(past).cuda()]
     check_attention(case, _down(out), lse.cpu().numpy())
+
+
+@pytest.mark.parametrize("tag", [K4V4, FP16])
+def test_starts_past_the_rows_of_the_call_are_their_number(torch, tag):
+    """A last start beyond num_tokens counts as num_tokens for all three calls: the rows that are there are the last ones
+    of their sequence, where they are written, read and attended from."""
+    from oracle import serving as os_
+    from paper_2609_26219_amd import serving
+
+    case = Case(92, tag, BF16, 1, 2, 64, 16, (20, 30), (4, 6))
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    batch.keep[0].copy_(torch.tensor([0, 4, 13], dtype=torch.int32))
+    serving.append(cache, batch, _up(torch, case.k, case), _up(torch, case.v, case))
+    want = case.copy_of_cache()
+    os_.append(want, tag, 16, case.where(), case.k, case.v, BF16)
+    got, _ = _state(torch, cache, case)
+    for g, w in zip(got, want["kv"] if tag == FP16 else [want["codes"], want["scales"]]):
+        assert np.array_equal(g.view(w.dtype), w)
+    case.cache = want
+    for which, t in enumerate(serving.read(cache, batch)):
+        check_read(case, _down(t), which)
+    out, lse = serving.attention(cache, batch, _up(torch, case.q, case), return_lse=True)
+    check_attention(case, _down(out), lse.cpu().numpy())
