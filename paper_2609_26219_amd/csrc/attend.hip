@@ -355,7 +355,9 @@ struct Running {
 // binary16 with room below, so the reference is chosen that the largest p (times scale) so far is
 // 2^kTop, and moved only when one passes that by kSlack (binary16 ends at 2^16): O is then rescaled once or
 // twice a row and not at every new maximum, of which 32 rows have one in nearly every tile.  A
-// scale counts as at least 2^-24, binary16's least.  bfloat16 needs no room: kTop = 0.
+// scale counts as at least 2^-24, binary16's least.  bfloat16 needs no room: kTop = 0.  (The largest score and the largest
+// scale of several tokens will not do: where a token of large scale is seen little of or not at all, the others'
+// probabilities would lose their bits, 2% of a result with scales 2^24 apart and all of it with 2^30.)
 constexpr float kSlack = 8.0f;
 template <bool HALF>
 constexpr float kTop = HALF ? 6.0f : 0.0f;
@@ -459,7 +461,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
       }
     if constexpr (!kCodes) hide(keep);
   }
-  // The reference of the exponents.
+  // The reference of the exponents.  Over codes it goes by score + log2(scale) of each token; that it stays is decided by
+  // the lane's largest score and its largest scale, which are no less and take one logarithm.
   float above = -kTop<kHalf>;
   if constexpr (kCodes) {
     float most = 0x1p-24f;
@@ -482,6 +485,18 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Span& spa
     move |= top[r] > st.ref[r] + kSlack;
   }
   if (__any(move)) {
+    if constexpr (kCodes) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) top[r] = -kInf;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float bits = __builtin_amdgcn_logf(__builtin_fmaxf(sc.vs(u, i), 0x1p-24f)) - kTop<kHalf>;
+#pragma unroll
+          for (int r = 0; r < RT; ++r) top[r] = __builtin_fmaxf(top[r], __builtin_fmaf(t[r][u][i], rows.f[r], bits));
+        }
+    }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       float next = over_c_max(top[r]);

@@ -536,3 +536,67 @@ def test_starts_past_the_rows_of_the_call_are_their_number(torch, tag):
         check_read(case, _down(t), which)
     out, lse = serving.attention(cache, batch, _up(torch, case.q, case), return_lse=True)
     check_attention(case, _down(out), lse.cpu().numpy())
+
+
+def _check_fine(case, out, lse):
+    """check_attention, and over codes with binary16 results its bound with 2^-21 in the place of 2^-11 (see
+    test_binary16_results_over_codes_carry_the_results_rounding_alone)."""
+    from oracle.restore import output_values
+
+    check_attention(case, _down(out), lse.cpu().numpy())
+    if case.dtype == HALF:
+        exact, _, mass, whole, reach = case.attend()
+        delta = 2.0 ** -23 * (case.D / 8 + 16) * reach
+        tol = 2.0 ** -11 * np.abs(exact) * (1 + 2.0 ** -11) + (2.0 ** -21 + 2.0 ** -24 * case.most_kv) * mass + \
+            (4 * delta + 2.0 ** -18)[:, :, None] * whole + 2.0 ** -25
+        off = np.abs(output_values(_down(out), HALF) - exact)
+        assert (off <= tol).all(), float((off / tol).max())
+
+
+def _rows_into(case, k, v):
+    """The case's cache holds rows k, v [tokens][H][D] of its one sequence."""
+    from oracle import serving as os_
+
+    where = [(0, t, int(case.table[0, t // case.P]), t % case.P) for t in range(int(case.lens[0]))]
+    os_.append(case.cache, case.tag, case.P, where, case.bits(k), case.bits(v), case.dtype)
+
+
+@pytest.mark.parametrize("apart", [8, 16, 20, 24, 30])
+@pytest.mark.parametrize("tag,D", [(K8V8, 128), (K4V4, 64), (K8V4, 256)])
+@pytest.mark.parametrize("dtype", [HALF, BF16])
+@pytest.mark.parametrize("new", [1, 110])
+def test_value_scales_far_apart(torch, tag, D, dtype, new, apart):
+    """Every fourth token has values 2^apart times the others' and a score so low that it hardly counts: the
+    others keep the precision they have by themselves."""
+    from paper_2609_26219_amd import serving
+
+    n = 200
+    case = Case(93, tag, dtype, 1, 2, D, 16, (n,), (new,))
+    rng = np.random.default_rng(apart)
+    k, v, q = (rng.standard_normal(s) for s in ((n, 1, D), (n, 1, D), (new, 2, D)))
+    large = np.arange(n) % 4 == 3
+    q[:, :, 0], k[:, :, 0] = 30.0, np.where(large, -45.0, 0.0)[:, None]  # scores 84 and more below the others'
+    top = 2.0 ** (12 if apart > 16 else 4)
+    v *= np.where(large, top, top / 2.0 ** apart)[:, None, None]
+    case.q = case.bits(q)
+    _rows_into(case, k, v)
+    out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
+    _check_fine(case, out, lse)
+
+
+@pytest.mark.parametrize("tag", [K8V8, K4V4])
+@pytest.mark.parametrize("dtype", [HALF, BF16])
+@pytest.mark.parametrize("new", [6, 110])
+def test_value_scales_of_tokens_that_other_rows_see(torch, tag, dtype, new):
+    """From one token on values are 2^24 times the earlier ones': rows before it, whose tile of tokens holds some, do not
+    notice."""
+    from paper_2609_26219_amd import serving
+
+    n, first = 120, 117
+    case = Case(94, tag, dtype, 1, 2, 128, 16, (n,), (new,))
+    rng = np.random.default_rng(7)
+    k, v = rng.standard_normal((n, 1, 128)), rng.standard_normal((n, 1, 128))
+    v *= np.where(np.arange(n) >= first, 2.0 ** 12, 2.0 ** -12)[:, None, None]
+    _rows_into(case, k, v)
+    out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
+    _check_fine(case, out, lse)
