@@ -450,7 +450,10 @@ pkv_status_t pkv_cache_size(const pkv_model_t* model, int32_t tag, uint64_t* cod
  * its tag (FP16: copied).  Row i of head h starts at k + i * token_stride +
  * h * head_stride elements of out_dtype (v likewise); both 16-byte aligned,
  * strides multiples of 8 and head_stride >= head_dim (views of a fused
- * projection will do).  Two rows of a call at one place leave either.  Every
+ * projection will do).  A place is written by one row of a call: where
+ * positions, or pages that sequences share, put several at one place, that place
+ * is left with pieces of each (codes of one, scale and zero of another) unless
+ * the rows are equal, and every other place with its own row.  Every
  * other byte of the cache stays.  One kernel on `hip_stream`.  Errors:
  * PKV_ERR_INVALID_ARGUMENT, PKV_ERR_BAD_TAG, PKV_ERR_DEVICE. */
 pkv_status_t pkv_cache_append(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,

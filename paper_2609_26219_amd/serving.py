@@ -180,7 +180,8 @@ def _stream(cache: PagedCache) -> int:
 
 
 def append(cache: PagedCache, batch: Batch, k, v, layer: int = 0) -> None:
-    """Write rows ``k``, ``v`` ``[num_tokens, H, D]`` into the cache at the batch's positions."""
+    """Write rows ``k``, ``v`` ``[num_tokens, H, D]`` into the cache at the batch's positions.  Each place is to be
+    written by one row of the call: several that differ leave pieces of each there."""
     _rows(cache, batch, cache.num_kv_heads, k, v)
     at = _strides(k)
     _need(at == _strides(v), "k and v have the same strides")

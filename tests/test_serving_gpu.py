@@ -600,3 +600,41 @@ def test_value_scales_of_tokens_that_other_rows_see(torch, tag, dtype, new):
     _rows_into(case, k, v)
     out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
     _check_fine(case, out, lse)
+
+
+@pytest.mark.parametrize("tag", [FP16, K8V4, K4V4])
+@pytest.mark.parametrize("equal", [True, False])
+def test_rows_at_one_place(torch, tag, equal):
+    """Equal rows at one place leave that row; rows that differ leave nothing in particular there, and every other place
+    as it should be."""
+    from oracle import serving as os_
+    from paper_2609_26219_amd import serving
+
+    n = 90
+    case = Case(95, tag, BF16, 3, 1, 128, 16, (100,), (n,), scattered=True)
+    case.positions[60:] = case.positions[:30][::-1]
+    if equal:
+        case.k[60:], case.v[60:] = case.k[:30][::-1], case.v[:30][::-1]
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    serving.append(cache, batch, _up(torch, case.k, case), _up(torch, case.v, case))
+    want = case.copy_of_cache()
+    os_.append(want, tag, 16, case.where(), case.k, case.v, BF16)
+    got, _ = _state(torch, cache, case)
+    want = want["kv"] if tag == FP16 else [want["codes"], want["scales"]]
+    twice = {(p, s) for _, _, p, s in case.where()[60:]}
+    for g, w in zip(got, want):
+        g = g.view(w.dtype)
+        if not equal:  # those places aside
+            for p, s in twice:
+                for a in (g, w):
+                    if tag == FP16:
+                        a[p, s] = 0
+                    elif a.ndim == 3:  # codes
+                        at = 0
+                        for bits in (wl.KEY_BITS[tag], wl.VALUE_BITS[tag]):
+                            row = 128 * bits // 8
+                            a[p, :, at + s * row:at + (s + 1) * row] = 0
+                            at += 16 * row
+                    else:
+                        a[p, :, :, s] = 0
+        assert np.array_equal(g, w)
