@@ -488,9 +488,10 @@ pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* c
  * out_dtype.  What a cache holds past kv_lens, on pages that are not there, before
  * every row's window and behind the sinks (NaN, infinities) does not matter; what
  * lies between places that rows of a sequence see should be finite.
- * num_tokens * num_q_heads < 2^31, and < 2^24 where a workspace is needed; num_seqs *
- * num_kv_heads * ceil(max_tokens * (num_q_heads / num_kv_heads) / 64) < 2^23 always
- * suffices for the launch; a page of 16-bit K and V, or of codes, below 4 GiB.
+ * num_tokens * num_q_heads < 2^31, and < 2^24 where a workspace is needed.  The launch
+ * has fewer than 2^24 workgroups, for which (num_seqs + 1) * num_kv_heads *
+ * ceil(max_tokens * (num_q_heads / num_kv_heads) / 16) < 2^23 always suffices.  A page
+ * of 16-bit K and V, or of codes, is below 4 GiB.
  * At most two kernels on `hip_stream`.  Errors as pkv_cache_append. */
 typedef struct {
   int32_t num_q_heads; /* a multiple of num_kv_heads */

@@ -200,3 +200,43 @@ def test_an_empty_batch_needs_nothing_however_long_its_sequences_may_be(dim, tag
     if tag == 3:  # (the codes that _call describes)
         assert _call(shape=s, batch=dict(pages_per_seq=1000, **empty),
                      attention=dict(q_head_stride=dim, out_head_stride=dim, workspace=None, workspace_bytes=0)) == OK
+
+
+def test_the_bound_of_a_launch_that_always_suffices():
+    """(num_seqs + 1) * heads * ceil(max_tokens * group / 16) < 2^23, over every form: sizes right below it are taken."""
+    rng = np.random.default_rng(1)
+    lib, taken = pb.load(), 0
+    for _ in range(4000):
+        dim, tag, heads = int(rng.choice([64, 128, 256])), int(rng.integers(4)), int(2 ** rng.uniform(0, 7))
+        group, most = int(2 ** rng.uniform(0, 6)), int(2 ** rng.uniform(0, 12))
+        if heads * dim > 4096:  # (a row of the model)
+            continue
+        per = heads * -(-most * group // 16)
+        seqs = ((1 << 23) - 1) // per - 1 - int(rng.integers(3))
+        if seqs < 1:
+            continue
+        tokens = max(most, min(seqs, ((1 << 24) - 1) // (heads * group)))
+        if tokens * heads * group >= 1 << 24:
+            continue
+        s = _shape(head_dim=dim, num_kv_heads=heads)
+        m, c = pb.make_model(s), pb.PkvPagedCache(tag=tag)
+        window = int(rng.choice([0, 100]))
+        b = pb.PkvBatch(num_seqs=seqs, num_tokens=tokens, max_tokens=most, pages_per_seq=int(2 ** rng.uniform(0, 13)))
+        a = pb.PkvAttention(num_q_heads=heads * group, window=window, scale=0.1)
+        out = ctypes.c_uint64()
+        st = lib.pkv_attention_workspace(ctypes.byref(m), ctypes.byref(c), ctypes.byref(b), ctypes.byref(a),
+                                         ctypes.byref(out))
+        assert st == OK, (dim, tag, heads, group, most, seqs, tokens)
+        taken += 1
+    assert taken > 1000
+
+
+@pytest.mark.parametrize("heads,group,tag,seqs,tokens,most", [(16, 33, 3, 390000, 1000, 1), (8, 1, 3, 900000, 900000, 48)])
+def test_launches_of_more_workgroups_are_refused(heads, group, tag, seqs, tokens, most):
+    """Three shares of rows, and pieces for half as many sequences again: past 2^24 workgroups at 256 channels."""
+    s = _shape(head_dim=256, num_kv_heads=heads)
+    m, c = pb.make_model(s), pb.PkvPagedCache(tag=tag)
+    b = pb.PkvBatch(num_seqs=seqs, num_tokens=tokens, max_tokens=most, pages_per_seq=1000)
+    with pytest.raises(pb.PkvError) as e:
+        pb.pkv_attention_workspace(m, c, b, pb.PkvAttention(num_q_heads=heads * group, scale=0.1))
+    assert e.value.status == BAD
