@@ -53,7 +53,7 @@ class _Geometry:
 class PagedCache:
     """A paged cache of all layers.
 
-    ``tag`` FP16: ``k_cache`` and ``v_cache`` of ``dtype``,
+    ``tag`` FP16: ``k_cache`` and ``v_cache`` of ``dtype`` (or int16, its bits),
     ``[L, pool_pages, P, H, D]`` (or without L for one layer), two tensors or
     the K and V views of one paired cache (``device.alloc_caches``).  Other
     tags: ``codes`` uint8 ``[L, pool_pages, H, bytes]`` and ``scales``
@@ -72,7 +72,8 @@ class PagedCache:
             num_layers, pool_pages = k.shape[0], k.shape[1]
             rows = (page_size, num_kv_heads, head_dim)
             _need(k.shape == v.shape and tuple(k.shape[2:]) == rows, "caches are [L, pool_pages, P, H, D]")
-            _need(k.element_size() == 2 and v.element_size() == 2, "caches hold 16-bit values")
+            _need(all(t.dtype in (dtype, torch.int16, torch.uint16) for t in (k, v)),
+                  f"caches hold {dtype} or its bits (int16)")
             page = page_size * num_kv_heads * head_dim
             inner = (num_kv_heads * head_dim, head_dim, 1)
             if k.untyped_storage().data_ptr() == v.untyped_storage().data_ptr() and \

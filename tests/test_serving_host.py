@@ -240,3 +240,20 @@ def test_launches_of_more_workgroups_are_refused(heads, group, tag, seqs, tokens
     with pytest.raises(pb.PkvError) as e:
         pb.pkv_attention_workspace(m, c, b, pb.PkvAttention(num_q_heads=heads * group, scale=0.1))
     assert e.value.status == BAD
+
+
+@pytest.mark.parametrize("dtype,held,ok", [
+    ("float16", "float16", True), ("bfloat16", "bfloat16", True), ("float16", "int16", True), ("bfloat16", "int16", True),
+    ("bfloat16", "uint16", True), ("float16", "bfloat16", False), ("bfloat16", "float16", False),
+    ("bfloat16", "float32", False), ("float16", "int8", False)])
+@pytest.mark.parametrize("which", ["both", "v"])
+def test_a_16_bit_cache_holds_its_own_type_or_bits(dtype, held, ok, which):
+    """Floating caches of the other 16-bit type would be read as this one; bits (as device.alloc_caches makes them) pass,
+    here as far as the refusal of host memory."""
+    torch = pytest.importorskip("torch")
+    from paper_2609_26219_amd import serving
+
+    of = lambda name: torch.zeros((2, 3, 16, 2, 64), dtype=getattr(torch, name))  # noqa: E731
+    with pytest.raises(ValueError, match="device memory" if ok else "hold"):
+        serving.PagedCache(2, 64, 16, getattr(torch, dtype), 0, k_cache=of(held if which == "both" else dtype),
+                           v_cache=of(held))
