@@ -638,3 +638,31 @@ def test_rows_at_one_place(torch, tag, equal):
                     else:
                         a[p, :, :, s] = 0
         assert np.array_equal(g, w)
+
+
+@pytest.mark.parametrize("tag,dtype,D", [(FP16, HALF, 64), (FP16, BF16, 128), (FP16, HALF, 256), (K8V8, BF16, 128),
+                                         (K8V4, HALF, 64), (K4V4, BF16, 256)])
+@pytest.mark.parametrize("new", [1, 4, 60])
+@pytest.mark.parametrize("P", [16, 4])
+def test_infinities_and_nans_that_no_row_sees(torch, tag, dtype, D, new, P):
+    """In few rows and many: behind the sinks and before every row's window, and past the end, in pages that rows do see."""
+    from paper_2609_26219_amd import serving
+
+    n, window, sinks = 150, 40, 5
+    case = Case(97, tag, dtype, 1, 4, D, P, (n,), (new,))
+    clean = case.copy_of_cache()
+    nan = {HALF: 0x7E00, BF16: 0x7FC0}[dtype]
+    inf = {HALF: 0x7C00, BF16: 0x7F80}[dtype]
+    unseen = range(sinks, n - new + 1 - window)
+    assert len(unseen) > 40
+    for t in unseen:
+        p, s = case.table[0, t // P], t % P
+        if tag == FP16:
+            for a in case.cache["kv"]:
+                a[p, s] = (nan, inf, inf | 0x8000)[t % 3]
+        else:
+            case.cache["scales"][p, :, :, s] = (0x7E00, 0x7C00, 0xFC00)[t % 3]
+    out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), window=window,
+                                 sinks=sinks, return_lse=True)
+    case.cache = clean
+    check_attention(case, _down(out), lse.cpu().numpy(), window, sinks)
