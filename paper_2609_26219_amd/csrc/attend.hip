@@ -908,7 +908,8 @@ __device__ __forceinline__ void few_piece(const ServeArgs& s, const AttendArgs& 
     }
   }
 
-  // Join the waves, a row tile at a time: every one's sums relative to the largest reference.
+  // Join the waves, a row tile at a time: every one's sums relative to the largest reference.  A wave whose tokens a row
+  // does not see has l = 0; one that sees NaN alone keeps its reference at -inf, and its l is NaN.
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const float l = over_c_sum(st.l[r]), ref = st.ref[r];
@@ -922,12 +923,12 @@ __device__ __forceinline__ void few_piece(const ServeArgs& s, const AttendArgs& 
     float all = -kInf;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) all = __builtin_fmaxf(all, m.join_ml[w][x][0]);
-    const float part = ref == -kInf ? 0.0f : exp2_of(ref - all);
+    const float part = exp2_of(ref - all);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < kChannels; ++j)
-        m.join[wave][x][(4 * c + i) * kChannels + j] = ref == -kInf ? 0.0f : (st.o[r][j][i] + o_zero) * part;
+        m.join[wave][x][(4 * c + i) * kChannels + j] = l == 0.0f ? 0.0f : (st.o[r][j][i] + o_zero) * part;
     __syncthreads();
     constexpr int kPerRow = kThreads / kRowTile, kPer = D / kPerRow;  // 16 threads to a row
     const int y = threadIdx.x / kPerRow, at = (threadIdx.x % kPerRow) * kPer;
@@ -940,7 +941,7 @@ __device__ __forceinline__ void few_piece(const ServeArgs& s, const AttendArgs& 
     for (int w = 0; w < kWaves; ++w) mm = __builtin_fmaxf(mm, m.join_ml[w][y][0]);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
-      ll += m.join_ml[w][y][0] == -kInf ? 0.0f : m.join_ml[w][y][1] * exp2_of(m.join_ml[w][y][0] - mm);
+      ll += m.join_ml[w][y][1] == 0.0f ? 0.0f : m.join_ml[w][y][1] * exp2_of(m.join_ml[w][y][0] - mm);
     float sum[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {

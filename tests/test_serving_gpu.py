@@ -666,3 +666,24 @@ def test_infinities_and_nans_that_no_row_sees(torch, tag, dtype, D, new, P):
                                  sinks=sinks, return_lse=True)
     case.cache = clean
     check_attention(case, _down(out), lse.cpu().numpy(), window, sinks)
+
+
+@pytest.mark.parametrize("tag", [FP16, K4V4])
+@pytest.mark.parametrize("n,at", [(1, 0), (33, 32), (100, 99), (3000, 2999)])
+def test_a_nan_that_a_row_sees_reaches_its_result(torch, tag, n, at):
+    """Keys of one token are NaN, the only one in its tile of 32, its wave or its row: the result is NaN, not that of the
+    other tokens (or, without others, of an empty row)."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(98, tag, BF16, 1, 2, 64, 16, (n,), (1,))
+    p, s = case.table[0, at // 16], at % 16
+    if tag == FP16:
+        case.cache["kv"][0][p, s] = 0x7FC0
+    else:
+        case.cache["scales"][p, :, 0, s] = 0x7E00
+    out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+    case.lens[0] = at  # up to that token
+    if at:
+        out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
+        check_attention(case, _down(out), lse.cpu().numpy())
