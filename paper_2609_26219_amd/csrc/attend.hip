@@ -1246,6 +1246,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * slot) = f32x2{st.ref[r], l};
       continue;
     }
+    // (A row that sees nothing has 0 times the values that others see, and those may be infinite.)
     const float inv = inverse(l);
     uint16_t* to = a.out + int64_t(g.start + token) * a.out_token_stride + int64_t(out_head) * a.out_head_stride;
 #pragma unroll
@@ -1254,7 +1255,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(ServeArgs s, A
       for (int j = 0; j < kChannels; j += 4) {
         float w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (st.o[r][j + e][i] + o_zero) * inv;
+        for (int e = 0; e < 4; ++e) w[e] = l == 0.0f ? 0.0f : (st.o[r][j + e][i] + o_zero) * inv;
         *reinterpret_cast<u32x2*>(to + (4 * c + i) * kChannels + j) =
             s.bf16 ? u32x2{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])} : u32x2{pack_f16(w[0], w[1]), pack_f16(w[2], w[3])};
       }

@@ -687,3 +687,19 @@ def test_a_nan_that_a_row_sees_reaches_its_result(torch, tag, n, at):
     if at:
         out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
         check_attention(case, _down(out), lse.cpu().numpy())
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF16])
+@pytest.mark.parametrize("n", [60, 5000])
+@pytest.mark.parametrize("new", [3, 45])
+def test_a_row_that_sees_nothing_is_zero_whatever_others_see(torch, dtype, n, new):
+    """Rows without a position beside rows that see infinite values."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(99, FP16, dtype, 1, 1, 128, 16, (n,), (new,), scattered=True)
+    case.positions[:] = n - 1
+    case.positions[1::3] = -1
+    case.cache["kv"][1][case.table[0, 1], 3] = {HALF: 0x7C00, BF16: 0x7F80}[dtype]
+    out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
+    assert (out[1::3] == 0).all() and torch.isneginf(lse[1::3]).all()
+    assert torch.isinf(out[0::3]).all() and torch.isfinite(lse[0::3]).all()
