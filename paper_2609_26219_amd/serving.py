@@ -123,7 +123,7 @@ class PagedCache:
     def _at(self, layer: int) -> binding.PkvPagedCache:
         """The cache of one layer as the library takes it.  No call writes to it: threads may be in calls of different
         layers at once."""
-        return self._layers[layer] if 0 <= layer < self.num_layers else self._of_layer(layer)  # (the library refuses it)
+        return self._layers[layer] if 0 <= layer < self.num_layers else self._of_layer(-1)  # (the library refuses it)
 
     def workspace(self, nbytes: int, stream: int) -> int:
         """Address of scratch memory for attention calls on one stream (they follow each other), grown as needed.  A
@@ -174,6 +174,11 @@ def _strides(t) -> tuple:
     return (token if tokens > 1 else heads * head), head
 
 
+def _int32(tokens: int) -> int:
+    """A number of tokens for the library: past every sequence where it is past 32 bits, below zero where it is."""
+    return max(-1, min(tokens, 0x7FFFFFFF))
+
+
 def _stream(cache: PagedCache) -> int:
     """The current stream of the cache's device (torch.cuda.current_stream(...).cuda_stream without the object: 0.1 us
     against 1.9)."""
@@ -219,9 +224,9 @@ def attention(cache: PagedCache, batch: Batch, q, scale: Optional[float] = None,
     else:
         _rows(cache, batch, heads, q, out)
     lse = q.new_empty((batch.num_tokens, heads), dtype=torch.float32) if return_lse else None
-    a = binding.PkvAttention(heads, window, sinks, cache.head_dim ** -0.5 if scale is None else scale, q.data_ptr(),
-                             *_strides(q), out.data_ptr(), *_strides(out), lse.data_ptr() if return_lse else None,
-                             None, 0)
+    a = binding.PkvAttention(heads, _int32(window), _int32(sinks), cache.head_dim ** -0.5 if scale is None else scale,
+                             q.data_ptr(), *_strides(q), out.data_ptr(), *_strides(out),
+                             lse.data_ptr() if return_lse else None, None, 0)
     stream = _stream(cache)
     struct = cache._at(layer)
     nbytes = binding.pkv_attention_workspace(cache.model, struct, batch.struct, a)

@@ -703,3 +703,17 @@ def test_a_row_that_sees_nothing_is_zero_whatever_others_see(torch, dtype, n, ne
     out, lse = serving.attention(_cache(torch, case), _batch(torch, case), _up(torch, case.q, case), return_lse=True)
     assert (out[1::3] == 0).all() and torch.isneginf(lse[1::3]).all()
     assert torch.isinf(out[0::3]).all() and torch.isfinite(lse[0::3]).all()
+
+
+@pytest.mark.parametrize("tag", [FP16, K4V4])
+@pytest.mark.parametrize("new", [2, 50])
+def test_windows_and_sinks_past_every_sequence_cover_it(torch, tag, new):
+    from paper_2609_26219_amd import serving
+
+    case = Case(101, tag, BF16, 1, 2, 64, 16, (1500, 70), (new,))
+    cache, batch, q = _cache(torch, case), _batch(torch, case), _up(torch, case.q, case)
+    want = serving.attention(cache, batch, q)
+    check_attention(case, _down(want), case.attend()[1].astype(np.float32))
+    for window, sinks in ((1 << 40, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 1 << 33), (1 << 32, 5)):
+        out, lse = serving.attention(cache, batch, q, window=window, sinks=sinks, return_lse=True)
+        check_attention(case, _down(out), lse.cpu().numpy())

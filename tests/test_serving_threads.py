@@ -156,3 +156,24 @@ def test_scratch_memory_is_free_again_after_a_refused_call(monkeypatch, one_stre
     again = Thread(lambda: serving.attention(cache, batch, _rows(4)))
     again.start()
     again.join()
+
+
+def test_numbers_past_32_bits_do_not_wrap(monkeypatch, one_stream):
+    """A layer past 32 bits is refused as any other that is not there; a window or sinks past them cover everything."""
+    cache, batch = _cache(), _batch(1)
+    for layer in (1 << 32, -(1 << 32), (1 << 32) + 1):
+        with pytest.raises(pb.PkvError) as e:
+            serving.append(cache, batch, _rows(2), _rows(2), layer=layer)
+        assert e.value.status == pb.PKV_ERR_INVALID_ARGUMENT
+    for past in (1 << 31, 1 << 32, (1 << 32) + 4, 1 << 70):
+        for kw in (dict(window=-past), dict(window=1 - past), dict(sinks=-past)):
+            with pytest.raises(pb.PkvError) as e:
+                serving.attention(cache, batch, _rows(4), **kw)
+            assert e.value.status == pb.PKV_ERR_INVALID_ARGUMENT
+    seen = []
+    monkeypatch.setattr(pb, "pkv_attention_workspace", lambda *a: 0)
+    monkeypatch.setattr(pb, "pkv_attention_status", lambda m, c, b, a, s: seen.append((a.window, a.sinks)) or pb.PKV_OK)
+    for past in (1 << 31, 1 << 32, (1 << 32) + 4, 1 << 70):
+        serving.attention(cache, batch, _rows(4), window=past, sinks=past)
+        serving.attention(cache, batch, _rows(4), window=7, sinks=2)
+    assert set(seen) == {(2 ** 31 - 1, 2 ** 31 - 1), (7, 2)}
