@@ -717,3 +717,39 @@ def test_windows_and_sinks_past_every_sequence_cover_it(torch, tag, new):
     for window, sinks in ((1 << 40, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 1 << 33), (1 << 32, 5)):
         out, lse = serving.attention(cache, batch, q, window=window, sinks=sinks, return_lse=True)
         check_attention(case, _down(out), lse.cpu().numpy())
+
+
+@pytest.mark.parametrize("own_stream", [True, False])
+def test_threads_on_one_cache(torch, own_stream):
+    """Two host threads, each on a layer of its own (of one cache), on streams of their own or on one: every attention has
+    the bits that it has alone."""
+    import threading
+
+    from paper_2609_26219_amd import serving
+
+    case = Case(103, K4V4, BF16, 2, 4, 64, 16, (1500, 300), (1,), layers=2, layer=0)
+    cache, batch, q = _cache(torch, case), _batch(torch, case), _up(torch, case.q, case)
+    cache.codes[1], cache.scales[1] = cache.codes[0].flip(-1), cache.scales[0] * 0.5
+    want = [serving.attention(cache, batch, q, layer=layer) for layer in range(2)]
+    assert not torch.equal(*want)
+    torch.cuda.synchronize()
+    results, errors = [[], []], []
+    shared = torch.cuda.Stream()
+
+    def work(layer):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream() if own_stream else shared):
+                for _ in range(40):
+                    results[layer].append(serving.attention(cache, batch, q, layer=layer))
+                torch.cuda.current_stream().synchronize()
+        except BaseException as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(layer,)) for layer in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not errors and [len(r) for r in results] == [40, 40]
+    for layer in range(2):
+        assert all(torch.equal(r, want[layer]) for r in results[layer])
