@@ -8,12 +8,17 @@
 // every wave rows of its own and shares the tokens in LDS.  A wave keeps the running maximum and
 // sum of the softmax, and what was cut is joined at the end: one pass over the cache.
 //
-// Few rows are bound by the cache's bytes and, in 4 bits, by decoding them: 32 ragged sequences (255 thousand tokens, 8
-// heads of 128, 4 query heads each) take 66 us, 4.2 TB/s, the vector units busy 51% of it; with a
-// window of 1024 over 16-bit pages 22.5 us, 5.0 TB/s.  Many rows are bound by the vector units (the softmax), which the
-// matrix units wait for: 2825 rows of 32 heads behind up to 10240 tokens in 8 and 4 bits run at 684 TFLOP/s,
-// vector units busy 60%, matrix units 26%, LDS 32%; 1229 scattered rows over 32768 tokens in 16 bits at 689 (41%, 28%,
-// 26%).  A large library product in bfloat16 reaches 1235.
+// Few rows wait for the cache's bytes and, over codes, for their decoding as well: 32 ragged sequences (255 thousand tokens,
+// 8 heads of 128, 4 query heads each) in 4 bits take 65 to 68 us, 4.1 to 4.3 TB/s where a large copy reaches 5.2, with the
+// vector units busy 52% of it; over 16-bit pages 203 us, 5.1 TB/s, and with a window of 1024 21.4 us, 5.3 TB/s (its
+// 113 MB partly in the 256 MB cache).
+// Many rows over codes share their time between the vector units (the softmax, scales and zeros) and the matrix units, which
+// two waves a SIMD seldom overlap: 2825 rows of 32 heads behind up to 10240 tokens in 8 and 4 bits run at 681 TFLOP/s,
+// vector units busy 62%, matrix units 27%, LDS 32%.  Over 16 bits no unit is busy half of the time (1229 scattered rows
+// over 32768 tokens: 675 to 689 TFLOP/s, 42%, 29%, 27%): two waves a SIMD do not cover each other's waits, and 250 of 256
+// registers leave no room for a third or for work of the next tile.  A large library product in bfloat16 reaches 1235.
+// At 256 channels the kernels over 16 bits spill registers (many rows 21, few rows 42,
+// 74 with pages below 16 slots): 2825 rows 571 TFLOP/s against 770 at 128 channels, a decode step 4.5 TB/s.
 //
 // For its tile a wave computes S^T = K Q^T and then O^T += V^T P^T with
 // 16x16x32 matrix instructions.  With lane l = (c = l / 16, x = l % 16):
@@ -41,7 +46,10 @@
 // without it) and is lost in a bfloat16 one's (1.6e-3): for binary16 results p_t s_t goes in as two binary16 numbers, the
 // second what the first leaves.
 // Queries go in as binary16 too, each row scaled by a power of two.  16-bit caches use the
-// matrix instructions of their own type, p_t rounded to it.
+// matrix instructions of their own type, p_t rounded to it: 2.2e-3 of a bfloat16 result in all, 1.5e-4 to 2.9e-4 of a
+// binary16 one (1.65e-3, and 1.2e-4 to 2.1e-4, are the result's own rounding).  With two numbers there as well, 8192 rows
+// with a window take 283 us instead of 240 and 1229 scattered rows 610 instead of 510, and an infinite value that a row
+// sees becomes NaN, the sum of both numbers' products with it, where one number keeps it.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -231,7 +239,8 @@ __device__ __forceinline__ void load_at(uint32_t* to, const void* base, uint32_t
 
 // Where a segment's cache begins, and where a tile's tokens lie in it.  WHOLE: pages hold 16 slots or more, so each
 // half of a tile lies on one page, whose number the wave shares (-1: not there); else every lane looks its tokens up
-// (32 ragged sequences over 4 bits: 65 us, and 231 with every lane's lookups).
+// (32 ragged sequences over 4 bits: 74 us, join included, on pages of 16; on pages of 8, with every lane's lookups, 271, of
+// 1 slot 229).
 // Tokens that are not there are read from page 0, which exists.
 struct Source {
   const char* k;           // page 0, slot 0 of the head
