@@ -216,7 +216,10 @@ def attention(cache: PagedCache, batch: Batch, q, scale: Optional[float] = None,
     """Attention of rows ``q`` ``[num_tokens, Hq, D]`` over the cache, causal by position: a row at position p sees
     tokens t <= p and, with a window, those with p - t < window or t < sinks.  ``scale`` defaults to D ** -0.5.
     Returns ``out`` ``[num_tokens, Hq, D]``, with ``return_lse`` also the rows' log-sum-exp, float32
-    ``[num_tokens, Hq]``.  A row that sees nothing gives 0 and -inf."""
+    ``[num_tokens, Hq]``.  A row that sees nothing gives 0 and -inf.
+
+    How a call is cut follows from its longest sequence of rows: a prompt's chunk and the decode rows of other
+    sequences are faster as two calls."""
     heads = q.shape[1]
     if out is None:
         out = torch.empty_like(q)
