@@ -562,19 +562,12 @@ __device__ __forceinline__ int32_t scalar_entry(const int32_t* table, int32_t at
 }
 
 // The rows of a call that a workgroup shares: one sequence's, of one KV head.
-struct Group {
+struct Group : SequenceRows {
   int32_t head, split, tile, seq;
-  int32_t start, count, kv_len, trail;  // rows [start, start + count); the last row of the sequence is `trail` rows on
 };
 
 __device__ __forceinline__ Group group_from(const ServeArgs& s, int32_t start, int32_t end, int32_t kv_len) {
-  Group g{};
-  g.start = start < 0 ? 0 : start;
-  end = end < s.num_tokens ? end : s.num_tokens;
-  g.trail = end - g.start;
-  g.count = g.trail < s.max_tokens ? g.trail : s.max_tokens;
-  g.kv_len = kv_len < 0 ? 0 : kv_len < s.max_kv ? kv_len : s.max_kv;
-  return g;
+  return Group{rows_of_sequence(s, start, end, kv_len), 0, 0, 0, 0};
 }
 
 __device__ __forceinline__ Group group_of_sequence(const ServeArgs& s, int32_t seq) {

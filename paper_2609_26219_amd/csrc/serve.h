@@ -38,6 +38,22 @@ struct ServeArgs {
   int32_t tag, bf16;
 };
 
+// A sequence's rows [start, start + count) of a call and its tokens in the cache; the last row is `trail` rows on from the first.
+struct SequenceRows {
+  int32_t start, count, kv_len, trail;
+};
+
+// From what the device's arrays hold, whatever that is (constexpr: for the kernels and the host's tests).
+constexpr SequenceRows rows_of_sequence(const ServeArgs& s, int32_t start, int32_t end, int32_t kv_len) {
+  SequenceRows r{};
+  r.start = start < 0 ? 0 : start < s.num_tokens ? start : s.num_tokens;
+  end = end < 0 ? 0 : end < s.num_tokens ? end : s.num_tokens;
+  r.trail = end - r.start;
+  r.count = r.trail < s.max_tokens ? r.trail : s.max_tokens;
+  r.kv_len = kv_len < 0 ? 0 : kv_len < s.max_kv ? kv_len : s.max_kv;
+  return r;
+}
+
 struct RowArgs {
   uint16_t* k;
   uint16_t* v;

@@ -753,3 +753,47 @@ def test_threads_on_one_cache(torch, own_stream):
     assert not errors and [len(r) for r in results] == [40, 40]
     for layer in range(2):
         assert all(torch.equal(r, want[layer]) for r in results[layer])
+
+
+LEAST, MOST = -2 ** 31, 2 ** 31 - 1
+GARBAGE = [
+    # token_start, kv_lens of three sequences
+    ([LEAST, 4, 4, MOST], [MOST, 0, MOST]),
+    ([0, 4, 9, LEAST], [LEAST, MOST, 50]),
+    ([3, LEAST, MOST, 7], [40, 50, LEAST]),
+    ([MOST, LEAST, MOST, LEAST], [MOST, MOST, MOST]),
+    ([-5, LEAST + 3, 6, 1 << 30], [-1, 1 << 30, 60]),
+]
+
+
+@pytest.mark.parametrize("starts,lens", GARBAGE)
+@pytest.mark.parametrize("tag,group,width", [(FP16, 1, 10), (FP16, 8, 10), (K4V4, 2, 200), (K8V4, 16, 200), (FP16, 16, 300)])
+@pytest.mark.parametrize("scattered", [False, True])
+def test_device_arrays_of_any_contents_stay_within_the_buffers(torch, tag, group, width, starts, lens, scattered):
+    """Starts, lengths, positions and page tables as memory that nobody has filled may hold them (the host cannot look):
+    every call ends, writes its own rows alone, and the next call is right."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(109, tag, BF16, 2, group, 64, 16, (70, 90, 130), (3, 4, 3), scattered=scattered, wide=width - 9)
+    cache, batch = _cache(torch, case), _batch(torch, case, bounds=False)
+    good = [None if t is None else t.clone() for t in batch.keep]
+    fused = torch.full((case.tokens + 8, 2 * group + 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    out, k, v = (fused[4:-4, a:b] for a, b in ((0, 2 * group), (2 * group, 2 * group + 2), (2 * group + 2, 2 * group + 4)))
+    q = _up(torch, case.q, case)
+    rng = np.random.default_rng(1)
+    up = lambda a: torch.from_numpy(np.asarray(a, np.int64).astype(np.int32)).cuda()  # noqa: E731
+    batch.keep[0].copy_(up(starts))
+    batch.keep[1].copy_(up(lens))
+    batch.keep[2].copy_(up(rng.choice([LEAST, -1, 0, 1, case.pool - 1, case.pool, MOST], case.table.shape)))
+    if scattered:
+        batch.keep[3].copy_(up(rng.choice([LEAST, -1, 0, 5, 159, 1 << 30, MOST], case.tokens)))
+    for window, sinks in ((0, 0), (20, 3)):
+        serving.attention(cache, batch, q, out=out, window=window, sinks=sinks, return_lse=True)
+    serving.read(cache, batch, out=(k, v))
+    torch.cuda.synchronize()
+    assert (fused[:4] == 7.0).all() and (fused[-4:] == 7.0).all()
+    for t, g in zip(batch.keep, good):
+        if t is not None:
+            t.copy_(g)
+    got, lse = serving.attention(cache, batch, q, return_lse=True)
+    check_attention(case, _down(got), lse.cpu().numpy())

@@ -257,3 +257,21 @@ def test_a_16_bit_cache_holds_its_own_type_or_bits(dtype, held, ok, which):
     with pytest.raises(ValueError, match="device memory" if ok else "hold"):
         serving.PagedCache(2, 64, 16, getattr(torch, dtype), 0, k_cache=of(held if which == "both" else dtype),
                            v_cache=of(held))
+
+
+def test_rows_of_a_sequence_stay_within_the_call(tmp_path):
+    """The kernels' clamps of what the host cannot see, compiled for the host (serve_rows_check.cpp)."""
+    import os
+    import shutil
+    import subprocess
+
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no g++")
+    here = os.path.dirname(os.path.abspath(__file__))
+    root, exe = os.path.dirname(here), str(tmp_path / "check")
+    subprocess.run([cxx, "-O1", "-fwrapv", "-std=c++17", "-Wall", "-Wextra", "-I", os.path.join(root, "include"),
+                    "-I", os.path.join(root, "paper_2609_26219_amd", "csrc"), os.path.join(here, "serve_rows_check.cpp"),
+                    "-o", exe], check=True)
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert run.returncode == 0, run.stdout + run.stderr
