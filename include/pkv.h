@@ -467,6 +467,42 @@ pkv_status_t pkv_cache_append(const pkv_model_t* model, const pkv_paged_cache_t*
 pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch, void* k,
                             void* v, int64_t token_stride, int64_t head_stride, void* hip_stream);
 
+/* Rotary positions: row i of a sequence at logical position p turns as at p +
+ * position_offset[sequence] (what an eviction took out before it), by the model's
+ * own RoPE (rope_style, rotary_dim, inv_freq or rope_theta of pkv_model_t):
+ *   pair j = (x, y) with a = (p + offset) * f_j becomes
+ *   amplitude * (x cos a - y sin a, x sin a + y cos a),
+ * channels past rotary_dim stay.  Angles, cosines and products are double precision
+ * (as in the restore, whose re-phased keys these are), rounded to single and then to
+ * out_dtype.  A row without a position (negative) is copied; rows of no sequence are
+ * not written.
+ *   x, out : [num_tokens][num_heads][head_dim] of out_dtype at the strides
+ *     (elements; alignment as in pkv_cache_append); out may be x itself with
+ *     the same strides, else must not overlap an input. */
+typedef struct {
+  int32_t num_heads;              /* >= 0; 0: x and out are not looked at */
+  float amplitude;                /* finite; 1 but for scaled long contexts */
+  const int32_t* position_offset; /* device [num_seqs], or NULL = 0 */
+  const void* x;
+  int64_t x_token_stride, x_head_stride;
+  void* out;
+  int64_t out_token_stride, out_head_stride;
+} pkv_rotation_t;
+
+/* Turn the rows rotation->x (queries or keys; positions from the batch, whose
+ * page_table is not read).  One kernel on `hip_stream`.  Errors:
+ * PKV_ERR_INVALID_ARGUMENT, PKV_ERR_DEVICE. */
+pkv_status_t pkv_rotate(const pkv_model_t* model, const pkv_batch_t* batch, const pkv_rotation_t* rotation,
+                        void* hip_stream);
+
+/* pkv_rotate of the queries rotation->x and pkv_cache_append of the keys k,
+ * turned alike (and rounded to out_dtype), and the values v, in one kernel on
+ * `hip_stream`: codes and scales are those of the two calls one after the other.
+ * k and v are only read.  Errors as pkv_cache_append. */
+pkv_status_t pkv_cache_append_rotated(const pkv_model_t* model, const pkv_paged_cache_t* cache,
+                                      const pkv_batch_t* batch, const void* k, const void* v, int64_t token_stride,
+                                      int64_t head_stride, const pkv_rotation_t* rotation, void* hip_stream);
+
 /* Attention of the batch's rows over the cache.  Row i of a sequence at position
  * p sees the cached tokens t with t < kv_lens, t <= p and, if window > 0,
  * p - t < window or t < sinks (the last `window` tokens and the first `sinks`).

@@ -1,5 +1,6 @@
 """Oracle of the serving calls (include/pkv.h, "Serving from a paged cache"):
-rows quantised into a paged cache, read back, and attention over it.
+rows quantised into a paged cache, read back, turned to their positions, and
+attention over it.
 
 Plain NumPy in fp64, one row and one head at a time.  Test infrastructure only;
 imports nothing from the package.  A cache is a dict with the arrays the
@@ -64,6 +65,23 @@ def append(cache, tag, page, where, k_bits, v_bits, dtype):
                 tile = cache["codes"][phys, h, lo:hi].reshape(page, -1)
                 tile[slot] = codes if bits == 8 else codes[0::2] | (codes[1::2] << 4)
                 cache["scales"][phys, h, which, slot] = np.array([scale, zero], np.float16).view(np.uint16)
+
+
+def rotate(x, where, offset, freq, interleaved, amplitude):
+    """Rows ``x`` (fp64 [tokens][heads][D]) turned to their positions, pair j by (position + offset[sequence]) * freq[j];
+    rows without a position as they are."""
+    out = x.copy()
+    n = 2 * len(freq)
+    first, second = (slice(0, n, 2), slice(1, n, 2)) if interleaved else (slice(0, n // 2), slice(n // 2, n))
+    for i, (s, pos, _, _) in enumerate(where):
+        if s < 0 or pos < 0:
+            continue
+        angle = (float(pos + int(offset[s])) * np.asarray(freq, np.float64)).astype(np.longdouble)
+        c, sn = amplitude * np.cos(angle), amplitude * np.sin(angle)
+        a, b = x[i][:, first], x[i][:, second]
+        out[i][:, first] = a * c - b * sn
+        out[i][:, second] = a * sn + b * c
+    return out
 
 
 def row(cache, tag, page, dtype, which, phys, slot, head):

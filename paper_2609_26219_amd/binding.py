@@ -27,7 +27,7 @@ PKV_ERR_DEVICE = -7
 EXPORTED = ("pkv_payload_size", "pkv_restore_plan", "pkv_restore", "pkv_restore_from_host", "pkv_free",
             "pkv_plan_query", "pkv_status_string", "pkv_checkpoint_plan", "pkv_quantize_gather", "pkv_plan_repair",
             "pkv_plan_payload_bytes", "pkv_restore_from_host_noalloc", "pkv_cache_size", "pkv_cache_append",
-            "pkv_cache_read", "pkv_attention_workspace", "pkv_attention")
+            "pkv_cache_read", "pkv_attention_workspace", "pkv_attention", "pkv_rotate", "pkv_cache_append_rotated")
 
 
 class PkvModel(ctypes.Structure):
@@ -69,6 +69,12 @@ class PkvBatch(ctypes.Structure):
     _fields_ = [("num_seqs", ctypes.c_int32), ("num_tokens", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
                 ("pages_per_seq", ctypes.c_int32), ("max_kv_len", ctypes.c_int64), ("token_start", ctypes.c_void_p),
                 ("kv_lens", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
+class PkvRotation(ctypes.Structure):
+    _fields_ = [("num_heads", ctypes.c_int32), ("amplitude", ctypes.c_float), ("position_offset", ctypes.c_void_p),
+                ("x", ctypes.c_void_p), ("x_token_stride", ctypes.c_int64), ("x_head_stride", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
 
 
 class PkvAttention(ctypes.Structure):
@@ -134,6 +140,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pkv_attention_workspace.restype = i32
     lib.pkv_attention.argtypes = [model, cache, batch, attention, vp]
     lib.pkv_attention.restype = i32
+    rotation = ctypes.POINTER(PkvRotation)
+    lib.pkv_rotate.argtypes = [model, batch, rotation, vp]
+    lib.pkv_rotate.restype = i32
+    lib.pkv_cache_append_rotated.argtypes = [model, cache, batch, vp, vp, i64, i64, rotation, vp]
+    lib.pkv_cache_append_rotated.restype = i32
     _lib = lib
     return lib
 
@@ -453,3 +464,12 @@ def pkv_attention_workspace(model: PkvModel, cache: PkvPagedCache, batch: PkvBat
 def pkv_attention_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, attention: PkvAttention,
                          stream=0) -> int:
     return load().pkv_attention(model, cache, batch, attention, stream or None)
+
+
+def pkv_rotate_status(model: PkvModel, batch: PkvBatch, rotation: PkvRotation, stream=0) -> int:
+    return load().pkv_rotate(model, batch, rotation, stream or None)
+
+
+def pkv_cache_append_rotated_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, k, v, token_stride: int,
+                                    head_stride: int, rotation: PkvRotation, stream=0) -> int:
+    return load().pkv_cache_append_rotated(model, cache, batch, k, v, token_stride, head_stride, rotation, stream or None)

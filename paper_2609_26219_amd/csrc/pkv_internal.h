@@ -431,6 +431,9 @@ uint64_t cache_bytes(const pkv_model_t& m);  // of each separate cache, or of th
 
 // The constraints of pkv_model_t.
 pkv_status_t check_model(const pkv_model_t* m);
+// Rotated channels per head, and the frequency of rotary pair i.
+int32_t rotary_dim(const pkv_model_t& m);
+double rope_frequency(const pkv_model_t& m, int64_t i);
 
 // The cache pointers of a call against the model's layout: both 16-byte
 // aligned; separate caches of cache_bytes each must not overlap; a paired

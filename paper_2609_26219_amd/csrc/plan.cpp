@@ -58,10 +58,6 @@ pkv_status_t check_model(const pkv_model_t* m) {
   return PKV_OK;
 }
 
-namespace {
-
-// RoPE helpers: rotated channels per head, the frequency of pair i, and the
-// pair that element e of key piece j rotates (k = 8j + e; -1 = none).
 int32_t rotary_dim(const pkv_model_t& m) { return m.rotary_dim ? m.rotary_dim : m.head_dim; }
 
 double rope_frequency(const pkv_model_t& m, int64_t i) {
@@ -69,6 +65,9 @@ double rope_frequency(const pkv_model_t& m, int64_t i) {
   return m.inv_freq ? m.inv_freq[i] : pow(m.rope_theta, -2.0 * double(i) / double(R));
 }
 
+namespace {
+
+// The pair that element e of key piece j rotates (k = 8j + e; -1 = none).
 int64_t rope_table_pair(const pkv_model_t& m, int64_t k) {
   const int64_t D = m.head_dim, R = rotary_dim(m);
   const int64_t j = k / 8, e = k % 8;

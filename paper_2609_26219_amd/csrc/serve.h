@@ -60,6 +60,20 @@ struct RowArgs {
   int64_t token_stride, head_stride;
 };
 
+// Rows turned to their positions, and how.
+struct RotateArgs {
+  const int32_t* offset;  // of each sequence, or null
+  const uint16_t* x;
+  uint16_t* out;
+  int64_t x_token_stride, x_head_stride, out_token_stride, out_head_stride;
+  double amplitude;
+  int32_t heads;
+  int32_t rotary;       // channels that turn
+  int32_t interleaved;  // pairs (2j, 2j + 1), else (j, j + rotary / 2)
+  int32_t reserved;
+  double freq[kMaxHeadDim / 2];  // of each pair: an argument, so that a call needs no device memory for it
+};
+
 struct AttendArgs {
   const uint16_t* q;
   uint16_t* out;
@@ -115,6 +129,8 @@ pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache
                         bool pointers, ServeArgs* out);
 pkv_status_t row_args(const ServeArgs& s, const void* k, const void* v, int64_t token_stride, int64_t head_stride,
                       RowArgs* out);
+pkv_status_t batch_args(const pkv_model_t* model, const pkv_batch_t* batch, bool pointers, ServeArgs* out);
+pkv_status_t rotate_args(const pkv_model_t& m, const ServeArgs& s, const pkv_rotation_t* rotation, RotateArgs* out);
 pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool pointers, AttendArgs* out);
 AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a);
 

@@ -60,28 +60,33 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   }
 }
 
-// Where row i of the call lies: its slot in the cache (page * P + slot in the
-// page), -1 where there is none, -2 for a row of no sequence.  `starts` is token_start, in LDS if it fits there.
-__device__ __forceinline__ int64_t place_of(const ServeArgs& a, const int32_t* starts, int32_t i) {
+// Row i of the call: its sequence (-1: of none) and its position there.  `starts` is token_start, in LDS if it fits there.
+struct RowOf {
+  int32_t seq;
+  int64_t pos;
+};
+__device__ __forceinline__ RowOf row_of(const ServeArgs& a, const int32_t* starts, int32_t i) {
   int32_t s = 0;
   for (int32_t end = a.num_seqs; end - s > 1;) {
     const int32_t mid = s + (end - s) / 2;
     if (starts[mid] <= i) s = mid; else end = mid;
   }
   const int32_t end = starts[s + 1] < a.num_tokens ? starts[s + 1] : a.num_tokens;
-  if (i < starts[s] || i >= end) return -2;
-  int64_t pos;
-  if (a.positions) {
-    pos = a.positions[i];
-  } else {
-    const int32_t len = a.kv_lens[s];
-    pos = int64_t(len < a.max_kv ? len : a.max_kv) - (end - i);
-  }
-  const int64_t page_at = pos >> a.log2P;
-  if (pos < 0 || page_at >= a.pages_per_seq) return -1;
-  const int64_t page = a.page_table[int64_t(s) * a.pages_per_seq + page_at];
+  if (i < starts[s] || i >= end) return RowOf{-1, -1};
+  if (a.positions) return RowOf{s, a.positions[i]};
+  const int32_t len = a.kv_lens[s];
+  return RowOf{s, int64_t(len < a.max_kv ? len : a.max_kv) - (end - i)};
+}
+
+// Where the row lies: its slot in the cache (page * P + slot in the
+// page), -1 where there is none, -2 for a row of no sequence.
+__device__ __forceinline__ int64_t place_of(const ServeArgs& a, const RowOf& row) {
+  if (row.seq < 0) return -2;
+  const int64_t page_at = row.pos >> a.log2P;
+  if (row.pos < 0 || page_at >= a.pages_per_seq) return -1;
+  const int64_t page = a.page_table[int64_t(row.seq) * a.pages_per_seq + page_at];
   if (page < 0 || page >= a.pool_pages) return -1;
-  return (page << a.log2P) | (pos & ((int64_t(1) << a.log2P) - 1));
+  return (page << a.log2P) | (row.pos & ((int64_t(1) << a.log2P) - 1));
 }
 
 // Where a token's rows of head 0 lie: bytes from the layer's first key (code) and value (code), words from its first scale; k < 0
@@ -90,16 +95,23 @@ struct Place {
   int64_t k, v, scale;
 };
 
-// The places of tokens [i0, i0 + n) into `place`, by the whole workgroup.
-template <int KB, int VB>
-__device__ __forceinline__ void find_places(const ServeArgs& a, int32_t i0, int32_t n, int32_t* starts, Place* place) {
+// The rows of tokens [i0, i0 + n), a thread each, by the whole workgroup.
+__device__ __forceinline__ RowOf find_row(const ServeArgs& a, int32_t i0, int32_t n, int32_t* starts) {
   const int tid = threadIdx.x;
   const bool in_lds = a.num_seqs < kStartsInLds;
   if (in_lds)
     for (int32_t j = tid; j <= a.num_seqs; j += kThreads) starts[j] = a.token_start[j];
   __syncthreads();
+  if (tid >= n) return RowOf{-1, -1};
+  return in_lds ? row_of(a, starts, i0 + tid) : row_of(a, a.token_start, i0 + tid);
+}
+
+// The places of their rows into `place`.
+template <int KB, int VB>
+__device__ __forceinline__ void find_places(const ServeArgs& a, const RowOf& row, int32_t n, Place* place) {
+  const int tid = threadIdx.x;
   if (tid < n) {
-    const int64_t at = in_lds ? place_of(a, starts, i0 + tid) : place_of(a, a.token_start, i0 + tid);
+    const int64_t at = place_of(a, row);
     Place p{at, at, at};
     if (at >= 0) {
       const int64_t page = at >> a.log2P, slot = at & ((int64_t(1) << a.log2P) - 1);
@@ -270,15 +282,135 @@ __device__ __forceinline__ u32x4 get(const uint8_t* row, uint32_t sz, int32_t pi
   return u32x4{pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3]), pack2<BF16>(x[4], x[5]), pack2<BF16>(x[6], x[7])};
 }
 
+// Sine and cosine of an angle.  The nearest multiple n of pi / 2 is taken off in three parts (Cody and Waite): n times
+// the first, whose last bit is 2^-52, off an angle of 1 or more is exact in one fused step; what the second leaves out
+// is 2^-108 n.  Then the Taylor series, which end below 2^-58 at pi / 4.
+__device__ __forceinline__ void sine_cosine(double angle, double* sine, double* cosine) {
+  const double n = __builtin_rint(angle * 0.63661977236758134);
+  double r = __builtin_fma(-n, 1.5707963267948966, angle);
+  r = __builtin_fma(-n, 6.123233995736766e-17, r);
+  r = __builtin_fma(-n, -1.4973849048591698e-33, r);
+  const double x = r * r;
+  // 1 / 3!, 1 / 5!, .. 1 / 17! and 1 / 2!, .. 1 / 18!, signs in turn
+  double s = __builtin_fma(x, 1.0 / 355687428096000.0, -1.0 / 1307674368000.0);
+  s = __builtin_fma(x, s, 1.0 / 6227020800.0);
+  s = __builtin_fma(x, s, -1.0 / 39916800.0);
+  s = __builtin_fma(x, s, 1.0 / 362880.0);
+  s = __builtin_fma(x, s, -1.0 / 5040.0);
+  s = __builtin_fma(x, s, 1.0 / 120.0);
+  s = __builtin_fma(x, s, -1.0 / 6.0);
+  s = __builtin_fma(x * r, s, r);
+  double c = __builtin_fma(x, -1.0 / 6402373705728000.0, 1.0 / 20922789888000.0);
+  c = __builtin_fma(x, c, -1.0 / 87178291200.0);
+  c = __builtin_fma(x, c, 1.0 / 479001600.0);
+  c = __builtin_fma(x, c, -1.0 / 3628800.0);
+  c = __builtin_fma(x, c, 1.0 / 40320.0);
+  c = __builtin_fma(x, c, -1.0 / 720.0);
+  c = __builtin_fma(x, c, 1.0 / 24.0);
+  c = __builtin_fma(x, c, -0.5);
+  c = __builtin_fma(x, c, 1.0);
+  const int quarter = static_cast<int>(n - 4.0 * __builtin_floor(n * 0.25));
+  const double a = quarter & 1 ? c : s, b = quarter & 1 ? s : c;
+  *sine = quarter & 2 ? -a : a;
+  *cosine = (quarter + 1) & 2 ? -b : b;
+}
+
+// What turns a token's pairs, one after the other: amplitude times cosine and sine.
+struct Turn {
+  double cosine, sine;
+};
+constexpr int kMostTurns = 4 * kThreads;  // of a workgroup: a thread's piece of 8 channels has 4 pairs
+
+// The turns of a workgroup's tokens, one to a thread and step: `turn`[token][pair], and `turns`[token] whether it has a
+// position.
+__device__ __forceinline__ void find_turns(const RotateArgs& r, const RowOf& row, int32_t n, double* at, Turn* turn) {
+  const int tid = threadIdx.x, pairs = r.rotary / 2;
+  if (tid < n) {
+    const double nowhere = __builtin_nan("");
+    at[tid] = row.seq >= 0 && row.pos >= 0
+                  ? static_cast<double>(row.pos + (r.offset ? int64_t(r.offset[row.seq]) : 0)) : nowhere;
+  }
+  __syncthreads();
+  for (int i = tid; i < n * pairs; i += kThreads) {
+    const int token = i / pairs;
+    Turn t;
+    sine_cosine(at[token] * r.freq[i - token * pairs], &t.sine, &t.cosine);
+    t.sine *= r.amplitude;
+    t.cosine *= r.amplitude;
+    turn[i] = t;
+  }
+  __syncthreads();
+}
+
+// How a thread turns its piece of a row, the same for all heads of its token: element e becomes cosine[e] times itself plus
+// sine[e] times the other of its pair, which lies `partner` channels on in halves and next to it in interleaved pairs.
+struct PieceTurn {
+  bool on;
+  bool next;  // the other of a pair is in the piece
+  int32_t partner;
+  double cosine[8], sine[8];
+};
+__device__ __forceinline__ PieceTurn piece_turn(const RotateArgs& r, const double* at, const Turn* turn, int32_t token,
+                                                int32_t piece) {
+  PieceTurn p;
+  const int32_t half = r.rotary / 2, channel = 8 * piece;
+  p.on = channel < r.rotary && at[token] == at[token];
+  p.next = r.interleaved != 0;
+  const bool second = channel >= half;
+  p.partner = p.next || !p.on ? 0 : second ? -half : half;
+  if (p.on) {
+    const Turn* t = turn + token * half + (p.next ? channel / 2 : second ? channel - half : channel);
+    if (p.next) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p.cosine[e] = t[e / 2].cosine;
+        p.sine[e] = e & 1 ? t[e / 2].sine : -t[e / 2].sine;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p.cosine[e] = t[e].cosine;
+        p.sine[e] = second ? t[e].sine : -t[e].sine;
+      }
+    }
+  }
+  return p;
+}
+
+// A piece turned; `other`: the piece that has the others of its pairs.
+template <bool BF16>
+__device__ __forceinline__ u32x4 turned(const PieceTurn& p, const u32x4& own, u32x4 other) {
+  if (!p.on) return own;
+  if (p.next) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) other[i] = __builtin_amdgcn_alignbit(own[i], own[i], 16);
+  }
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    y[e] = static_cast<float>(__builtin_fma(static_cast<double>(value<BF16>(own, e)), p.cosine[e],
+                                            static_cast<double>(value<BF16>(other, e)) * p.sine[e]));
+  return u32x4{pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3]), pack2<BF16>(y[4], y[5]), pack2<BF16>(y[6], y[7])};
+}
+
 struct RowWork {
   int32_t log2_tokens;  // of a workgroup
   int32_t log2_lanes;   // of a row
 };
 
-template <bool BF16, int KB, int VB, bool WRITE>
-__global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, RowWork w) {
-  __shared__ int32_t starts[kStartsInLds];
-  __shared__ Place place[kMostTokens];
+// What a workgroup keeps in LDS; the turns only where it turns rows.
+struct RowShared {
+  int32_t starts[kStartsInLds];
+  Place place[kMostTokens];
+};
+struct TurnShared {
+  double at[kMostTokens];
+  Turn turn[kMostTurns];
+};
+
+template <bool BF16, int KB, int VB, bool WRITE, bool ROTATE>
+__device__ __forceinline__ void move_rows(const ServeArgs& a, const RowArgs& r, const RowWork& w, const RotateArgs* rot,
+                                          RowShared& lds, TurnShared* turns) {
   constexpr bool kCodes = KB != 16;
   const int32_t tokens = 1 << w.log2_tokens, lanes = 1 << w.log2_lanes;
   const int32_t i0 = int32_t(blockIdx.x) << w.log2_tokens;
@@ -290,13 +422,20 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, 
   const int32_t heads = (kThreads >> w.log2_lanes) >> w.log2_tokens;
   const bool mine = 8 * piece < a.D && t < n;
   int64_t off = int64_t(i0 + t) * r.token_stride + head0 * r.head_stride + 8 * piece;
-  u32x4 k{}, v{};
+  u32x4 k{}, v{}, other{};
   if (WRITE && mine && head0 < a.H) {  // on their way while the places are found
     k = *reinterpret_cast<const u32x4*>(r.k + off);
     v = *reinterpret_cast<const u32x4*>(r.v + off);
   }
-  find_places<KB, VB>(a, i0, n, starts, place);
-  const Place at = place[t < n ? t : 0];
+  const RowOf row = find_row(a, i0, n, lds.starts);
+  PieceTurn turn;
+  if constexpr (ROTATE) find_turns(*rot, row, n, turns->at, turns->turn);
+  find_places<KB, VB>(a, row, n, lds.place);
+  if constexpr (ROTATE) {
+    turn = piece_turn(*rot, turns->at, turns->turn, t < n ? t : 0, piece);
+    if (mine && head0 < a.H) other = *reinterpret_cast<const u32x4*>(r.k + off + turn.partner);
+  }
+  const Place at = lds.place[t < n ? t : 0];
   const bool on = mine && at.k >= 0;
   uint8_t* codes = a.codes + head0 * a.head_stride;
   uint32_t* scales = a.scales + at.scale + ((int64_t(head0) * 2) << a.log2P);
@@ -306,10 +445,13 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, 
   for (int32_t head = head0; head < a.H; head += heads) {
     const int64_t next = off + heads * r.head_stride;
     if constexpr (WRITE) {
-      const u32x4 k_now = k, v_now = v;
+      u32x4 k_now = k;
+      const u32x4 v_now = v;
+      if constexpr (ROTATE) k_now = turned<BF16>(turn, k, other);
       if (mine && head + heads < a.H) {
         k = *reinterpret_cast<const u32x4*>(r.k + next);
         v = *reinterpret_cast<const u32x4*>(r.v + next);
+        if constexpr (ROTATE) other = *reinterpret_cast<const u32x4*>(r.k + next + turn.partner);
       }
       if constexpr (kCodes) {
         float mn[2] = {__builtin_inff(), __builtin_inff()}, mx[2] = {-__builtin_inff(), -__builtin_inff()};
@@ -360,18 +502,85 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, 
   }
 }
 
-template <bool WRITE>
-pkv_status_t launch_rows(const ServeArgs& s, const RowArgs& r, hipStream_t stream) {
+template <bool BF16, int KB, int VB, bool WRITE>
+__global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, RowWork w) {
+  __shared__ RowShared lds;
+  move_rows<BF16, KB, VB, WRITE, false>(a, r, w, nullptr, lds, nullptr);
+}
+
+// Rows turned into r.out, as move_rows deals rows: a thread stays with its token and piece, whose turns it keeps in
+// registers over the heads.  Every lane of a row has loaded both its pieces before one stores (a row is in one wave), so
+// out may be x.
+template <bool BF16>
+__device__ __forceinline__ void turn_rows(const ServeArgs& a, const RotateArgs& r, const RowWork& w, RowShared& lds,
+                                          TurnShared& turns) {
+  const int32_t tokens = 1 << w.log2_tokens, lanes = 1 << w.log2_lanes;
+  const int32_t i0 = int32_t(blockIdx.x) << w.log2_tokens;
+  const int32_t n = tokens < a.num_tokens - i0 ? tokens : a.num_tokens - i0;
+  const int32_t piece = threadIdx.x & (lanes - 1), group = threadIdx.x >> w.log2_lanes;
+  const int32_t t = group & (tokens - 1), head0 = group >> w.log2_tokens;
+  const int32_t heads = (kThreads >> w.log2_lanes) >> w.log2_tokens;
+  const bool mine = 8 * piece < a.D && t < n;
+  const uint16_t* x = r.x + int64_t(i0 + t) * r.x_token_stride + head0 * r.x_head_stride + 8 * piece;
+  uint16_t* out = r.out + int64_t(i0 + t) * r.out_token_stride + head0 * r.out_head_stride + 8 * piece;
+  u32x4 own{}, other{};
+  if (mine && head0 < r.heads) own = *reinterpret_cast<const u32x4*>(x);
+  const RowOf row = find_row(a, i0, n, lds.starts);
+  if (int32_t(threadIdx.x) < n) lds.place[threadIdx.x].k = row.seq;
+  find_turns(r, row, n, turns.at, turns.turn);
+  const PieceTurn turn = piece_turn(r, turns.at, turns.turn, t < n ? t : 0, piece);
+  if (!mine || lds.place[t].k < 0) return;
+  if (head0 < r.heads) other = *reinterpret_cast<const u32x4*>(x + turn.partner);
+  for (int32_t head = head0; head < r.heads; head += heads) {
+    const u32x4 now = turned<BF16>(turn, own, other);
+    x += heads * r.x_head_stride;
+    if (head + heads < r.heads) {
+      own = *reinterpret_cast<const u32x4*>(x);
+      other = *reinterpret_cast<const u32x4*>(x + turn.partner);
+    }
+    *reinterpret_cast<u32x4*>(out) = now;
+    out += heads * r.out_head_stride;
+  }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void turn_kernel(ServeArgs a, RowWork w, RotateArgs r) {
+  __shared__ RowShared lds;
+  __shared__ TurnShared turns;
+  turn_rows<BF16>(a, r, w, lds, turns);
+}
+
+// Workgroups (.., 0) turn and write keys and write values, (.., 1) turn queries.
+template <bool BF16, int KB, int VB>
+__global__ __launch_bounds__(kThreads) void turn_append_kernel(ServeArgs a, RowArgs rows, RowWork w, RotateArgs r) {
+  __shared__ RowShared lds;
+  __shared__ TurnShared turns;
+  if (blockIdx.y == 0) move_rows<BF16, KB, VB, true, true>(a, rows, w, &r, lds, &turns);
+  else turn_rows<BF16>(a, r, w, lds, turns);
+}
+
+// Enough tokens for one pass of a workgroup; up to a pass of one head while that leaves eight workgroups to a compute
+// unit (a prompt of 8192 tokens, append and read back: 15.2 + 9.2 us; with four 18.1 + 10.2, with sixteen 15.9 + 9.4).
+RowWork row_work(const ServeArgs& s, int32_t heads) {
   RowWork w{0, 0};
   while ((8 << w.log2_lanes) < s.D) ++w.log2_lanes;
-  // Enough tokens for one pass of a workgroup; up to a pass of one head while that leaves eight workgroups to a compute
-  // unit (a prompt of 8192 tokens, append and read back: 15.2 + 9.2 us; with four 18.1 + 10.2, with sixteen 15.9 + 9.4).
   const int32_t pass = kThreads >> w.log2_lanes;
   while ((1 << w.log2_tokens) < pass &&
-         ((s.H << w.log2_tokens) < pass || (s.num_tokens >> w.log2_tokens) >= 2048))
+         ((heads << w.log2_tokens) < pass || (s.num_tokens >> w.log2_tokens) >= 2048))
     ++w.log2_tokens;
-  const dim3 grid((uint32_t(s.num_tokens) + (1u << w.log2_tokens) - 1) >> w.log2_tokens);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, s, r, w); };
+  return w;
+}
+
+dim3 row_grid(const ServeArgs& s, const RowWork& w, uint32_t roles) {
+  return dim3((uint32_t(s.num_tokens) + (1u << w.log2_tokens) - 1) >> w.log2_tokens, roles);
+}
+
+pkv_status_t launched() { return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_DEVICE; }
+
+template <bool WRITE>
+pkv_status_t launch_rows(const ServeArgs& s, const RowArgs& r, hipStream_t stream) {
+  const RowWork w = row_work(s, s.H);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, row_grid(s, w, 1), dim3(kThreads), 0, stream, s, r, w); };
   const int which = s.tag * 2 + (s.bf16 ? 1 : 0);
   switch (which) {
     case 0:  // 16-bit rows are copied as they are
@@ -383,7 +592,34 @@ pkv_status_t launch_rows(const ServeArgs& s, const RowArgs& r, hipStream_t strea
     case 6: go(rows_kernel<false, 4, 4, WRITE>); break;
     default: go(rows_kernel<true, 4, 4, WRITE>); break;
   }
-  return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_DEVICE;
+  return launched();
+}
+
+pkv_status_t launch_turn(const ServeArgs& s, const RotateArgs& t, hipStream_t stream) {
+  const RowWork w = row_work(s, t.heads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, row_grid(s, w, 1), dim3(kThreads), 0, stream, s, w, t); };
+  if (s.bf16) go(turn_kernel<true>);
+  else go(turn_kernel<false>);
+  return launched();
+}
+
+pkv_status_t launch_turn_append(const ServeArgs& s, const RowArgs& r, const RotateArgs& t, hipStream_t stream) {
+  const RowWork w = row_work(s, s.H);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, row_grid(s, w, t.heads > 0 ? 2 : 1), dim3(kThreads), 0, stream, s, r, w, t);
+  };
+  const int which = s.tag * 2 + (s.bf16 ? 1 : 0);
+  switch (which) {
+    case 0: go(turn_append_kernel<false, 16, 16>); break;
+    case 1: go(turn_append_kernel<true, 16, 16>); break;
+    case 2: go(turn_append_kernel<false, 8, 8>); break;
+    case 3: go(turn_append_kernel<true, 8, 8>); break;
+    case 4: go(turn_append_kernel<false, 8, 4>); break;
+    case 5: go(turn_append_kernel<true, 8, 4>); break;
+    case 6: go(turn_append_kernel<false, 4, 4>); break;
+    default: go(turn_append_kernel<true, 4, 4>); break;
+  }
+  return launched();
 }
 
 // Whether every buffer of a call is memory of the current device.
@@ -420,6 +656,10 @@ pkv_status_t rows_call(const pkv_model_t* model, const pkv_paged_cache_t* cache,
   return launch_rows<WRITE>(s, r, static_cast<hipStream_t>(hip_stream));
 }
 
+bool rotation_here(const OnDevice& here, const RotateArgs& t) {
+  return here.has(t.offset) && (t.heads == 0 || (here.has(t.x) && here.has(t.out)));
+}
+
 }  // namespace
 
 // One per head_dim, in objects of their own (attend.hip).
@@ -440,6 +680,35 @@ pkv_status_t pkv_cache_append(const pkv_model_t* model, const pkv_paged_cache_t*
 pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch, void* k,
                             void* v, int64_t token_stride, int64_t head_stride, void* hip_stream) {
   return pkv::rows_call<false>(model, cache, batch, k, v, token_stride, head_stride, hip_stream);
+}
+
+pkv_status_t pkv_rotate(const pkv_model_t* model, const pkv_batch_t* batch, const pkv_rotation_t* rotation,
+                        void* hip_stream) {
+  pkv::ServeArgs s;
+  pkv::RotateArgs t{};
+  pkv_status_t st = pkv::batch_args(model, batch, true, &s);
+  if (st == PKV_OK) st = pkv::rotate_args(*model, s, rotation, &t);
+  if (st != PKV_OK || s.num_seqs == 0 || s.num_tokens == 0 || t.heads == 0) return st;
+  const pkv::OnDevice here;
+  if (!here.ok) return PKV_ERR_DEVICE;
+  if (!here.has(s) || !pkv::rotation_here(here, t)) return PKV_ERR_INVALID_ARGUMENT;
+  return pkv::launch_turn(s, t, static_cast<hipStream_t>(hip_stream));
+}
+
+pkv_status_t pkv_cache_append_rotated(const pkv_model_t* model, const pkv_paged_cache_t* cache,
+                                      const pkv_batch_t* batch, const void* k, const void* v, int64_t token_stride,
+                                      int64_t head_stride, const pkv_rotation_t* rotation, void* hip_stream) {
+  pkv::ServeArgs s;
+  pkv::RowArgs r;
+  pkv::RotateArgs t{};
+  pkv_status_t st = pkv::serve_args(model, cache, batch, true, &s);
+  if (st == PKV_OK) st = pkv::row_args(s, k, v, token_stride, head_stride, &r);
+  if (st == PKV_OK) st = pkv::rotate_args(*model, s, rotation, &t);
+  if (st != PKV_OK || s.num_seqs == 0 || s.num_tokens == 0) return st;
+  const pkv::OnDevice here;
+  if (!here.ok) return PKV_ERR_DEVICE;
+  if (!here.has(s) || !here.has(r.k) || !here.has(r.v) || !pkv::rotation_here(here, t)) return PKV_ERR_INVALID_ARGUMENT;
+  return pkv::launch_turn_append(s, r, t, static_cast<hipStream_t>(hip_stream));
 }
 
 pkv_status_t pkv_attention(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,

@@ -29,14 +29,11 @@ bool stride_ok(int64_t token, int64_t head, int32_t dim) {
 
 }  // namespace
 
-pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
-                        bool pointers, ServeArgs* out) {
+pkv_status_t batch_args(const pkv_model_t* model, const pkv_batch_t* batch, bool pointers, ServeArgs* out) {
   const pkv_status_t st = check_model(model);
   if (st != PKV_OK) return st;
-  if (!cache || !batch) return PKV_ERR_INVALID_ARGUMENT;
+  if (!batch) return PKV_ERR_INVALID_ARGUMENT;
   const pkv_model_t& m = *model;
-  if (cache->tag < PKV_TAG_FP16 || cache->tag > PKV_TAG_K4V4) return PKV_ERR_BAD_TAG;
-  if (cache->layer < 0 || cache->layer >= m.num_layers) return PKV_ERR_INVALID_ARGUMENT;
   const pkv_batch_t& b = *batch;
   if (b.num_seqs >= kMostGroups || b.num_tokens >= kMostGroups) return PKV_ERR_INVALID_ARGUMENT;
   if (b.num_seqs < 0 || b.num_tokens < 0 || b.max_tokens < 0 || b.pages_per_seq < 1 || b.max_kv_len < 0)
@@ -57,8 +54,28 @@ pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache
   s.log2P = log2_of(m.page_size);
   s.H = m.num_kv_heads;
   s.D = m.head_dim;
-  s.tag = cache->tag;
   s.bf16 = m.out_dtype == PKV_OUT_BF16;
+  if (pointers && s.num_seqs > 0 && s.num_tokens > 0) {
+    if (!b.token_start || !b.kv_lens || !b.page_table) return PKV_ERR_INVALID_ARGUMENT;
+    if (!aligned(b.token_start, 4) || !aligned(b.kv_lens, 4) || !aligned(b.page_table, 4) || !aligned(b.positions, 4))
+      return PKV_ERR_INVALID_ARGUMENT;
+  }
+  *out = s;
+  return PKV_OK;
+}
+
+pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                        bool pointers, ServeArgs* out) {
+  pkv_status_t st = check_model(model);
+  if (st != PKV_OK) return st;
+  if (!cache || !batch) return PKV_ERR_INVALID_ARGUMENT;
+  const pkv_model_t& m = *model;
+  if (cache->tag < PKV_TAG_FP16 || cache->tag > PKV_TAG_K4V4) return PKV_ERR_BAD_TAG;
+  if (cache->layer < 0 || cache->layer >= m.num_layers) return PKV_ERR_INVALID_ARGUMENT;
+  ServeArgs s{};
+  st = batch_args(model, batch, pointers, &s);
+  if (st != PKV_OK) return st;
+  s.tag = cache->tag;
   if (s.tag == PKV_TAG_FP16) {
     s.page_stride = int64_t(m.page_size) * s.H * s.D * (m.kv_layout == PKV_KV_PAIRED ? 2 : 1);
   } else {
@@ -68,11 +85,6 @@ pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache
     s.v_offset = int64_t(m.page_size) * s.D * kKeyBits[s.tag] / 8;
   }
   if (pointers) {
-    if (s.num_seqs > 0 && s.num_tokens > 0) {
-      if (!b.token_start || !b.kv_lens || !b.page_table) return PKV_ERR_INVALID_ARGUMENT;
-      if (!aligned(b.token_start, 4) || !aligned(b.kv_lens, 4) || !aligned(b.page_table, 4) || !aligned(b.positions, 4))
-        return PKV_ERR_INVALID_ARGUMENT;
-    }
     if (s.tag == PKV_TAG_FP16) {
       if (!cache->k_cache || !cache->v_cache || cache->cache_bytes < cache_bytes(m)) return PKV_ERR_INVALID_ARGUMENT;
       ByteRange ranges[2];
@@ -92,6 +104,35 @@ pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache
     }
   }
   *out = s;
+  return PKV_OK;
+}
+
+pkv_status_t rotate_args(const pkv_model_t& m, const ServeArgs& s, const pkv_rotation_t* rotation, RotateArgs* out) {
+  if (!rotation) return PKV_ERR_INVALID_ARGUMENT;
+  const pkv_rotation_t& r = *rotation;
+  if (r.num_heads < 0 || !isfinite(r.amplitude) || !aligned(r.position_offset, 4)) return PKV_ERR_INVALID_ARGUMENT;
+  if (int64_t(s.num_tokens) * r.num_heads >= (int64_t(1) << 31)) return PKV_ERR_INVALID_ARGUMENT;
+  if (r.num_heads > 0) {
+    if (!stride_ok(r.x_token_stride, r.x_head_stride, s.D) || !stride_ok(r.out_token_stride, r.out_head_stride, s.D))
+      return PKV_ERR_INVALID_ARGUMENT;
+    if (s.num_tokens > 0 && s.num_seqs > 0 && (!r.x || !r.out)) return PKV_ERR_INVALID_ARGUMENT;
+    if (!aligned(r.x, 16) || !aligned(r.out, 16)) return PKV_ERR_INVALID_ARGUMENT;
+    if (r.x == r.out && (r.x_token_stride != r.out_token_stride || r.x_head_stride != r.out_head_stride))
+      return PKV_ERR_INVALID_ARGUMENT;
+  }
+  out->offset = r.position_offset;
+  out->x = static_cast<const uint16_t*>(r.x);
+  out->out = static_cast<uint16_t*>(r.out);
+  out->x_token_stride = r.x_token_stride;
+  out->x_head_stride = r.x_head_stride;
+  out->out_token_stride = r.out_token_stride;
+  out->out_head_stride = r.out_head_stride;
+  out->amplitude = r.amplitude;
+  out->heads = r.num_heads;
+  out->rotary = rotary_dim(m);
+  out->interleaved = m.rope_style == PKV_ROPE_INTERLEAVED;
+  out->reserved = 0;
+  for (int32_t j = 0; j < out->rotary / 2; ++j) out->freq[j] = rope_frequency(m, j);
   return PKV_OK;
 }
 

@@ -8,7 +8,9 @@ fills anew each step, and calls
 * :func:`append`     write new rows (quantised, where the cache holds codes);
 * :func:`read`       read rows back;
 * :func:`attention`  attention of new or recomputed rows over the cache, with an
-  optional sliding window and sinks.
+  optional sliding window and sinks;
+* :func:`rotate`, :func:`append_rotated`  rows turned to their rotary positions,
+  the keys on their way into the cache.
 
 Nothing here waits for the device or copies from it.  Several host threads may
 use one cache, on one stream or on streams of their own.
@@ -16,13 +18,15 @@ use one cache, on one stream or on streams of their own.
 from __future__ import annotations
 
 import dataclasses
+import math
 import threading
 from typing import Optional
 
 import torch
 
 from . import binding
-from .workloads import KEY_BITS, KV_PAIRED, KV_SEPARATE, OUT_BF16, OUT_FP16, TAG_FP16, VALUE_BITS
+from .workloads import (KEY_BITS, KV_PAIRED, KV_SEPARATE, OUT_BF16, OUT_FP16, ROPE_HALF, ROPE_INTERLEAVED, TAG_FP16,
+                        VALUE_BITS)
 
 _DTYPES = {torch.float16: OUT_FP16, torch.bfloat16: OUT_BF16}
 
@@ -46,8 +50,11 @@ class _Geometry:
     pool_pages: int
     out_dtype: int
     kv_layout: int
+    rope_theta: float
+    rope_style: int
+    rotary_dim: int
+    inv_freq: tuple
     block_tokens: int = 32  # of checkpoints; the serving calls have no use for it
-    rope_theta: float = 10000.0
 
 
 class PagedCache:
@@ -58,12 +65,27 @@ class PagedCache:
     the K and V views of one paired cache (``device.alloc_caches``).  Other
     tags: ``codes`` uint8 ``[L, pool_pages, H, bytes]`` and ``scales``
     float16 ``[L, pool_pages, H, 2, P, 2]`` (or without L), allocated here when
-    not given (``pool_pages`` and ``device`` then say how many and where)."""
+    not given (``pool_pages`` and ``device`` then say how many and where).
+
+    The model's RoPE, for the calls that turn rows, as ``workloads.Shape`` has it: ``rope_style`` ROPE_HALF or
+    ROPE_INTERLEAVED, ``rotary_dim`` channels (0: all), pair j's frequency ``inv_freq[j]`` (as
+    ``workloads.llama3_inv_freq`` gives for long contexts) or ``rope_theta ** (-2 j / rotary_dim)``; turned pairs are
+    multiplied by ``rope_amplitude``."""
 
     def __init__(self, num_kv_heads: int, head_dim: int, page_size: int, dtype, tag: int, codes=None, scales=None,
-                 k_cache=None, v_cache=None, num_layers: int = 1, pool_pages: Optional[int] = None, device="cuda"):
+                 k_cache=None, v_cache=None, num_layers: int = 1, pool_pages: Optional[int] = None, device="cuda",
+                 rope_theta: float = 10000.0, rope_style: int = ROPE_HALF, rotary_dim: int = 0, inv_freq=None,
+                 rope_amplitude: float = 1.0):
         _need(dtype in _DTYPES, "dtype is float16 or bfloat16")
         _need(0 <= tag < 4, "tag is a TAG_* value")
+        _need(rope_style in (ROPE_HALF, ROPE_INTERLEAVED), "rope_style is ROPE_HALF or ROPE_INTERLEAVED")
+        rotary = rotary_dim or head_dim
+        _need(rotary % 16 == 0 and 16 <= rotary <= head_dim, "rotary_dim is a multiple of 16, at most head_dim")
+        _need(math.isfinite(rope_theta) and rope_theta > 0, "rope_theta is above zero")
+        if inv_freq is None:  # (here, that calls need not work them out)
+            inv_freq = [rope_theta ** (-2.0 * j / rotary) for j in range(rotary // 2)]
+        _need(len(inv_freq) == rotary // 2, f"inv_freq has {rotary // 2} values")
+        _need(all(math.isfinite(f) for f in inv_freq) and math.isfinite(rope_amplitude), "frequencies are finite")
         layout = KV_SEPARATE
         if tag == TAG_FP16:
             _need(k_cache is not None and v_cache is not None, "16-bit pages need k_cache and v_cache")
@@ -110,7 +132,9 @@ class PagedCache:
         _need(self.device.type == "cuda", "the cache is device memory")
         self._index = self.device.index
         self.model = binding.make_model(_Geometry(num_layers, num_kv_heads, head_dim, page_size, pool_pages,
-                                                  _DTYPES[dtype], layout))
+                                                  _DTYPES[dtype], layout, rope_theta, rope_style, rotary_dim,
+                                                  tuple(inv_freq)))
+        self.rope_amplitude = rope_amplitude
         self._layers = [self._of_layer(layer) for layer in range(num_layers)]
         self._workspace = {}
         self._scratch = threading.Lock()  # held from taking scratch memory until the kernels that use it are enqueued
@@ -209,6 +233,52 @@ def read(cache: PagedCache, batch: Batch, layer: int = 0, out=None):
     _check(binding.pkv_cache_read_status(cache.model, cache._at(layer), batch.struct, k.data_ptr(), v.data_ptr(), *at,
                                          _stream(cache)), "pkv_cache_read")
     return k, v
+
+
+def _per_sequence(batch: Batch, t, what: str) -> Optional[int]:
+    """Address of an int32 tensor with a number for each sequence, or None."""
+    if t is None:
+        return None
+    _need(t.dtype == torch.int32 and t.is_contiguous() and t.numel() == batch.struct.num_seqs,
+          f"{what} is int32, one for each sequence")
+    return t.data_ptr()
+
+
+def _rotation(cache: PagedCache, batch: Batch, x, out, position_offset):
+    """The rotation of rows ``x`` into ``out`` (new if None), and ``out``."""
+    heads = x.shape[1]
+    if out is None:
+        _rows(cache, batch, heads, x)
+        out = torch.empty((batch.num_tokens, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
+    else:
+        _rows(cache, batch, heads, x, out)
+    offset = _per_sequence(batch, position_offset, "position_offset")
+    return binding.PkvRotation(heads, cache.rope_amplitude, offset, x.data_ptr(), *_strides(x), out.data_ptr(),
+                               *_strides(out)), out
+
+
+def rotate(cache: PagedCache, batch: Batch, x, out=None, position_offset=None):
+    """Rows ``x`` ``[num_tokens, heads, D]`` (queries or keys) turned to the batch's positions by the cache's RoPE, into
+    ``out`` (which may be ``x``).  ``position_offset``, int32 ``[S]``, is added to the positions of each sequence: after
+    an eviction its rows stand further on than their places in the cache.  Rows at negative positions are
+    copied, rows of no sequence left as they are."""
+    rotation, out = _rotation(cache, batch, x, out, position_offset)
+    _check(binding.pkv_rotate_status(cache.model, batch.struct, rotation, _stream(cache)), "pkv_rotate")
+    return out
+
+
+def append_rotated(cache: PagedCache, batch: Batch, q, k, v, layer: int = 0, out=None, position_offset=None):
+    """:func:`rotate` of the queries ``q`` ``[num_tokens, Hq, D]`` and :func:`append` of the keys ``k``, turned alike, and the
+    values ``v``, in one kernel.  Returns the turned queries (``out``, which may be ``q``); ``k`` and ``v`` are only
+    read."""
+    rotation, out = _rotation(cache, batch, q, out, position_offset)
+    _rows(cache, batch, cache.num_kv_heads, k, v)
+    at = _strides(k)
+    _need(at == _strides(v), "k and v have the same strides")
+    _check(binding.pkv_cache_append_rotated_status(cache.model, cache._at(layer), batch.struct, k.data_ptr(),
+                                                   v.data_ptr(), *at, rotation, _stream(cache)),
+           "pkv_cache_append_rotated")
+    return out
 
 
 def attention(cache: PagedCache, batch: Batch, q, scale: Optional[float] = None, window: int = 0, sinks: int = 0,
