@@ -551,6 +551,43 @@ pkv_status_t pkv_attention_workspace(const pkv_model_t* model, const pkv_paged_c
 pkv_status_t pkv_attention(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
                            const pkv_attention_t* attention, void* hip_stream);
 
+/* ----------------------------------------------------------------------------
+ * Eviction: which cached tokens receive least attention, and a cache without
+ * them.  One call weighs what an attention call's rows looked at, one chooses the
+ * tokens that stay under a budget, one moves their rows to the front.
+ * ---------------------------------------------------------------------------- */
+
+/* A number for each cached token: token t of KV head h of sequence s at
+ * s * seq_stride + h * head_stride + t (floats; heads 1: of all heads together). */
+typedef struct {
+  int32_t heads;          /* 1 or num_kv_heads */
+  float decay;            /* finite; pkv_attention_weights only */
+  int64_t tokens;         /* of a row, >= the batch's bound of kv_lens */
+  int64_t head_stride;    /* >= tokens (heads > 1) */
+  int64_t seq_stride;     /* >= (heads - 1) * head_stride + tokens (several sequences) */
+  const float* weights;   /* before; not read where decay is 0, may be NULL then */
+  float* out;             /* after; may be weights itself, else must not overlap it */
+} pkv_weights_t;
+
+/* The attention weight that each cached token receives from the batch's rows:
+ *   out[s, h, t] = decay * weights[s, h, t] + sum exp(scale * q . k_t - lse)
+ * over the rows and query heads (of KV head h, or all) that see token t, for t <
+ * kv_lens; what lies behind stays.  `attention` is the structure of the pkv_attention
+ * call whose rows they are: its q, scale and masks, its lse (here an input, not
+ * NULL) and a workspace of pkv_attention_weights_workspace's bytes; out is not
+ * looked at.  A row with lse = -inf gives nothing, a token on a page that is not
+ * there receives nothing.  Sums are single precision in an order that depends on the
+ * sizes alone; scores are as in pkv_attention, keys that no row sees do not matter.
+ * The launch has fewer than 2^24 workgroups, for which num_seqs * num_kv_heads *
+ * (max_kv_len / 128 + 1) * 8 < 2^24 always suffices.  At most two
+ * kernels on `hip_stream`.  Errors as pkv_attention. */
+pkv_status_t pkv_attention_weights_workspace(const pkv_model_t* model, const pkv_paged_cache_t* cache,
+                                             const pkv_batch_t* batch, const pkv_attention_t* attention,
+                                             const pkv_weights_t* weights, uint64_t* bytes);
+
+pkv_status_t pkv_attention_weights(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                                   const pkv_attention_t* attention, const pkv_weights_t* weights, void* hip_stream);
+
 /* Static description of a status code. */
 const char* pkv_status_string(pkv_status_t status);
 

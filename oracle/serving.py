@@ -139,3 +139,35 @@ def attend(cache, tag, page, dtype, where, kv_lens, page_table, pool_pages, q_bi
                 lse[i, at] = top + np.log(total)
                 reach[i, at] = scale * (np.abs(k) @ np.abs(x)).max()
     return out, lse, mass, whole, reach
+
+
+def weigh(cache, tag, page, dtype, where, kv_lens, page_table, pool_pages, q_bits, lse, heads, scale, window, sinks):
+    """The attention weight that each cached token receives, fp64 [S][H][max kv_lens], for rows' log-sum-exp ``lse`` (fp32
+    [tokens][Hq]); and what error bounds need, of the same shape: the sum of each exponential times scale * (sum |q| (|k -
+    zero| + |zero|)) + |score| + |lse|, and the number of exponentials."""
+    q = cache_values(q_bits, dtype)
+    group = q.shape[1] // heads
+    shape = (len(kv_lens), heads, max(1, int(max(kv_lens))))
+    out, slack, terms = np.zeros(shape), np.zeros(shape), np.zeros(shape)
+    for s in range(len(kv_lens)):
+        mine = [(i, pos) for i, (at, pos, _, _) in enumerate(where) if at == s]
+        tok = [(t, int(page_table[s, t // page])) for t in range(int(kv_lens[s])) if t // page < page_table.shape[1]]
+        tok = [(t, p) for t, p in tok if 0 <= p < pool_pages]
+        if not mine or not tok:
+            continue
+        t_all = np.array([t for t, _ in tok])
+        for h in range(heads):
+            rows = [row(cache, tag, page, dtype, 0, p, t % page, h) for t, p in tok]
+            k, wide = np.stack([r[0] for r in rows]), np.stack([r[1] + r[2] for r in rows])
+            for i, pos in mine:
+                sees = (t_all <= pos) & ((pos - t_all < window) | (t_all < sinks) if window else True)
+                for g in range(h * group, (h + 1) * group):
+                    if lse[i, g] == -np.inf or not sees.any():
+                        continue
+                    score = scale * (k[sees] @ q[i, g])
+                    p = np.exp(score - float(lse[i, g]))
+                    out[s, h, t_all[sees]] += p
+                    reach = scale * (wide[sees] @ np.abs(q[i, g]))
+                    slack[s, h, t_all[sees]] += p * (reach + np.abs(score) + abs(float(lse[i, g])))
+                    terms[s, h, t_all[sees]] += 1
+    return out, slack, terms

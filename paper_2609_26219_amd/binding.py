@@ -27,7 +27,8 @@ PKV_ERR_DEVICE = -7
 EXPORTED = ("pkv_payload_size", "pkv_restore_plan", "pkv_restore", "pkv_restore_from_host", "pkv_free",
             "pkv_plan_query", "pkv_status_string", "pkv_checkpoint_plan", "pkv_quantize_gather", "pkv_plan_repair",
             "pkv_plan_payload_bytes", "pkv_restore_from_host_noalloc", "pkv_cache_size", "pkv_cache_append",
-            "pkv_cache_read", "pkv_attention_workspace", "pkv_attention", "pkv_rotate", "pkv_cache_append_rotated")
+            "pkv_cache_read", "pkv_attention_workspace", "pkv_attention", "pkv_rotate", "pkv_cache_append_rotated",
+            "pkv_attention_weights_workspace", "pkv_attention_weights")
 
 
 class PkvModel(ctypes.Structure):
@@ -83,6 +84,12 @@ class PkvAttention(ctypes.Structure):
                 ("q_head_stride", ctypes.c_int64), ("out", ctypes.c_void_p), ("out_token_stride", ctypes.c_int64),
                 ("out_head_stride", ctypes.c_int64), ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_uint64)]
+
+
+class PkvWeights(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("decay", ctypes.c_float), ("tokens", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("seq_stride", ctypes.c_int64), ("weights", ctypes.c_void_p),
+                ("out", ctypes.c_void_p)]
 
 
 class PkvError(RuntimeError):
@@ -145,6 +152,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pkv_rotate.restype = i32
     lib.pkv_cache_append_rotated.argtypes = [model, cache, batch, vp, vp, i64, i64, rotation, vp]
     lib.pkv_cache_append_rotated.restype = i32
+    weights = ctypes.POINTER(PkvWeights)
+    lib.pkv_attention_weights_workspace.argtypes = [model, cache, batch, attention, weights, ctypes.POINTER(u64)]
+    lib.pkv_attention_weights_workspace.restype = i32
+    lib.pkv_attention_weights.argtypes = [model, cache, batch, attention, weights, vp]
+    lib.pkv_attention_weights.restype = i32
     _lib = lib
     return lib
 
@@ -473,3 +485,17 @@ def pkv_rotate_status(model: PkvModel, batch: PkvBatch, rotation: PkvRotation, s
 def pkv_cache_append_rotated_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, k, v, token_stride: int,
                                     head_stride: int, rotation: PkvRotation, stream=0) -> int:
     return load().pkv_cache_append_rotated(model, cache, batch, k, v, token_stride, head_stride, rotation, stream or None)
+
+
+def pkv_attention_weights_workspace(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, attention: PkvAttention,
+                                    weights: PkvWeights) -> int:
+    out = ctypes.c_uint64()
+    st = load().pkv_attention_weights_workspace(model, cache, batch, attention, weights, ctypes.byref(out))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_attention_weights_workspace")
+    return out.value
+
+
+def pkv_attention_weights_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, attention: PkvAttention,
+                                 weights: PkvWeights, stream=0) -> int:
+    return load().pkv_attention_weights(model, cache, batch, attention, weights, stream or None)

@@ -24,7 +24,7 @@ CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra", f"-I{INCLUDE}", f
 HOST_SRC = ("plan.cpp", "serve_plan.cpp")
 # The attention kernels are built once for each head_dim.
 HIP_SRC = (("restore.hip", ()), ("gather.hip", ()), ("serve.hip", ()),
-           *(("attend.hip", (f"-DPKV_HEAD_DIM={d}",)) for d in (64, 128, 256)))
+           *((src, (f"-DPKV_HEAD_DIM={d}",)) for src in ("attend.hip", "weigh.hip") for d in (64, 128, 256)))
 
 
 def _run(cmd, verbose):

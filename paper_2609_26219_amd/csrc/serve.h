@@ -102,6 +102,33 @@ struct AttendLaunch {
   uint64_t workspace_bytes; // both
 };
 
+struct WeighArgs {
+  const uint16_t* q;
+  const float* lse;      // [num_tokens][Hq]
+  const float* weights;  // before, or null (decay 0)
+  float* out;
+  float* part;           // [splits][H][num_seqs][max_kv], or null: sums go straight to out
+  int64_t q_token_stride, q_head_stride, seq_stride, head_stride;
+  float decay;
+  float scale;           // scale * log2(e)
+  int32_t Hq, group, window, sinks;
+  int32_t joint;         // one weight a token, of all heads
+  int32_t tiles;         // workgroups along a sequence's tokens
+  int32_t chunk, subs;   // few rows: tokens of a workgroup, and the parts that its waves take
+  int32_t splits;        // many rows: workgroups that share the rows of a tile of tokens
+};
+
+// How a call of weights is launched.
+struct WeighLaunch {
+  int32_t row_tiles;    // of few rows, or 0: many
+  int32_t tiles, chunk, subs, splits;
+  int64_t groups, join_groups;
+  uint64_t workspace_bytes;
+};
+
+constexpr int kMostChunk = 512;  // tokens of a workgroup of few rows
+constexpr int weigh_tokens(int head_dim) { return head_dim > 128 ? 128 : 256; }  // of many rows
+
 // A launch has fewer than 2^32 threads, in workgroups of 256.
 constexpr int64_t kMostGroups = int64_t(1) << 24;
 
@@ -133,6 +160,8 @@ pkv_status_t batch_args(const pkv_model_t* model, const pkv_batch_t* batch, bool
 pkv_status_t rotate_args(const pkv_model_t& m, const ServeArgs& s, const pkv_rotation_t* rotation, RotateArgs* out);
 pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool pointers, AttendArgs* out);
 AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a);
+pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_weights_t* w, bool pointers, WeighArgs* out,
+                        WeighLaunch* launch);
 
 }  // namespace pkv
 

@@ -666,6 +666,9 @@ bool rotation_here(const OnDevice& here, const RotateArgs& t) {
 pkv_status_t launch_attend_64(const ServeArgs& s, const AttendArgs& a, int64_t groups, hipStream_t stream);
 pkv_status_t launch_attend_128(const ServeArgs& s, const AttendArgs& a, int64_t groups, hipStream_t stream);
 pkv_status_t launch_attend_256(const ServeArgs& s, const AttendArgs& a, int64_t groups, hipStream_t stream);
+pkv_status_t launch_weigh_64(const ServeArgs& s, const WeighArgs& a, const WeighLaunch& l, hipStream_t stream);
+pkv_status_t launch_weigh_128(const ServeArgs& s, const WeighArgs& a, const WeighLaunch& l, hipStream_t stream);
+pkv_status_t launch_weigh_256(const ServeArgs& s, const WeighArgs& a, const WeighLaunch& l, hipStream_t stream);
 
 }  // namespace pkv
 
@@ -727,6 +730,24 @@ pkv_status_t pkv_attention(const pkv_model_t* model, const pkv_paged_cache_t* ca
   if (s.D == 64) return pkv::launch_attend_64(s, a, l.groups, stream);
   if (s.D == 128) return pkv::launch_attend_128(s, a, l.groups, stream);
   return pkv::launch_attend_256(s, a, l.groups, stream);
+}
+
+pkv_status_t pkv_attention_weights(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                                   const pkv_attention_t* attention, const pkv_weights_t* weights, void* hip_stream) {
+  pkv::ServeArgs s;
+  pkv::WeighArgs a;
+  pkv::WeighLaunch l;
+  pkv_status_t st = pkv::serve_args(model, cache, batch, true, &s);
+  if (st == PKV_OK) st = pkv::weigh_args(s, attention, weights, true, &a, &l);
+  if (st != PKV_OK || s.num_seqs == 0) return st;
+  const pkv::OnDevice here;
+  if (!here.ok) return PKV_ERR_DEVICE;
+  if (!here.has(s) || !here.has(a.q) || !here.has(a.lse) || !here.has(a.weights) || !here.has(a.out) || !here.has(a.part))
+    return PKV_ERR_INVALID_ARGUMENT;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (s.D == 64) return pkv::launch_weigh_64(s, a, l, stream);
+  if (s.D == 128) return pkv::launch_weigh_128(s, a, l, stream);
+  return pkv::launch_weigh_256(s, a, l, stream);
 }
 
 }  // extern "C"

@@ -237,6 +237,100 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a) {
   return l;
 }
 
+namespace {
+
+// The arrays of a call that goes over sequences, whether it has rows or not.
+bool seqs_ok(const ServeArgs& s) {
+  return s.token_start && s.kv_lens && s.page_table && aligned(s.token_start, 4) && aligned(s.kv_lens, 4) &&
+         aligned(s.page_table, 4);
+}
+
+// Rows of numbers, one a token: whether they are laid out without overlap.
+bool weights_ok(const ServeArgs& s, const pkv_weights_t& w) {
+  const int64_t most = int64_t(1) << 40;
+  if ((w.heads != 1 && w.heads != s.H) || w.tokens < s.max_kv || w.tokens > most) return false;
+  if (w.heads > 1 && (w.head_stride < w.tokens || w.head_stride > most)) return false;
+  const int64_t whole = (w.heads > 1 ? (w.heads - 1) * w.head_stride : 0) + w.tokens;
+  return s.num_seqs <= 1 || (w.seq_stride >= whole && w.seq_stride <= most);
+}
+
+}  // namespace
+
+pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_weights_t* weights, bool pointers,
+                        WeighArgs* out, WeighLaunch* launch) {
+  if (!a || !weights) return PKV_ERR_INVALID_ARGUMENT;
+  const pkv_weights_t& w = *weights;
+  if (s.D != 64 && s.D != 128 && s.D != 256) return PKV_ERR_INVALID_ARGUMENT;
+  if (a->num_q_heads < 1 || a->num_q_heads % s.H || a->window < 0 || a->sinks < 0) return PKV_ERR_INVALID_ARGUMENT;
+  if (!(isfinite(a->scale) && a->scale > 0.0f) || !isfinite(w.decay)) return PKV_ERR_INVALID_ARGUMENT;
+  if (int64_t(s.num_tokens) * a->num_q_heads >= (int64_t(1) << 31)) return PKV_ERR_INVALID_ARGUMENT;
+  // The kernels multiply page numbers by 32-bit strides.
+  const int64_t most = (int64_t(1) << 32) - 1;
+  if (s.page_stride * (s.tag == PKV_TAG_FP16 ? 2 : 1) > most || s.scale_stride > most) return PKV_ERR_INVALID_ARGUMENT;
+  if (!weights_ok(s, w)) return PKV_ERR_INVALID_ARGUMENT;
+  WeighArgs r{};
+  r.Hq = a->num_q_heads;
+  r.group = r.Hq / s.H;
+  r.window = a->window;
+  r.sinks = a->sinks;
+  r.scale = a->scale * 1.44269504088896340736f;
+  r.joint = w.heads == 1;
+  r.decay = w.decay;
+  r.seq_stride = w.seq_stride;
+  r.head_stride = w.heads > 1 ? w.head_stride : 0;
+
+  WeighLaunch l{};
+  l.splits = l.subs = 1;
+  if (s.num_seqs > 0) {
+    const int64_t rows = int64_t(s.max_tokens) * r.group;
+    if (rows <= kRowTile * few_tiles(s.D)) {
+      l.row_tiles = rows <= kRowTile ? 1 : 2;
+      // A workgroup's 8 waves take a KV head each, or parts of the tokens where there are fewer.
+      while (l.subs < 8 && l.subs * 2 * s.H <= 8) l.subs *= 2;
+      l.chunk = kTokenTile * l.subs;
+      while (l.chunk < kMostChunk && int64_t(s.num_seqs) * s.max_kv / l.chunk >= 2048) l.chunk *= 2;
+      l.tiles = int32_t((int64_t(s.max_kv) + l.chunk - 1) / l.chunk);
+      l.groups = int64_t(s.num_seqs) * l.tiles;
+    } else {
+      const int tokens = weigh_tokens(s.D);
+      l.tiles = int32_t((int64_t(s.max_kv) + tokens - 1) / tokens);
+      const int64_t base = int64_t(s.num_seqs) * l.tiles * s.H;
+      l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(6 * 256 / base, rows / 256)));
+      l.groups = base * l.splits;
+      if (l.splits > 1 || (r.joint && s.H > 1)) {
+        l.workspace_bytes = uint64_t(l.splits) * s.H * s.num_seqs * s.max_kv * 4;
+        l.join_groups = int64_t(s.num_seqs) * w.heads * ((int64_t(s.max_kv) + 255) / 256);
+      }
+    }
+    if (l.groups >= kMostGroups || l.join_groups >= kMostGroups) return PKV_ERR_INVALID_ARGUMENT;
+  }
+  r.tiles = l.tiles;
+  r.chunk = l.chunk;
+  r.subs = l.subs;
+  r.splits = l.splits;
+  if (pointers) {
+    if (!stride_ok(a->q_token_stride, a->q_head_stride, s.D)) return PKV_ERR_INVALID_ARGUMENT;
+    if (s.num_seqs > 0) {  // (a call without rows still lets the weights fade)
+      if (!seqs_ok(s) || !w.out || (w.decay != 0.0f && !w.weights)) return PKV_ERR_INVALID_ARGUMENT;
+      if (s.num_tokens > 0 && (!a->q || !a->lse)) return PKV_ERR_INVALID_ARGUMENT;
+    }
+    if (!aligned(a->q, 16) || !aligned(a->lse, 4) || !aligned(w.weights, 4) || !aligned(w.out, 4) ||
+        !aligned(a->workspace, 16))
+      return PKV_ERR_INVALID_ARGUMENT;
+    if (l.workspace_bytes && (!a->workspace || a->workspace_bytes < l.workspace_bytes)) return PKV_ERR_INVALID_ARGUMENT;
+    r.q = static_cast<const uint16_t*>(a->q);
+    r.q_token_stride = a->q_token_stride;
+    r.q_head_stride = a->q_head_stride;
+    r.lse = a->lse;
+    r.weights = w.decay != 0.0f ? w.weights : nullptr;
+    r.out = w.out;
+    r.part = l.workspace_bytes ? static_cast<float*>(a->workspace) : nullptr;
+  }
+  *out = r;
+  *launch = l;
+  return PKV_OK;
+}
+
 }  // namespace pkv
 
 extern "C" {
@@ -261,6 +355,20 @@ pkv_status_t pkv_attention_workspace(const pkv_model_t* model, const pkv_paged_c
   if (st == PKV_OK) st = pkv::attend_args(s, attention, false, &a);
   if (st != PKV_OK) return st;
   *bytes = pkv::attend_launch(s, a).workspace_bytes;
+  return PKV_OK;
+}
+
+pkv_status_t pkv_attention_weights_workspace(const pkv_model_t* model, const pkv_paged_cache_t* cache,
+                                             const pkv_batch_t* batch, const pkv_attention_t* attention,
+                                             const pkv_weights_t* weights, uint64_t* bytes) {
+  if (!bytes) return PKV_ERR_INVALID_ARGUMENT;
+  pkv::ServeArgs s;
+  pkv::WeighArgs a;
+  pkv::WeighLaunch l;
+  pkv_status_t st = pkv::serve_args(model, cache, batch, false, &s);
+  if (st == PKV_OK) st = pkv::weigh_args(s, attention, weights, false, &a, &l);
+  if (st != PKV_OK) return st;
+  *bytes = l.workspace_bytes;
   return PKV_OK;
 }
 

@@ -311,3 +311,47 @@ def attention(cache: PagedCache, batch: Batch, q, scale: Optional[float] = None,
         status = binding.pkv_attention_status(cache.model, struct, batch.struct, a, stream)
     _check(status, "pkv_attention")
     return (out, lse) if return_lse else out
+
+
+def _weights(cache: PagedCache, batch: Batch, out, weights=None, decay: float = 0.0) -> binding.PkvWeights:
+    """Numbers of cached tokens as the library takes them: float32 ``[S, 1 or H, tokens]``, tokens together."""
+    for t in (out, weights):
+        if t is not None and (t.dtype != torch.float32 or t.dim() != 3 or t.shape[0] != batch.struct.num_seqs or
+                              t.shape[1] not in (1, cache.num_kv_heads) or (t.shape[2] > 1 and t.stride(2) != 1)):
+            raise ValueError("weights are float32 [S, 1 or H, tokens], a row's tokens consecutive")
+    seqs, heads, tokens = out.shape
+    head = out.stride(1) if heads > 1 else tokens
+    seq = out.stride(0) if seqs > 1 else heads * head
+    _need(weights is None or weights.shape == out.shape, "weights before and after have the same shape")
+    if weights is not None:
+        _need((heads == 1 or weights.stride(1) == head) and (seqs == 1 or weights.stride(0) == seq),
+              "weights before and after have the same strides")
+    return binding.PkvWeights(heads, decay, tokens, head, seq, None if weights is None else weights.data_ptr(),
+                              out.data_ptr())
+
+
+def attention_weights(cache: PagedCache, batch: Batch, q, lse, out, weights=None, decay: float = 1.0,
+                      scale: Optional[float] = None, window: int = 0, sinks: int = 0, layer: int = 0):
+    """The attention weight that each cached token receives from the rows of an :func:`attention` call (the same ``q``,
+    ``scale`` and masks, and the ``lse`` that it returned), added to ``decay`` times what it had before:
+    ``out = decay * weights + sum``, float32 ``[S, H, tokens]`` for each KV head or ``[S, 1, tokens]`` for all together,
+    with as many tokens as the batch's bound.  ``weights`` may be ``out`` (added in place) or None (nothing before).  Tokens
+    past ``kv_lens`` are left as they are.  Returns ``out``."""
+    heads = q.shape[1]
+    _rows(cache, batch, heads, q)
+    _need(lse.dtype == torch.float32 and lse.shape == (batch.num_tokens, heads) and lse.is_contiguous(),
+          "lse is contiguous float32 [num_tokens, Hq]")
+    w = _weights(cache, batch, out, weights, decay if weights is not None else 0.0)
+    a = binding.PkvAttention(heads, _int32(window), _int32(sinks), cache.head_dim ** -0.5 if scale is None else scale,
+                             q.data_ptr(), *_strides(q), None, 0, 0, lse.data_ptr(), None, 0)
+    stream = _stream(cache)
+    struct = cache._at(layer)
+    nbytes = binding.pkv_attention_weights_workspace(cache.model, struct, batch.struct, a, w)
+    if nbytes:
+        with cache._scratch:
+            a.workspace, a.workspace_bytes = cache.workspace(nbytes, stream), nbytes
+            status = binding.pkv_attention_weights_status(cache.model, struct, batch.struct, a, w, stream)
+    else:
+        status = binding.pkv_attention_weights_status(cache.model, struct, batch.struct, a, w, stream)
+    _check(status, "pkv_attention_weights")
+    return out
