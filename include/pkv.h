@@ -588,6 +588,45 @@ pkv_status_t pkv_attention_weights_workspace(const pkv_model_t* model, const pkv
 pkv_status_t pkv_attention_weights(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
                                    const pkv_attention_t* attention, const pkv_weights_t* weights, void* hip_stream);
 
+/* The tokens of each sequence that stay: row (s, h) of kept holds their indices,
+ * ascending, then -1. */
+typedef struct {
+  int32_t heads;            /* 1: one choice for all heads; num_kv_heads: one for each */
+  int32_t budget;           /* most tokens that a sequence keeps; 0 <= budget <= 2^30 */
+  int32_t sinks;            /* >= 0: the first tokens, which stay */
+  int32_t recent;           /* >= 0: the last tokens, which stay where the budget has room beside the sinks */
+  const int32_t* budgets;   /* device [num_seqs], each sequence's own (at most budget), or NULL */
+  int32_t* kept;            /* device [num_seqs][heads][budget] */
+  int32_t* kept_lens;       /* device [num_seqs] */
+} pkv_kept_t;
+
+/* Choose the tokens that stay under the budget.  Of n = kv_lens[s] tokens
+ * m = min(n, budget) stay: the first min(sinks, m), the last min(recent, what is
+ * left), and of those between the ones of the largest weight (weights->weights, as many
+ * heads as kept->heads), equal weights (+0 and -0 too) lowest index first, NaN after
+ * everything.  Writes kept and kept_lens (m).  Of the batch only its sizes and kv_lens
+ * are read.  num_seqs * heads < 2^22.  One kernel on `hip_stream`.  Errors:
+ * PKV_ERR_INVALID_ARGUMENT, PKV_ERR_DEVICE. */
+pkv_status_t pkv_cache_keep(const pkv_model_t* model, const pkv_batch_t* batch, const pkv_weights_t* weights,
+                            const pkv_kept_t* kept, void* hip_stream);
+
+/* Move the rows that stay to the front of their sequence: row j of head h (K, V and
+ * their scales) becomes row kept[s][h][j], for j < kept_lens[s] (at most kv_lens[s]).
+ *   page_table : NULL: in place; kept ascends, and a sequence's pages are no
+ *     other's.  Else device [num_seqs][table_pages]: the rows go to its pages,
+ *     which hold no row that stays (pages shared with another sequence keep
+ *     theirs);
+ *   weights    : NULL, or weights->out (kept->heads heads) is moved alike, in place, and
+ *     0 from kept_lens[s] to kv_lens[s].
+ * Indices outside [0, kv_lens) and rows whose page is not there, before or after, are
+ * left out; every other byte stays.  The lengths after it are kept_lens: kv_lens is
+ * only read, so that each layer finds it.  Fewer than 2^24 workgroups: num_seqs *
+ * num_kv_heads * ceil(head_dim / 32) * (2 + budget / 512) < 2^22 always suffices.  One
+ * kernel on `hip_stream`.  Errors as pkv_cache_append. */
+pkv_status_t pkv_cache_evict(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                             const pkv_kept_t* kept, const pkv_weights_t* weights, const int32_t* page_table,
+                             int32_t table_pages, void* hip_stream);
+
 /* Static description of a status code. */
 const char* pkv_status_string(pkv_status_t status);
 

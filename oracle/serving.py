@@ -1,6 +1,7 @@
 """Oracle of the serving calls (include/pkv.h, "Serving from a paged cache"):
-rows quantised into a paged cache, read back, turned to their positions, and
-attention over it.
+rows quantised into a paged cache, read back, turned to their positions,
+attention over it, the weight its tokens receive, and a cache without the
+tokens that receive least.
 
 Plain NumPy in fp64, one row and one head at a time.  Test infrastructure only;
 imports nothing from the package.  A cache is a dict with the arrays the
@@ -171,3 +172,56 @@ def weigh(cache, tag, page, dtype, where, kv_lens, page_table, pool_pages, q_bit
                     slack[s, h, t_all[sees]] += p * (reach + np.abs(score) + abs(float(lse[i, g])))
                     terms[s, h, t_all[sees]] += 1
     return out, slack, terms
+
+
+def keep(weights, kv_lens, budgets, sinks, recent):
+    """Which tokens stay: for each sequence and head of ``weights`` [S][heads][tokens] a list of indices, ascending."""
+    out = []
+    for w, n, budget in zip(weights, kv_lens, budgets):
+        n, rows = int(n), []
+        m = min(n, max(0, int(budget)))
+        first = min(sinks, m)
+        last = min(recent, m - first)
+        for x in w:
+            key = [(0, 0.0) if np.isnan(v) else (1, float(v)) for v in x[:n]]
+            between = sorted(range(first, n - last), key=lambda t: ((-key[t][0], -key[t][1]), t))[:m - first - last]
+            rows.append(list(range(first)) + sorted(between) + list(range(n - last, n)))
+        out.append(rows)
+    return out
+
+
+def evict(cache, tag, page, kept, kv_lens, table, to_table, weights=None):
+    """Rows that stay, moved: ``kept`` as of :func:`keep`, one list for all heads or one for each.  New copies of the cache
+    and the weights."""
+    pool = (cache["kv"][0] if tag == TAG_FP16 else cache["codes"]).shape[0]
+    new = {k: ([a.copy() for a in v] if isinstance(v, list) else v.copy()) for k, v in cache.items()}
+    moved = None if weights is None else weights.copy()
+
+    def place(t, s, j):
+        p = int(t[s, j // page]) if 0 <= j // page < t.shape[1] else -1
+        return (p, j % page) if 0 <= p < pool else None
+
+    heads = cache["kv"][0].shape[2] if tag == TAG_FP16 else cache["codes"].shape[1]
+    for s, rows in enumerate(kept):
+        for h in range(heads):
+            for j, t in enumerate(rows[h if len(rows) > 1 else 0]):
+                a, b = place(table, s, t), place(to_table, s, j)
+                if a is None or b is None or (to_table is table and t == j):
+                    continue
+                if tag == TAG_FP16:
+                    for w in range(2):
+                        new["kv"][w][b[0], b[1], h] = cache["kv"][w][a[0], a[1], h]
+                    continue
+                size = cache["codes"].shape[2]
+                dim = size * 8 // (page * (KEY_BITS[tag] + VALUE_BITS[tag]))
+                for w in range(2):
+                    lo, hi = tile_bounds(tag, page, dim, w)
+                    new["codes"][b[0], h, lo:hi].reshape(page, -1)[b[1]] = \
+                        cache["codes"][a[0], h, lo:hi].reshape(page, -1)[a[1]]
+                    new["scales"][b[0], h, w, b[1]] = cache["scales"][a[0], h, w, a[1]]
+        if moved is not None:
+            for h, row_ in enumerate(rows):
+                n = int(kv_lens[s])
+                moved[s, h, :len(row_)] = weights[s, h, row_]
+                moved[s, h, len(row_):n] = 0.0
+    return new, moved

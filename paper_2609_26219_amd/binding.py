@@ -28,7 +28,7 @@ EXPORTED = ("pkv_payload_size", "pkv_restore_plan", "pkv_restore", "pkv_restore_
             "pkv_plan_query", "pkv_status_string", "pkv_checkpoint_plan", "pkv_quantize_gather", "pkv_plan_repair",
             "pkv_plan_payload_bytes", "pkv_restore_from_host_noalloc", "pkv_cache_size", "pkv_cache_append",
             "pkv_cache_read", "pkv_attention_workspace", "pkv_attention", "pkv_rotate", "pkv_cache_append_rotated",
-            "pkv_attention_weights_workspace", "pkv_attention_weights")
+            "pkv_attention_weights_workspace", "pkv_attention_weights", "pkv_cache_keep", "pkv_cache_evict")
 
 
 class PkvModel(ctypes.Structure):
@@ -90,6 +90,12 @@ class PkvWeights(ctypes.Structure):
     _fields_ = [("heads", ctypes.c_int32), ("decay", ctypes.c_float), ("tokens", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64), ("seq_stride", ctypes.c_int64), ("weights", ctypes.c_void_p),
                 ("out", ctypes.c_void_p)]
+
+
+class PkvKept(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("budget", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("recent", ctypes.c_int32), ("budgets", ctypes.c_void_p), ("kept", ctypes.c_void_p),
+                ("kept_lens", ctypes.c_void_p)]
 
 
 class PkvError(RuntimeError):
@@ -157,6 +163,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pkv_attention_weights_workspace.restype = i32
     lib.pkv_attention_weights.argtypes = [model, cache, batch, attention, weights, vp]
     lib.pkv_attention_weights.restype = i32
+    kept = ctypes.POINTER(PkvKept)
+    lib.pkv_cache_keep.argtypes = [model, batch, weights, kept, vp]
+    lib.pkv_cache_keep.restype = i32
+    lib.pkv_cache_evict.argtypes = [model, cache, batch, kept, weights, vp, i32, vp]
+    lib.pkv_cache_evict.restype = i32
     _lib = lib
     return lib
 
@@ -499,3 +510,12 @@ def pkv_attention_weights_workspace(model: PkvModel, cache: PkvPagedCache, batch
 def pkv_attention_weights_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, attention: PkvAttention,
                                  weights: PkvWeights, stream=0) -> int:
     return load().pkv_attention_weights(model, cache, batch, attention, weights, stream or None)
+
+
+def pkv_cache_keep_status(model: PkvModel, batch: PkvBatch, weights: PkvWeights, kept: PkvKept, stream=0) -> int:
+    return load().pkv_cache_keep(model, batch, weights, kept, stream or None)
+
+
+def pkv_cache_evict_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, kept: PkvKept,
+                           weights: Optional[PkvWeights], page_table, table_pages: int, stream=0) -> int:
+    return load().pkv_cache_evict(model, cache, batch, kept, weights, page_table, table_pages, stream or None)

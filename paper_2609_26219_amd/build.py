@@ -23,7 +23,7 @@ HIP_FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC", "-Wall",
 CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra", f"-I{INCLUDE}", f"-I{CSRC}"]
 HOST_SRC = ("plan.cpp", "serve_plan.cpp")
 # The attention kernels are built once for each head_dim.
-HIP_SRC = (("restore.hip", ()), ("gather.hip", ()), ("serve.hip", ()),
+HIP_SRC = (("restore.hip", ()), ("gather.hip", ()), ("serve.hip", ()), ("evict.hip", ()),
            *((src, (f"-DPKV_HEAD_DIM={d}",)) for src in ("attend.hip", "weigh.hip") for d in (64, 128, 256)))
 
 

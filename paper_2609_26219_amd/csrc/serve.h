@@ -54,6 +54,21 @@ constexpr SequenceRows rows_of_sequence(const ServeArgs& s, int32_t start, int32
   return r;
 }
 
+// Of a sequence's rows that are the last of its tokens, those [first, end) that see one of tokens [begin, last], with a
+// window (0: none) and sinks (a superset: all of the tokens may be between sinks and window).  Always within the rows.
+struct RowRange {
+  int32_t first, end;
+};
+constexpr RowRange rows_that_see(const SequenceRows& g, int32_t begin, int32_t last, int32_t window, int32_t sinks) {
+  if (g.count <= 0) return RowRange{0, 0};
+  const int64_t pos0 = int64_t(g.kv_len) - g.trail;  // of row 0; below zero where rows are more than tokens
+  int64_t first = begin - pos0, end = g.count;
+  if (window > 0 && begin >= sinks && int64_t(last) + window - pos0 < end) end = int64_t(last) + window - pos0;
+  end = end < 0 ? 0 : end;
+  first = first < 0 ? 0 : first < end ? first : end;
+  return RowRange{int32_t(first), int32_t(end)};
+}
+
 struct RowArgs {
   uint16_t* k;
   uint16_t* v;
@@ -126,6 +141,41 @@ struct WeighLaunch {
   uint64_t workspace_bytes;
 };
 
+// The tokens of each sequence (and head) that stay.
+struct KeepArgs {
+  const float* weights;
+  const int32_t* budgets;  // of each sequence, or null
+  int32_t* kept;           // [num_seqs][heads][budget]
+  int32_t* kept_lens;
+  int64_t seq_stride, head_stride;
+  int32_t heads, budget, sinks, recent;
+};
+
+// Rows of a cache moved to where they stay, and the weights with them.
+struct EvictArgs {
+  const int32_t* kept;
+  const int32_t* kept_lens;
+  const int32_t* table;    // pages that the rows go to, or null: in place
+  float* weights;
+  int64_t seq_stride, weight_stride;
+  int32_t heads, budget;
+  int32_t table_pages;
+  int32_t weight_units;    // workgroups of a sequence that move weights,
+  int32_t units;           // and all of them: H * 2 * slices * splits more
+  int32_t slices, splits;  // of a row's bytes; of the rows
+  int32_t k_slices, v_slices, k_bytes, v_bytes;  // of a row
+  int32_t piece_bytes, log2_lanes;               // a lane's part of a row, and the lanes of a slice
+};
+
+// Tokens of a sequence, and how many of them stay, from what the device's arrays hold.
+constexpr int32_t kept_len(const ServeArgs& s, int32_t kv_len) {
+  return kv_len < 0 ? 0 : kv_len < s.max_kv ? kv_len : s.max_kv;
+}
+constexpr int32_t kept_budget(const KeepArgs& a, int32_t n, int32_t budget) {
+  budget = budget < 0 ? 0 : budget < a.budget ? budget : a.budget;
+  return budget < n ? budget : n;
+}
+
 constexpr int kMostChunk = 512;  // tokens of a workgroup of few rows
 constexpr int weigh_tokens(int head_dim) { return head_dim > 128 ? 128 : 256; }  // of many rows
 
@@ -162,6 +212,10 @@ pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool poin
 AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a);
 pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_weights_t* w, bool pointers, WeighArgs* out,
                         WeighLaunch* launch);
+
+pkv_status_t keep_args(const ServeArgs& s, const pkv_weights_t* w, const pkv_kept_t* k, KeepArgs* out);
+pkv_status_t evict_args(const ServeArgs& s, const pkv_kept_t* k, const pkv_weights_t* w, const int32_t* page_table,
+                        int32_t table_pages, EvictArgs* out);
 
 }  // namespace pkv
 

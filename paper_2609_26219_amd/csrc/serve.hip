@@ -669,6 +669,9 @@ pkv_status_t launch_attend_256(const ServeArgs& s, const AttendArgs& a, int64_t 
 pkv_status_t launch_weigh_64(const ServeArgs& s, const WeighArgs& a, const WeighLaunch& l, hipStream_t stream);
 pkv_status_t launch_weigh_128(const ServeArgs& s, const WeighArgs& a, const WeighLaunch& l, hipStream_t stream);
 pkv_status_t launch_weigh_256(const ServeArgs& s, const WeighArgs& a, const WeighLaunch& l, hipStream_t stream);
+// (evict.hip)
+pkv_status_t launch_keep(const ServeArgs& s, const KeepArgs& a, hipStream_t stream);
+pkv_status_t launch_evict(const ServeArgs& s, const EvictArgs& a, hipStream_t stream);
 
 }  // namespace pkv
 
@@ -748,6 +751,35 @@ pkv_status_t pkv_attention_weights(const pkv_model_t* model, const pkv_paged_cac
   if (s.D == 64) return pkv::launch_weigh_64(s, a, l, stream);
   if (s.D == 128) return pkv::launch_weigh_128(s, a, l, stream);
   return pkv::launch_weigh_256(s, a, l, stream);
+}
+
+pkv_status_t pkv_cache_keep(const pkv_model_t* model, const pkv_batch_t* batch, const pkv_weights_t* weights,
+                            const pkv_kept_t* kept, void* hip_stream) {
+  pkv::ServeArgs s;
+  pkv::KeepArgs a;
+  pkv_status_t st = pkv::batch_args(model, batch, false, &s);
+  if (st == PKV_OK) st = pkv::keep_args(s, weights, kept, &a);
+  if (st != PKV_OK || s.num_seqs == 0) return st;
+  const pkv::OnDevice here;
+  if (!here.ok) return PKV_ERR_DEVICE;
+  if (!here.has(s.kv_lens) || !here.has(a.weights) || !here.has(a.budgets) || !here.has(a.kept) || !here.has(a.kept_lens))
+    return PKV_ERR_INVALID_ARGUMENT;
+  return pkv::launch_keep(s, a, static_cast<hipStream_t>(hip_stream));
+}
+
+pkv_status_t pkv_cache_evict(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
+                             const pkv_kept_t* kept, const pkv_weights_t* weights, const int32_t* page_table,
+                             int32_t table_pages, void* hip_stream) {
+  pkv::ServeArgs s;
+  pkv::EvictArgs a;
+  pkv_status_t st = pkv::serve_args(model, cache, batch, true, &s);
+  if (st == PKV_OK) st = pkv::evict_args(s, kept, weights, page_table, table_pages, &a);
+  if (st != PKV_OK || s.num_seqs == 0) return st;
+  const pkv::OnDevice here;
+  if (!here.ok) return PKV_ERR_DEVICE;
+  if (!here.has(s) || !here.has(a.kept) || !here.has(a.kept_lens) || !here.has(a.table) || !here.has(a.weights))
+    return PKV_ERR_INVALID_ARGUMENT;
+  return pkv::launch_evict(s, a, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

@@ -331,6 +331,72 @@ pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_
   return PKV_OK;
 }
 
+namespace {
+
+pkv_status_t kept_ok(const ServeArgs& s, const pkv_kept_t* k, const pkv_weights_t* w) {
+  if (!k || (k->heads != 1 && k->heads != s.H)) return PKV_ERR_INVALID_ARGUMENT;
+  if (k->budget < 0 || k->budget > (1 << 30) || k->sinks < 0 || k->recent < 0) return PKV_ERR_INVALID_ARGUMENT;
+  if (w && (!weights_ok(s, *w) || w->heads != k->heads)) return PKV_ERR_INVALID_ARGUMENT;
+  if (int64_t(s.num_seqs) * k->heads >= kMostGroups / 4) return PKV_ERR_INVALID_ARGUMENT;  // (of 1024 threads)
+  if (!aligned(k->kept, 4) || !aligned(k->kept_lens, 4) || !aligned(k->budgets, 4) || !aligned(s.kv_lens, 4))
+    return PKV_ERR_INVALID_ARGUMENT;
+  if (s.num_seqs > 0 && (!s.kv_lens || !k->kept_lens || (k->budget > 0 && !k->kept))) return PKV_ERR_INVALID_ARGUMENT;
+  return PKV_OK;
+}
+
+}  // namespace
+
+pkv_status_t keep_args(const ServeArgs& s, const pkv_weights_t* w, const pkv_kept_t* k, KeepArgs* out) {
+  if (!w) return PKV_ERR_INVALID_ARGUMENT;
+  const pkv_status_t st = kept_ok(s, k, w);
+  if (st != PKV_OK) return st;
+  if (!aligned(w->weights, 4) || (s.num_seqs > 0 && !w->weights)) return PKV_ERR_INVALID_ARGUMENT;
+  *out = KeepArgs{w->weights, k->budgets, k->kept, k->kept_lens, w->seq_stride, w->heads > 1 ? w->head_stride : 0,
+                  k->heads, k->budget, k->sinks, k->recent};
+  return PKV_OK;
+}
+
+pkv_status_t evict_args(const ServeArgs& s, const pkv_kept_t* k, const pkv_weights_t* w, const int32_t* page_table,
+                        int32_t table_pages, EvictArgs* out) {
+  const pkv_status_t st = kept_ok(s, k, w);
+  if (st != PKV_OK) return st;
+  if (!aligned(page_table, 4) || (page_table && table_pages < 1)) return PKV_ERR_INVALID_ARGUMENT;
+  if (w && (!aligned(w->out, 4) || (s.num_seqs > 0 && !w->out))) return PKV_ERR_INVALID_ARGUMENT;
+  if (s.num_seqs > 0 && (!s.page_table || !aligned(s.page_table, 4))) return PKV_ERR_INVALID_ARGUMENT;
+  EvictArgs e{};
+  e.kept = k->kept;
+  e.kept_lens = k->kept_lens;
+  e.table = page_table;
+  e.table_pages = table_pages;
+  e.heads = k->heads;
+  e.budget = k->budget;
+  if (w) {
+    e.weights = w->out;
+    e.seq_stride = w->seq_stride;
+    e.weight_stride = w->heads > 1 ? w->head_stride : 0;
+    e.weight_units = w->heads;
+  }
+  e.k_bytes = s.D * kKeyBits[s.tag] / 8;
+  e.v_bytes = s.D * kValueBits[s.tag] / 8;
+  e.piece_bytes = e.k_bytes % 16 || e.v_bytes % 16 ? 8 : 16;
+  const int32_t pieces = std::max(e.k_bytes, e.v_bytes) / e.piece_bytes;
+  while (e.log2_lanes < 2 && (1 << e.log2_lanes) < pieces) ++e.log2_lanes;
+  auto slices_of = [&](int32_t bytes) {
+    return (bytes / e.piece_bytes + (1 << e.log2_lanes) - 1) >> e.log2_lanes;
+  };
+  e.k_slices = slices_of(e.k_bytes);
+  e.v_slices = slices_of(e.v_bytes);
+  e.slices = std::max(e.k_slices, e.v_slices);
+  const int64_t chunk = 2048 >> e.log2_lanes;  // rows of a workgroup at a time
+  e.splits = 1;
+  if (page_table) e.splits = int32_t(std::max<int64_t>(1, (std::min<int64_t>(e.budget, s.max_kv) + chunk - 1) / chunk));
+  const int64_t units = e.weight_units + int64_t(s.H) * 2 * e.slices * e.splits;
+  if (units * std::max(1, s.num_seqs) >= kMostGroups) return PKV_ERR_INVALID_ARGUMENT;
+  e.units = int32_t(units);
+  *out = e;
+  return PKV_OK;
+}
+
 }  // namespace pkv
 
 extern "C" {

@@ -368,16 +368,9 @@ __global__ __launch_bounds__(kThreads, 2) void many_kernel(ServeArgs s, WeighArg
   }
 
   // The row tiles that see one of the workgroup's tokens, and this split's of them.
-  int64_t rows = int64_t(g.count) * a.group, first_row = 0;
-  if (!s.positions && g.count > 0) {
-    const int32_t pos0 = g.kv_len - g.trail;
-    const int64_t first = begin > pos0 ? begin - pos0 : 0;
-    int64_t end = g.count;
-    if (a.window > 0 && begin >= a.sinks && int64_t(last) + a.window - pos0 < end) end = int64_t(last) + a.window - pos0;
-    first_row = (first < end ? first : end) * a.group;
-    rows = (end > 0 ? end : 0) * a.group;
-    first_row = first_row < rows ? first_row : rows;
-  }
+  RowRange see_us{0, g.count > 0 ? g.count : 0};
+  if (!s.positions) see_us = rows_that_see(g, begin, last, a.window, a.sinks);
+  const int64_t first_row = int64_t(see_us.first) * a.group, rows = int64_t(see_us.end) * a.group;
   const int64_t tile0 = first_row / kRows, tiles = rows > first_row ? (rows + kRows - 1) / kRows - tile0 : 0;
   const int32_t from = int32_t(tile0 + tiles * split / a.splits), upto = int32_t(tile0 + tiles * (split + 1) / a.splits);
   const int32_t most = g.count * a.group;  // (below 2^31: num_tokens * Hq)

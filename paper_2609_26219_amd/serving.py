@@ -10,7 +10,9 @@ fills anew each step, and calls
 * :func:`attention`  attention of new or recomputed rows over the cache, with an
   optional sliding window and sinks;
 * :func:`rotate`, :func:`append_rotated`  rows turned to their rotary positions,
-  the keys on their way into the cache.
+  the keys on their way into the cache;
+* :func:`attention_weights`, :func:`keep`, :func:`evict`  how much attention cached
+  tokens receive, which stay under a budget, and the cache without the others.
 
 Nothing here waits for the device or copies from it.  Several host threads may
 use one cache, on one stream or on streams of their own.
@@ -355,3 +357,41 @@ def attention_weights(cache: PagedCache, batch: Batch, q, lse, out, weights=None
         status = binding.pkv_attention_weights_status(cache.model, struct, batch.struct, a, w, stream)
     _check(status, "pkv_attention_weights")
     return out
+
+
+def keep(cache: PagedCache, batch: Batch, weights, budget: int, sinks: int = 0, recent: int = 0, budgets=None, out=None):
+    """The tokens of each sequence that stay under a ``budget``: the first ``sinks``, the last ``recent``, and of those
+    between the ones of the largest ``weights`` (float32 ``[S, 1, tokens]``: one choice for all heads, or
+    ``[S, H, tokens]``: each head its own), equal ones lowest index first.  ``budgets``, int32 ``[S]``, sets a sequence's
+    own, up to ``budget``.  Returns ``(kept, kept_lens)``, int32 ``[S, 1 or H, budget]``, ascending and then -1, and
+    ``[S]`` (``out`` if given)."""
+    w = _weights(cache, batch, weights, weights)
+    if out is None:
+        out = (torch.empty((batch.struct.num_seqs, w.heads, max(0, budget)), dtype=torch.int32, device=cache.device),
+               torch.empty(batch.struct.num_seqs, dtype=torch.int32, device=cache.device))
+    kept = _kept(batch, *out, budgets, _int32(sinks), _int32(recent))
+    _need(kept.heads == w.heads and kept.budget == budget, "kept is [S, heads of weights, budget]")
+    _check(binding.pkv_cache_keep_status(cache.model, batch.struct, w, kept, _stream(cache)), "pkv_cache_keep")
+    return out
+
+
+def _kept(batch: Batch, kept, kept_lens, budgets=None, sinks: int = 0, recent: int = 0) -> binding.PkvKept:
+    _need(kept.dtype == torch.int32 and kept.dim() == 3 and kept.shape[0] == batch.struct.num_seqs and
+          kept.is_contiguous(), "kept is contiguous int32 [S, 1 or H, budget]")
+    return binding.PkvKept(kept.shape[1], kept.shape[2], sinks, recent, _per_sequence(batch, budgets, "budgets"),
+                           kept.data_ptr(), _per_sequence(batch, kept_lens, "kept_lens"))
+
+
+def evict(cache: PagedCache, batch: Batch, kept, kept_lens, weights=None, page_table=None, layer: int = 0) -> None:
+    """Move the rows that stay to the front of their sequence: row j becomes row ``kept[s, h, j]``, in place, or with a
+    ``page_table`` ``[S, pages]`` of other pages (where the batch's are shared, they keep theirs).  ``weights`` are moved
+    alike, in place, and 0 behind the rows that stayed.  The batch's ``kv_lens`` are only read: after the last layer the
+    lengths are ``kept_lens``, and what a sequence lost is added to its ``position_offset``."""
+    k = _kept(batch, kept, kept_lens)
+    w = None if weights is None else _weights(cache, batch, weights)
+    _need(page_table is None or (page_table.dtype == torch.int32 and page_table.dim() == 2 and
+                                 page_table.is_contiguous() and page_table.shape[0] == batch.struct.num_seqs),
+          "page_table is contiguous int32 [S, pages]")
+    table, pages = (None, 0) if page_table is None else (page_table.data_ptr(), page_table.shape[1])
+    _check(binding.pkv_cache_evict_status(cache.model, cache._at(layer), batch.struct, k, w, table, pages,
+                                          _stream(cache)), "pkv_cache_evict")
