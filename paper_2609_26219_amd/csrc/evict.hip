@@ -15,14 +15,19 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // ---- Which tokens stay ----
 //
-// The weights' bits as whole numbers in their order; the number of the last one kept is found a digit of 8 bits at a time
-// from the top (a count of each digit among those that share the digits found, in LDS), and then the tokens above it and the
-// first ones equal to it are written in order.  A workgroup takes one row of weights, each wave a run of it.
+// The weights' bits as whole numbers in their order (keys).  The key of the last token kept is found by its digits from the top:
+// how many tokens have each value of the first 11 bits; the ones that share the last one's are copied to LDS, and their next
+// bits are counted there (all tokens again, where they are too many).  Then the tokens above it and the first ones
+// equal to it are written in order.  A workgroup takes one row of weights, each wave a run of it, whose keys it keeps
+// in registers as far as they go.
 
 constexpr int kKeepThreads = 1024;
 constexpr int kKeepWaves = kKeepThreads / 64;
-constexpr int kCopies = 16;      // of a digit's count, so that lanes seldom meet in one
-constexpr int kHeldKeys = 32;    // a lane's keys that stay in registers
+constexpr int kDigits = 2048;       // of 11 bits
+constexpr int kCopies = 4;          // of their counts, so that lanes seldom meet in one
+constexpr int kListed = 20480;      // keys in LDS
+constexpr int kHeldKeys = 32;       // a lane's keys in registers
+constexpr int kLoadsAhead = 8;      // of the others, a lane's on their way at once
 
 // Larger weights have larger keys; +0 and -0 are one, NaN is below everything.
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -36,11 +41,63 @@ __device__ __forceinline__ int32_t before(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
 }
 
-template <bool HELD>
+struct KeepShared {
+  uint32_t count[kDigits * kCopies];
+  uint32_t list[kListed];
+  uint32_t sums[kKeepWaves];
+  int32_t above[kKeepWaves], equal[kKeepWaves];
+  uint32_t digit, left, among, listed;
+};
+
+// Adds a lane's digit to the counts, all lanes of a wave at once where they agree.
+__device__ __forceinline__ void count_digit(KeepShared& lds, bool on, uint32_t digit, int lane) {
+  const uint64_t who = __ballot(on);
+  if (!who) return;
+  const uint32_t one = uint32_t(__shfl(int(digit), __builtin_ctzll(who)));
+  if (__ballot(on && digit == one) == who) {
+    if (lane == 0) atomicAdd(&lds.count[one * kCopies], uint32_t(__builtin_popcountll(who)));
+  } else if (on) {
+    atomicAdd(&lds.count[digit * kCopies + (lane & (kCopies - 1))], 1u);
+  }
+}
+
+// The digit of the `need`-th largest key among those counted: lds.digit; lds.left of them are to be kept among the lds.among
+// that have it.  The counts are cleared for the next digit.
+__device__ __forceinline__ void find_digit(KeepShared& lds, uint32_t need) {
+  static_assert(kDigits == 2 * kKeepThreads, "two digits to a thread");
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t mine[2];
+#pragma unroll
+  for (int d = 0; d < 2; ++d) {  // digits from the top
+    const int at = (kDigits - 1 - 2 * tid - d) * kCopies;
+    u32x4& c = *reinterpret_cast<u32x4*>(&lds.count[at]);
+    mine[d] = c[0] + c[1] + c[2] + c[3];
+    c = u32x4{};
+  }
+  uint32_t upto = mine[0] + mine[1];
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t other = __shfl_up(upto, off);
+    upto += lane >= off ? other : 0;
+  }
+  if (lane == 63) lds.sums[wave] = upto;
+  __syncthreads();
+  uint32_t upper = upto - mine[0] - mine[1];  // keys of larger digits
+  for (int i = 0; i < wave; ++i) upper += lds.sums[i];
+#pragma unroll
+  for (int d = 0; d < 2; ++d) {
+    if (upper < need && need <= upper + mine[d]) {
+      lds.digit = uint32_t(kDigits - 1 - 2 * tid - d);
+      lds.left = need - upper;
+      lds.among = mine[d];
+    }
+    upper += mine[d];
+  }
+  __syncthreads();
+}
+
 __global__ __launch_bounds__(kKeepThreads) void keep_kernel(ServeArgs s, KeepArgs a) {
-  __shared__ uint32_t count[256 * kCopies];
-  __shared__ uint32_t digit, left;
-  __shared__ int32_t above[kKeepWaves], equal[kKeepWaves];
+  __shared__ KeepShared lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t seq = int32_t(blockIdx.x / uint32_t(a.heads)), head = int32_t(blockIdx.x % uint32_t(a.heads));
   const float* w = a.weights + int64_t(seq) * a.seq_stride + int64_t(head) * a.head_stride;
@@ -48,97 +105,111 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(ServeArgs s, KeepArg
   const int32_t n = kept_len(s, s.kv_lens[seq]);
   const int32_t m = kept_budget(a, n, a.budgets ? a.budgets[seq] : a.budget);
   const int32_t first = a.sinks < m ? a.sinks : m, last = a.recent < m - first ? a.recent : m - first;
-  if (head == 0 && tid == 0) a.kept_lens[seq] = m;
-  const int32_t middle = n - first - last;  // tokens to choose from,
+  const int32_t middle = n - first - last;     // tokens to choose from,
   uint32_t need = uint32_t(m - first - last);  // and how many of them stay
-  for (int32_t j = tid; j < first; j += kKeepThreads) kept[j] = j;
-  for (int32_t j = tid; j < last; j += kKeepThreads) kept[m - last + j] = n - last + j;
-  for (int32_t j = m + tid; j < a.budget; j += kKeepThreads) kept[j] = -1;
-  if (need == 0) return;
-  if (need == uint32_t(middle)) {
-    for (int32_t j = tid; j < middle; j += kKeepThreads) kept[first + j] = first + j;
-    return;
-  }
 
   // The wave's run of the middle.
   const int32_t run = ((middle + kKeepThreads - 1) / kKeepThreads) * 64;
-  const int32_t from = wave * run, upto = from + run < middle ? from + run : middle;
+  const int32_t from = wave * run < middle ? wave * run : middle, upto = from + run < middle ? from + run : middle;
   w += first;
-  uint32_t held[HELD ? kHeldKeys : 1];
-  if constexpr (HELD) {
+  const bool choose = need != 0 && need != uint32_t(middle);
+  uint32_t held[kHeldKeys];
+  if (choose) {
 #pragma unroll
     for (int i = 0; i < kHeldKeys; ++i) {
       const int32_t at = from + 64 * i + lane;
-      held[i] = at < upto ? key_of(w[at]) : 0;
+      held[i] = at < upto ? __float_as_uint(w[at]) : 0;
     }
   }
-  auto each = [&](auto f) {
-    if constexpr (HELD) {
+  if (head == 0 && tid == 0) a.kept_lens[seq] = m;
+  for (int32_t j = tid; j < first; j += kKeepThreads) kept[j] = j;
+  for (int32_t j = tid; j < last; j += kKeepThreads) kept[m - last + j] = n - last + j;
+  for (int32_t j = m + tid; j < a.budget; j += kKeepThreads) kept[j] = -1;
+  if (!choose) {
+    if (need)
+      for (int32_t j = tid; j < middle; j += kKeepThreads) kept[first + j] = first + j;
+    return;
+  }
+  for (int i = tid; i < kDigits * kCopies; i += kKeepThreads) lds.count[i] = 0;
+  if (tid == 0) lds.listed = 0;
+  __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kHeldKeys; ++i)
-        if (from + 64 * i < upto) f(from + 64 * i + lane, held[i]);
-    } else {
-      for (int32_t i = from; i < upto; i += 64) f(i + lane, i + lane < upto ? key_of(w[i + lane]) : 0);
+  for (int i = 0; i < kHeldKeys; ++i) held[i] = key_of(__uint_as_float(held[i]));
+
+  // f(place in the middle, whether there is such a token, its key) for the wave's run in order, all lanes at once.
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < kHeldKeys; ++i)
+      if (from + 64 * i < upto) f(from + 64 * i + lane, from + 64 * i + lane < upto, held[i]);
+    for (int32_t i = from + 64 * kHeldKeys; i < upto; i += 64 * kLoadsAhead) {
+      float v[kLoadsAhead];
+#pragma unroll
+      for (int e = 0; e < kLoadsAhead; ++e) v[e] = i + 64 * e + lane < upto ? w[i + 64 * e + lane] : 0.0f;
+#pragma unroll
+      for (int e = 0; e < kLoadsAhead; ++e)
+        if (i + 64 * e < upto) f(i + 64 * e + lane, i + 64 * e + lane < upto, key_of(v[e]));
     }
   };
 
-  uint32_t found = 0;  // digits found so far
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256 * kCopies; i += kKeepThreads) count[i] = 0;
-    __syncthreads();
-    each([&](int32_t at, uint32_t key) {
-      if (at < upto && uint64_t(key) >> (shift + 8) == found)
-        atomicAdd(&count[((key >> shift) & 255) * kCopies + (lane & (kCopies - 1))], 1u);
+  each([&](int32_t, bool is, uint32_t key) { count_digit(lds, is, key >> 21, lane); });
+  __syncthreads();
+  find_digit(lds, need);
+  uint32_t found = lds.digit;  // the digits found so far
+  need = lds.left;
+  const uint32_t among = lds.among;
+  const bool few = among <= kListed;
+  if (few) {
+    each([&](int32_t, bool is, uint32_t key) {
+      const bool on = is && key >> 21 == found;
+      const uint64_t who = __ballot(on);
+      if (!who) return;
+      uint32_t at = 0;
+      if (lane == 0) at = atomicAdd(&lds.listed, uint32_t(__builtin_popcountll(who)));
+      at = uint32_t(__shfl(int(at), 0));
+      if (on) lds.list[at + before(who)] = key;
     });
     __syncthreads();
-    if (tid < 64) {  // digits 255 - 4 tid .. downwards
-      uint32_t mine[4], sum = 0;
+  }
+  constexpr int kAt[2] = {10, 0}, kBits[2] = {11, 10};
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        uint32_t c = 0;
-        for (int i = 0; i < kCopies; ++i) c += count[(255 - 4 * lane - d) * kCopies + ((i + lane) & (kCopies - 1))];
-        mine[d] = c;
-        sum += c;
+  for (int d = 0; d < 2; ++d) {
+    const int shift = kAt[d], bits = kBits[d];
+    const uint32_t mask = (1u << bits) - 1;
+    if (few) {
+      for (uint32_t i = tid - lane; i < among; i += kKeepThreads) {
+        const bool is = i + lane < among;
+        const uint32_t key = is ? lds.list[i + lane] : 0;
+        count_digit(lds, is && key >> (shift + bits) == found, key >> shift & mask, lane);
       }
-      uint32_t upper = sum;
-      for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t other = __shfl_up(upper, off);
-        upper += lane >= off ? other : 0;
-      }
-      upper -= sum;  // of larger digits
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        if (upper < need && need <= upper + mine[d]) {
-          digit = uint32_t(255 - 4 * lane - d);
-          left = need - upper;
-        }
-        upper += mine[d];
-      }
+    } else {
+      each([&](int32_t, bool is, uint32_t key) {
+        count_digit(lds, is && key >> (shift + bits) == found, key >> shift & mask, lane);
+      });
     }
     __syncthreads();
-    found = found << 8 | digit;
-    need = left;
+    find_digit(lds, need);
+    found = found << bits | lds.digit;
+    need = lds.left;
   }
 
   // `found` is the last key kept, `need` of its tokens stay.
   int32_t more = 0, same = 0;
-  each([&](int32_t at, uint32_t key) {
-    more += __builtin_popcountll(__ballot(at < upto && key > found));
-    same += __builtin_popcountll(__ballot(at < upto && key == found));
+  each([&](int32_t, bool is, uint32_t key) {
+    more += __builtin_popcountll(__ballot(is && key > found));
+    same += __builtin_popcountll(__ballot(is && key == found));
   });
   if (lane == 0) {
-    above[wave] = more;
-    equal[wave] = same;
+    lds.above[wave] = more;
+    lds.equal[wave] = same;
   }
   __syncthreads();
   int32_t higher = 0, ties = 0;  // in the runs before
   for (int i = 0; i < wave; ++i) {
-    higher += above[i];
-    ties += equal[i];
+    higher += lds.above[i];
+    ties += lds.equal[i];
   }
   const int32_t most = int32_t(need);
-  each([&](int32_t at, uint32_t key) {
-    const bool is = at < upto;
+  each([&](int32_t at, bool is, uint32_t key) {
     const uint64_t gt = __ballot(is && key > found), eq = __ballot(is && key == found);
     const int32_t tie = ties + before(eq);
     const int32_t place = higher + before(gt) + (tie < most ? tie : most);
@@ -152,11 +223,8 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(ServeArgs s, KeepArg
 //
 // Row j of a sequence becomes its row kept[j] >= j.  In place that is one chain: a workgroup goes over one slice of the rows'
 // bytes (of one head's K or V) in order, reads a chunk of rows, and writes it once all its threads have read theirs; what later
-// chunks read lies behind what it writes.  Chains are many because every head, K and V, and every 64 bytes of a row are one
-// of their own.  To other pages there is no order to keep, and chunks are workgroups too.
-
-constexpr int kThreads = 256;
-constexpr int kRowsAhead = 8;  // rows of a thread in a chunk
+// chunks read lies behind what it writes.  Chains are many because every head, K and V, and every slice of a row are one
+// of their own, and a chunk is as much as 1024 threads hold.  To other pages there is no order to keep, and chunks are workgroups.
 
 template <int BYTES>
 struct Piece;
@@ -165,18 +233,21 @@ struct Piece<16> { typedef u32x4 type; };
 template <>
 struct Piece<8> { typedef u32x2 type; };
 
-// Rows that are not there.
-constexpr int32_t kNone = -1;
+// Where a row goes from and to: page and slot, page -1 for none.
+struct Move {
+  int32_t from_page, from_slot, to_page, to_slot;
+};
 
 __device__ __forceinline__ int32_t page_at(const int32_t* table, int32_t width, int64_t pool, int32_t at) {
-  if (at >= width) return kNone;
+  if (at >= width) return -1;
   const int32_t p = table[at];
-  return p >= 0 && p < pool ? p : kNone;
+  return p >= 0 && p < pool ? p : -1;
 }
 
-template <int BYTES>
-__global__ __launch_bounds__(kThreads) void evict_kernel(ServeArgs s, EvictArgs a) {
+template <int BYTES, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 4) void evict_kernel(ServeArgs s, EvictArgs a) {
   typedef typename Piece<BYTES>::type Word;
+  __shared__ Move moves[move_rows(THREADS, 2)];
   const int tid = threadIdx.x;
   const int32_t seq = int32_t(blockIdx.x / uint32_t(a.units));
   int32_t unit = int32_t(blockIdx.x % uint32_t(a.units));
@@ -190,23 +261,25 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(ServeArgs s, EvictArgs 
     float* w = a.weights + int64_t(seq) * a.seq_stride + int64_t(unit) * a.weight_stride;
     const int32_t* kept = a.kept + (int64_t(seq) * a.heads + unit) * a.budget;
     if (m >= n) return;
-    for (int32_t c0 = 0; c0 < m; c0 += kThreads * kRowsAhead) {
+    for (int32_t c0 = 0; c0 < m; c0 += THREADS * kRowsAhead) {
+      int32_t from[kRowsAhead];
       float v[kRowsAhead];
 #pragma unroll
       for (int i = 0; i < kRowsAhead; ++i) {
-        const int32_t j = c0 + i * kThreads + tid;
-        const int32_t from = j < m ? kept[j] : kNone;
-        v[i] = from >= 0 && from < n ? w[from] : 0.0f;
+        const int32_t j = c0 + i * THREADS + tid;
+        from[i] = j < m ? kept[j] : -1;
       }
+#pragma unroll
+      for (int i = 0; i < kRowsAhead; ++i) v[i] = from[i] >= 0 && from[i] < n ? w[from[i]] : 0.0f;
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < kRowsAhead; ++i) {
-        const int32_t j = c0 + i * kThreads + tid;
+        const int32_t j = c0 + i * THREADS + tid;
         if (j < m) w[j] = v[i];
       }
     }
     __syncthreads();
-    for (int64_t j = m + tid; j < n; j += kThreads) w[j] = 0.0f;
+    for (int64_t j = m + tid; j < n; j += THREADS) w[j] = 0.0f;
     return;
   }
   unit -= a.weight_units;
@@ -223,8 +296,9 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(ServeArgs s, EvictArgs 
   const int32_t target_pages = in_place ? s.pages_per_seq : a.table_pages;
 
   // A row's slice is 1 << log2_lanes pieces, one to a lane.
-  const int32_t piece = (slice << a.log2_lanes) + (tid & ((1 << a.log2_lanes) - 1)), row_of = tid >> a.log2_lanes;
-  const int32_t per = kThreads >> a.log2_lanes, chunk = per * kRowsAhead;
+  const int32_t lane = tid & ((1 << a.log2_lanes) - 1), row0 = tid >> a.log2_lanes;
+  const int32_t piece = (slice << a.log2_lanes) + lane;
+  const int32_t per = THREADS >> a.log2_lanes, chunk = move_rows(THREADS, a.log2_lanes);
   const int32_t row_bytes = which ? a.v_bytes : a.k_bytes;
   const bool mine = piece * BYTES < row_bytes;
   const bool scaled = s.tag != PKV_TAG_FP16 && piece == 0;  // the lane with a row's scale and zero
@@ -241,37 +315,43 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(ServeArgs s, EvictArgs 
   }
   uint32_t* scales = s.scales + ((int64_t(head) * 2 + which) << s.log2P);
   const int32_t slots = (1 << s.log2P) - 1;
-  for (int32_t c0 = split * chunk; c0 < m; c0 += a.splits * chunk) {
+  for (int64_t c0 = int64_t(split) * chunk; c0 < m; c0 += int64_t(a.splits) * chunk) {
+    // The chunk's moves, a row to a thread.
+    for (int32_t r = tid; r < chunk; r += THREADS) {
+      const int64_t j = c0 + r;
+      Move v{-1, 0, -1, int32_t(j) & slots};
+      const int32_t at = j < m ? kept[j] : -1;
+      if (at >= 0 && at < n && (!in_place || at != j)) {
+        v.from_page = page_at(source_table, s.pages_per_seq, s.pool_pages, at >> s.log2P);
+        v.from_slot = at & slots;
+        v.to_page = page_at(target_table, target_pages, s.pool_pages, int32_t(j >> s.log2P));
+        if (v.to_page < 0) v.from_page = -1;
+      }
+      moves[r] = v;
+    }
+    __syncthreads();
     Word v[kRowsAhead];
     uint32_t sz[kRowsAhead];
-    int32_t from[kRowsAhead], to[kRowsAhead];
 #pragma unroll
     for (int i = 0; i < kRowsAhead; ++i) {
-      const int32_t j = c0 + i * per + row_of;
-      from[i] = j < m ? kept[j] : kNone;
-    }
-#pragma unroll
-    for (int i = 0; i < kRowsAhead; ++i) {
-      const int32_t j = c0 + i * per + row_of, at = from[i];
-      to[i] = kNone;
-      if (mine && at >= 0 && at < n && (!in_place || at != j)) {
-        const int32_t page = page_at(source_table, s.pages_per_seq, s.pool_pages, at >> s.log2P);
-        if (page >= 0) {
-          to[i] = page_at(target_table, target_pages, s.pool_pages, j >> s.log2P);
-          v[i] = *reinterpret_cast<const Word*>(base + page * page_bytes + (at & slots) * slot_bytes);
-          if (scaled) sz[i] = scales[page * s.scale_stride + (at & slots)];
-        }
+      if (i * per >= chunk) break;
+      const Move& at = moves[i * per + row0];
+      if (mine && at.from_page >= 0) {
+        v[i] = *reinterpret_cast<const Word*>(base + at.from_page * page_bytes + at.from_slot * slot_bytes);
+        if (scaled) sz[i] = scales[at.from_page * s.scale_stride + at.from_slot];
       }
     }
     if (in_place) __syncthreads();
 #pragma unroll
     for (int i = 0; i < kRowsAhead; ++i) {
-      const int32_t j = c0 + i * per + row_of;
-      if (to[i] >= 0) {
-        *reinterpret_cast<Word*>(base + to[i] * page_bytes + (j & slots) * slot_bytes) = v[i];
-        if (scaled) scales[to[i] * s.scale_stride + (j & slots)] = sz[i];
+      if (i * per >= chunk) break;
+      const Move& at = moves[i * per + row0];
+      if (mine && at.from_page >= 0) {
+        *reinterpret_cast<Word*>(base + at.to_page * page_bytes + at.to_slot * slot_bytes) = v[i];
+        if (scaled) scales[at.to_page * s.scale_stride + at.to_slot] = sz[i];
       }
     }
+    __syncthreads();
   }
 }
 
@@ -279,15 +359,20 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(ServeArgs s, EvictArgs 
 
 pkv_status_t launch_keep(const ServeArgs& s, const KeepArgs& a, hipStream_t stream) {
   const dim3 grid(uint32_t(s.num_seqs) * uint32_t(a.heads));
-  if (s.max_kv <= kHeldKeys * kKeepThreads) hipLaunchKernelGGL(keep_kernel<true>, grid, dim3(kKeepThreads), 0, stream, s, a);
-  else hipLaunchKernelGGL(keep_kernel<false>, grid, dim3(kKeepThreads), 0, stream, s, a);
+  hipLaunchKernelGGL(keep_kernel, grid, dim3(kKeepThreads), 0, stream, s, a);
   return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_DEVICE;
 }
 
 pkv_status_t launch_evict(const ServeArgs& s, const EvictArgs& a, hipStream_t stream) {
   const dim3 grid(uint32_t(s.num_seqs) * uint32_t(a.units));
-  if (a.piece_bytes == 16) hipLaunchKernelGGL(evict_kernel<16>, grid, dim3(kThreads), 0, stream, s, a);
-  else hipLaunchKernelGGL(evict_kernel<8>, grid, dim3(kThreads), 0, stream, s, a);
+  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, s, a); };
+  if (a.table) {
+    if (a.piece_bytes == 16) go(evict_kernel<16, kMoveThreads>, kMoveThreads);
+    else go(evict_kernel<8, kMoveThreads>, kMoveThreads);
+  } else {
+    if (a.piece_bytes == 16) go(evict_kernel<16, kChainThreads>, kChainThreads);
+    else go(evict_kernel<8, kChainThreads>, kChainThreads);
+  }
   return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_DEVICE;
 }
 

@@ -167,6 +167,13 @@ struct EvictArgs {
   int32_t piece_bytes, log2_lanes;               // a lane's part of a row, and the lanes of a slice
 };
 
+constexpr int kMoveThreads = 256;    // of a workgroup that moves rows to other pages,
+constexpr int kChainThreads = 1024;  // and in place
+constexpr int kRowsAhead = 8;        // rows of a thread on their way at once
+// Rows of a workgroup on their way at once, whose slices are so many lanes wide (narrow ones fewer than that, for their
+// places are in LDS).
+constexpr int move_rows(int threads, int log2_lanes) { return (threads * kRowsAhead) >> (log2_lanes < 2 ? 2 : log2_lanes); }
+
 // Tokens of a sequence, and how many of them stay, from what the device's arrays hold.
 constexpr int32_t kept_len(const ServeArgs& s, int32_t kv_len) {
   return kv_len < 0 ? 0 : kv_len < s.max_kv ? kv_len : s.max_kv;

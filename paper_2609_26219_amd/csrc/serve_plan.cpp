@@ -379,15 +379,20 @@ pkv_status_t evict_args(const ServeArgs& s, const pkv_kept_t* k, const pkv_weigh
   e.k_bytes = s.D * kKeyBits[s.tag] / 8;
   e.v_bytes = s.D * kValueBits[s.tag] / 8;
   e.piece_bytes = e.k_bytes % 16 || e.v_bytes % 16 ? 8 : 16;
+  // Slices: whole rows (up to 256 bytes) to other pages; in place as wide as leaves a compute unit its workgroup, 64 bytes at
+  // least.
   const int32_t pieces = std::max(e.k_bytes, e.v_bytes) / e.piece_bytes;
-  while (e.log2_lanes < 2 && (1 << e.log2_lanes) < pieces) ++e.log2_lanes;
+  while (e.log2_lanes < 4 && (1 << e.log2_lanes) < pieces) ++e.log2_lanes;
   auto slices_of = [&](int32_t bytes) {
     return (bytes / e.piece_bytes + (1 << e.log2_lanes) - 1) >> e.log2_lanes;
   };
+  while (!page_table && e.log2_lanes > 2 &&
+         int64_t(s.num_seqs) * s.H * (slices_of(e.k_bytes) + slices_of(e.v_bytes)) < 256)
+    --e.log2_lanes;
   e.k_slices = slices_of(e.k_bytes);
   e.v_slices = slices_of(e.v_bytes);
   e.slices = std::max(e.k_slices, e.v_slices);
-  const int64_t chunk = 2048 >> e.log2_lanes;  // rows of a workgroup at a time
+  const int64_t chunk = move_rows(kMoveThreads, e.log2_lanes);
   e.splits = 1;
   if (page_table) e.splits = int32_t(std::max<int64_t>(1, (std::min<int64_t>(e.budget, s.max_kv) + chunk - 1) / chunk));
   const int64_t units = e.weight_units + int64_t(s.H) * 2 * e.slices * e.splits;

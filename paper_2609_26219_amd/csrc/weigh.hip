@@ -103,7 +103,7 @@ __device__ __forceinline__ u32x4 query_operand(const float (&v)[8], float down) 
 constexpr int kFewWaves = 8;
 
 template <bool BF16, int KB, bool WHOLE, int RT>
-__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(ServeArgs s, WeighArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, KB * D * RT <= 512 ? 4 : 2) void few_kernel(ServeArgs s, WeighArgs a) {
   constexpr bool kCodes = KB != 16;
   constexpr bool kHalf = kCodes || !BF16;
   constexpr int kSteps = D / 32;
@@ -123,7 +123,58 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(ServeArgs s, WeighA
     __syncthreads();
   }
 
+  // What the rows see between them; tiles of which none sees anything are not looked at.
+  int32_t hi_most = -1, lo_least = 0x7FFFFFFF;
+  if (g.count > 0 && !s.positions) {
+    hi_most = g.kv_len - g.trail + g.count - 1;
+    lo_least = sight_of(s, a, g, 0).lo;
+  } else if (s.positions) {
+    for (int32_t i = lane; i < g.count; i += 64) {
+      const Sight see = sight_of(s, a, g, i);
+      hi_most = max(hi_most, see.hi);
+      if (see.hi >= 0) lo_least = min(lo_least, see.lo);
+    }
+    for (int off = 1; off < 64; off <<= 1) {
+      hi_most = max(hi_most, __shfl_xor(hi_most, off));
+      lo_least = min(lo_least, __shfl_xor(lo_least, off));
+    }
+  }
+  hi_most = __builtin_amdgcn_readfirstlane(hi_most);
+  lo_least = __builtin_amdgcn_readfirstlane(lo_least);
+  auto seen = [&](int32_t t0) { return t0 <= hi_most && (t0 + kTokenTile - 1 > lo_least || t0 < a.sinks); };
+
   for (int32_t head = first_head; head < s.H && from < upto; head += heads) {
+    const Source src = source_of<KB>(s, seq, head);
+    Keys<KB> keys[2];  // of two tiles: one is used while the other is on its way
+    uint32_t words[2][2];
+    bool there[2][2];
+    auto load = [&](int b, int32_t t0) {
+      if (t0 >= upto || !seen(t0)) return;
+      Tile tile{t0, {-1, -1}};
+      if constexpr (WHOLE) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int32_t at = (t0 + 16 * u) >> s.log2P;
+          if (at < s.pages_per_seq) {
+            const int32_t p = scalar_entry(src.table, at);
+            tile.page[u] = p >= 0 && p < s.pool_pages ? p : -1;
+          }
+        }
+      }
+      load_keys<KB, WHOLE>(s, src, tile, c, x, keys[b]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int32_t t = t0 + 16 * u + x;
+        const int32_t page = WHOLE ? tile.page[u] : page_of(s, src.table, t >> s.log2P);
+        there[b][u] = page >= 0 && t < g.kv_len;
+        if constexpr (kCodes)
+          words[b][u] = src.scales[uint64_t(uint32_t(page < 0 ? 0 : page)) * uint32_t(s.scale_stride) +
+                                uint32_t(t & ((1 << s.log2P) - 1))];
+      }
+    };
+    load(0, from);
+    load(1, from + kTokenTile);
+
     // Row x of each row tile: its queries, and what it is scaled by.
     u32x4 q[RT][kSteps];
     f32x4 f[RT], less[RT], sum[RT];
@@ -181,52 +232,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(ServeArgs s, WeighA
       }
     }
 
-    // What the rows see between them; tiles of which none sees anything are not looked at.
-    int32_t hi_most = -1, lo_least = 0x7FFFFFFF;
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        hi_most = max(hi_most, hi[r][i]);
-        if (hi[r][i] >= 0) lo_least = min(lo_least, lo[r][i]);
-      }
-    hi_most = max(hi_most, __shfl_xor(hi_most, 16));
-    lo_least = min(lo_least, __shfl_xor(lo_least, 16));
-    hi_most = __builtin_amdgcn_readfirstlane(max(hi_most, __shfl_xor(hi_most, 32)));
-    lo_least = __builtin_amdgcn_readfirstlane(min(lo_least, __shfl_xor(lo_least, 32)));
-    auto seen = [&](int32_t t0) { return t0 <= hi_most && (t0 + kTokenTile - 1 > lo_least || t0 < a.sinks); };
-
-    const Source src = source_of<KB>(s, seq, head);
-    Keys<KB> keys;
-    uint32_t words[2];
-    bool there[2];
-    auto load = [&](int32_t t0) {
-      Tile tile{t0, {-1, -1}};
-      if constexpr (WHOLE) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int32_t at = (t0 + 16 * u) >> s.log2P;
-          if (at < s.pages_per_seq) {
-            const int32_t p = scalar_entry(src.table, at);
-            tile.page[u] = p >= 0 && p < s.pool_pages ? p : -1;
-          }
-        }
-      }
-      load_keys<KB, WHOLE>(s, src, tile, c, x, keys);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int32_t t = t0 + 16 * u + x;
-        const int32_t page = WHOLE ? tile.page[u] : page_of(s, src.table, t >> s.log2P);
-        there[u] = page >= 0 && t < g.kv_len;
-        if constexpr (kCodes)
-          words[u] = src.scales[uint64_t(uint32_t(page < 0 ? 0 : page)) * uint32_t(s.scale_stride) +
-                                uint32_t(t & ((1 << s.log2P) - 1))];
-      }
-    };
-    if (seen(from)) load(from);
-    for (int32_t t0 = from; t0 < upto; t0 += kTokenTile) {
-      const int32_t next = t0 + kTokenTile;
-      const bool more = next < upto && seen(next);
+    auto weigh = [&](int b, int32_t t0) {
       float w[2] = {0.0f, 0.0f};
       if (seen(t0)) {
         f32x4 score[RT][2];
@@ -234,21 +240,21 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(ServeArgs s, WeighA
         bool is[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          is[u] = there[u];
+          is[u] = there[b][u];
           if constexpr (kCodes) {
-            ks[u] = f16_float(words[u]);
-            kz[u] = __builtin_fmaf(ks[u], float(1 << (KB - 1)), f16_float(words[u] >> 16));
+            ks[u] = f16_float(words[b][u]);
+            kz[u] = __builtin_fmaf(ks[u], float(1 << (KB - 1)), f16_float(words[b][u] >> 16));
           }
 #pragma unroll
           for (int r = 0; r < RT; ++r) score[r][u] = f32x4{};
 #pragma unroll
           for (int i = 0; i < kSteps; ++i) {
-            const u32x4 k = k_operand<KB>(m, keys.w[u], i);
+            const u32x4 k = k_operand<KB>(m, keys[b].w[u], i);
 #pragma unroll
             for (int r = 0; r < RT; ++r) score[r][u] = mfma16<kHalf>(q[r][i], k, score[r][u]);
           }
         }
-        if (more) load(next);
+        load(b, t0 + 2 * kTokenTile);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int32_t tok = t0 + 16 * u + x;
@@ -266,8 +272,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(ServeArgs s, WeighA
           w[u] = over_c_sum(total);
           if (!is[u]) w[u] = 0.0f;
         }
-      } else if (more) {
-        load(next);
+      } else {
+        load(b, t0 + 2 * kTokenTile);
       }
       const int32_t tok = t0 + (lane & 31);
       if (lane < 32 && tok < upto) {
@@ -275,6 +281,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(ServeArgs s, WeighA
         if (a.joint) sums[wave][tok - from] += mine;
         else put(a, int64_t(seq) * a.seq_stride + int64_t(head) * a.head_stride + tok, mine);
       }
+    };
+    for (int32_t t0 = from; t0 < upto; t0 += 2 * kTokenTile) {
+      weigh(0, t0);
+      if (t0 + kTokenTile < upto) weigh(1, t0 + kTokenTile);
     }
   }
   if (!a.joint) return;
@@ -314,7 +324,8 @@ struct RowTile {
   u32x4 q[2 * D / 16][kRows + 1];  // [step][half][row], 4 banks on from one to the next
   float f[kRows], less[kRows], sum[kRows];
   int32_t hi[kRows], lo[kRows];
-  int32_t all_hi, any_hi, all_lo, any_lo;  // least and most of hi, most and least of lo
+  int32_t off;                             // whether some row gives nothing
+  int32_t all_hi, any_hi, all_lo, any_lo;  // rows at positions of their own: least and most of hi, most and least of lo
 };
 
 template <bool BF16, int KB>
@@ -375,28 +386,50 @@ __global__ __launch_bounds__(kThreads, 2) void many_kernel(ServeArgs s, WeighArg
   const int32_t from = int32_t(tile0 + tiles * split / a.splits), upto = int32_t(tile0 + tiles * (split + 1) / a.splits);
   const int32_t most = g.count * a.group;  // (below 2^31: num_tokens * Hq)
 
-  // A thread's part of a row tile: a piece of 8 channels of some rows, and one row's numbers.
+  // A thread's part of a row tile: a piece of 8 channels of some rows, and one row's numbers.  From one tile to the
+  // next its rows are kRows on, so that their tokens and heads are stepped, not divided for.
+  struct Cursor {
+    int32_t row, token, sub;
+  };
+  const int32_t step_token = kRows / a.group, step_sub = kRows % a.group;
+  auto cursor = [&](int64_t row) {
+    return Cursor{int32_t(row), int32_t(row / a.group), int32_t(row % a.group)};
+  };
+  auto step = [&](Cursor& at) {
+    at.row += kRows;
+    at.token += step_token;
+    at.sub += step_sub;
+    if (at.sub >= a.group) {
+      at.sub -= a.group;
+      ++at.token;
+    }
+  };
   const int piece = tid % kRowPieces, row0 = tid / kRowPieces;
+  const uint16_t* q_head = a.q + int64_t(g.start) * a.q_token_stride + int64_t(head * a.group) * a.q_head_stride + 8 * piece;
+  const float* lse = a.lse + int64_t(g.start) * a.Hq + head * a.group;
+  Cursor mine_rows[kPasses], my_row = cursor(int64_t(from) * kRows + (tid & (kRows - 1)));
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) mine_rows[i] = cursor(int64_t(from) * kRows + row0 + i * (kThreads / kRowPieces));
   u32x4 w[kPasses];
   float less = -kInf;
   Sight see{-1, -1};
-  auto fetch = [&](int32_t at) {
+  auto fetch = [&] {
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-      const int32_t row = at * kRows + row0 + i * (kThreads / kRowPieces);
+      Cursor& at = mine_rows[i];
       w[i] = u32x4{};
-      if (row < most)
-        w[i] = *reinterpret_cast<const u32x4*>(a.q + int64_t(g.start + row / a.group) * a.q_token_stride +
-                                               int64_t(head * a.group + row % a.group) * a.q_head_stride + 8 * piece);
+      if (at.row < most)
+        w[i] = *reinterpret_cast<const u32x4*>(q_head + int64_t(at.token) * a.q_token_stride + at.sub * a.q_head_stride);
+      step(at);
     }
     if (tid < kRows) {
-      const int32_t row = at * kRows + tid;
       less = -kInf;
       see = Sight{-1, -1};
-      if (row < most) {
-        less = less_of(a, g, row / a.group, head * a.group + row % a.group);
-        if (less != -kInf) see = sight_of(s, a, g, row / a.group);
+      if (my_row.row < most) {
+        less = lse[int64_t(my_row.token) * a.Hq + my_row.sub];
+        see = sight_of(s, a, g, my_row.token);
       }
+      step(my_row);
     }
   };
   auto leave = [&](RowTile& to) {
@@ -427,37 +460,54 @@ __global__ __launch_bounds__(kThreads, 2) void many_kernel(ServeArgs s, WeighArg
       }
     }
     if (tid < kRows) {
-      to.less[tid] = less;
+      if (less == -kInf) see = Sight{-1, -1};  // it saw nothing, and gives nothing
+      to.less[tid] = less == -kInf ? -kInf : less * -1.44269504088896340736f;
       to.hi[tid] = see.hi;
       to.lo[tid] = see.lo;
-      int32_t all_hi = see.hi, any_hi = see.hi, all_lo = see.lo, any_lo = see.hi < 0 ? 0x7FFFFFFF : see.lo;
-      for (int off = 1; off < kRows; off <<= 1) {
-        all_hi = min(all_hi, __shfl_xor(all_hi, off));
-        any_hi = max(any_hi, __shfl_xor(any_hi, off));
-        all_lo = max(all_lo, __shfl_xor(all_lo, off));
-        any_lo = min(any_lo, __shfl_xor(any_lo, off));
-      }
-      if (tid == 0) {
-        to.all_hi = all_hi;
-        to.any_hi = any_hi;
-        to.all_lo = all_lo;
-        to.any_lo = any_lo;
+      const bool off = __any(see.hi < 0);
+      if (tid == 0) to.off = off;
+      if (s.positions) {
+        int32_t all_hi = see.hi, any_hi = see.hi, all_lo = see.lo, any_lo = see.hi < 0 ? 0x7FFFFFFF : see.lo;
+        for (int by = 1; by < kRows; by <<= 1) {
+          all_hi = min(all_hi, __shfl_xor(all_hi, by));
+          any_hi = max(any_hi, __shfl_xor(any_hi, by));
+          all_lo = max(all_lo, __shfl_xor(all_lo, by));
+          any_lo = min(any_lo, __shfl_xor(any_lo, by));
+        }
+        if (tid == 0) {
+          to.all_hi = all_hi;
+          to.any_hi = any_hi;
+          to.all_lo = all_lo;
+          to.any_lo = any_lo;
+        }
       }
     }
   };
+  // First and last row of a tile, for rows in order.
+  Cursor first_of = cursor(int64_t(from) * kRows), last_of = cursor(int64_t(from) * kRows + kRows - 1);
 
   float total[kNT] = {};
   if (from < upto) {
-    fetch(from);
+    fetch();
     leave(lds[0]);
   }
   __syncthreads();
   for (int32_t at = from; at < upto; ++at) {
     const RowTile& r = lds[(at - from) & 1];
-    if (at + 1 < upto) fetch(at + 1);
+    if (at + 1 < upto) fetch();
     const int32_t end = mine + 32 * kNT - 1;
-    const int32_t any_hi = __builtin_amdgcn_readfirstlane(r.any_hi), any_lo = __builtin_amdgcn_readfirstlane(r.any_lo);
-    const int32_t all_hi = __builtin_amdgcn_readfirstlane(r.all_hi), all_lo = __builtin_amdgcn_readfirstlane(r.all_lo);
+    int32_t any_hi, any_lo, all_hi, all_lo;
+    if (s.positions) {
+      any_hi = __builtin_amdgcn_readfirstlane(r.any_hi), any_lo = __builtin_amdgcn_readfirstlane(r.any_lo);
+      all_hi = __builtin_amdgcn_readfirstlane(r.all_hi), all_lo = __builtin_amdgcn_readfirstlane(r.all_lo);
+    } else {
+      const Sight begins = sight_of(s, a, g, first_of.token);
+      const Sight ends = sight_of(s, a, g, last_of.token < g.count ? last_of.token : g.count - 1);
+      all_hi = begins.hi, any_hi = ends.hi, any_lo = begins.lo, all_lo = ends.lo;
+      step(first_of);
+      step(last_of);
+    }
+    const bool off = __builtin_amdgcn_readfirstlane(r.off);
     const bool none = any_hi < mine || (any_lo >= end && mine >= a.sinks);
     if (!none) {
       f32x16 score[kNT];
@@ -471,7 +521,7 @@ __global__ __launch_bounds__(kThreads, 2) void many_kernel(ServeArgs s, WeighArg
 #pragma unroll
         for (int t = 0; t < kNT; ++t) score[t] = mfma32<kHalf>(q, k[t][i], score[t]);
       }
-      const bool all = all_hi >= end && (all_lo < mine || end < a.sinks);
+      const bool all = !off && all_hi >= end && (all_lo < mine || end < a.sinks);
       // Value e of a lane is row 8 (e / 4) + 4 half + e % 4.
 #pragma unroll
       for (int t = 0; t < kNT; ++t) {
