@@ -131,14 +131,18 @@ struct WeighArgs {
   int32_t tiles;         // workgroups along a sequence's tokens
   int32_t chunk, subs;   // few rows: tokens of a workgroup, and the parts that its waves take
   int32_t splits;        // many rows: workgroups that share the rows of a tile of tokens
+  int32_t row_tiles;     // most tiles of rows of a sequence,
+  int64_t all_tiles;     // and of all of them
+  void* rows;            // the tiles, [H][all_tiles]
 };
 
 // How a call of weights is launched.
 struct WeighLaunch {
-  int32_t row_tiles;    // of few rows, or 0: many
-  int32_t tiles, chunk, subs, splits;
-  int64_t groups, join_groups;
-  uint64_t workspace_bytes;
+  int32_t few_tiles;    // tiles of few rows, or 0: many
+  int32_t tiles, chunk, subs, splits, row_tiles;
+  int64_t all_tiles, groups, prepare_groups, join_groups;
+  uint64_t part_bytes;      // of WeighArgs::part, then rows
+  uint64_t workspace_bytes; // both
 };
 
 // The tokens of each sequence (and head) that stay.
@@ -184,7 +188,10 @@ constexpr int32_t kept_budget(const KeepArgs& a, int32_t n, int32_t budget) {
 }
 
 constexpr int kMostChunk = 512;  // tokens of a workgroup of few rows
-constexpr int weigh_tokens(int head_dim) { return head_dim > 128 ? 128 : 256; }  // of many rows
+// Of many rows: tokens of a workgroup, rows of a tile, and its bytes (queries, and 5 numbers a row and 8 of all).
+constexpr int weigh_tokens(int head_dim) { return head_dim > 128 ? 128 : 256; }
+constexpr int kWeighRows = 32;
+constexpr int weigh_tile_bytes(int head_dim) { return kWeighRows * (2 * head_dim + 20) + 32; }
 
 // A launch has fewer than 2^32 threads, in workgroups of 256.
 constexpr int64_t kMostGroups = int64_t(1) << 24;

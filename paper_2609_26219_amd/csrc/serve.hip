@@ -745,7 +745,8 @@ pkv_status_t pkv_attention_weights(const pkv_model_t* model, const pkv_paged_cac
   if (st != PKV_OK || s.num_seqs == 0) return st;
   const pkv::OnDevice here;
   if (!here.ok) return PKV_ERR_DEVICE;
-  if (!here.has(s) || !here.has(a.q) || !here.has(a.lse) || !here.has(a.weights) || !here.has(a.out) || !here.has(a.part))
+  if (!here.has(s) || !here.has(a.q) || !here.has(a.lse) || !here.has(a.weights) || !here.has(a.out) || !here.has(a.part) ||
+      !here.has(a.rows))
     return PKV_ERR_INVALID_ARGUMENT;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (s.D == 64) return pkv::launch_weigh_64(s, a, l, stream);

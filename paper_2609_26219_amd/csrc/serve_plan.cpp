@@ -284,7 +284,7 @@ pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_
   if (s.num_seqs > 0) {
     const int64_t rows = int64_t(s.max_tokens) * r.group;
     if (rows <= kRowTile * few_tiles(s.D)) {
-      l.row_tiles = rows <= kRowTile ? 1 : 2;
+      l.few_tiles = rows <= kRowTile ? 1 : 2;
       // A workgroup's 8 waves take a KV head each, or parts of the tokens where there are fewer.
       while (l.subs < 8 && l.subs * 2 * s.H <= 8) l.subs *= 2;
       l.chunk = kTokenTile * l.subs;
@@ -295,19 +295,26 @@ pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_
       const int tokens = weigh_tokens(s.D);
       l.tiles = int32_t((int64_t(s.max_kv) + tokens - 1) / tokens);
       const int64_t base = int64_t(s.num_seqs) * l.tiles * s.H;
-      l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(6 * 256 / base, rows / 256)));
+      l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(12 * 256 / base, rows / 256)));
       l.groups = base * l.splits;
       if (l.splits > 1 || (r.joint && s.H > 1)) {
-        l.workspace_bytes = uint64_t(l.splits) * s.H * s.num_seqs * s.max_kv * 4;
+        l.part_bytes = (uint64_t(l.splits) * s.H * s.num_seqs * s.max_kv * 4 + 15) / 16 * 16;
         l.join_groups = int64_t(s.num_seqs) * w.heads * ((int64_t(s.max_kv) + 255) / 256);
       }
+      l.row_tiles = int32_t((rows + kWeighRows - 1) / kWeighRows);
+      l.all_tiles = int64_t(s.num_tokens) * r.group / kWeighRows + s.num_seqs + 1;
+      l.prepare_groups = int64_t(s.num_seqs) * l.row_tiles * s.H;
+      l.workspace_bytes = l.part_bytes + uint64_t(l.all_tiles) * s.H * weigh_tile_bytes(s.D);
     }
-    if (l.groups >= kMostGroups || l.join_groups >= kMostGroups) return PKV_ERR_INVALID_ARGUMENT;
+    if (l.groups >= kMostGroups || l.join_groups >= kMostGroups || l.prepare_groups >= kMostGroups)
+      return PKV_ERR_INVALID_ARGUMENT;
   }
   r.tiles = l.tiles;
   r.chunk = l.chunk;
   r.subs = l.subs;
   r.splits = l.splits;
+  r.row_tiles = l.row_tiles;
+  r.all_tiles = l.all_tiles;
   if (pointers) {
     if (!stride_ok(a->q_token_stride, a->q_head_stride, s.D)) return PKV_ERR_INVALID_ARGUMENT;
     if (s.num_seqs > 0) {  // (a call without rows still lets the weights fade)
@@ -324,7 +331,8 @@ pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_
     r.lse = a->lse;
     r.weights = w.decay != 0.0f ? w.weights : nullptr;
     r.out = w.out;
-    r.part = l.workspace_bytes ? static_cast<float*>(a->workspace) : nullptr;
+    r.part = l.part_bytes ? static_cast<float*>(a->workspace) : nullptr;
+    r.rows = l.workspace_bytes ? static_cast<char*>(a->workspace) + l.part_bytes : nullptr;
   }
   *out = r;
   *launch = l;

@@ -13,6 +13,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "pkv.h"
 #include "paged_tiles.h"
 #include "pkv_internal.h"
@@ -22,6 +24,7 @@ namespace pkv {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 // A sequence's rows, from what the device holds.
 __device__ __forceinline__ SequenceRows sequence_rows(const ServeArgs& s, int32_t seq) {
@@ -29,14 +32,17 @@ __device__ __forceinline__ SequenceRows sequence_rows(const ServeArgs& s, int32_
                           scalar_entry(s.kv_lens, seq));
 }
 
-// Position of a sequence's row `token`, and what it sees.
-__device__ __forceinline__ Sight sight_of(const ServeArgs& s, const WeighArgs& a, const SequenceRows& g, int32_t token) {
-  const int32_t pos = s.positions ? s.positions[g.start + token] : g.kv_len - g.trail + token;
+// What a row at position `pos` sees.
+__device__ __forceinline__ Sight sight_at(const WeighArgs& a, const SequenceRows& g, int32_t pos) {
   Sight see;
   see.hi = pos < g.kv_len ? pos : g.kv_len - 1;
   see.hi = see.hi < -1 ? -1 : see.hi;
   see.lo = a.window > 0 && pos >= a.window ? pos - a.window : -1;
   return see;
+}
+
+__device__ __forceinline__ Sight sight_of(const ServeArgs& s, const WeighArgs& a, const SequenceRows& g, int32_t token) {
+  return sight_at(a, g, s.positions ? s.positions[g.start + token] : g.kv_len - g.trail + token);
 }
 
 // What a row's scores are turned into probabilities by: exp2(f * (q . k) + less), the query's sum for the zeros of codes.
@@ -103,7 +109,7 @@ __device__ __forceinline__ u32x4 query_operand(const float (&v)[8], float down) 
 constexpr int kFewWaves = 8;
 
 template <bool BF16, int KB, bool WHOLE, int RT>
-__global__ __launch_bounds__(64 * kFewWaves, KB * D * RT <= 512 ? 4 : 2) void few_kernel(ServeArgs s, WeighArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ? 4 : 2) void few_kernel(ServeArgs s, WeighArgs a) {
   constexpr bool kCodes = KB != 16;
   constexpr bool kHalf = kCodes || !BF16;
   constexpr int kSteps = D / 32;
@@ -145,9 +151,10 @@ __global__ __launch_bounds__(64 * kFewWaves, KB * D * RT <= 512 ? 4 : 2) void fe
 
   for (int32_t head = first_head; head < s.H && from < upto; head += heads) {
     const Source src = source_of<KB>(s, seq, head);
-    Keys<KB> keys[2];  // of two tiles: one is used while the other is on its way
-    uint32_t words[2][2];
-    bool there[2][2];
+    constexpr int kTiles = KB * D > 2048 ? 1 : 2;  // on their way while one is used, as registers allow
+    Keys<KB> keys[kTiles];
+    uint32_t words[kTiles][2];
+    bool there[kTiles][2];
     auto load = [&](int b, int32_t t0) {
       if (t0 >= upto || !seen(t0)) return;
       Tile tile{t0, {-1, -1}};
@@ -172,8 +179,8 @@ __global__ __launch_bounds__(64 * kFewWaves, KB * D * RT <= 512 ? 4 : 2) void fe
                                 uint32_t(t & ((1 << s.log2P) - 1))];
       }
     };
-    load(0, from);
-    load(1, from + kTokenTile);
+#pragma unroll
+    for (int b = 0; b < kTiles; ++b) load(b, from + b * kTokenTile);
 
     // Row x of each row tile: its queries, and what it is scaled by.
     u32x4 q[RT][kSteps];
@@ -254,7 +261,7 @@ __global__ __launch_bounds__(64 * kFewWaves, KB * D * RT <= 512 ? 4 : 2) void fe
             for (int r = 0; r < RT; ++r) score[r][u] = mfma16<kHalf>(q[r][i], k, score[r][u]);
           }
         }
-        load(b, t0 + 2 * kTokenTile);
+        load(b, t0 + kTiles * kTokenTile);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int32_t tok = t0 + 16 * u + x;
@@ -267,13 +274,13 @@ __global__ __launch_bounds__(64 * kFewWaves, KB * D * RT <= 512 ? 4 : 2) void fe
               float t = score[r][u][i];
               if constexpr (kCodes) t = __builtin_fmaf(ks[u], t, kz[u] * sum[r][i]);
               const float p = exp2_of(__builtin_fmaf(t, f[r][i], less[r][i]));
-              total += tok <= hi[r][i] && (tok > lo[r][i] || sink) ? p : 0.0f;
+              total += (tok <= hi[r][i]) & ((tok > lo[r][i]) | sink) ? p : 0.0f;
             }
           w[u] = over_c_sum(total);
           if (!is[u]) w[u] = 0.0f;
         }
       } else {
-        load(b, t0 + 2 * kTokenTile);
+        load(b, t0 + kTiles * kTokenTile);
       }
       const int32_t tok = t0 + (lane & 31);
       if (lane < 32 && tok < upto) {
@@ -282,9 +289,10 @@ __global__ __launch_bounds__(64 * kFewWaves, KB * D * RT <= 512 ? 4 : 2) void fe
         else put(a, int64_t(seq) * a.seq_stride + int64_t(head) * a.head_stride + tok, mine);
       }
     };
-    for (int32_t t0 = from; t0 < upto; t0 += 2 * kTokenTile) {
-      weigh(0, t0);
-      if (t0 + kTokenTile < upto) weigh(1, t0 + kTokenTile);
+    for (int32_t t0 = from; t0 < upto; t0 += kTiles * kTokenTile) {
+#pragma unroll
+      for (int b = 0; b < kTiles; ++b)
+        if (t0 + b * kTokenTile < upto) weigh(b, t0 + b * kTokenTile);
     }
   }
   if (!a.joint) return;
@@ -300,41 +308,125 @@ __global__ __launch_bounds__(64 * kFewWaves, KB * D * RT <= 512 ? 4 : 2) void fe
 
 // ---- Many rows ----
 //
-// A workgroup keeps the keys of 4 * kTokens tokens of one sequence and KV head in registers (each wave its own) and goes
-// over the rows that see them, 32 at a time, which its threads bring to LDS in the operands' order, the next ones on
-// their way while these are used.
+// Every row is used by all the tokens that it sees, so the rows are prepared once: their queries in the order of the matrix
+// operands, 32 rows to a tile, what they are scaled by and what they see.  Then every wave keeps the keys of 32 * kNT tokens
+// of one sequence and KV head in registers and goes over the tiles, a tile ahead of use loaded straight to registers as they
+// lie (the four waves of a workgroup find them in L1 after the first of them; through LDS the barrier of every tile cost more
+// than the loads).  While the exponentials of some scores are worked out the matrix units work on the next ones.
 
 constexpr int kThreads = 256;
 constexpr int kNT = D > 128 ? 1 : 2;  // token tiles of 32 of a wave
-constexpr int kRows = 32;
+constexpr int kRows = kWeighRows;
 constexpr int kRowPieces = D / 8;
+constexpr int kQueries = 2 * D / 16 * kRows;  // pieces of 8 channels of a tile
 
-// First channel of the 8 that lane half k has in instruction `step`, from pieces of up to 16 bytes; and the other way round.
+// Which operand the 8 channels from `channel` on are part of (2 * step + lane half), with lanes that load pieces of up to 16
+// bytes of keys.
 template <int BITS>
 struct Halves {
   static constexpr int kBytes = D / 2 * BITS / 8 < 16 ? D / 2 * BITS / 8 : 16, kPer = kBytes * 8 / BITS, kOps = kPer / 8;
   static constexpr int kPieces = D / 2 * BITS / 8 / kBytes;
-  static __device__ constexpr int slot(int channel) {  // 2 * step + half
+  static __device__ constexpr int slot(int channel) {
     const int piece = channel / kPer, step = piece / 2 * kOps + channel % kPer / 8;
     return 2 * step + (piece & 1);
   }
 };
 
-struct RowTile {
-  u32x4 q[2 * D / 16][kRows + 1];  // [step][half][row], 4 banks on from one to the next
-  float f[kRows], less[kRows], sum[kRows];
+struct RowNumbers {
+  float less[kRows];
+  // Whether some row gives nothing; least and most of hi, most and least of lo.
+  int32_t off, all_hi, any_hi, all_lo, any_lo, unused[3];
+  float f[kRows], sum[kRows];
   int32_t hi[kRows], lo[kRows];
-  int32_t off;                             // whether some row gives nothing
-  int32_t all_hi, any_hi, all_lo, any_lo;  // rows at positions of their own: least and most of hi, most and least of lo
 };
+struct RowTile {
+  u32x4 q[kQueries];  // [step][half][row]
+  RowNumbers row;
+};
+static_assert(sizeof(RowTile) == weigh_tile_bytes(D), "the workspace's tiles");
+
+// The first tile of a sequence: sequences' tiles do not meet, since each has at most one that is not full.
+__device__ __forceinline__ int64_t first_tile(const WeighArgs& a, const SequenceRows& g, int32_t seq) {
+  return int64_t(g.start) * a.group / kRows + seq;
+}
+
+template <int KB>
+__global__ __launch_bounds__(kThreads) void prepare_kernel(ServeArgs s, WeighArgs a) {
+  constexpr bool kCodes = KB != 16;
+  const int tid = threadIdx.x;
+  uint32_t b = blockIdx.x;
+  const int32_t head = int32_t(b % uint32_t(s.H));
+  b /= uint32_t(s.H);
+  const int32_t tile = int32_t(b % uint32_t(a.row_tiles)), seq = int32_t(b / uint32_t(a.row_tiles));
+  const SequenceRows g = sequence_rows(s, seq);
+  const int32_t row_first = tile * kRows, rows = g.count * a.group;  // (below 2^31: num_tokens * Hq)
+  if (row_first >= rows) return;
+  RowTile& to = static_cast<RowTile*>(a.rows)[head * a.all_tiles + first_tile(a, g, seq) + tile];
+  const int piece = tid % kRowPieces;
+  for (int row = tid / kRowPieces; row < kRows; row += kThreads / kRowPieces) {
+    const uint32_t at = uint32_t(row_first + row), token = at / uint32_t(a.group), sub = at % uint32_t(a.group);
+    u32x4 w{};
+    if (int32_t(at) < rows)
+      w = *reinterpret_cast<const u32x4*>(a.q + int64_t(g.start + token) * a.q_token_stride +
+                                          int64_t(head * a.group + sub) * a.q_head_stride + 8 * piece);
+    if constexpr (kCodes) {
+      float v[8], down, up, sum = 0.0f;
+      uint32_t top = 0;
+      widen(s.bf16, w, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t mag = __float_as_uint(v[e]) & 0x7FFFFFFF;
+        top = top > mag ? top : mag;
+      }
+      for (int off = 1; off < kRowPieces; off <<= 1) top = max(top, uint32_t(__shfl_xor(int(top), off)));
+      row_scale(top, down, up);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += v[e] * down;
+      for (int off = 1; off < kRowPieces; off <<= 1) sum += __shfl_xor(sum, off);
+      w = query_operand<KB>(v, down);
+      if (piece == 0) {
+        to.row.f[row] = a.scale * up;
+        to.row.sum[row] = sum;
+      }
+    }
+    to.q[Halves<KB>::slot(8 * piece) * kRows + row] = w;
+  }
+  if (tid < kRows) {
+    const uint32_t at = uint32_t(row_first + tid), token = at / uint32_t(a.group), sub = at % uint32_t(a.group);
+    float less = -kInf;
+    Sight see{-1, -1};
+    if (int32_t(at) < rows) {
+      less = less_of(a, g, int32_t(token), head * a.group + int32_t(sub));
+      if constexpr (!kCodes) less /= a.scale;  // (in the scores' unit)
+      if (less != -kInf) see = sight_of(s, a, g, int32_t(token));  // else it saw nothing, and gives nothing
+    }
+    to.row.less[tid] = less;
+    to.row.hi[tid] = see.hi;
+    to.row.lo[tid] = see.lo;
+    int32_t all_hi = see.hi, any_hi = see.hi, all_lo = see.lo, any_lo = see.hi < 0 ? 0x7FFFFFFF : see.lo;
+    for (int by = 1; by < kRows; by <<= 1) {
+      all_hi = min(all_hi, __shfl_xor(all_hi, by));
+      any_hi = max(any_hi, __shfl_xor(any_hi, by));
+      all_lo = max(all_lo, __shfl_xor(all_lo, by));
+      any_lo = min(any_lo, __shfl_xor(any_lo, by));
+    }
+    if (tid == 0) {
+      to.row.off = all_hi < 0;
+      to.row.all_hi = all_hi;
+      to.row.any_hi = any_hi;
+      to.row.all_lo = all_lo;
+      to.row.any_lo = any_lo;
+    }
+  }
+}
 
 template <bool BF16, int KB>
 __global__ __launch_bounds__(kThreads, 2) void many_kernel(ServeArgs s, WeighArgs a) {
   constexpr bool kCodes = KB != 16;
   constexpr bool kHalf = kCodes || !BF16;
-  constexpr int kSteps = D / 16, kPasses = kRows * kRowPieces / kThreads;
+  constexpr int kSteps = D / 16, kNumbers = kCodes ? 3 : 1;
   typedef Halves<KB> Order;
-  __shared__ RowTile lds[2];
+  __shared__ float lds[kThreads / 64][2][kNumbers][kRows];  // rows' numbers, each wave its own
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, half = lane >> 5;
   uint32_t b = blockIdx.x;
@@ -383,176 +475,159 @@ __global__ __launch_bounds__(kThreads, 2) void many_kernel(ServeArgs s, WeighArg
   if (!s.positions) see_us = rows_that_see(g, begin, last, a.window, a.sinks);
   const int64_t first_row = int64_t(see_us.first) * a.group, rows = int64_t(see_us.end) * a.group;
   const int64_t tile0 = first_row / kRows, tiles = rows > first_row ? (rows + kRows - 1) / kRows - tile0 : 0;
-  const int32_t from = int32_t(tile0 + tiles * split / a.splits), upto = int32_t(tile0 + tiles * (split + 1) / a.splits);
-  const int32_t most = g.count * a.group;  // (below 2^31: num_tokens * Hq)
+  // A split is the same rows for all tiles of tokens, whose workgroups run side by side and find them in L2.
+  const int64_t every = (int64_t(g.count > 0 ? g.count : 0) * a.group + kRows - 1) / kRows;
+  const int64_t begin_split = every * split / a.splits, end_split = every * (split + 1) / a.splits;
+  const int32_t from = int32_t(tile0 > begin_split ? tile0 : begin_split);
+  const int32_t upto = int32_t(tile0 + tiles < end_split ? tile0 + tiles : end_split);
 
-  // A thread's part of a row tile: a piece of 8 channels of some rows, and one row's numbers.  From one tile to the
-  // next its rows are kRows on, so that their tokens and heads are stepped, not divided for.
-  struct Cursor {
-    int32_t row, token, sub;
+  // A tile in registers: its queries and row n's numbers (other half: of all rows).  Past the last tile it is that one again.
+  struct Loaded {
+    u32x4 q[kSteps];
+    float number[kNumbers];
   };
-  const int32_t step_token = kRows / a.group, step_sub = kRows % a.group;
-  auto cursor = [&](int64_t row) {
-    return Cursor{int32_t(row), int32_t(row / a.group), int32_t(row % a.group)};
+  const RowTile* tiles_of = static_cast<const RowTile*>(a.rows) + head * a.all_tiles + first_tile(a, g, seq);
+  auto fetch_query = [&](int32_t at, int i, Loaded& to) {
+    to.q[i] = tiles_of[at < upto ? at : upto - 1].q[64 * i + lane];
   };
-  auto step = [&](Cursor& at) {
-    at.row += kRows;
-    at.token += step_token;
-    at.sub += step_sub;
-    if (at.sub >= a.group) {
-      at.sub -= a.group;
-      ++at.token;
-    }
+  auto fetch_numbers = [&](int32_t at, Loaded& to) {
+    const float* from = tiles_of[at < upto ? at : upto - 1].row.less;
+    to.number[0] = from[half && n >= 8 ? n : lane];
+#pragma unroll
+    for (int i = 1; i < kNumbers; ++i) to.number[i] = from[40 + kRows * (i - 1) + n];
   };
-  const int piece = tid % kRowPieces, row0 = tid / kRowPieces;
-  const uint16_t* q_head = a.q + int64_t(g.start) * a.q_token_stride + int64_t(head * a.group) * a.q_head_stride + 8 * piece;
-  const float* lse = a.lse + int64_t(g.start) * a.Hq + head * a.group;
-  Cursor mine_rows[kPasses], my_row = cursor(int64_t(from) * kRows + (tid & (kRows - 1)));
+  auto fetch = [&](int32_t at, Loaded& to) {
 #pragma unroll
-  for (int i = 0; i < kPasses; ++i) mine_rows[i] = cursor(int64_t(from) * kRows + row0 + i * (kThreads / kRowPieces));
-  u32x4 w[kPasses];
-  float less = -kInf;
-  Sight see{-1, -1};
-  auto fetch = [&] {
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-      Cursor& at = mine_rows[i];
-      w[i] = u32x4{};
-      if (at.row < most)
-        w[i] = *reinterpret_cast<const u32x4*>(q_head + int64_t(at.token) * a.q_token_stride + at.sub * a.q_head_stride);
-      step(at);
-    }
-    if (tid < kRows) {
-      less = -kInf;
-      see = Sight{-1, -1};
-      if (my_row.row < most) {
-        less = lse[int64_t(my_row.token) * a.Hq + my_row.sub];
-        see = sight_of(s, a, g, my_row.token);
-      }
-      step(my_row);
-    }
+    for (int i = 0; i < kSteps; ++i) fetch_query(at, i, to);
+    fetch_numbers(at, to);
   };
-  auto leave = [&](RowTile& to) {
+  // The numbers where every lane finds those of its rows: value e of a lane's scores is row 8 (e / 4) + 4 half + e % 4.
+  float(*numbers)[kNumbers][kRows] = lds[wave];
+  auto leave = [&](const Loaded& in, int which) {
+    if (half == 0) {
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-      const int row = row0 + i * (kThreads / kRowPieces);
-      if constexpr (kCodes) {
-        float v[8], down, up, sum = 0.0f;
-        uint32_t top = 0;
-        widen(s.bf16, w[i], v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t mag = __float_as_uint(v[e]) & 0x7FFFFFFF;
-          top = top > mag ? top : mag;
-        }
-        for (int off = 1; off < kRowPieces; off <<= 1) top = max(top, uint32_t(__shfl_xor(int(top), off)));
-        row_scale(top, down, up);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum += v[e] * down;
-        for (int off = 1; off < kRowPieces; off <<= 1) sum += __shfl_xor(sum, off);
-        to.q[Order::slot(8 * piece)][row] = query_operand<KB>(v, down);
-        if (piece == 0) {
-          to.f[row] = a.scale * up;
-          to.sum[row] = sum;
-        }
-      } else {
-        to.q[Order::slot(8 * piece)][row] = w[i];
-      }
+      for (int i = 0; i < kNumbers; ++i) numbers[which][i][n] = in.number[i];
     }
-    if (tid < kRows) {
-      if (less == -kInf) see = Sight{-1, -1};  // it saw nothing, and gives nothing
-      to.less[tid] = less == -kInf ? -kInf : less * -1.44269504088896340736f;
-      to.hi[tid] = see.hi;
-      to.lo[tid] = see.lo;
-      const bool off = __any(see.hi < 0);
-      if (tid == 0) to.off = off;
-      if (s.positions) {
-        int32_t all_hi = see.hi, any_hi = see.hi, all_lo = see.lo, any_lo = see.hi < 0 ? 0x7FFFFFFF : see.lo;
-        for (int by = 1; by < kRows; by <<= 1) {
-          all_hi = min(all_hi, __shfl_xor(all_hi, by));
-          any_hi = max(any_hi, __shfl_xor(any_hi, by));
-          all_lo = max(all_lo, __shfl_xor(all_lo, by));
-          any_lo = min(any_lo, __shfl_xor(any_lo, by));
-        }
-        if (tid == 0) {
-          to.all_hi = all_hi;
-          to.any_hi = any_hi;
-          to.all_lo = all_lo;
-          to.any_lo = any_lo;
-        }
-      }
-    }
+    __builtin_amdgcn_wave_barrier();
   };
-  // First and last row of a tile, for rows in order.
-  Cursor first_of = cursor(int64_t(from) * kRows), last_of = cursor(int64_t(from) * kRows + kRows - 1);
+  auto number = [&](int which, int i, int e4) {
+    return *reinterpret_cast<const f32x4*>(&numbers[which][i][8 * e4 + 4 * half]);
+  };
 
   float total[kNT] = {};
-  if (from < upto) {
-    fetch();
-    leave(lds[0]);
-  }
-  __syncthreads();
-  for (int32_t at = from; at < upto; ++at) {
-    const RowTile& r = lds[(at - from) & 1];
-    if (at + 1 < upto) fetch();
+  // The scores of a tile and token tile t; `then(i)` after the i-th operand.  (16 bits: less the rows' lse in the scores' unit,
+  // which the sums begin with.)
+  auto begin_scores = [&](int which, f32x16& score) {
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      f32x4 v{};
+      if constexpr (!kCodes) v = number(which, 0, e4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) score[4 * e4 + e] = v[e];
+    }
+  };
+  auto scores = [&](const Loaded& r, auto t, f32x16& score, auto then) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      score = mfma32<kHalf>(r.q[i], k[t][i], score);
+      then(i);
+    }
+  };
+  auto nothing = [](int) {};
+  // The sum of their exponentials.
+  auto sum_of = [&](auto masked, int32_t at, int which, auto t, const f32x16& score) {
+    constexpr bool kMasked = decltype(masked)::value;
+    const int32_t tok = mine + 32 * t + n;
+    const bool sink = tok < a.sinks;
+    float part[4] = {};
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      f32x4 f, sum, ls;
+      i32x4 hi, lo;
+      if constexpr (kCodes) {
+        ls = number(which, 0, e4);
+        f = number(which, 1, e4);
+        sum = number(which, 2, e4);
+      }
+      if constexpr (kMasked) {
+        const RowNumbers& row = tiles_of[at].row;
+        hi = *reinterpret_cast<const i32x4*>(&row.hi[8 * e4 + 4 * half]);
+        lo = *reinterpret_cast<const i32x4*>(&row.lo[8 * e4 + 4 * half]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x = score[4 * e4 + e];
+        if constexpr (kCodes) x = __builtin_fmaf(__builtin_fmaf(ks[t], x, kz[t] * sum[e]), f[e], ls[e]);
+        else x *= a.scale;
+        float p = exp2_of(x);
+        if constexpr (kMasked) p = (tok <= hi[e]) & ((tok > lo[e]) | sink) ? p : 0.0f;
+        part[e] += p;
+      }
+    }
+    return (part[0] + part[1]) + (part[2] + part[3]);
+  };
+  // The exponentials of one tile while the matrix units work on the next scores: a matrix instruction of 32 cycles, then the
+  // vector instructions of as long.
+  auto both = [&](bool all, bool none, int32_t at, int which, auto t, const f32x16& score, const Loaded& next, auto next_t,
+                  f32x16& later, auto then) {
+    scores(next, next_t, later, then);
+    float sum = sum_of(std::false_type{}, at, which, t, score);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                 // matrix
+      __builtin_amdgcn_sched_group_barrier(0x002, (kCodes ? 68 : 36) / kSteps + 1, 0);  // vector
+    }
+    asm("" : "+v"(sum));  // (here, beside the matrix instructions, not where it turns out to be of use)
+    // (Masked they are worked out again: the matrix instructions stay in one place, where their results need no moves.)
+    if (!all) sum = none ? 0.0f : sum_of(std::true_type{}, at, which, t, score);
+    total[t] += sum;
+  };
+  constexpr std::integral_constant<int, 0> kFirst{};
+  constexpr std::integral_constant<int, kNT - 1> kLast{};
+  f32x16 score_a, score_b;
+  // Tile `at` of parity `which`, in `r`, whose first scores are in `now`; the next one is in `next` (of 256 channels its queries
+  // in `queries`).
+  auto iterate = [&](int32_t at, int which, Loaded& r, Loaded& next, Loaded& queries, f32x16& now, f32x16& later) {
     const int32_t end = mine + 32 * kNT - 1;
-    int32_t any_hi, any_lo, all_hi, all_lo;
-    if (s.positions) {
-      any_hi = __builtin_amdgcn_readfirstlane(r.any_hi), any_lo = __builtin_amdgcn_readfirstlane(r.any_lo);
-      all_hi = __builtin_amdgcn_readfirstlane(r.all_hi), all_lo = __builtin_amdgcn_readfirstlane(r.all_lo);
-    } else {
-      const Sight begins = sight_of(s, a, g, first_of.token);
-      const Sight ends = sight_of(s, a, g, last_of.token < g.count ? last_of.token : g.count - 1);
-      all_hi = begins.hi, any_hi = ends.hi, any_lo = begins.lo, all_lo = ends.lo;
-      step(first_of);
-      step(last_of);
-    }
-    const bool off = __builtin_amdgcn_readfirstlane(r.off);
+    auto of_all = [&](int i) { return __builtin_amdgcn_readlane(__float_as_int(r.number[0]), 32 + i); };
+    const int32_t off = of_all(0), all_hi = of_all(1), any_hi = of_all(2), all_lo = of_all(3), any_lo = of_all(4);
     const bool none = any_hi < mine || (any_lo >= end && mine >= a.sinks);
-    if (!none) {
-      f32x16 score[kNT];
-#pragma unroll
-      for (int t = 0; t < kNT; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) score[t][e] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        const u32x4 q = r.q[2 * i + half][n];
-#pragma unroll
-        for (int t = 0; t < kNT; ++t) score[t] = mfma32<kHalf>(q, k[t][i], score[t]);
+    const bool all = !off && all_hi >= end && (all_lo < mine || end < a.sinks);
+    if constexpr (kNT == 2) {
+      begin_scores(which, later);
+      both(all, none, at, which, kFirst, now, r, kLast, later, nothing);
+      fetch(at + 2, r);
+      leave(next, which ^ 1);
+      begin_scores(which ^ 1, now);
+      both(all, none, at, which, kLast, later, next, kFirst, now, nothing);
+    } else {
+      leave(next, which ^ 1);
+      begin_scores(which ^ 1, later);
+      fetch_numbers(at + 2, r);
+      both(all, none, at, which, kFirst, now, queries, kFirst, later, [&](int i) { fetch_query(at + 2, i, queries); });
+    }
+  };
+  if (from < upto) {
+    Loaded even, odd;
+    fetch(from, even);
+    leave(even, 0);
+    begin_scores(0, score_a);
+    if constexpr (kNT == 2) {
+      fetch(from + 1, odd);
+      scores(even, kFirst, score_a, nothing);
+      // (After the last tile its scores are worked out again and not used.)
+      for (int32_t at = from; at < upto; at += 2) {
+        iterate(at, 0, even, odd, even, score_a, score_b);
+        if (at + 1 < upto) iterate(at + 1, 1, odd, even, even, score_a, score_b);
       }
-      const bool all = !off && all_hi >= end && (all_lo < mine || end < a.sinks);
-      // Value e of a lane is row 8 (e / 4) + 4 half + e % 4.
-#pragma unroll
-      for (int t = 0; t < kNT; ++t) {
-        const int32_t tok = mine + 32 * t + n;
-        float part[4] = {};
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-          const int at_row = 8 * e4 + 4 * half;
-          const f32x4 ls = *reinterpret_cast<const f32x4*>(&r.less[at_row]);
-          f32x4 f, sum;
-          if constexpr (kCodes) {
-            f = *reinterpret_cast<const f32x4*>(&r.f[at_row]);
-            sum = *reinterpret_cast<const f32x4*>(&r.sum[at_row]);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = score[t][4 * e4 + e];
-            if constexpr (kCodes) x = __builtin_fmaf(ks[t], x, kz[t] * sum[e]);
-            float p = exp2_of(__builtin_fmaf(x, kCodes ? f[e] : a.scale, ls[e]));
-            if (!all) {
-              const int32_t hi = r.hi[at_row + e], lo = r.lo[at_row + e];
-              p = tok <= hi && (tok > lo || tok < a.sinks) ? p : 0.0f;
-            }
-            part[e] += p;
-          }
-        }
-        total[t] += (part[0] + part[1]) + (part[2] + part[3]);
+    } else {
+      fetch_numbers(from + 1, odd);
+      scores(even, kFirst, score_a, [&](int i) { fetch_query(from + 1, i, even); });
+      for (int32_t at = from; at < upto; at += 2) {
+        iterate(at, 0, even, odd, even, score_a, score_b);
+        if (at + 1 < upto) iterate(at + 1, 1, odd, even, even, score_b, score_a);
       }
     }
-    if (at + 1 < upto) leave(lds[(at + 1 - from) & 1]);
-    __syncthreads();
   }
 
 #pragma unroll
@@ -592,10 +667,10 @@ void launch(const ServeArgs& s, const WeighArgs& a, const WeighLaunch& l, hipStr
   auto few = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(uint32_t(l.groups)), dim3(64 * kFewWaves), 0, stream, s, a);
   };
-  if (l.row_tiles) {
+  if (l.few_tiles) {
     const bool whole = s.log2P >= 4;
     if constexpr (D <= 128) {
-      if (l.row_tiles > 1) {
+      if (l.few_tiles > 1) {
         if (whole) few(few_kernel<BF16, KB, true, 2>);
         else few(few_kernel<BF16, KB, false, 2>);
         return;
@@ -605,6 +680,8 @@ void launch(const ServeArgs& s, const WeighArgs& a, const WeighLaunch& l, hipStr
     else few(few_kernel<BF16, KB, false, 1>);
     return;
   }
+  if (l.prepare_groups)
+    hipLaunchKernelGGL(prepare_kernel<KB>, dim3(uint32_t(l.prepare_groups)), dim3(kThreads), 0, stream, s, a);
   hipLaunchKernelGGL((many_kernel<BF16, KB>), dim3(uint32_t(l.groups)), dim3(kThreads), 0, stream, s, a);
   if (l.join_groups)
     hipLaunchKernelGGL(join_kernel, dim3(uint32_t(l.join_groups)), dim3(kThreads), 0, stream, s, a,

@@ -113,7 +113,7 @@ def test_null_structures():
 
 
 def test_workspace():
-    """None where a token's sum is one workgroup's, parts of the rows or of the heads otherwise."""
+    """None of few rows; of many the prepared rows, and sums of each head where they are joined."""
     s = _shape(pool_pages=4096)
     m, c = pb.make_model(s), pb.PkvPagedCache(tag=3)
     a = pb.PkvAttention(num_q_heads=16, scale=0.1)
@@ -123,7 +123,9 @@ def test_workspace():
     assert pb.pkv_attention_weights_workspace(m, c, one, a, each) == 0
     assert pb.pkv_attention_weights_workspace(m, c, one, a, all_) == 0
     many = pb.PkvBatch(num_seqs=3, num_tokens=192, max_tokens=64, pages_per_seq=4096)
-    assert pb.pkv_attention_weights_workspace(m, c, many, a, all_) % (3 * 4 * 65536 * 4) == 0
+    rows = (192 * 4 // 32 + 3 + 1) * 4 * (32 * (2 * 128 + 20) + 32)
+    assert pb.pkv_attention_weights_workspace(m, c, many, a, each) == rows
+    assert pb.pkv_attention_weights_workspace(m, c, many, a, all_) == rows + 3 * 4 * 65536 * 4
 
 
 def test_rows_of_a_tile_stay_within_the_sequence(tmp_path):
