@@ -129,7 +129,7 @@ struct WeighArgs {
   int32_t Hq, group, window, sinks;
   int32_t joint;         // one weight a token, of all heads
   int32_t tiles;         // workgroups along a sequence's tokens
-  int32_t chunk, subs;   // few rows: tokens of a workgroup, and the parts that its waves take
+  int32_t chunk, subs;   // few rows: tokens of a workgroup (0: an even share), and the parts that its waves take
   int32_t splits;        // many rows: workgroups that share the rows of a tile of tokens
   int32_t row_tiles;     // most tiles of rows of a sequence,
   int64_t all_tiles;     // and of all of them
@@ -187,7 +187,9 @@ constexpr int32_t kept_budget(const KeepArgs& a, int32_t n, int32_t budget) {
   return budget < n ? budget : n;
 }
 
-constexpr int kMostChunk = 512;  // tokens of a workgroup of few rows
+constexpr int kMostChunk = 512;   // tokens of a wave of few rows at a time
+constexpr int kMostShared = 512;  // sequences whose tokens are shared evenly (every workgroup adds up their lengths),
+constexpr int kShares = 512;      // by that many workgroups
 // Of many rows: tokens of a workgroup, rows of a tile, and its bytes (queries, and 5 numbers a row and 8 of all).
 constexpr int weigh_tokens(int head_dim) { return head_dim > 128 ? 128 : 256; }
 constexpr int kWeighRows = 32;

@@ -287,15 +287,19 @@ pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_
       l.few_tiles = rows <= kRowTile ? 1 : 2;
       // A workgroup's 8 waves take a KV head each, or parts of the tokens where there are fewer.
       while (l.subs < 8 && l.subs * 2 * s.H <= 8) l.subs *= 2;
-      l.chunk = kTokenTile * l.subs;
-      while (l.chunk < kMostChunk && int64_t(s.num_seqs) * s.max_kv / l.chunk >= 2048) l.chunk *= 2;
-      l.tiles = int32_t((int64_t(s.max_kv) + l.chunk - 1) / l.chunk);
-      l.groups = int64_t(s.num_seqs) * l.tiles;
+      if (r.window == 0 && s.num_seqs <= kMostShared) {
+        l.groups = std::max<int64_t>(1, std::min<int64_t>(kShares, (int64_t(s.num_seqs) * s.max_kv - 1) / (kTokenTile * l.subs) + 1));
+      } else {
+        l.chunk = kTokenTile * l.subs;
+        while (l.chunk < kMostChunk && int64_t(s.num_seqs) * s.max_kv / l.chunk >= 4096) l.chunk *= 2;
+        l.tiles = int32_t((int64_t(s.max_kv) + l.chunk - 1) / l.chunk);
+        l.groups = int64_t(s.num_seqs) * l.tiles;
+      }
     } else {
       const int tokens = weigh_tokens(s.D);
       l.tiles = int32_t((int64_t(s.max_kv) + tokens - 1) / tokens);
       const int64_t base = int64_t(s.num_seqs) * l.tiles * s.H;
-      l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(12 * 256 / base, rows / 256)));
+      l.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(24 * 256 / base, rows / 1024)));
       l.groups = base * l.splits;
       if (l.splits > 1 || (r.joint && s.H > 1)) {
         l.part_bytes = (uint64_t(l.splits) * s.H * s.num_seqs * s.max_kv * 4 + 15) / 16 * 16;

@@ -103,51 +103,69 @@ __device__ __forceinline__ u32x4 query_operand(const float (&v)[8], float down) 
 // ---- Few rows ----
 //
 // The rows of a sequence and KV head fit RT tiles of 16, whose queries a wave keeps in registers while it goes over
-// tokens: the call waits for the cache's bytes.  A workgroup takes `chunk` tokens of one sequence and all heads: wave w the
-// w % subs-th part of them, of heads w / subs and on.  Where heads are joined, the waves' sums of a token meet in LDS.
+// tokens.  A workgroup takes tokens of one sequence and all heads: wave w the w % subs-th part of them, of heads w / subs and
+// on.  Where heads are joined, the waves' sums of a token meet in LDS.  All sequences' tokens are cut into even shares, one to a
+// workgroup, so that the GPU is done at once whatever their lengths; with a window, of whose tokens most are not looked at, into
+// chunks.
 
 constexpr int kFewWaves = 8;
 
+// Tokens [begin, end) of one sequence (end at most kv_len), by the whole workgroup.
 template <bool BF16, int KB, bool WHOLE, int RT>
-__global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ? 4 : 2) void few_kernel(ServeArgs s, WeighArgs a) {
+__device__ __forceinline__ void weigh_tokens(const ServeArgs& s, const WeighArgs& a, float (*sums)[kMostChunk],
+                                             const SequenceRows& g, int32_t seq, int32_t begin, int32_t end) {
   constexpr bool kCodes = KB != 16;
   constexpr bool kHalf = kCodes || !BF16;
   constexpr int kSteps = D / 32;
-  __shared__ float sums[kFewWaves][kMostChunk];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane >> 4, x = lane & 15;
-  const int32_t seq = int32_t(blockIdx.x / uint32_t(a.tiles)), tile0 = int32_t(blockIdx.x % uint32_t(a.tiles));
-  const SequenceRows g = sequence_rows(s, seq);
-  const int64_t begin = int64_t(tile0) * a.chunk;
-  if (begin >= g.kv_len) return;
-  const int32_t part = a.chunk / a.subs, sub = wave % a.subs, first_head = wave / a.subs, heads = kFewWaves / a.subs;
-  const int32_t from = int32_t(begin) + sub * part;
-  const int32_t upto = g.kv_len - from < part ? g.kv_len : from + part;
+  const int32_t each = kTokenTile * a.subs, part = (end - begin + each - 1) / each * kTokenTile;
+  const int32_t sub = wave % a.subs, first_head = wave / a.subs, heads = kFewWaves / a.subs;
+  const int32_t from = begin + sub * part;
+  const int32_t upto = end - from < part ? end : from + part;
   const Magic m = magic();
   if (a.joint) {
     for (int32_t i = lane; i < part; i += 64) sums[wave][i] = 0.0f;
     __syncthreads();
   }
 
-  // What the rows see between them; tiles of which none sees anything are not looked at.
-  int32_t hi_most = -1, lo_least = 0x7FFFFFFF;
+  // What the rows see between them: tiles of which none sees anything are not looked at, and of which all see everything need
+  // no masks.
+  int32_t hi_most = -1, lo_least = 0x7FFFFFFF, hi_least = 0x7FFFFFFF, lo_most = -1;
   if (g.count > 0 && !s.positions) {
-    hi_most = g.kv_len - g.trail + g.count - 1;
-    lo_least = sight_of(s, a, g, 0).lo;
+    const Sight begins = sight_of(s, a, g, 0), ends = sight_of(s, a, g, g.count - 1);
+    hi_least = begins.hi, lo_least = begins.lo, hi_most = ends.hi, lo_most = ends.lo;
   } else if (s.positions) {
     for (int32_t i = lane; i < g.count; i += 64) {
       const Sight see = sight_of(s, a, g, i);
       hi_most = max(hi_most, see.hi);
+      hi_least = min(hi_least, see.hi);
+      lo_most = max(lo_most, see.lo);
       if (see.hi >= 0) lo_least = min(lo_least, see.lo);
     }
     for (int off = 1; off < 64; off <<= 1) {
       hi_most = max(hi_most, __shfl_xor(hi_most, off));
+      hi_least = min(hi_least, __shfl_xor(hi_least, off));
+      lo_most = max(lo_most, __shfl_xor(lo_most, off));
       lo_least = min(lo_least, __shfl_xor(lo_least, off));
     }
   }
   hi_most = __builtin_amdgcn_readfirstlane(hi_most);
+  hi_least = __builtin_amdgcn_readfirstlane(hi_least);
+  lo_most = __builtin_amdgcn_readfirstlane(lo_most);
   lo_least = __builtin_amdgcn_readfirstlane(lo_least);
   auto seen = [&](int32_t t0) { return t0 <= hi_most && (t0 + kTokenTile - 1 > lo_least || t0 < a.sinks); };
+  auto open = [&](int32_t t0) {
+    const int32_t end = t0 + kTokenTile - 1;
+    return end <= hi_least && (lo_most < t0 || end < a.sinks);
+  };
+
+  // The pages of the wave's part, a half of a tile to a lane, so that no load waits for its page.
+  static_assert(kMostChunk <= 64 * 16, "a lane each");
+  int32_t pages = -1;
+  if constexpr (WHOLE) {
+    if (from + 16 * lane < upto) pages = page_of(s, s.page_table + int64_t(seq) * s.pages_per_seq, (from + 16 * lane) >> s.log2P);
+  }
 
   for (int32_t head = first_head; head < s.H && from < upto; head += heads) {
     const Source src = source_of<KB>(s, seq, head);
@@ -160,13 +178,7 @@ __global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ?
       Tile tile{t0, {-1, -1}};
       if constexpr (WHOLE) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int32_t at = (t0 + 16 * u) >> s.log2P;
-          if (at < s.pages_per_seq) {
-            const int32_t p = scalar_entry(src.table, at);
-            tile.page[u] = p >= 0 && p < s.pool_pages ? p : -1;
-          }
-        }
+        for (int u = 0; u < 2; ++u) tile.page[u] = __builtin_amdgcn_readlane(pages, (t0 - from) / 16 + u);
       }
       load_keys<KB, WHOLE>(s, src, tile, c, x, keys[b]);
 #pragma unroll
@@ -183,6 +195,7 @@ __global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ?
     for (int b = 0; b < kTiles; ++b) load(b, from + b * kTokenTile);
 
     // Row x of each row tile: its queries, and what it is scaled by.
+    bool plain = true;  // no row with a mask of its own
     u32x4 q[RT][kSteps];
     f32x4 f[RT], less[RT], sum[RT];
     int32_t hi[RT][4], lo[RT][4];
@@ -195,6 +208,7 @@ __global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ?
       if (on) {
         rs.less = less_of(a, g, token, qhead);
         if (rs.less != -kInf) see = sight_of(s, a, g, token);
+        else plain = false;
       }
       const uint16_t* rowq = a.q + int64_t(g.start + (on ? token : 0)) * a.q_token_stride + int64_t(qhead) * a.q_head_stride;
       float v[kSteps][8];
@@ -239,6 +253,7 @@ __global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ?
       }
     }
 
+    plain = __all(plain);
     auto weigh = [&](int b, int32_t t0) {
       float w[2] = {0.0f, 0.0f};
       if (seen(t0)) {
@@ -262,23 +277,29 @@ __global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ?
           }
         }
         load(b, t0 + kTiles * kTokenTile);
+        // (Rows past the last have less = -inf and queries of 0: nothing, but for keys that are no numbers.)
+        auto sums_of = [&](auto masked) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int32_t tok = t0 + 16 * u + x;
-          const bool sink = tok < a.sinks;
-          float total = 0.0f;
+          for (int u = 0; u < 2; ++u) {
+            const int32_t tok = t0 + 16 * u + x;
+            const bool sink = tok < a.sinks;
+            float total = 0.0f;
 #pragma unroll
-          for (int r = 0; r < RT; ++r)
+            for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float t = score[r][u][i];
-              if constexpr (kCodes) t = __builtin_fmaf(ks[u], t, kz[u] * sum[r][i]);
-              const float p = exp2_of(__builtin_fmaf(t, f[r][i], less[r][i]));
-              total += (tok <= hi[r][i]) & ((tok > lo[r][i]) | sink) ? p : 0.0f;
-            }
-          w[u] = over_c_sum(total);
-          if (!is[u]) w[u] = 0.0f;
-        }
+              for (int i = 0; i < 4; ++i) {
+                float t = score[r][u][i];
+                if constexpr (kCodes) t = __builtin_fmaf(ks[u], t, kz[u] * sum[r][i]);
+                float p = exp2_of(__builtin_fmaf(t, f[r][i], less[r][i]));
+                if constexpr (decltype(masked)::value) p = (tok <= hi[r][i]) & ((tok > lo[r][i]) | sink) ? p : 0.0f;
+                total += p;
+              }
+            w[u] = over_c_sum(total);
+            if (!is[u]) w[u] = 0.0f;
+          }
+        };
+        if (open(t0) && plain) sums_of(std::false_type{});
+        else sums_of(std::true_type{});
       } else {
         load(b, t0 + kTiles * kTokenTile);
       }
@@ -297,12 +318,73 @@ __global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ?
   }
   if (!a.joint) return;
   __syncthreads();
-  for (int32_t i = threadIdx.x; i < a.chunk; i += 64 * kFewWaves) {
-    const int32_t tok = int32_t(begin) + i;
-    if (tok >= g.kv_len) break;
+  for (int32_t i = threadIdx.x; i < end - begin; i += 64 * kFewWaves) {
+    const int32_t tok = begin + i;
     float total = 0.0f;
     for (int32_t w = i / part; w < kFewWaves; w += a.subs) total += sums[w][i % part];
     put(a, int64_t(seq) * a.seq_stride + tok, total);
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int32_t token_tiles(const ServeArgs& s, int32_t seq) {
+  if (seq >= s.num_seqs) return 0;
+  const int32_t len = s.kv_lens[seq];
+  return ((len < 0 ? 0 : len < s.max_kv ? len : s.max_kv) + kTokenTile - 1) / kTokenTile;
+}
+
+// Inclusive sums over the lanes of a wave.
+__device__ __forceinline__ int64_t wave_sums(int64_t v, int lane) {
+  for (int off = 1; off < 64; off <<= 1) {
+    const int64_t other = __shfl_up(v, off);
+    v += lane >= off ? other : 0;
+  }
+  return v;
+}
+
+template <bool BF16, int KB, bool WHOLE, int RT>
+__global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ? 4 : 2) void few_kernel(ServeArgs s, WeighArgs a) {
+  __shared__ float sums[kFewWaves][kMostChunk];
+  const int lane = threadIdx.x & 63;
+  int32_t seq = 0, tile = 0, left = 0;  // the workgroup's first sequence, its first tile there, and its tiles
+  if (a.chunk) {  // a chunk of one sequence
+    seq = int32_t(blockIdx.x / uint32_t(a.tiles));
+    tile = int32_t(blockIdx.x % uint32_t(a.tiles)) * (a.chunk / kTokenTile);
+    const int32_t rest = token_tiles(s, seq) - tile;
+    left = rest < a.chunk / kTokenTile ? rest : a.chunk / kTokenTile;
+  } else {  // an even share of all sequences' tiles, whose number only the device knows
+    int64_t all = 0;
+    for (int32_t s0 = 0; s0 < s.num_seqs; s0 += 64) all += __shfl(wave_sums(token_tiles(s, s0 + lane), lane), 63);
+    const int64_t step = int64_t(gridDim.x) * a.subs, share = (all + step - 1) / step * a.subs;
+    int64_t at = share * blockIdx.x;
+    for (int32_t s0 = 0; s0 < s.num_seqs; s0 += 64) {
+      const int32_t mine = token_tiles(s, s0 + lane);
+      const int64_t upto = wave_sums(mine, lane), here = __shfl(upto, 63);
+      if (at < here) {
+        const int which = __builtin_ctzll(__ballot(upto > at));
+        seq = s0 + which;
+        tile = int32_t(at - __shfl(upto - mine, which));
+        left = int32_t(share < (int64_t(1) << 30) ? share : int64_t(1) << 30);
+        break;
+      }
+      at -= here;
+    }
+  }
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  tile = __builtin_amdgcn_readfirstlane(tile);
+  left = __builtin_amdgcn_readfirstlane(left);
+  for (; left > 0 && seq < s.num_seqs; ++seq, tile = 0) {
+    const SequenceRows g = sequence_rows(s, seq);
+    int32_t tiles = (g.kv_len + kTokenTile - 1) / kTokenTile - tile;
+    tiles = tiles < left ? tiles : left;
+    left -= tiles;
+    while (tiles > 0) {
+      const int32_t most = kMostChunk / kTokenTile * a.subs, now = tiles < most ? tiles : most;  // what the waves' parts hold
+      const int32_t begin = tile * kTokenTile, end = begin + now * kTokenTile;
+      weigh_tokens<BF16, KB, WHOLE, RT>(s, a, sums, g, seq, begin, end < g.kv_len ? end : g.kv_len);
+      tile += now;
+      tiles -= now;
+    }
   }
 }
 

@@ -125,6 +125,20 @@ def test_weights_without_bounds(torch):
         _run(torch, case, joint=False, decay=1.0, bounds=False)
 
 
+@pytest.mark.parametrize("H,joint", [(1, False), (2, True), (3, False), (5, True)])
+def test_shares_of_ragged_sequences_added_in_place(torch, H, joint):
+    """Workgroups' even shares end inside sequences and inside their waves' parts: every token is added to once."""
+    lens = tuple(int(n) for n in np.random.default_rng(H).integers(0, 400, 37)) + (0, 1, 33, 1000)
+    case = Case(35 + H, K4V4, BF16, H, 2, 64, 16, lens, (1,))
+    _run(torch, case, joint=joint, decay=1.0, in_place=True)
+
+
+def test_more_sequences_than_are_shared(torch):
+    lens = tuple(int(n) for n in np.random.default_rng(9).integers(0, 20, 530))
+    case = Case(39, K4V4, HALF, 1, 1, 64, 16, lens, (1,))
+    _run(torch, case, joint=True, decay=1.0, in_place=True)
+
+
 @pytest.mark.parametrize("tag", [FP16, K8V4, K4V4])
 @pytest.mark.parametrize("new", [(1,), (40,)])
 def test_a_scale_of_its_own_and_large_scores(torch, tag, new):
