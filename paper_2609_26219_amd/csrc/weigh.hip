@@ -560,8 +560,8 @@ __global__ __launch_bounds__(kThreads, 2) void many_kernel(ServeArgs s, WeighArg
   // A split is the same rows for all tiles of tokens, whose workgroups run side by side and find them in L2.
   const int64_t every = (int64_t(g.count > 0 ? g.count : 0) * a.group + kRows - 1) / kRows;
   const int64_t begin_split = every * split / a.splits, end_split = every * (split + 1) / a.splits;
-  const int32_t from = int32_t(tile0 > begin_split ? tile0 : begin_split);
-  const int32_t upto = int32_t(tile0 + tiles < end_split ? tile0 + tiles : end_split);
+  int32_t from = int32_t(tile0 > begin_split ? tile0 : begin_split);
+  int32_t upto = int32_t(tile0 + tiles < end_split ? tile0 + tiles : end_split);
 
   // A tile in registers: its queries and row n's numbers (other half: of all rows).  Past the last tile it is that one again.
   struct Loaded {
@@ -569,6 +569,22 @@ __global__ __launch_bounds__(kThreads, 2) void many_kernel(ServeArgs s, WeighArg
     float number[kNumbers];
   };
   const RowTile* tiles_of = static_cast<const RowTile*>(a.rows) + head * a.all_tiles + first_tile(a, g, seq);
+  if (s.positions) {  // from the first tile of rows that sees one of the wave's tokens to the last one
+    int32_t first = upto, end = from;
+    for (int32_t t0 = from; t0 < upto; t0 += 64) {
+      bool sees = false;
+      if (t0 + lane < upto) {
+        const RowNumbers& row = tiles_of[t0 + lane].row;
+        sees = row.any_hi >= mine && (row.any_lo < mine + 32 * kNT - 1 || mine < a.sinks);
+      }
+      const uint64_t who = __ballot(sees);
+      if (!who) continue;
+      first = first < upto ? first : t0 + __builtin_ctzll(who);
+      end = t0 + 64 - __builtin_clzll(who);
+    }
+    from = __builtin_amdgcn_readfirstlane(first);
+    upto = __builtin_amdgcn_readfirstlane(end);
+  }
   auto fetch_query = [&](int32_t at, int i, Loaded& to) {
     to.q[i] = tiles_of[at < upto ? at : upto - 1].q[64 * i + lane];
   };
