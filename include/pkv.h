@@ -579,8 +579,8 @@ typedef struct {
  * there receives nothing.  Sums are single precision in an order that depends on the
  * sizes alone; scores are as in pkv_attention, keys that no row sees do not matter.
  * The launch has fewer than 2^24 workgroups, for which num_seqs * num_kv_heads *
- * (max_kv_len / 128 + 1) * 8 < 2^24 always suffices.  At most two
- * kernels on `hip_stream`.  Errors as pkv_attention. */
+ * (max(max_kv_len / 128, max_tokens * (num_q_heads / num_kv_heads) / 32) + 24) < 2^24
+ * always suffices.  At most three kernels on `hip_stream`.  Errors as pkv_attention. */
 pkv_status_t pkv_attention_weights_workspace(const pkv_model_t* model, const pkv_paged_cache_t* cache,
                                              const pkv_batch_t* batch, const pkv_attention_t* attention,
                                              const pkv_weights_t* weights, uint64_t* bytes);
@@ -598,6 +598,9 @@ typedef struct {
   const int32_t* budgets;   /* device [num_seqs], each sequence's own (at most budget), or NULL */
   int32_t* kept;            /* device [num_seqs][heads][budget] */
   int32_t* kept_lens;       /* device [num_seqs] */
+  void* workspace;          /* pkv_cache_keep only: device memory of pkv_cache_keep_workspace's bytes (0: may be NULL),
+                             * 16-byte aligned, contents of no matter; calls that may overlap need one each */
+  uint64_t workspace_bytes;
 } pkv_kept_t;
 
 /* Choose the tokens that stay under the budget.  Of n = kv_lens[s] tokens
@@ -605,8 +608,12 @@ typedef struct {
  * left), and of those between the ones of the largest weight (weights->weights, as many
  * heads as kept->heads), equal weights (+0 and -0 too) lowest index first, NaN after
  * everything.  Writes kept and kept_lens (m).  Of the batch only its sizes and kv_lens
- * are read.  num_seqs * heads < 2^22.  One kernel on `hip_stream`.  Errors:
- * PKV_ERR_INVALID_ARGUMENT, PKV_ERR_DEVICE. */
+ * are read.  num_seqs * heads < 2^22, and times max_kv_len / 8192 where a workspace is
+ * needed.  At most four kernels on `hip_stream`.  Errors: PKV_ERR_INVALID_ARGUMENT,
+ * PKV_ERR_DEVICE. */
+pkv_status_t pkv_cache_keep_workspace(const pkv_model_t* model, const pkv_batch_t* batch, const pkv_weights_t* weights,
+                                      const pkv_kept_t* kept, uint64_t* bytes);
+
 pkv_status_t pkv_cache_keep(const pkv_model_t* model, const pkv_batch_t* batch, const pkv_weights_t* weights,
                             const pkv_kept_t* kept, void* hip_stream);
 

@@ -28,7 +28,8 @@ EXPORTED = ("pkv_payload_size", "pkv_restore_plan", "pkv_restore", "pkv_restore_
             "pkv_plan_query", "pkv_status_string", "pkv_checkpoint_plan", "pkv_quantize_gather", "pkv_plan_repair",
             "pkv_plan_payload_bytes", "pkv_restore_from_host_noalloc", "pkv_cache_size", "pkv_cache_append",
             "pkv_cache_read", "pkv_attention_workspace", "pkv_attention", "pkv_rotate", "pkv_cache_append_rotated",
-            "pkv_attention_weights_workspace", "pkv_attention_weights", "pkv_cache_keep", "pkv_cache_evict")
+            "pkv_attention_weights_workspace", "pkv_attention_weights", "pkv_cache_keep_workspace",
+            "pkv_cache_keep", "pkv_cache_evict")
 
 
 class PkvModel(ctypes.Structure):
@@ -95,7 +96,7 @@ class PkvWeights(ctypes.Structure):
 class PkvKept(ctypes.Structure):
     _fields_ = [("heads", ctypes.c_int32), ("budget", ctypes.c_int32), ("sinks", ctypes.c_int32),
                 ("recent", ctypes.c_int32), ("budgets", ctypes.c_void_p), ("kept", ctypes.c_void_p),
-                ("kept_lens", ctypes.c_void_p)]
+                ("kept_lens", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64)]
 
 
 class PkvError(RuntimeError):
@@ -164,6 +165,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pkv_attention_weights.argtypes = [model, cache, batch, attention, weights, vp]
     lib.pkv_attention_weights.restype = i32
     kept = ctypes.POINTER(PkvKept)
+    lib.pkv_cache_keep_workspace.argtypes = [model, batch, weights, kept, ctypes.POINTER(u64)]
+    lib.pkv_cache_keep_workspace.restype = i32
     lib.pkv_cache_keep.argtypes = [model, batch, weights, kept, vp]
     lib.pkv_cache_keep.restype = i32
     lib.pkv_cache_evict.argtypes = [model, cache, batch, kept, weights, vp, i32, vp]
@@ -510,6 +513,14 @@ def pkv_attention_weights_workspace(model: PkvModel, cache: PkvPagedCache, batch
 def pkv_attention_weights_status(model: PkvModel, cache: PkvPagedCache, batch: PkvBatch, attention: PkvAttention,
                                  weights: PkvWeights, stream=0) -> int:
     return load().pkv_attention_weights(model, cache, batch, attention, weights, stream or None)
+
+
+def pkv_cache_keep_workspace(model: PkvModel, batch: PkvBatch, weights: PkvWeights, kept: PkvKept) -> int:
+    out = ctypes.c_uint64()
+    st = load().pkv_cache_keep_workspace(model, batch, weights, kept, ctypes.byref(out))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_cache_keep_workspace")
+    return out.value
 
 
 def pkv_cache_keep_status(model: PkvModel, batch: PkvBatch, weights: PkvWeights, kept: PkvKept, stream=0) -> int:

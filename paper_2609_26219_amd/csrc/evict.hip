@@ -51,29 +51,28 @@ struct KeepShared {
 
 // Adds a lane's digit to the counts, all lanes of a wave at once where they agree.
 __device__ __forceinline__ void count_digit(KeepShared& lds, bool on, uint32_t digit, int lane) {
-  const uint64_t who = __ballot(on);
-  if (!who) return;
-  const uint32_t one = uint32_t(__shfl(int(digit), __builtin_ctzll(who)));
-  if (__ballot(on && digit == one) == who) {
-    if (lane == 0) atomicAdd(&lds.count[one * kCopies], uint32_t(__builtin_popcountll(who)));
-  } else if (on) {
+  if (!on) return;
+  const uint64_t who = __ballot(1);
+  if (__ballot(digit == uint32_t(__builtin_amdgcn_readfirstlane(int(digit)))) == who) {
+    if (before(who) == 0) atomicAdd(&lds.count[digit * kCopies], uint32_t(__builtin_popcountll(who)));
+  } else {
     atomicAdd(&lds.count[digit * kCopies + (lane & (kCopies - 1))], 1u);
   }
 }
 
 // The digit of the `need`-th largest key among those counted: lds.digit; lds.left of them are to be kept among the lds.among
 // that have it.  The counts are cleared for the next digit.
-__device__ __forceinline__ void find_digit(KeepShared& lds, uint32_t need) {
-  static_assert(kDigits == 2 * kKeepThreads, "two digits to a thread");
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint32_t mine[2];
+__device__ __forceinline__ void take_counts(KeepShared& lds, uint32_t (&mine)[2]) {
+  static_assert(kDigits == 2 * kKeepThreads && kCopies == 4, "two digits to a thread");
 #pragma unroll
   for (int d = 0; d < 2; ++d) {  // digits from the top
-    const int at = (kDigits - 1 - 2 * tid - d) * kCopies;
-    u32x4& c = *reinterpret_cast<u32x4*>(&lds.count[at]);
+    u32x4& c = *reinterpret_cast<u32x4*>(&lds.count[(kDigits - 1 - 2 * int(threadIdx.x) - d) * kCopies]);
     mine[d] = c[0] + c[1] + c[2] + c[3];
     c = u32x4{};
   }
+}
+__device__ __forceinline__ void find_digit(KeepShared& lds, const uint32_t (&mine)[2], uint32_t need) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t upto = mine[0] + mine[1];
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
@@ -83,7 +82,8 @@ __device__ __forceinline__ void find_digit(KeepShared& lds, uint32_t need) {
   if (lane == 63) lds.sums[wave] = upto;
   __syncthreads();
   uint32_t upper = upto - mine[0] - mine[1];  // keys of larger digits
-  for (int i = 0; i < wave; ++i) upper += lds.sums[i];
+#pragma unroll
+  for (int i = 0; i < kKeepWaves; ++i) upper += i < wave ? lds.sums[i] : 0;  // (all read at once)
 #pragma unroll
   for (int d = 0; d < 2; ++d) {
     if (upper < need && need <= upper + mine[d]) {
@@ -96,23 +96,68 @@ __device__ __forceinline__ void find_digit(KeepShared& lds, uint32_t need) {
   __syncthreads();
 }
 
+// One row of weights and what is to be chosen of it.
+struct Choice {
+  const float* w;      // of the tokens between the first and the last ones,
+  int32_t middle;      // so many,
+  uint32_t need;       // of which so many stay
+  int32_t n, m, first, last;
+  int32_t* kept;
+  bool choose;
+};
+__device__ __forceinline__ Choice choice_of(const ServeArgs& s, const KeepArgs& a, int32_t row) {
+  const int32_t seq = int32_t(uint32_t(row) / uint32_t(a.heads)), head = int32_t(uint32_t(row) % uint32_t(a.heads));
+  Choice c;
+  c.n = kept_len(s, s.kv_lens[seq]);
+  c.m = kept_budget(a, c.n, a.budgets ? a.budgets[seq] : a.budget);
+  c.first = a.sinks < c.m ? a.sinks : c.m;
+  c.last = a.recent < c.m - c.first ? a.recent : c.m - c.first;
+  c.middle = c.n - c.first - c.last;
+  c.need = uint32_t(c.m - c.first - c.last);
+  c.kept = a.kept + int64_t(row) * a.budget;
+  c.w = a.weights + int64_t(seq) * a.seq_stride + int64_t(head) * a.head_stride + c.first;
+  c.choose = c.need != 0 && c.need != uint32_t(c.middle);
+  if (head == 0 && threadIdx.x == 0) a.kept_lens[seq] = c.m;
+  return c;
+}
+// What of a row is known without its weights.
+__device__ __forceinline__ void keep_ends(const KeepArgs& a, const Choice& c) {
+  const int tid = threadIdx.x;
+  for (int32_t j = tid; j < c.first; j += kKeepThreads) c.kept[j] = j;
+  for (int32_t j = tid; j < c.last; j += kKeepThreads) c.kept[c.m - c.last + j] = c.n - c.last + j;
+  for (int32_t j = c.m + tid; j < a.budget; j += kKeepThreads) c.kept[j] = -1;
+  if (!c.choose && c.need)
+    for (int32_t j = tid; j < c.middle; j += kKeepThreads) c.kept[c.first + j] = c.first + j;
+}
+
+// Writes a wave's tokens that stay: those of larger keys than `found` and the first `most` equal to it, after `higher` and
+// `ties` of such tokens before the wave's.
+template <typename Each>
+__device__ __forceinline__ void keep_in_order(const Choice& c, uint32_t found, int32_t most, int32_t higher, int32_t ties,
+                                              Each each) {
+  each([&](int32_t at, bool is, uint32_t key) {
+    const uint64_t gt = __ballot(is && key > found), eq = __ballot(is && key == found);
+    const int32_t tie = ties + before(eq);
+    const int32_t place = higher + before(gt) + (tie < most ? tie : most);
+    if (is && (key > found || (key == found && tie < most))) c.kept[c.first + place] = c.first + at;
+    higher += __builtin_popcountll(gt);
+    ties += __builtin_popcountll(eq);
+  });
+}
+
 __global__ __launch_bounds__(kKeepThreads) void keep_kernel(ServeArgs s, KeepArgs a) {
   __shared__ KeepShared lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int32_t seq = int32_t(blockIdx.x / uint32_t(a.heads)), head = int32_t(blockIdx.x % uint32_t(a.heads));
-  const float* w = a.weights + int64_t(seq) * a.seq_stride + int64_t(head) * a.head_stride;
-  int32_t* kept = a.kept + (int64_t(seq) * a.heads + head) * a.budget;
-  const int32_t n = kept_len(s, s.kv_lens[seq]);
-  const int32_t m = kept_budget(a, n, a.budgets ? a.budgets[seq] : a.budget);
-  const int32_t first = a.sinks < m ? a.sinks : m, last = a.recent < m - first ? a.recent : m - first;
-  const int32_t middle = n - first - last;     // tokens to choose from,
-  uint32_t need = uint32_t(m - first - last);  // and how many of them stay
+  const Choice c = choice_of(s, a, int32_t(blockIdx.x));
+  const int32_t first = c.first, middle = c.middle;
+  const bool choose = c.choose;
+  uint32_t need = c.need;
+  const float* w = c.w;
+  int32_t* kept = c.kept;
 
   // The wave's run of the middle.
   const int32_t run = ((middle + kKeepThreads - 1) / kKeepThreads) * 64;
   const int32_t from = wave * run < middle ? wave * run : middle, upto = from + run < middle ? from + run : middle;
-  w += first;
-  const bool choose = need != 0 && need != uint32_t(middle);
   uint32_t held[kHeldKeys];
   if (choose) {
 #pragma unroll
@@ -121,15 +166,8 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(ServeArgs s, KeepArg
       held[i] = at < upto ? __float_as_uint(w[at]) : 0;
     }
   }
-  if (head == 0 && tid == 0) a.kept_lens[seq] = m;
-  for (int32_t j = tid; j < first; j += kKeepThreads) kept[j] = j;
-  for (int32_t j = tid; j < last; j += kKeepThreads) kept[m - last + j] = n - last + j;
-  for (int32_t j = m + tid; j < a.budget; j += kKeepThreads) kept[j] = -1;
-  if (!choose) {
-    if (need)
-      for (int32_t j = tid; j < middle; j += kKeepThreads) kept[first + j] = first + j;
-    return;
-  }
+  keep_ends(a, c);
+  if (!choose) return;
   for (int i = tid; i < kDigits * kCopies; i += kKeepThreads) lds.count[i] = 0;
   if (tid == 0) lds.listed = 0;
   __syncthreads();
@@ -153,7 +191,9 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(ServeArgs s, KeepArg
 
   each([&](int32_t, bool is, uint32_t key) { count_digit(lds, is, key >> 21, lane); });
   __syncthreads();
-  find_digit(lds, need);
+  uint32_t mine[2];
+  take_counts(lds, mine);
+  find_digit(lds, mine, need);
   uint32_t found = lds.digit;  // the digits found so far
   need = lds.left;
   const uint32_t among = lds.among;
@@ -187,7 +227,8 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(ServeArgs s, KeepArg
       });
     }
     __syncthreads();
-    find_digit(lds, need);
+    take_counts(lds, mine);
+    find_digit(lds, mine, need);
     found = found << bits | lds.digit;
     need = lds.left;
   }
@@ -204,19 +245,202 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(ServeArgs s, KeepArg
   }
   __syncthreads();
   int32_t higher = 0, ties = 0;  // in the runs before
-  for (int i = 0; i < wave; ++i) {
-    higher += lds.above[i];
-    ties += lds.equal[i];
+#pragma unroll
+  for (int i = 0; i < kKeepWaves; ++i) {
+    higher += i < wave ? lds.above[i] : 0;
+    ties += i < wave ? lds.equal[i] : 0;
   }
-  const int32_t most = int32_t(need);
-  each([&](int32_t at, bool is, uint32_t key) {
-    const uint64_t gt = __ballot(is && key > found), eq = __ballot(is && key == found);
-    const int32_t tie = ties + before(eq);
-    const int32_t place = higher + before(gt) + (tie < most ? tie : most);
-    if (is && (key > found || (key == found && tie < most))) kept[first + place] = first + at;
-    higher += __builtin_popcountll(gt);
-    ties += __builtin_popcountll(eq);
+  keep_in_order(c, found, int32_t(need), higher, ties, each);
+}
+
+// The same of long rows that are few, by many workgroups: a segment of a row is one's, in four launches.  The first digits are
+// counted; with the row's counts together every workgroup knows the last one kept and lists its keys that have it; one
+// workgroup a row finds the last key among them, and how many tokens of each segment are above it and equal to it; and the
+// segments write their tokens.
+constexpr int kSegmentKeys = kKeepSegment / kKeepThreads;  // of a lane
+
+// A lane's keys of a segment, each wave a run of it: f(place in the middle, whether there is such a token, its key).
+struct Segment {
+  int32_t from, upto;
+  uint32_t key[kSegmentKeys];
+  template <typename F>
+  __device__ __forceinline__ void each(int lane, F f) const {
+#pragma unroll
+    for (int i = 0; i < kSegmentKeys; ++i)
+      if (from + 64 * i < upto) f(from + 64 * i + lane, from + 64 * i + lane < upto, key[i]);
+  }
+};
+__device__ __forceinline__ Segment segment_of(const Choice& c, int32_t segment, int lane, int wave) {
+  Segment g;
+  const int64_t begin = int64_t(segment) * kKeepSegment + wave * (64 * kSegmentKeys);
+  g.from = int32_t(begin < c.middle ? begin : c.middle);
+  g.upto = int32_t(begin + 64 * kSegmentKeys < c.middle ? begin + 64 * kSegmentKeys : c.middle);
+  float w[kSegmentKeys];
+#pragma unroll
+  for (int i = 0; i < kSegmentKeys; ++i) w[i] = g.from + 64 * i + lane < g.upto ? c.w[g.from + 64 * i + lane] : 0.0f;
+#pragma unroll
+  for (int i = 0; i < kSegmentKeys; ++i) g.key[i] = key_of(w[i]);
+  return g;
+}
+__device__ __forceinline__ int32_t segments_of(const Choice& c) { return (c.middle + kKeepSegment - 1) / kKeepSegment; }
+
+__global__ __launch_bounds__(kKeepThreads) void keep_count_kernel(ServeArgs s, KeepArgs a) {
+  __shared__ KeepShared lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t row = int32_t(blockIdx.x / uint32_t(a.segments)), segment = int32_t(blockIdx.x % uint32_t(a.segments));
+  const Choice c = choice_of(s, a, row);
+  if (segment == 0) keep_ends(a, c);
+  if (!c.choose || segment >= segments_of(c)) return;
+  const Segment g = segment_of(c, segment, lane, wave);
+  for (int i = tid; i < kDigits * kCopies; i += kKeepThreads) lds.count[i] = 0;
+  __syncthreads();
+  g.each(lane, [&](int32_t, bool is, uint32_t key) { count_digit(lds, is, key >> 21, lane); });
+  __syncthreads();
+  uint32_t mine[2];
+  take_counts(lds, mine);
+  reinterpret_cast<u32x2*>(a.counts)[int64_t(blockIdx.x) * kKeepThreads + tid] = u32x2{mine[0], mine[1]};
+}
+
+__global__ __launch_bounds__(kKeepThreads) void keep_list_kernel(ServeArgs s, KeepArgs a) {
+  __shared__ KeepShared lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t row = int32_t(blockIdx.x / uint32_t(a.segments)), segment = int32_t(blockIdx.x % uint32_t(a.segments));
+  const Choice c = choice_of(s, a, row);
+  const int32_t segments = segments_of(c);
+  if (!c.choose || segment >= segments) return;
+  const Segment g = segment_of(c, segment, lane, wave);
+  const u32x2* counts = reinterpret_cast<const u32x2*>(a.counts) + int64_t(row) * a.segments * kKeepThreads + tid;
+  uint32_t mine[2] = {};
+  for (int32_t i = 0; i < segments; i += 8) {
+    u32x2 v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i + e < segments ? counts[int64_t(i + e) * kKeepThreads] : u32x2{};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      mine[0] += v[e][0];
+      mine[1] += v[e][1];
+    }
+  }
+  if (tid == 0) {
+    lds.listed = 0;
+    lds.above[0] = 0;
+  }
+  find_digit(lds, mine, c.need);
+  const uint32_t found = lds.digit;
+  uint32_t* list = a.lists + int64_t(blockIdx.x) * kKeepSegment;
+  int32_t more = 0;
+  g.each(lane, [&](int32_t, bool is, uint32_t key) {
+    more += __builtin_popcountll(__ballot(is && key >> 21 > found));
+    const bool on = is && key >> 21 == found;
+    const uint64_t who = __ballot(on);
+    if (!who) return;
+    uint32_t at = 0;
+    if (lane == 0) at = atomicAdd(&lds.listed, uint32_t(__builtin_popcountll(who)));
+    at = uint32_t(__builtin_amdgcn_readfirstlane(int(at)));
+    if (on) list[at + before(who)] = key;
   });
+  if (lane == 0) atomicAdd(&lds.above[0], more);
+  __syncthreads();
+  if (tid == 0) {
+    a.segment[blockIdx.x] = KeepSegment{int32_t(lds.listed), lds.above[0]};
+    if (segment == 0) a.row[row] = KeepRow{found, lds.left};
+  }
+}
+
+__global__ __launch_bounds__(kKeepThreads) void keep_find_kernel(ServeArgs s, KeepArgs a) {
+  __shared__ KeepShared lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t row = int32_t(blockIdx.x);
+  const Choice c = choice_of(s, a, row);
+  if (!c.choose) return;
+  const int32_t segments = segments_of(c);
+  KeepSegment* segment = a.segment + int64_t(row) * a.segments;
+  const uint32_t* lists = a.lists + int64_t(row) * a.segments * kKeepSegment;
+  uint32_t found = a.row[row].last, need = a.row[row].need;
+  for (int i = tid; i < kDigits * kCopies; i += kKeepThreads) lds.count[i] = 0;
+  __syncthreads();
+  // The listed keys of each segment, a wave to a segment.
+  auto each = [&](int32_t which, auto f) {
+    const int32_t many = segment[which].listed;
+    const uint32_t* list = lists + int64_t(which) * kKeepSegment;
+    for (int32_t i = 0; i < many; i += 64 * kLoadsAhead) {
+      uint32_t v[kLoadsAhead];
+#pragma unroll
+      for (int e = 0; e < kLoadsAhead; ++e) v[e] = i + 64 * e + lane < many ? list[i + 64 * e + lane] : 0;
+#pragma unroll
+      for (int e = 0; e < kLoadsAhead; ++e)
+        if (i + 64 * e < many) f(i + 64 * e + lane < many, v[e]);
+    }
+  };
+  constexpr int kAt[2] = {10, 0}, kBits[2] = {11, 10};
+#pragma unroll
+  for (int d = 0; d < 2; ++d) {
+    const int shift = kAt[d], bits = kBits[d];
+    for (int32_t i = wave; i < segments; i += kKeepWaves)
+      each(i, [&](bool is, uint32_t key) {
+        count_digit(lds, is && key >> (shift + bits) == found, key >> shift & ((1u << bits) - 1), lane);
+      });
+    __syncthreads();
+    uint32_t mine[2];
+    take_counts(lds, mine);
+    find_digit(lds, mine, need);
+    found = found << bits | lds.digit;
+    need = lds.left;
+  }
+  if (tid == 0) a.row[row] = KeepRow{found, need};
+  // Tokens of each segment above the last key and equal to it, then those of the segments before.
+  for (int32_t i = wave; i < segments; i += kKeepWaves) {
+    int32_t more = segment[i].above, same = 0;
+    each(i, [&](bool is, uint32_t key) {
+      more += __builtin_popcountll(__ballot(is && key > found));
+      same += __builtin_popcountll(__ballot(is && key == found));
+    });
+    if (lane == 0) segment[i] = KeepSegment{same, more};
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  int32_t higher = 0, ties = 0;
+  for (int32_t i0 = 0; i0 < segments; i0 += 64) {
+    const KeepSegment mine = i0 + lane < segments ? segment[i0 + lane] : KeepSegment{0, 0};
+    int32_t more = mine.above, same = mine.listed;
+    for (int off = 1; off < 64; off <<= 1) {
+      const int32_t m = __shfl_up(more, off), e = __shfl_up(same, off);
+      more += lane >= off ? m : 0;
+      same += lane >= off ? e : 0;
+    }
+    if (i0 + lane < segments) segment[i0 + lane] = KeepSegment{ties + same - mine.listed, higher + more - mine.above};
+    higher += __shfl(more, 63);
+    ties += __shfl(same, 63);
+  }
+}
+
+__global__ __launch_bounds__(kKeepThreads) void keep_write_kernel(ServeArgs s, KeepArgs a) {
+  __shared__ int32_t above[kKeepWaves], equal[kKeepWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t row = int32_t(blockIdx.x / uint32_t(a.segments)), segment = int32_t(blockIdx.x % uint32_t(a.segments));
+  const Choice c = choice_of(s, a, row);
+  if (!c.choose || segment >= segments_of(c)) return;
+  const Segment g = segment_of(c, segment, lane, wave);
+  const KeepRow last = a.row[row];
+  const KeepSegment begin = a.segment[blockIdx.x];
+  const uint32_t found = last.last;
+  int32_t more = 0, same = 0;
+  g.each(lane, [&](int32_t, bool is, uint32_t key) {
+    more += __builtin_popcountll(__ballot(is && key > found));
+    same += __builtin_popcountll(__ballot(is && key == found));
+  });
+  if (lane == 0) {
+    above[wave] = more;
+    equal[wave] = same;
+  }
+  __syncthreads();
+  int32_t higher = begin.above, ties = begin.listed;
+#pragma unroll
+  for (int i = 0; i < kKeepWaves; ++i) {
+    higher += i < wave ? above[i] : 0;
+    ties += i < wave ? equal[i] : 0;
+  }
+  keep_in_order(c, found, int32_t(last.need), higher, ties, [&](auto f) { g.each(lane, f); });
 }
 
 // ---- Their rows to the front ----
@@ -358,8 +582,18 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 4) void evict_kernel(S
 }  // namespace
 
 pkv_status_t launch_keep(const ServeArgs& s, const KeepArgs& a, hipStream_t stream) {
-  const dim3 grid(uint32_t(s.num_seqs) * uint32_t(a.heads));
-  hipLaunchKernelGGL(keep_kernel, grid, dim3(kKeepThreads), 0, stream, s, a);
+  const uint32_t rows = uint32_t(s.num_seqs) * uint32_t(a.heads);
+  auto go = [&](auto kernel, uint32_t groups) {
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(kKeepThreads), 0, stream, s, a);
+  };
+  if (a.segments) {
+    go(keep_count_kernel, rows * uint32_t(a.segments));
+    go(keep_list_kernel, rows * uint32_t(a.segments));
+    go(keep_find_kernel, rows);
+    go(keep_write_kernel, rows * uint32_t(a.segments));
+  } else {
+    go(keep_kernel, rows);
+  }
   return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_DEVICE;
 }
 

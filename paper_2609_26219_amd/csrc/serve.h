@@ -145,6 +145,15 @@ struct WeighLaunch {
   uint64_t workspace_bytes; // both
 };
 
+// Of a segment of a long row: its keys that share the first digit of the last one kept, and those of larger digits; then the
+// tokens before it that are equal to the last one kept, and above it.
+struct KeepSegment {
+  int32_t listed, above;
+};
+struct KeepRow {  // the last key kept (its first digit at first), and how many of those equal to it stay
+  uint32_t last, need;
+};
+
 // The tokens of each sequence (and head) that stay.
 struct KeepArgs {
   const float* weights;
@@ -153,7 +162,18 @@ struct KeepArgs {
   int32_t* kept_lens;
   int64_t seq_stride, head_stride;
   int32_t heads, budget, sinks, recent;
+  int32_t segments;        // workgroups of a row, or 0: one
+  uint32_t* counts;        // [rows][segments][2048]
+  uint32_t* lists;         // [rows][segments][kKeepSegment]
+  KeepSegment* segment;    // [rows][segments]
+  KeepRow* row;            // [rows]
 };
+
+constexpr int kKeepSegment = 8192;  // tokens of a segment
+// Rows up to which a long row is cut into segments, and its length: 2 x 8 rows of up to 131072 tokens 105.7 us by one workgroup
+// each.
+constexpr int kFewKeptRows = 128;
+constexpr int kWholeRow = 32768;
 
 // Rows of a cache moved to where they stay, and the weights with them.
 struct EvictArgs {
@@ -229,7 +249,8 @@ AttendLaunch attend_launch(const ServeArgs& s, const AttendArgs& a);
 pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_weights_t* w, bool pointers, WeighArgs* out,
                         WeighLaunch* launch);
 
-pkv_status_t keep_args(const ServeArgs& s, const pkv_weights_t* w, const pkv_kept_t* k, KeepArgs* out);
+pkv_status_t keep_args(const ServeArgs& s, const pkv_weights_t* w, const pkv_kept_t* k, bool pointers, KeepArgs* out,
+                       uint64_t* workspace_bytes);
 pkv_status_t evict_args(const ServeArgs& s, const pkv_kept_t* k, const pkv_weights_t* w, const int32_t* page_table,
                         int32_t table_pages, EvictArgs* out);
 

@@ -759,11 +759,13 @@ pkv_status_t pkv_cache_keep(const pkv_model_t* model, const pkv_batch_t* batch, 
   pkv::ServeArgs s;
   pkv::KeepArgs a;
   pkv_status_t st = pkv::batch_args(model, batch, false, &s);
-  if (st == PKV_OK) st = pkv::keep_args(s, weights, kept, &a);
+  uint64_t bytes = 0;
+  if (st == PKV_OK) st = pkv::keep_args(s, weights, kept, true, &a, &bytes);
   if (st != PKV_OK || s.num_seqs == 0) return st;
   const pkv::OnDevice here;
   if (!here.ok) return PKV_ERR_DEVICE;
-  if (!here.has(s.kv_lens) || !here.has(a.weights) || !here.has(a.budgets) || !here.has(a.kept) || !here.has(a.kept_lens))
+  if (!here.has(s.kv_lens) || !here.has(a.weights) || !here.has(a.budgets) || !here.has(a.kept) || !here.has(a.kept_lens) ||
+      !here.has(a.counts))
     return PKV_ERR_INVALID_ARGUMENT;
   return pkv::launch_keep(s, a, static_cast<hipStream_t>(hip_stream));
 }

@@ -345,11 +345,12 @@ pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_
 
 namespace {
 
-pkv_status_t kept_ok(const ServeArgs& s, const pkv_kept_t* k, const pkv_weights_t* w) {
+pkv_status_t kept_ok(const ServeArgs& s, const pkv_kept_t* k, const pkv_weights_t* w, bool pointers) {
   if (!k || (k->heads != 1 && k->heads != s.H)) return PKV_ERR_INVALID_ARGUMENT;
   if (k->budget < 0 || k->budget > (1 << 30) || k->sinks < 0 || k->recent < 0) return PKV_ERR_INVALID_ARGUMENT;
   if (w && (!weights_ok(s, *w) || w->heads != k->heads)) return PKV_ERR_INVALID_ARGUMENT;
   if (int64_t(s.num_seqs) * k->heads >= kMostGroups / 4) return PKV_ERR_INVALID_ARGUMENT;  // (of 1024 threads)
+  if (!pointers) return PKV_OK;
   if (!aligned(k->kept, 4) || !aligned(k->kept_lens, 4) || !aligned(k->budgets, 4) || !aligned(s.kv_lens, 4))
     return PKV_ERR_INVALID_ARGUMENT;
   if (s.num_seqs > 0 && (!s.kv_lens || !k->kept_lens || (k->budget > 0 && !k->kept))) return PKV_ERR_INVALID_ARGUMENT;
@@ -358,19 +359,49 @@ pkv_status_t kept_ok(const ServeArgs& s, const pkv_kept_t* k, const pkv_weights_
 
 }  // namespace
 
-pkv_status_t keep_args(const ServeArgs& s, const pkv_weights_t* w, const pkv_kept_t* k, KeepArgs* out) {
+pkv_status_t keep_args(const ServeArgs& s, const pkv_weights_t* w, const pkv_kept_t* k, bool pointers, KeepArgs* out,
+                       uint64_t* workspace_bytes) {
   if (!w) return PKV_ERR_INVALID_ARGUMENT;
-  const pkv_status_t st = kept_ok(s, k, w);
+  const pkv_status_t st = kept_ok(s, k, w, pointers);
   if (st != PKV_OK) return st;
-  if (!aligned(w->weights, 4) || (s.num_seqs > 0 && !w->weights)) return PKV_ERR_INVALID_ARGUMENT;
-  *out = KeepArgs{w->weights, k->budgets, k->kept, k->kept_lens, w->seq_stride, w->heads > 1 ? w->head_stride : 0,
-                  k->heads, k->budget, k->sinks, k->recent};
+  if (pointers && (!aligned(w->weights, 4) || (s.num_seqs > 0 && !w->weights))) return PKV_ERR_INVALID_ARGUMENT;
+  KeepArgs a{};
+  a.weights = w->weights;
+  a.budgets = k->budgets;
+  a.kept = k->kept;
+  a.kept_lens = k->kept_lens;
+  a.seq_stride = w->seq_stride;
+  a.head_stride = w->heads > 1 ? w->head_stride : 0;
+  a.heads = k->heads;
+  a.budget = k->budget;
+  a.sinks = k->sinks;
+  a.recent = k->recent;
+  const int64_t rows = int64_t(s.num_seqs) * k->heads;
+  uint64_t counts = 0, lists = 0, segment = 0;
+  if (rows > 0 && rows <= kFewKeptRows && s.max_kv > kWholeRow) {
+    a.segments = (s.max_kv + kKeepSegment - 1) / kKeepSegment;
+    const uint64_t all = uint64_t(rows) * a.segments;
+    counts = all * 2048 * 4;
+    lists = all * kKeepSegment * 4;
+    segment = (all * sizeof(KeepSegment) + 15) / 16 * 16;
+    if (int64_t(all) >= kMostGroups / 4) return PKV_ERR_INVALID_ARGUMENT;
+  }
+  *workspace_bytes = a.segments ? counts + lists + segment + uint64_t(rows) * sizeof(KeepRow) : 0;
+  if (pointers && a.segments) {
+    if (!k->workspace || !aligned(k->workspace, 16) || k->workspace_bytes < *workspace_bytes) return PKV_ERR_INVALID_ARGUMENT;
+    char* at = static_cast<char*>(k->workspace);
+    a.counts = reinterpret_cast<uint32_t*>(at);
+    a.lists = reinterpret_cast<uint32_t*>(at + counts);
+    a.segment = reinterpret_cast<KeepSegment*>(at + counts + lists);
+    a.row = reinterpret_cast<KeepRow*>(at + counts + lists + segment);
+  }
+  *out = a;
   return PKV_OK;
 }
 
 pkv_status_t evict_args(const ServeArgs& s, const pkv_kept_t* k, const pkv_weights_t* w, const int32_t* page_table,
                         int32_t table_pages, EvictArgs* out) {
-  const pkv_status_t st = kept_ok(s, k, w);
+  const pkv_status_t st = kept_ok(s, k, w, true);
   if (st != PKV_OK) return st;
   if (!aligned(page_table, 4) || (page_table && table_pages < 1)) return PKV_ERR_INVALID_ARGUMENT;
   if (w && (!aligned(w->out, 4) || (s.num_seqs > 0 && !w->out))) return PKV_ERR_INVALID_ARGUMENT;
@@ -453,6 +484,16 @@ pkv_status_t pkv_attention_weights_workspace(const pkv_model_t* model, const pkv
   if (st != PKV_OK) return st;
   *bytes = l.workspace_bytes;
   return PKV_OK;
+}
+
+pkv_status_t pkv_cache_keep_workspace(const pkv_model_t* model, const pkv_batch_t* batch, const pkv_weights_t* weights,
+                                      const pkv_kept_t* kept, uint64_t* bytes) {
+  if (!bytes) return PKV_ERR_INVALID_ARGUMENT;
+  pkv::ServeArgs s;
+  pkv::KeepArgs a;
+  pkv_status_t st = pkv::batch_args(model, batch, false, &s);
+  if (st == PKV_OK) st = pkv::keep_args(s, weights, kept, false, &a, bytes);
+  return st;
 }
 
 }  // extern "C"

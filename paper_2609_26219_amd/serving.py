@@ -371,7 +371,15 @@ def keep(cache: PagedCache, batch: Batch, weights, budget: int, sinks: int = 0, 
                torch.empty(batch.struct.num_seqs, dtype=torch.int32, device=cache.device))
     kept = _kept(batch, *out, budgets, _int32(sinks), _int32(recent))
     _need(kept.heads == w.heads and kept.budget == budget, "kept is [S, heads of weights, budget]")
-    _check(binding.pkv_cache_keep_status(cache.model, batch.struct, w, kept, _stream(cache)), "pkv_cache_keep")
+    stream = _stream(cache)
+    nbytes = binding.pkv_cache_keep_workspace(cache.model, batch.struct, w, kept)
+    if nbytes:
+        with cache._scratch:
+            kept.workspace, kept.workspace_bytes = cache.workspace(nbytes, stream), nbytes
+            status = binding.pkv_cache_keep_status(cache.model, batch.struct, w, kept, stream)
+    else:
+        status = binding.pkv_cache_keep_status(cache.model, batch.struct, w, kept, stream)
+    _check(status, "pkv_cache_keep")
     return out
 
 
