@@ -457,6 +457,8 @@ struct Piece<16> { typedef u32x4 type; };
 template <>
 struct Piece<8> { typedef u32x2 type; };
 
+constexpr int kPart = 2;  // rows of a thread, of the kRowsAhead of a chunk, that are written while as many are read
+
 // Where a row goes from and to: page and slot, page -1 for none.
 struct Move {
   int32_t from_page, from_slot, to_page, to_slot;
@@ -554,26 +556,33 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 4) void evict_kernel(S
       moves[r] = v;
     }
     __syncthreads();
-    Word v[kRowsAhead];
-    uint32_t sz[kRowsAhead];
+    // In place a part of the chunk is written while the next one is read: a barrier between a part's loads and its stores.
+    Word v[2][kPart];
+    uint32_t sz[2][kPart];
+    auto each = [&](int p, auto f) {
 #pragma unroll
-    for (int i = 0; i < kRowsAhead; ++i) {
-      if (i * per >= chunk) break;
-      const Move& at = moves[i * per + row0];
-      if (mine && at.from_page >= 0) {
-        v[i] = *reinterpret_cast<const Word*>(base + at.from_page * page_bytes + at.from_slot * slot_bytes);
-        if (scaled) sz[i] = scales[at.from_page * s.scale_stride + at.from_slot];
+      for (int e = 0; e < kPart; ++e) {
+        const int32_t r = (p * kPart + e) * per + row0;
+        if (r >= chunk) break;
+        const Move at = moves[r];
+        if (mine && at.from_page >= 0) f(e, at);
       }
-    }
-    if (in_place) __syncthreads();
+    };
+    auto load = [&](int p) {
+      each(p, [&](int e, const Move& at) {
+        v[p & 1][e] = *reinterpret_cast<const Word*>(base + at.from_page * page_bytes + at.from_slot * slot_bytes);
+        if (scaled) sz[p & 1][e] = scales[at.from_page * s.scale_stride + at.from_slot];
+      });
+    };
+    load(0);
 #pragma unroll
-    for (int i = 0; i < kRowsAhead; ++i) {
-      if (i * per >= chunk) break;
-      const Move& at = moves[i * per + row0];
-      if (mine && at.from_page >= 0) {
-        *reinterpret_cast<Word*>(base + at.to_page * page_bytes + at.to_slot * slot_bytes) = v[i];
-        if (scaled) scales[at.to_page * s.scale_stride + at.to_slot] = sz[i];
-      }
+    for (int p = 0; p < kRowsAhead / kPart; ++p) {
+      if (p + 1 < kRowsAhead / kPart) load(p + 1);
+      if (in_place) __syncthreads();
+      each(p, [&](int e, const Move& at) {
+        *reinterpret_cast<Word*>(base + at.to_page * page_bytes + at.to_slot * slot_bytes) = v[p & 1][e];
+        if (scaled) scales[at.to_page * s.scale_stride + at.to_slot] = sz[p & 1][e];
+      });
     }
     __syncthreads();
   }
