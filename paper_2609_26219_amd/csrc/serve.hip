@@ -508,6 +508,8 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(ServeArgs a, RowArgs r, 
   move_rows<BF16, KB, VB, WRITE, false>(a, r, w, nullptr, lds, nullptr);
 }
 
+constexpr int kHeadsAhead = 2;  // a thread's rows on their way while one is turned
+
 // Rows turned into r.out, as move_rows deals rows: a thread stays with its token and piece, whose turns it keeps in
 // registers over the heads.  Every lane of a row has loaded both its pieces before one stores (a row is in one wave), so
 // out may be x.
@@ -523,23 +525,36 @@ __device__ __forceinline__ void turn_rows(const ServeArgs& a, const RotateArgs& 
   const bool mine = 8 * piece < a.D && t < n;
   const uint16_t* x = r.x + int64_t(i0 + t) * r.x_token_stride + head0 * r.x_head_stride + 8 * piece;
   uint16_t* out = r.out + int64_t(i0 + t) * r.out_token_stride + head0 * r.out_head_stride + 8 * piece;
-  u32x4 own{}, other{};
-  if (mine && head0 < r.heads) own = *reinterpret_cast<const u32x4*>(x);
+  u32x4 own[kHeadsAhead]{}, other[kHeadsAhead]{};
+#pragma unroll
+  for (int i = 0; i < kHeadsAhead; ++i)
+    if (mine && head0 + i * heads < r.heads) own[i] = *reinterpret_cast<const u32x4*>(x + i * heads * r.x_head_stride);
   const RowOf row = find_row(a, i0, n, lds.starts);
   if (int32_t(threadIdx.x) < n) lds.place[threadIdx.x].k = row.seq;
   find_turns(r, row, n, turns.at, turns.turn);
   const PieceTurn turn = piece_turn(r, turns.at, turns.turn, t < n ? t : 0, piece);
   if (!mine || lds.place[t].k < 0) return;
-  if (head0 < r.heads) other = *reinterpret_cast<const u32x4*>(x + turn.partner);
-  for (int32_t head = head0; head < r.heads; head += heads) {
-    const u32x4 now = turned<BF16>(turn, own, other);
-    x += heads * r.x_head_stride;
-    if (head + heads < r.heads) {
-      own = *reinterpret_cast<const u32x4*>(x);
-      other = *reinterpret_cast<const u32x4*>(x + turn.partner);
+  auto load_other = [&](int i, const uint16_t* at) {  // (interleaved pairs have both in one piece)
+    if (turn.partner) other[i] = *reinterpret_cast<const u32x4*>(at + turn.partner);
+  };
+#pragma unroll
+  for (int i = 0; i < kHeadsAhead; ++i)
+    if (head0 + i * heads < r.heads) load_other(i, x + i * heads * r.x_head_stride);
+  const int64_t step = heads * r.x_head_stride;
+  for (int32_t head = head0; head < r.heads; head += kHeadsAhead * heads) {
+#pragma unroll
+    for (int i = 0; i < kHeadsAhead; ++i) {
+      const int32_t mine_now = head + i * heads;
+      if (mine_now >= r.heads) return;
+      const u32x4 now = turned<BF16>(turn, own[i], other[i]);
+      if (mine_now + kHeadsAhead * heads < r.heads) {
+        own[i] = *reinterpret_cast<const u32x4*>(x + kHeadsAhead * step);
+        load_other(i, x + kHeadsAhead * step);
+      }
+      *reinterpret_cast<u32x4*>(out) = now;
+      x += step;
+      out += heads * r.out_head_stride;
     }
-    *reinterpret_cast<u32x4*>(out) = now;
-    out += heads * r.out_head_stride;
   }
 }
 
