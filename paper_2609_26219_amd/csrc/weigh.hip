@@ -32,6 +32,14 @@ __device__ __forceinline__ SequenceRows sequence_rows(const ServeArgs& s, int32_
                           scalar_entry(s.kv_lens, seq));
 }
 
+// over_c_sum by lane swaps.
+__device__ __forceinline__ float over_c_add(float v) {
+  u32x2 w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+
 // What a row at position `pos` sees.
 __device__ __forceinline__ Sight sight_at(const WeighArgs& a, const SequenceRows& g, int32_t pos) {
   Sight see;
@@ -198,16 +206,16 @@ __device__ __forceinline__ void weigh_tokens(const ServeArgs& s, const WeighArgs
     bool plain = true;  // no row with a mask of its own
     u32x4 q[RT][kSteps];
     f32x4 f[RT], less[RT], sum[RT];
-    int32_t hi[RT][4], lo[RT][4];
+    Sight see[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const int32_t row = 16 * r + x, token = row / a.group, qhead = head * a.group + row % a.group;
       const bool on = token < g.count;
-      Sight see{-1, -1};
+      see[r] = Sight{-1, -1};
       RowScale rs{a.scale, -kInf, 0.0f};
       if (on) {
         rs.less = less_of(a, g, token, qhead);
-        if (rs.less != -kInf) see = sight_of(s, a, g, token);
+        if (rs.less != -kInf) see[r] = sight_of(s, a, g, token);
         else plain = false;
       }
       const uint16_t* rowq = a.q + int64_t(g.start + (on ? token : 0)) * a.q_token_stride + int64_t(qhead) * a.q_head_stride;
@@ -248,8 +256,6 @@ __device__ __forceinline__ void weigh_tokens(const ServeArgs& s, const WeighArgs
         f[r][i] = __shfl(rs.f, 4 * c + i);
         less[r][i] = __shfl(rs.less, 4 * c + i);
         sum[r][i] = __shfl(rs.sum, 4 * c + i);
-        hi[r][i] = __shfl(see.hi, 4 * c + i);
-        lo[r][i] = __shfl(see.lo, 4 * c + i);
       }
     }
 
@@ -279,6 +285,17 @@ __device__ __forceinline__ void weigh_tokens(const ServeArgs& s, const WeighArgs
         load(b, t0 + kTiles * kTokenTile);
         // (Rows past the last have less = -inf and queries of 0: nothing, but for keys that are no numbers.)
         auto sums_of = [&](auto masked) {
+          constexpr bool kMasked = decltype(masked)::value;
+          int32_t hi[RT][4], lo[RT][4];
+          if constexpr (kMasked) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                hi[r][i] = __shfl(see[r].hi, 4 * c + i);
+                lo[r][i] = __shfl(see[r].lo, 4 * c + i);
+              }
+          }
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const int32_t tok = t0 + 16 * u + x;
@@ -291,10 +308,10 @@ __device__ __forceinline__ void weigh_tokens(const ServeArgs& s, const WeighArgs
                 float t = score[r][u][i];
                 if constexpr (kCodes) t = __builtin_fmaf(ks[u], t, kz[u] * sum[r][i]);
                 float p = exp2_of(__builtin_fmaf(t, f[r][i], less[r][i]));
-                if constexpr (decltype(masked)::value) p = (tok <= hi[r][i]) & ((tok > lo[r][i]) | sink) ? p : 0.0f;
+                if constexpr (kMasked) p = (tok <= hi[r][i]) & ((tok > lo[r][i]) | sink) ? p : 0.0f;
                 total += p;
               }
-            w[u] = over_c_sum(total);
+            w[u] = over_c_add(total);
             if (!is[u]) w[u] = 0.0f;
           }
         };
