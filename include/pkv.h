@@ -619,8 +619,8 @@ pkv_status_t pkv_cache_keep(const pkv_model_t* model, const pkv_batch_t* batch, 
 
 /* Move the rows that stay to the front of their sequence: row j of head h (K, V and
  * their scales) becomes row kept[s][h][j], for j < kept_lens[s] (at most kv_lens[s]).
- *   page_table : NULL: in place; kept ascends, and a sequence's pages are no
- *     other's.  Else device [num_seqs][table_pages]: the rows go to its pages,
+ *   page_table : NULL (or the batch's): in place; kept ascends, and a sequence's pages
+ *     are no other's.  Else device [num_seqs][table_pages]: the rows go to its pages,
  *     which hold no row that stays (pages shared with another sequence keep
  *     theirs);
  *   weights    : NULL, or weights->out (kept->heads heads) is moved alike, in place, and

@@ -170,10 +170,11 @@ struct KeepArgs {
 };
 
 constexpr int kKeepSegment = 8192;  // tokens of a segment
-// Rows up to which a long row is cut into segments, and its length: 2 x 8 rows of up to 131072 tokens 105.7 us by one workgroup
-// each.
-constexpr int kFewKeptRows = 128;
-constexpr int kWholeRow = 32768;
+// A choice of up to kFewKeptRows rows that may be longer than kWholeRow is made by segments.  Whole calls, us, by segments | by a
+// workgroup a row: 32 rows of 16384 tokens 25.3 | 22.3, of 32768 25.9 | 29.9; 128 of 32768 38.5 | 30.4; 2 x 8 rows of 131072 and
+// 40001 27 | 106; 512 of 65536 230 | 123.
+constexpr int kFewKeptRows = 64;
+constexpr int kWholeRow = 24576;
 
 // Rows of a cache moved to where they stay, and the weights with them.
 struct EvictArgs {
@@ -207,9 +208,13 @@ constexpr int32_t kept_budget(const KeepArgs& a, int32_t n, int32_t budget) {
   return budget < n ? budget : n;
 }
 
-constexpr int kMostChunk = 512;   // tokens of a wave of few rows at a time
-constexpr int kMostShared = 512;  // sequences whose tokens are shared evenly (every workgroup adds up their lengths),
-constexpr int kShares = 512;      // by that many workgroups
+// Of few rows (up to few_tiles row tiles of 16 a sequence and KV head; 32 sequences of 8192 tokens, 8 heads of 128, 32 rows, as few |
+// as many: 60 | 82 us in 4 bits, 104 | 153 in 16; 4 rows 42 | 99 and 101 | 169): tokens of a wave at a time; sequences whose tokens
+// are shared evenly (every workgroup adds up their lengths) and by how many workgroups.  32 ragged sequences of 255 thousand tokens in
+// 4 bits: even shares 53 us, chunks of 128, 256 and 512 tokens 65, 60 and 68.
+constexpr int kMostChunk = 512;
+constexpr int kMostShared = 512;
+constexpr int kShares = 512;
 // Of many rows: tokens of a workgroup, rows of a tile, and its bytes (queries, and 5 numbers a row and 8 of all).
 constexpr int weigh_tokens(int head_dim) { return head_dim > 128 ? 128 : 256; }
 constexpr int kWeighRows = 32;

@@ -108,6 +108,58 @@ def test_keep_of_long_rows(torch, n, kind):
         assert kept_lens.tolist() == [min(length, budget) for length in lens]
 
 
+def test_keep_of_many_long_rows(torch):
+    """More rows than are cut into segments: one workgroup each, longer than its registers."""
+    from paper_2609_26219_amd import serving
+
+    n, S = 33000, 130
+    lens = tuple(n - 7 * s for s in range(S))
+    cache, batch = _sequences(torch, lens)
+    w = _kinds(np.random.default_rng(3), (S, 1, n), "ties")
+    w[5] = 1.0  # more equal ones than LDS lists
+    kept, kept_lens = serving.keep(cache, batch, torch.from_numpy(w).cuda(), 4000, 3, 50)
+    got = kept.cpu().numpy()
+    for s in range(0, S, 5):
+        order = np.argsort(-w[s, 0, 3:lens[s] - 50], kind="stable")[:4000 - 53] + 3
+        want = np.concatenate([np.arange(3), np.sort(order), np.arange(lens[s] - 50, lens[s])])
+        assert np.array_equal(got[s, 0], want)
+    assert (kept_lens == 4000).all()
+
+
+def test_keep_on_streams_and_in_graphs(torch):
+    """Long rows' workspaces: two streams at once, and two graphs replayed in turn as weights and lengths change."""
+    from paper_2609_26219_amd import serving
+
+    n = 50000
+    cache, batch = _sequences(torch, (n, n - 9), 2)
+    ws = [torch.rand((2, 2, n), device="cuda") for _ in range(2)]
+    outs = [tuple(torch.empty_like(t) for t in serving.keep(cache, batch, ws[0], 6000, 4, 9)) for _ in ws]
+    want = [serving.keep(cache, batch, w, 6000, 4, 9)[0].clone() for w in ws]
+    streams = [torch.cuda.Stream() for _ in ws]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for w, out, stream in zip(ws, outs, streams):
+            with torch.cuda.stream(stream):
+                serving.keep(cache, batch, w, 6000, 4, 9, out=out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[0], x) for o, x in zip(outs, want))
+    graphs = []
+    for w, out in zip(ws, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            serving.keep(cache, batch, w, 6000, 4, 9, out=out)
+        graphs.append(g)
+    for i in range(4):
+        for w in ws:
+            w.copy_(torch.rand_like(w))
+        batch.keep[1].sub_(11)
+        graphs[i % 2].replay()
+        graphs[1 - i % 2].replay()
+        for w, out in zip(ws, outs):
+            eager = serving.keep(cache, batch, w, 6000, 4, 9)
+            assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1])
+
+
 def test_keep_with_budgets_of_their_own_and_wild_lengths(torch):
     """Budgets and lengths are the device's: below zero, above their bounds, zero."""
     from paper_2609_26219_amd import serving
@@ -187,6 +239,19 @@ def test_evict(torch, tag, dtype, H, D, P, lens, budget, joint, moved):
     for g, x in zip(got, want["kv"] if tag == FP16 else [want["codes"], want["scales"]]):
         assert np.array_equal(g.view(x.dtype), x)
     assert others and np.array_equal(dw.cpu().numpy(), want_w)
+
+
+def test_evict_to_the_same_pages_is_in_place(torch):
+    from paper_2609_26219_amd import serving
+
+    case = Case(49, K4V4, BF16, 2, 1, 64, 16, (3000, 70), (1,))
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    w = np.random.default_rng(0).exponential(1.0, (2, 1, 3000)).astype(np.float32)
+    kept = os_.keep(w, case.lens, [2500, 2500], 4, 4)
+    want, _ = os_.evict(case.cache, K4V4, 16, kept, case.lens, case.table, case.table)
+    serving.evict(cache, batch, _dev(torch, _expect(kept, 2500, 1, 2)), _dev(torch, [2500, 70]), page_table=batch.keep[2])
+    for g, x in zip(_state(torch, cache, case)[0], [want["codes"], want["scales"]]):
+        assert np.array_equal(g.view(x.dtype), x)
 
 
 @pytest.mark.parametrize("paired", [False, True])

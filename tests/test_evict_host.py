@@ -67,7 +67,7 @@ def test_weights_are_not_needed_where_they_are_not_read():
 
 
 @pytest.mark.parametrize("attention", [dict(num_q_heads=6), dict(window=-1), dict(sinks=-1), dict(scale=0.0),
-                                       dict(scale=float("nan")), dict(q=None), dict(q=A + 8), dict(lse=None),
+                                       dict(scale=1e-30), dict(scale=float("nan")), dict(q=None), dict(q=A + 8), dict(lse=None),
                                        dict(lse=A + 2), dict(q_token_stride=3), dict(q_head_stride=64),
                                        dict(workspace=A + 8), dict(workspace_bytes=8)])
 def test_attention_refusals(attention):
@@ -140,6 +140,23 @@ def test_rows_of_a_tile_stay_within_the_sequence(tmp_path):
                     exe], check=True)
     run = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert run.returncode == 0, run.stdout + run.stderr
+
+
+def test_workspace_of_the_choice():
+    """Few long rows are cut into segments, which need one."""
+    m = pb.make_model(_shape())
+    def nbytes(seqs, pages, heads=1):
+        b = pb.PkvBatch(num_seqs=seqs, pages_per_seq=pages)
+        tokens = pages * 16
+        w = pb.PkvWeights(heads=heads, tokens=tokens, head_stride=tokens, seq_stride=heads * tokens)
+        return pb.pkv_cache_keep_workspace(m, b, w, pb.PkvKept(heads=heads, budget=9))
+    assert nbytes(1, 1536) == 0 and nbytes(65, 8192) == 0 and nbytes(0, 8192) == 0
+    assert nbytes(3, 2049, 4) == 12 * 5 * (2048 * 4 + 8192 * 4 + 8) + 12 * 8
+    assert _call("keep", batch=dict(num_seqs=1, pages_per_seq=4096), weights=dict(tokens=65536, head_stride=65536)) == BAD
+
+
+def test_evict_to_the_same_table_of_another_width():
+    assert _call("evict", batch=dict(num_seqs=2), table=(A, 3)) == BAD
 
 
 def test_oracle_weights_are_column_sums():

@@ -81,6 +81,8 @@ FEW = [
     (FP16, BF16, 1, 16, 256, 64, (600,), (1,)),
     (K4V4, BF16, 12, 1, 64, 2, (50, 50), (32,)),
     (K8V8, BF16, 4, 16, 128, 16, (65,), (2,)),
+    (FP16, HALF, 2, 16, 128, 16, (300, 45), (2,)),
+    (FP16, BF16, 2, 16, 64, 4, (70, 45), (2,)),
 ]
 MANY = [
     (K4V4, BF16, 2, 4, 64, 16, (40, 3, 0, 300), (40, 3, 1, 50)),
@@ -123,6 +125,15 @@ def test_weights_without_bounds(torch):
     for new in ((1,), (30,)):
         case = Case(24, K4V4, BF16, 2, 2, 64, 16, (40, 33), new, wide=3)
         _run(torch, case, joint=False, decay=1.0, bounds=False)
+
+
+@pytest.mark.parametrize("tag,dtype,D,group,joint", [(FP16, BF16, 64, 16, False), (K4V4, HALF, 128, 8, True),
+                                                     (K8V4, BF16, 256, 9, False), (FP16, HALF, 128, 7, True)])
+def test_many_rows_in_splits(torch, tag, dtype, D, group, joint):
+    """So many rows that several workgroups share a tile of tokens, whose parts are joined."""
+    case = Case(40 + D, tag, dtype, 1, group, D, 16, (330, 290), (330, 9))
+    _run(torch, case, joint=joint, decay=0.5)
+    _run(torch, case, joint=joint, decay=1.0, window=33, sinks=3, in_place=True)
 
 
 @pytest.mark.parametrize("H,joint", [(1, False), (2, True), (3, False), (5, True)])
@@ -284,7 +295,7 @@ def test_refusals(torch):
     for kw in bad:
         with pytest.raises(ValueError):
             serving.attention_weights(cache, batch, q, **{**dict(lse=lse, out=out), **kw})
-    for kw in (dict(out=out[..., :19]), dict(out=out.cpu()), dict(decay=float("nan"), weights=out), dict(scale=0.0),
+    for kw in (dict(out=out[..., :19]), dict(out=out.cpu()), dict(decay=float("nan"), weights=out), dict(scale=0.0), dict(scale=1e-30),
                dict(window=-1), dict(sinks=-1), dict(layer=1)):
         with pytest.raises(pb.PkvError):
             serving.attention_weights(cache, batch, q, **{**dict(lse=lse, out=out), **kw})
