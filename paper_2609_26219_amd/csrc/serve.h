@@ -210,11 +210,12 @@ constexpr int32_t kept_budget(const KeepArgs& a, int32_t n, int32_t budget) {
 
 // Of few rows (up to few_tiles row tiles of 16 a sequence and KV head; 32 sequences of 8192 tokens, 8 heads of 128, 32 rows, as few |
 // as many: 60 | 82 us in 4 bits, 104 | 153 in 16; 4 rows 42 | 99 and 101 | 169): tokens of a wave at a time; sequences whose tokens
-// are shared evenly (every workgroup adds up their lengths) and by how many workgroups.  32 ragged sequences of 255 thousand tokens in
-// 4 bits: even shares 53 us, chunks of 128, 256 and 512 tokens 65, 60 and 68.
+// are shared evenly (every workgroup adds up their lengths) and by how many workgroups, three to a compute unit.  32 ragged sequences of
+// 255 thousand tokens in 4 bits: 768 shares 54.6 us, 1024 57.1, 1536 55.2; chunks of 128, 256 and 512 tokens 65, 60 and 68.
+constexpr int kFewWaves = 4;
 constexpr int kMostChunk = 512;
 constexpr int kMostShared = 512;
-constexpr int kShares = 512;
+constexpr int kShares = 768;
 // Of many rows: tokens of a workgroup, rows of a tile, and its bytes (queries, and 5 numbers a row and 8 of all).
 constexpr int weigh_tokens(int head_dim) { return head_dim > 128 ? 128 : 256; }
 constexpr int kWeighRows = 32;

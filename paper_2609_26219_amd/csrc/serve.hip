@@ -14,6 +14,12 @@
 // take 106 us, 4.9 TB/s (a plain copy of 512 MiB: 5.2).  Appending is bound by the vector
 // units, which are busy 79% of the time with ranges, roundings and packing: 87541
 // rows of 8 heads into 4 bits take 126 us, 3.6 TB/s.
+//
+// Rows turned to their positions (pkv_rotate, pkv_cache_append_rotated) are dealt alike.  A token's cosines and sines
+// are worked out once for all its heads, in double precision like the products, so that a key is what the restore's
+// re-phasing would give and lands on the same code: 32 registers of a thread for its piece, and less than a third of the vector
+// units' time.  32999 rows of 32 heads of 128 take 113 us, 4.8 TB/s; 8192 rows of 32 query and 8 key and value heads, into 8 and 4
+// bits, 44 us, 4.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

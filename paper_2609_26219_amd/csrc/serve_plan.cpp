@@ -286,8 +286,8 @@ pkv_status_t weigh_args(const ServeArgs& s, const pkv_attention_t* a, const pkv_
     const int64_t rows = int64_t(s.max_tokens) * r.group;
     if (rows <= kRowTile * few_tiles(s.D)) {
       l.few_tiles = rows <= kRowTile ? 1 : 2;
-      // A workgroup's 8 waves take a KV head each, or parts of the tokens where there are fewer.
-      while (l.subs < 8 && l.subs * 2 * s.H <= 8) l.subs *= 2;
+      // A workgroup's waves take a KV head each, or parts of the tokens where there are fewer.
+      while (l.subs < kFewWaves && l.subs * 2 * s.H <= kFewWaves) l.subs *= 2;
       if (r.window == 0 && s.num_seqs <= kMostShared) {
         l.groups = std::max<int64_t>(1, std::min<int64_t>(kShares, (int64_t(s.num_seqs) * s.max_kv - 1) / (kTokenTile * l.subs) + 1));
       } else {

@@ -10,6 +10,14 @@
 //
 // Codes go in as attention takes them (integers around mid-code, exact in binary16), a token's scale and zero
 // act on its lane: q . k_t = s_t (q . codes_t) + z'_t sum(q).
+//
+// Few rows wait for the cache's bytes, in 16 bits for nothing else (32 sequences of 8192 tokens, 8 heads of 128, 537 MB: 101 us,
+// 5.3 TB/s, where a large copy reaches 5.3); over codes the vector units decode them as well (32 ragged sequences of 255 thousand
+// tokens in 4 bits, 142 MB: 53 to 55 us, 2.6 TB/s, vector units busy 58% of the time that a compute unit has work).  Many rows share
+// their time between the matrix units and the exponentials: 8192 rows of 32 heads over 8192 tokens of 16 bits take 29 us to
+// prepare and 335 to 345 to weigh (275 GFLOP that the mask leaves, 810 TFLOP/s; a large library product reaches 1218), vector units
+// busy 62% and matrix units 46% of that time.  A wave's own instructions of both kinds, taken in turn, run one behind the other
+// (430 us with three waves a SIMD); through LDS with a barrier for each tile of rows 502.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -115,8 +123,6 @@ __device__ __forceinline__ u32x4 query_operand(const float (&v)[8], float down) 
 // on.  Where heads are joined, the waves' sums of a token meet in LDS.  All sequences' tokens are cut into even shares, one to a
 // workgroup, so that the GPU is done at once whatever their lengths; with a window, of whose tokens most are not looked at, into
 // chunks.
-
-constexpr int kFewWaves = 8;
 
 // Tokens [begin, end) of one sequence (end at most kv_len), by the whole workgroup.
 template <bool BF16, int KB, bool WHOLE, int RT>
@@ -360,7 +366,7 @@ __device__ __forceinline__ int64_t wave_sums(int64_t v, int lane) {
 }
 
 template <bool BF16, int KB, bool WHOLE, int RT>
-__global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ? 4 : 2) void few_kernel(ServeArgs s, WeighArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, WHOLE && RT == 1 && KB * D <= 512 ? 3 : 2) void few_kernel(ServeArgs s, WeighArgs a) {
   __shared__ float sums[kFewWaves][kMostChunk];
   const int lane = threadIdx.x & 63;
   int32_t seq = 0, tile = 0, left = 0;  // the workgroup's first sequence, its first tile there, and its tiles
