@@ -13,11 +13,11 @@
 //
 // Few rows wait for the cache's bytes, in 16 bits for nothing else (32 sequences of 8192 tokens, 8 heads of 128, 537 MB: 101 us,
 // 5.3 TB/s, where a large copy reaches 5.3); over codes the vector units decode them as well (32 ragged sequences of 255 thousand
-// tokens in 4 bits, 142 MB: 53 to 55 us, 2.6 TB/s, vector units busy 58% of the time that a compute unit has work).  Many rows share
+// tokens in 4 bits, 141 MB: 53 to 55 us, 2.6 TB/s, vector units busy 42% of the launch).  Many rows share
 // their time between the matrix units and the exponentials: 8192 rows of 32 heads over 8192 tokens of 16 bits take 29 us to
 // prepare and 335 to 345 to weigh (275 GFLOP that the mask leaves, 810 TFLOP/s; a large library product reaches 1218), vector units
-// busy 62% and matrix units 46% of that time.  A wave's own instructions of both kinds, taken in turn, run one behind the other
-// (430 us with three waves a SIMD); through LDS with a barrier for each tile of rows 502.
+// busy 51% and matrix units 37% of it, of which the last workgroups' end is a fifth.  A wave's own instructions of both kinds,
+// taken in turn, run one behind the other (430 us with three waves a SIMD); through LDS with a barrier for each tile of rows 502.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
