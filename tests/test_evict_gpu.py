@@ -421,3 +421,45 @@ def test_refusals(torch):
             serving.evict(cache, batch, kept, kept_lens, **kw)
     with pytest.raises(pb.PkvError):
         serving.evict(cache, batch, kept.cpu(), kept_lens)
+
+
+@pytest.mark.parametrize("tag", [FP16, K8V8])
+def test_offsets_past_32_bits(torch, tag):
+    """A cache whose used pages lie past 4 GiB from its start: rows turned and appended, weighed and moved there are those of a
+    small cache."""
+    from paper_2609_26219_amd import serving
+
+    H, D, P, n = 8, 256, 64, 300
+    need, pool = 5, 20000 if tag == FP16 else 9000
+    made = []
+    for pages in (need + 5, pool):
+        kw = dict(num_kv_heads=H, head_dim=D, page_size=P, dtype=torch.bfloat16, tag=tag)
+        if tag == FP16:
+            cache = serving.PagedCache(k_cache=torch.zeros((pages, P, H, D), dtype=torch.bfloat16, device="cuda"),
+                                       v_cache=torch.zeros((pages, P, H, D), dtype=torch.bfloat16, device="cuda"), **kw)
+        else:
+            cache = serving.PagedCache(pool_pages=pages, **kw)
+        table = torch.arange(pages - need, pages, dtype=torch.int32, device="cuda").flip(0).contiguous()[None]
+        other = torch.arange(pages - need - 5, pages - need, dtype=torch.int32, device="cuda")[None].contiguous()
+        made.append((cache, table, other))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn((n, h, D), generator=gen, device="cuda").bfloat16() for h in (2 * H, H, H))
+    got = []
+    for cache, table, other in made:
+        batch = serving.Batch(_dev(torch, [0, n]), _dev(torch, [n]), table, n, max_kv_len=n)
+        turned = serving.append_rotated(cache, batch, q, k, v)
+        last = serving.Batch(_dev(torch, [0, 1]), _dev(torch, [n]), table, 1, max_tokens=1, max_kv_len=n)
+        w = torch.zeros((1, H, n), device="cuda")
+        for b, rows in ((batch, turned), (last, turned[-1:])):
+            _, lse = serving.attention(cache, b, rows, return_lse=True)
+            serving.attention_weights(cache, b, rows, lse, w, w)
+        kept = serving.keep(cache, last, w, 100, 2, 9)
+        serving.evict(cache, last, *kept, page_table=other)
+        moved = serving.read(cache, serving.Batch(_dev(torch, [0, 100]), _dev(torch, [100]), other, 100))
+        weights = w.clone()
+        serving.evict(cache, last, *kept, w)
+        here = serving.read(cache, serving.Batch(_dev(torch, [0, 100]), _dev(torch, [100]), table, 100))
+        got.append((turned, weights, *kept, w, *moved, *here))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    small = got[0]
+    assert torch.equal(small[5], small[7]) and torch.equal(small[6], small[8]) and small[5].float().abs().sum() > 0
