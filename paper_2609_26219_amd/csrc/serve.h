@@ -192,8 +192,10 @@ struct EvictArgs {
   int32_t piece_bytes, log2_lanes;               // a lane's part of a row, and the lanes of a slice
 };
 
-constexpr int kMoveThreads = 256;    // of a workgroup that moves rows to other pages,
-constexpr int kChainThreads = 1024;  // and in place
+// Threads of a workgroup that moves rows to other pages, and in place (32 ragged sequences cut to 2048 tokens of 4 bits: 1024
+// threads 39 us, 512 45, 256 57).
+constexpr int kMoveThreads = 256;
+constexpr int kChainThreads = 1024;
 constexpr int kRowsAhead = 8;        // rows of a thread on their way at once
 // Rows of a workgroup on their way at once, whose slices are so many lanes wide (narrow ones fewer than that, for their
 // places are in LDS).
