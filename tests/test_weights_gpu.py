@@ -299,3 +299,61 @@ def test_refusals(torch):
                dict(window=-1), dict(sinks=-1), dict(layer=1)):
         with pytest.raises(pb.PkvError):
             serving.attention_weights(cache, batch, q, **{**dict(lse=lse, out=out), **kw})
+
+
+INFINITE = [
+    # dtype, H, group, D, P, lens, new: rows of a KV head that are part of a tile, a tile and part of one, two; many
+    (BF16, 2, 4, 128, 16, (75,), (1,)),
+    (HALF, 2, 5, 64, 16, (75, 40), (1,)),
+    (BF16, 1, 3, 256, 1, (75,), (1,)),
+    (HALF, 1, 1, 128, 32, (600,), (1,)),
+    (BF16, 2, 6, 64, 8, (75,), (3,)),
+    (HALF, 3, 8, 128, 16, (100,), (4,)),
+    (BF16, 1, 3, 128, 16, (300,), (40,)),
+    (HALF, 2, 4, 64, 4, (300, 290), (40, 37)),
+    (BF16, 1, 2, 256, 16, (200,), (50,)),
+]
+
+
+@pytest.mark.parametrize("dtype,H,group,D,P,lens,new", INFINITE)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (30, 4)])
+@pytest.mark.parametrize("value", [-np.inf, np.inf])
+@pytest.mark.parametrize("mixed", [False, True])
+def test_an_infinite_key_weighs_what_its_scores_say(torch, dtype, H, group, D, P, lens, new, window, sinks, value, mixed):
+    """A channel of some keys is infinite, so every score there is too: -inf adds nothing, +inf makes the weight infinite,
+    wherever the token lies in its tile and however many rows there are.  Other tokens' weights keep their bits."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(36 + D, FP16, dtype, H, group, D, P, lens, new)
+    rng = np.random.default_rng(D + H)
+    channel, sign = 13, 0x8000
+    if not mixed:
+        case.q[:, :, channel] &= 0x7FFF
+    case.q[:, :, channel] |= 0x2000  # (not zero, and of 2 and more so large that finite keys' scores overflow as well)
+    lse = rng.normal(4.0, 1.0, (case.tokens, H * group)).astype(np.float32)
+    before = rng.exponential(1.0, (len(lens), H, max(lens))).astype(np.float32)
+    q, dlse, dbefore = _up(torch, case.q, case), torch.from_numpy(lse).cuda(), torch.from_numpy(before).cuda()
+    batch = _batch(torch, case)
+
+    def weigh():
+        return serving.attention_weights(_cache(torch, case), batch, q, dlse, torch.full_like(dbefore, 77.0), dbefore, decay=0.75,
+                                         window=window, sinks=sinks).cpu().numpy()
+
+    finite = weigh()
+    bad = np.zeros((len(lens), max(lens)), bool)
+    infinite = {HALF: 0x7C00, BF16: 0x7F80}[dtype] | (sign if value < 0 else 0)
+    for s, n in enumerate(lens):
+        for t in (1, 17, n // 2, n - 33, n - 2, n - 1):
+            bad[s, t] = True
+            case.cache["kv"][0][case.table[s, t // P], t % P, :, channel] = infinite
+    got = weigh()
+    with np.errstate(all="ignore"):
+        want, _, _ = os_.weigh(case.cache, FP16, P, dtype, case.where(), case.lens, case.table, case.pool, case.q, lse, H,
+                               D ** -0.5, window, sinks)
+        want = (want + 0.75 * before).astype(np.float32)
+    for s in range(len(lens)):
+        assert np.array_equal(got[s][:, bad[s]], want[s][:, bad[s]])
+        assert np.array_equal(got[s][:, ~bad[s]], finite[s][:, ~bad[s]])
+    assert not np.isnan(got).any()
+    reached = np.concatenate([want[s][:, bad[s]].ravel() for s in range(len(lens))])
+    assert mixed or np.isinf(reached).any() == (value > 0)
