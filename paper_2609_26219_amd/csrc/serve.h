@@ -223,7 +223,7 @@ constexpr int weigh_tokens(int head_dim) { return head_dim > 128 ? 128 : 256; }
 constexpr int kWeighRows = 32;
 constexpr int weigh_tile_bytes(int head_dim) { return kWeighRows * (2 * head_dim + 20) + 32; }
 
-// A launch has fewer than 2^32 threads, in workgroups of 256.
+// A launch has fewer than 2^32 threads: so many workgroups of 256, a quarter of them of 1024.
 constexpr int64_t kMostGroups = int64_t(1) << 24;
 
 constexpr int kRowTile = 16;   // rows (token, query head of one KV head) of a matrix instruction

@@ -443,7 +443,8 @@ pkv_status_t evict_args(const ServeArgs& s, const pkv_kept_t* k, const pkv_weigh
   e.splits = 1;
   if (e.table) e.splits = int32_t(std::max<int64_t>(1, (std::min<int64_t>(e.budget, s.max_kv) + chunk - 1) / chunk));
   const int64_t units = e.weight_units + int64_t(s.H) * 2 * e.slices * e.splits;
-  if (units * std::max(1, s.num_seqs) >= kMostGroups) return PKV_ERR_INVALID_ARGUMENT;
+  if (units * std::max(1, s.num_seqs) >= (e.table ? kMostGroups : kMostGroups / (kChainThreads / 256)))
+    return PKV_ERR_INVALID_ARGUMENT;
   e.units = int32_t(units);
   *out = e;
   return PKV_OK;

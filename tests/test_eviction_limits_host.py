@@ -1,0 +1,47 @@
+"""What the eviction calls refuse and what they do not, on the host: each refusal beside the same call that passes every check
+(without a GPU it ends at the device).  Every array has an address of its own."""
+import pytest
+
+from paper_2609_26219_amd import binding as pb
+from test_serving_host import A, BAD, OK, _gpu_present, _shape
+
+PASSES = pb.PKV_ERR_DEVICE
+
+pytestmark = pytest.mark.skipif(_gpu_present(), reason="with a GPU these addresses are no device memory")
+
+
+def _evict(num_seqs, shape, heads, budget, table=None, pages=4, tag=3, **kept):
+    m = pb.make_model(shape)
+    if tag:
+        cb, sb = pb.pkv_cache_size(shape, tag)
+        c = pb.PkvPagedCache(tag=tag, codes=A, code_bytes=cb, scales=2 * A, scale_bytes=sb)
+    else:
+        nbytes = 2 * shape.num_layers * shape.pool_pages * shape.page_size * shape.num_kv_heads * shape.head_dim
+        c = pb.PkvPagedCache(tag=0, k_cache=A << 10, v_cache=A << 11, cache_bytes=nbytes)
+    b = pb.PkvBatch(num_seqs, 0, 0, pages, 0, 3 * A, 4 * A, None, 5 * A)
+    tokens = pages * shape.page_size
+    w = pb.PkvWeights(heads, 1.0, tokens, tokens, heads * tokens, 6 * A, 6 * A)
+    k = pb.PkvKept(**{**dict(heads=heads, budget=budget, kept=7 * A, kept_lens=8 * A), **kept})
+    return pb.pkv_cache_evict_status(m, c, b, k, w, table, pages)
+
+
+def test_launches_in_place_have_workgroups_of_1024_threads():
+    """4 heads are 12 workgroups a sequence (weights, keys, values): below 2^22 in place and 2^24 to other pages."""
+    most = ((1 << 22) - 1) // 12
+    assert _evict(most, _shape(), 4, 9) == PASSES
+    assert _evict(most + 1, _shape(), 4, 9) == BAD
+    assert _evict(most + 1, _shape(), 4, 9, table=9 * A) == PASSES
+    assert _evict(1 << 20, _shape(), 4, 9, table=9 * A) == BAD
+
+
+@pytest.mark.parametrize("heads,dim", [(1, 32), (1, 16), (4, 128), (2, 256), (3, 48), (1, 512)])
+@pytest.mark.parametrize("tag", range(4))
+@pytest.mark.parametrize("budget", [0, 1, 100, 5000])
+@pytest.mark.parametrize("table", [None, 9 * A])
+def test_the_stated_bound_suffices(heads, dim, tag, budget, table):
+    """num_seqs * num_kv_heads * ceil(head_dim / 32) * (3 + budget / 128) < 2^22."""
+    shape = _shape(num_kv_heads=heads, head_dim=dim)
+    per = heads * -(-dim // 32) * (3 * 128 + budget)
+    seqs = ((1 << 22) * 128 - 1) // per
+    assert seqs * per < (1 << 22) * 128
+    assert _evict(seqs, shape, heads, budget, table, pages=512, tag=tag) == PASSES
