@@ -480,7 +480,7 @@ pkv_status_t pkv_cache_read(const pkv_model_t* model, const pkv_paged_cache_t* c
  *     (elements; alignment as in pkv_cache_append); out may be x itself with
  *     the same strides, else must not overlap an input. */
 typedef struct {
-  int32_t num_heads;              /* >= 0; 0: x and out are not looked at */
+  int32_t num_heads;              /* 0 to 2^30, times num_tokens < 2^31; 0: x and out are not looked at */
   float amplitude;                /* finite; 1 but for scaled long contexts */
   const int32_t* position_offset; /* device [num_seqs], or NULL = 0 */
   const void* x;

@@ -111,7 +111,8 @@ pkv_status_t rotate_args(const pkv_model_t& m, const ServeArgs& s, const pkv_rot
   if (!rotation) return PKV_ERR_INVALID_ARGUMENT;
   const pkv_rotation_t& r = *rotation;
   if (r.num_heads < 0 || !isfinite(r.amplitude) || !aligned(r.position_offset, 4)) return PKV_ERR_INVALID_ARGUMENT;
-  if (int64_t(s.num_tokens) * r.num_heads >= (int64_t(1) << 31)) return PKV_ERR_INVALID_ARGUMENT;
+  // (A workgroup counts a token's heads past the last by up to 2 * 128.)
+  if (r.num_heads > (1 << 30) || int64_t(s.num_tokens) * r.num_heads >= (int64_t(1) << 31)) return PKV_ERR_INVALID_ARGUMENT;
   if (r.num_heads > 0) {
     if (!stride_ok(r.x_token_stride, r.x_head_stride, s.D) || !stride_ok(r.out_token_stride, r.out_head_stride, s.D))
       return PKV_ERR_INVALID_ARGUMENT;

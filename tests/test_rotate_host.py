@@ -11,7 +11,7 @@ import pytest
 
 from paper_2609_26219_amd import binding as pb
 from paper_2609_26219_amd import build as pkv_build
-from test_serving_host import A, BAD, OK, TAG, _shape
+from test_serving_host import A, BAD, OK, TAG, _gpu_present, _shape
 
 
 def _call(which="rotate", shape=None, batch=None, rotation=None, rows=None, cache=None):
@@ -110,3 +110,12 @@ def test_sine_and_cosine(tmp_path):
         want = np.longdouble(a)
         assert abs(np.longdouble(s.value) - np.sin(want)) <= 2.0 ** -52 and \
             abs(np.longdouble(c.value) - np.cos(want)) <= 2.0 ** -52, a
+
+
+@BOTH
+def test_heads_that_a_workgroup_can_count(which):
+    """A workgroup goes over a token's heads in steps, whose count stays within 32 bits up to 2^30 heads."""
+    for heads in ((1 << 30) + 1, (1 << 31) - 1):
+        assert _call(which, batch=dict(num_tokens=1), rotation=dict(num_heads=heads)) == BAD
+    if not _gpu_present():  # (past every check, and no device)
+        assert _call(which, batch=dict(num_tokens=1), rotation=dict(num_heads=1 << 30)) == pb.PKV_ERR_DEVICE
