@@ -250,6 +250,7 @@ pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache
                         bool pointers, ServeArgs* out);
 pkv_status_t row_args(const ServeArgs& s, const void* k, const void* v, int64_t token_stride, int64_t head_stride,
                       RowArgs* out);
+// (serve_args' part of the batch, without its page_table.)
 pkv_status_t batch_args(const pkv_model_t* model, const pkv_batch_t* batch, bool pointers, ServeArgs* out);
 pkv_status_t rotate_args(const pkv_model_t& m, const ServeArgs& s, const pkv_rotation_t* rotation, RotateArgs* out);
 pkv_status_t attend_args(const ServeArgs& s, const pkv_attention_t* a, bool pointers, AttendArgs* out);

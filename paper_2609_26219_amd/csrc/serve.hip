@@ -716,6 +716,7 @@ pkv_status_t pkv_rotate(const pkv_model_t* model, const pkv_batch_t* batch, cons
   pkv_status_t st = pkv::batch_args(model, batch, true, &s);
   if (st == PKV_OK) st = pkv::rotate_args(*model, s, rotation, &t);
   if (st != PKV_OK || s.num_seqs == 0 || s.num_tokens == 0 || t.heads == 0) return st;
+  s.page_table = nullptr;  // (not read)
   const pkv::OnDevice here;
   if (!here.ok) return PKV_ERR_DEVICE;
   if (!here.has(s) || !pkv::rotation_here(here, t)) return PKV_ERR_INVALID_ARGUMENT;

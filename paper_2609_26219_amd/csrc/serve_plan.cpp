@@ -56,9 +56,8 @@ pkv_status_t batch_args(const pkv_model_t* model, const pkv_batch_t* batch, bool
   s.D = m.head_dim;
   s.bf16 = m.out_dtype == PKV_OUT_BF16;
   if (pointers && s.num_seqs > 0 && s.num_tokens > 0) {
-    if (!b.token_start || !b.kv_lens || !b.page_table) return PKV_ERR_INVALID_ARGUMENT;
-    if (!aligned(b.token_start, 4) || !aligned(b.kv_lens, 4) || !aligned(b.page_table, 4) || !aligned(b.positions, 4))
-      return PKV_ERR_INVALID_ARGUMENT;
+    if (!b.token_start || !b.kv_lens) return PKV_ERR_INVALID_ARGUMENT;
+    if (!aligned(b.token_start, 4) || !aligned(b.kv_lens, 4) || !aligned(b.positions, 4)) return PKV_ERR_INVALID_ARGUMENT;
   }
   *out = s;
   return PKV_OK;
@@ -85,6 +84,7 @@ pkv_status_t serve_args(const pkv_model_t* model, const pkv_paged_cache_t* cache
     s.v_offset = int64_t(m.page_size) * s.D * kKeyBits[s.tag] / 8;
   }
   if (pointers) {
+    if (s.num_seqs > 0 && s.num_tokens > 0 && (!s.page_table || !aligned(s.page_table, 4))) return PKV_ERR_INVALID_ARGUMENT;
     if (s.tag == PKV_TAG_FP16) {
       if (!cache->k_cache || !cache->v_cache || cache->cache_bytes < cache_bytes(m)) return PKV_ERR_INVALID_ARGUMENT;
       ByteRange ranges[2];

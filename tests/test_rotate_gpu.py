@@ -251,3 +251,16 @@ def test_refusals(torch):
                dict(rope_amplitude=float("nan")), dict(inv_freq=[float("inf")] * 32)):
         with pytest.raises(ValueError):
             serving.PagedCache(2, 64, 16, torch.bfloat16, K4V4, pool_pages=4, **kw)
+
+
+def test_rotate_without_a_page_table(torch):
+    from paper_2609_26219_amd import serving
+
+    case = Case(77, K4V4, BF16, 2, 3, 64, 16, (20, 9), (4, 2))
+    cache, batch, q = _cache(torch, case), _batch(torch, case), _up(torch, case.q, case)
+    want, out = serving.rotate(cache, batch, q), torch.empty_like(q)
+    b = pb.PkvBatch.from_buffer_copy(batch.struct)
+    b.page_table = None
+    r = pb.PkvRotation(6, 1.0, None, q.data_ptr(), 6 * 64, 64, out.data_ptr(), 6 * 64, 64)
+    assert pb.pkv_rotate_status(cache.model, b, r, torch.cuda.current_stream().cuda_stream) == pb.PKV_OK
+    assert torch.equal(out, want)

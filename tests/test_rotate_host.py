@@ -119,3 +119,11 @@ def test_heads_that_a_workgroup_can_count(which):
         assert _call(which, batch=dict(num_tokens=1), rotation=dict(num_heads=heads)) == BAD
     if not _gpu_present():  # (past every check, and no device)
         assert _call(which, batch=dict(num_tokens=1), rotation=dict(num_heads=1 << 30)) == pb.PKV_ERR_DEVICE
+
+
+@pytest.mark.skipif(_gpu_present(), reason="with a GPU these addresses are no device memory")
+def test_the_page_table_of_a_rotation_is_not_read():
+    for table in (None, A + 2):
+        assert _call(batch=dict(num_tokens=3, page_table=table)) == pb.PKV_ERR_DEVICE  # (past every check, and no device)
+        assert _call("append", batch=dict(num_tokens=3, page_table=table)) == BAD
+    assert _call("append", batch=dict(num_tokens=3)) == pb.PKV_ERR_DEVICE
