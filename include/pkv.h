@@ -597,7 +597,7 @@ typedef struct {
   int32_t recent;           /* >= 0: the last tokens, which stay where the budget has room beside the sinks */
   const int32_t* budgets;   /* device [num_seqs], each sequence's own (at most budget), or NULL */
   int32_t* kept;            /* device [num_seqs][heads][budget] */
-  int32_t* kept_lens;       /* device [num_seqs] */
+  int32_t* kept_lens;       /* device [num_seqs]; pkv_cache_keep: not the batch's kv_lens, nor budgets */
   void* workspace;          /* pkv_cache_keep only: device memory of pkv_cache_keep_workspace's bytes (0: may be NULL),
                              * 16-byte aligned, contents of no matter; calls that may overlap need one each */
   uint64_t workspace_bytes;

@@ -369,6 +369,14 @@ pkv_status_t keep_args(const ServeArgs& s, const pkv_weights_t* w, const pkv_kep
   const pkv_status_t st = kept_ok(s, k, w, pointers);
   if (st != PKV_OK) return st;
   if (pointers && (!aligned(w->weights, 4) || (s.num_seqs > 0 && !w->weights))) return PKV_ERR_INVALID_ARGUMENT;
+  // Workgroups read lengths and budgets while others write kept_lens.
+  auto apart = [&](const int32_t* p, const int32_t* q) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+    return (x < y ? y - x : x - y) >= uintptr_t(s.num_seqs) * 4;
+  };
+  if (pointers && s.num_seqs > 0 &&
+      (!apart(k->kept_lens, s.kv_lens) || (k->budgets && !apart(k->kept_lens, k->budgets))))
+    return PKV_ERR_INVALID_ARGUMENT;
   KeepArgs a{};
   a.weights = w->weights;
   a.budgets = k->budgets;

@@ -364,7 +364,7 @@ def keep(cache: PagedCache, batch: Batch, weights, budget: int, sinks: int = 0, 
     between the ones of the largest ``weights`` (float32 ``[S, 1, tokens]``: one choice for all heads, or
     ``[S, H, tokens]``: each head its own), equal ones lowest index first.  ``budgets``, int32 ``[S]``, sets a sequence's
     own, up to ``budget``.  Returns ``(kept, kept_lens)``, int32 ``[S, 1 or H, budget]``, ascending and then -1, and
-    ``[S]`` (``out`` if given)."""
+    ``[S]`` (``out`` if given, which is neither the batch's lengths nor ``budgets``)."""
     w = _weights(cache, batch, weights, weights)
     if out is None:
         out = (torch.empty((batch.struct.num_seqs, w.heads, max(0, budget)), dtype=torch.int32, device=cache.device),

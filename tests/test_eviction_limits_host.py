@@ -45,3 +45,27 @@ def test_the_stated_bound_suffices(heads, dim, tag, budget, table):
     seqs = ((1 << 22) * 128 - 1) // per
     assert seqs * per < (1 << 22) * 128
     assert _evict(seqs, shape, heads, budget, table, pages=512, tag=tag) == PASSES
+
+
+def _keep(num_seqs=5, workspace=False, **kw):
+    m = pb.make_model(_shape())
+    at = {**dict(kv_lens=4 * A, budgets=9 * A, kept_lens=8 * A), **kw}
+    b = pb.PkvBatch(num_seqs, 0, 0, 1 << 14 if workspace else 4, 0, 3 * A, at["kv_lens"], None, None)
+    tokens = 16 << 14 if workspace else 64
+    w = pb.PkvWeights(4, 1.0, tokens, tokens, 4 * tokens, 6 * A, None)
+    k = pb.PkvKept(4, 16, 2, 3, at["budgets"], 7 * A, at["kept_lens"], 10 * A, 1 << 40)
+    return pb.pkv_cache_keep_status(m, b, w, k)
+
+
+@pytest.mark.parametrize("workspace", [False, True])
+def test_the_choice_writes_none_of_what_it_reads(workspace):
+    """Workgroups read lengths and budgets while others write kept_lens, so these lie apart."""
+    assert _keep(workspace=workspace) == PASSES
+    assert _keep(workspace=workspace, budgets=None) == PASSES
+    for off in (0, 4, -4, 16, -16):
+        assert _keep(workspace=workspace, kept_lens=4 * A + off) == BAD
+        assert _keep(workspace=workspace, kept_lens=9 * A + off) == BAD
+    for off in (20, -20):
+        assert _keep(workspace=workspace, kept_lens=4 * A + off) == PASSES
+        assert _keep(workspace=workspace, kept_lens=9 * A + off) == PASSES
+    assert _keep(0, kept_lens=4 * A) == OK
