@@ -625,11 +625,12 @@ pkv_status_t pkv_cache_keep(const pkv_model_t* model, const pkv_batch_t* batch, 
  *     theirs);
  *   weights    : NULL, or weights->out (kept->heads heads) is moved alike, in place, and
  *     0 from kept_lens[s] to kv_lens[s].
- * Indices outside [0, kv_lens) and rows whose page is not there, before or after, are
- * left out; every other byte stays.  The lengths after it are kept_lens: kv_lens is
- * only read, so that each layer finds it.  The launch has fewer than 2^24 workgroups,
- * in place fewer than 2^22: num_seqs * num_kv_heads * ceil(head_dim / 32) * (3 + budget / 128) <
- * 2^22 always suffices.  One kernel on `hip_stream`.  Errors as pkv_cache_append. */
+ * Indices outside [0, kv_lens) are left out (row and weight j stay what they were), and
+ * so are rows whose page is not there, before or after (their weights move); every other
+ * byte stays.  The lengths after it are kept_lens: kv_lens is only read, so that each layer
+ * finds it.  The launch has fewer than 2^24 workgroups, in place fewer than 2^22: num_seqs *
+ * num_kv_heads * ceil(head_dim / 32) * (3 + budget / 128) < 2^22 always suffices.  One kernel
+ * on `hip_stream`.  Errors as pkv_cache_append. */
 pkv_status_t pkv_cache_evict(const pkv_model_t* model, const pkv_paged_cache_t* cache, const pkv_batch_t* batch,
                              const pkv_kept_t* kept, const pkv_weights_t* weights, const int32_t* page_table,
                              int32_t table_pages, void* hip_stream);

@@ -500,15 +500,14 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 4) void evict_kernel(S
       for (int i = 0; i < kRowsAhead; ++i) {
         const int32_t j = c0 + i * THREADS + tid;
         from[i] = j < m ? kept[j] : -1;
+        if (from[i] >= n) from[i] = -1;
       }
 #pragma unroll
-      for (int i = 0; i < kRowsAhead; ++i) v[i] = from[i] >= 0 && from[i] < n ? w[from[i]] : 0.0f;
+      for (int i = 0; i < kRowsAhead; ++i) v[i] = from[i] >= 0 ? w[from[i]] : 0.0f;
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kRowsAhead; ++i) {
-        const int32_t j = c0 + i * THREADS + tid;
-        if (j < m) w[j] = v[i];
-      }
+      for (int i = 0; i < kRowsAhead; ++i)
+        if (from[i] >= 0) w[c0 + i * THREADS + tid] = v[i];
     }
     __syncthreads();
     for (int64_t j = m + tid; j < n; j += THREADS) w[j] = 0.0f;

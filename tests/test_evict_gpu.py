@@ -463,3 +463,31 @@ def test_offsets_past_32_bits(torch, tag):
     assert all(torch.equal(a, b) for a, b in zip(*got))
     small = got[0]
     assert torch.equal(small[5], small[7]) and torch.equal(small[6], small[8]) and small[5].float().abs().sum() > 0
+
+
+@pytest.mark.parametrize("heads", [1, 2])
+@pytest.mark.parametrize("moved", [False, True])
+def test_weights_at_indices_outside_are_left_out(torch, heads, moved):
+    """As the rows there: the weight at such a place stays what it was.  A row whose page is not there moves its weight all
+    the same."""
+    from paper_2609_26219_amd import serving
+
+    case = Case(54, K4V4, BF16, 2, 1, 64, 4, (20, 9000), (1,), spare_pages=8)
+    case.table[0, 7 // 4] = -1
+    cache, batch = _cache(torch, case), _batch(torch, case)
+    w = np.random.default_rng(2).exponential(1.0, (2, heads, 9000)).astype(np.float32)
+    kept = np.full((2, heads, 8500), -1, np.int32)
+    kept[0, :, :6] = [3, 20, 7, -5, 9, 2 ** 31 - 1]
+    kept[1] = np.arange(500, 9000)
+    kept[1, :, [17, 8192, 8499]] = [[9000], [-1], [-2 ** 31]]
+    want = w.copy()
+    want[0, :, [0, 2, 4]] = w[0, :, [3, 7, 9]]
+    want[0, :, 6:20] = 0.0
+    stay = np.isin(np.arange(8500), [17, 8192, 8499])
+    want[1, :, :8500] = np.where(stay, w[1, :, :8500], w[1, :, 500:])
+    want[1, :, 8500:] = 0.0
+    free = [p for p in range(case.pool) if p not in set(case.table[case.table >= 0])]
+    to = _dev(torch, np.array(free[:2], np.int32).reshape(2, 1)) if moved else None
+    dw = torch.from_numpy(w).cuda()
+    serving.evict(cache, batch, _dev(torch, kept), _dev(torch, [6, 8500]), dw, to)
+    assert np.array_equal(dw.cpu().numpy(), want)
