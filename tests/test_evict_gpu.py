@@ -491,3 +491,35 @@ def test_weights_at_indices_outside_are_left_out(torch, heads, moved):
     dw = torch.from_numpy(w).cuda()
     serving.evict(cache, batch, _dev(torch, kept), _dev(torch, [6, 8500]), dw, to)
     assert np.array_equal(dw.cpu().numpy(), want)
+
+
+def test_codes_past_4_gib(torch):
+    """Codes whose pages lie past 4 GiB from the cache's start: rows turned and appended, weighed and moved there (in place
+    and to other pages) are those of a small cache."""
+    from paper_2609_26219_amd import serving
+
+    H, D, P, n, need, pool = 8, 256, 64, 300, 5, 20000
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn((n, h, D), generator=gen, device="cuda").bfloat16() for h in (2 * H, H, H))
+    got = []
+    for pages in (2 * need, pool):
+        cache = serving.PagedCache(H, D, P, torch.bfloat16, K8V8, pool_pages=pages)
+        used = pages - 2 * need
+        assert pages != pool or used * (cache.codes.numel() // pages) > 2 ** 32
+        other = torch.arange(used, used + need, dtype=torch.int32, device="cuda")[None].contiguous()
+        table = (other + need).flip(1).contiguous()
+        batch = serving.Batch(_dev(torch, [0, n]), _dev(torch, [n]), table, n, max_kv_len=n)
+        last = serving.Batch(_dev(torch, [0, 1]), _dev(torch, [n]), table, 1, max_tokens=1, max_kv_len=n)
+        turned = serving.append_rotated(cache, batch, q, k, v)
+        w = torch.zeros((1, H, n), device="cuda")
+        for b, rows in ((batch, turned), (last, turned[-1:])):
+            _, lse = serving.attention(cache, b, rows, return_lse=True)
+            serving.attention_weights(cache, b, rows, lse, w, w)
+        kept = serving.keep(cache, last, w, 100, 2, 9)
+        serving.evict(cache, last, *kept, page_table=other)
+        weights = w.clone()
+        serving.evict(cache, last, *kept, w)
+        got.append((turned, weights, *kept, w, cache.codes[:, used:].clone(), cache.scales[:, used:].view(torch.int16).clone()))
+        assert not cache.codes[:, :used].any()
+        del cache
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][5].any()

@@ -69,3 +69,44 @@ def test_the_choice_writes_none_of_what_it_reads(workspace):
         assert _keep(workspace=workspace, kept_lens=4 * A + off) == PASSES
         assert _keep(workspace=workspace, kept_lens=9 * A + off) == PASSES
     assert _keep(0, kept_lens=4 * A) == OK
+
+
+def _weigh(decay, weights):
+    m, s = pb.make_model(_shape()), _shape()
+    cb, sb = pb.pkv_cache_size(s, 3)
+    c = pb.PkvPagedCache(tag=3, codes=A, code_bytes=cb, scales=2 * A, scale_bytes=sb)
+    b = pb.PkvBatch(2, 0, 0, 4, 0, 3 * A, 4 * A, None, 5 * A)
+    a = pb.PkvAttention(num_q_heads=8, scale=0.1, q=6 * A, q_token_stride=1024, q_head_stride=128, lse=7 * A)
+    w = pb.PkvWeights(4, decay, 64, 64, 256, weights, 8 * A)
+    return pb.pkv_attention_weights_status(m, c, b, a, w)
+
+
+def test_weights_before_are_needed_only_where_they_are_read():
+    assert _weigh(0.5, 9 * A) == PASSES and _weigh(0.0, None) == PASSES
+    assert _weigh(0.5, None) == BAD and _weigh(float("nan"), 9 * A) == BAD
+
+
+def test_an_eviction_needs_no_weights():
+    m, s = pb.make_model(_shape()), _shape()
+    cb, sb = pb.pkv_cache_size(s, 3)
+    c = pb.PkvPagedCache(tag=3, codes=A, code_bytes=cb, scales=2 * A, scale_bytes=sb)
+    b = pb.PkvBatch(2, 0, 0, 4, 0, 3 * A, 4 * A, None, 5 * A)
+    k = pb.PkvKept(heads=4, budget=16, kept=6 * A, kept_lens=7 * A)
+    assert pb.pkv_cache_evict_status(m, c, b, k, None, None, 0) == PASSES
+    for out, status in ((None, BAD), (8 * A + 2, BAD), (8 * A, PASSES)):
+        assert pb.pkv_cache_evict_status(m, c, b, k, pb.PkvWeights(4, 1.0, 64, 64, 256, None, out), None, 0) == status
+
+
+@pytest.mark.parametrize("kept", [dict(heads=2), dict(budget=-1), dict(budget=(1 << 30) + 1), dict(sinks=-1), dict(recent=-1),
+                                  dict(kept=None), dict(kept=7 * A + 2), dict(kept_lens=None), dict(kept_lens=8 * A + 1),
+                                  dict(budgets=9 * A + 3)])
+def test_what_is_kept_is_refused_for_itself(kept):
+    """The same call with nothing wrong passes, and with budget 0 it needs no place for the tokens."""
+    def keep(**kw):
+        m, b = pb.make_model(_shape()), pb.PkvBatch(2, 0, 0, 4, 0, 3 * A, 4 * A, None, None)
+        w = pb.PkvWeights(4, 1.0, 64, 64, 256, 6 * A, None)
+        at = dict(heads=4, budget=16, sinks=2, recent=3, budgets=9 * A, kept=7 * A, kept_lens=8 * A)
+        return pb.pkv_cache_keep_status(m, b, w, pb.PkvKept(**{**at, **kw}))
+
+    assert keep() == PASSES and keep(budget=0, kept=None) == PASSES
+    assert keep(**kept) == BAD
