@@ -575,9 +575,11 @@ typedef struct {
  * kv_lens; what lies behind stays.  `attention` is the structure of the pkv_attention
  * call whose rows they are: its q, scale and masks, its lse (here an input, not
  * NULL) and a workspace of pkv_attention_weights_workspace's bytes; out is not
- * looked at.  A row with lse = -inf gives nothing, a token on a page that is not
- * there receives nothing.  Sums are single precision in an order that depends on the
- * sizes alone; scores are as in pkv_attention, keys that no row sees do not matter.
+ * looked at.  The scale is 2^-64 or more (the rows' lse is divided by it).  A row with
+ * lse = -inf or past max_tokens gives nothing, a token on a page that is not there receives
+ * nothing.  Sums are single precision in an order that depends on the sizes alone; scores
+ * are as in pkv_attention, keys that no row sees do not matter, an infinite one weighs what
+ * exp makes of its scores.
  * The launch has fewer than 2^24 workgroups, for which num_seqs * num_kv_heads *
  * (max(max_kv_len / 128, max_tokens * (num_q_heads / num_kv_heads) / 32) + 24) < 2^24
  * always suffices.  At most three kernels on `hip_stream`.  Errors as pkv_attention. */

@@ -171,8 +171,9 @@ struct KeepArgs {
 
 constexpr int kKeepSegment = 8192;  // tokens of a segment
 // A choice of up to kFewKeptRows rows that may be longer than kWholeRow is made by segments.  Whole calls, us, by segments | by a
-// workgroup a row: 32 rows of 16384 tokens 25.3 | 22.3, of 32768 25.9 | 29.9; 128 of 32768 38.5 | 30.4; 2 x 8 rows of 131072 and
-// 40001 27 | 106; 512 of 65536 230 | 123.
+// workgroup a row: 32 rows of 16384 tokens 25.3 | 22.3; of 32768 32 rows 25 | 31, 64 27 | 31, 72 38 | 31, 128 41 | 32, 256 67 | 32; of
+// 65536 32 rows 29 | 56, 64 43 | 57, 96 57 | 58, 128 72 | 58; of 131072 64 rows 72 | 110, 72 86 | 113, 96 101 | 114, 128 129 | 115.  (So
+// up to some hundred rows of 131072 would still be faster by segments; the rule does not go by length.)
 constexpr int kFewKeptRows = 64;
 constexpr int kWholeRow = 24576;
 
@@ -212,8 +213,13 @@ constexpr int32_t kept_budget(const KeepArgs& a, int32_t n, int32_t budget) {
 
 // Of few rows (up to few_tiles row tiles of 16 a sequence and KV head; 32 sequences of 8192 tokens, 8 heads of 128, 32 rows, as few |
 // as many: 60 | 82 us in 4 bits, 104 | 153 in 16; 4 rows 42 | 99 and 101 | 169): tokens of a wave at a time; sequences whose tokens
-// are shared evenly (every workgroup adds up their lengths) and by how many workgroups, three to a compute unit.  32 ragged sequences of
-// 255 thousand tokens in 4 bits: 768 shares 54.6 us, 1024 57.1, 1536 55.2; chunks of 128, 256 and 512 tokens 65, 60 and 68.
+// are shared evenly (every workgroup adds up their lengths), and by how many workgroups: as many as run at once of the smallest
+// form (4 bits of 128 channels, one row tile: three to a compute unit; others have two).  32 ragged sequences of 255 thousand tokens,
+// 512 | 768 | 1024 | 1536 shares: 4 bits 51 | 52 | 54 | 53 us, in two row tiles 66 | 85 | 75 | 85; 8 bits 65 | 80 | 72 | 78; 16 bits
+// 114 | 130 | 116 | 120 (512 would do for all); chunks of 128, 256 and 512 tokens, 4 bits, 65, 60 and 68.
+// With a window tokens are cut into chunks of up to kMostChunk that leave two to four thousand, where there are that many.
+// Window 1024 and 4 sinks, chunks of 32 | 64 | 128 | 256 | 512: the same sequences 4 bits 87 | 53 | 41 | 39 | 44 us, 16 bits 103 | 65 |
+// 53 | 51 | 69 (the rule: 256); one of 131072 42 | 26 | 22 | 21 | 33 (64).  Four of 700, window 256: 9.4 | 10.6 | 13.6 | 17 | 21 (32).
 constexpr int kFewWaves = 4;
 constexpr int kMostChunk = 512;
 constexpr int kMostShared = 512;

@@ -338,7 +338,7 @@ def attention_weights(cache: PagedCache, batch: Batch, q, lse, out, weights=None
     ``scale`` and masks, and the ``lse`` that it returned), added to ``decay`` times what it had before:
     ``out = decay * weights + sum``, float32 ``[S, H, tokens]`` for each KV head or ``[S, 1, tokens]`` for all together,
     with as many tokens as the batch's bound.  ``weights`` may be ``out`` (added in place) or None (nothing before).  Tokens
-    past ``kv_lens`` are left as they are.  Returns ``out``."""
+    past ``kv_lens`` are left as they are.  ``scale`` is 2^-64 or more.  Returns ``out``."""
     heads = q.shape[1]
     _rows(cache, batch, heads, q)
     _need(lse.dtype == torch.float32 and lse.shape == (batch.num_tokens, heads) and lse.is_contiguous(),
